@@ -135,8 +135,8 @@ def _adamw_inputs(case, seed):
             t.update(rows=case["rows"], row_mask=read.to(torch.uint8) if case["rows"] == "mask" else None)
         if case["bits"] == 8 and p.numel() >= 4096:           # small tensors keep moments of 32 bits
             i = torch.arange(rows * d, device=DEV).view(rows, d)
-            m, t["m_scale"] = _encode(m, E4M3, _offset(i, 9, OFFSET_M))
-            v, t["v_scale"] = _encode(v, E5M2, _offset(i, 9, OFFSET_V))
+            m, t["m_scale"] = _encode(m, E4M3, _offset(i, 9, E4M3))
+            v, t["v_scale"] = _encode(v, E5M2, _offset(i, 9, E5M2))
         if case["copy"] and not by_rows and wd:
             t["copy"] = p.to(torch.bfloat16)
         tensors.append(dict(t, m=m, v=v))
@@ -196,15 +196,16 @@ def _norm(x):
 
 
 # An 8-bit moment: a power of two per block of 256 elements of a row brings the block's largest magnitude to at most the
-# format's largest number; a magnitude between two of the format's numbers goes to the lower one, or with an offset u in
-# [0, 1) of their distance to the upper one, u from a Weyl sequence over elements and steps.
-E4M3 = dict(type=torch.float8_e4m3fn, digits=3, least=-6, most=448.0, top=8)
-E5M2 = dict(type=torch.float8_e5m2, digits=2, least=-14, most=57344.0, top=15)
-OFFSET_M, OFFSET_V = (0xC2B2AE35, 0x9E3779B9), (0x85EBCA6B, 0x61C88647)
+# format's largest number; a magnitude that lies a fraction f of their distance above the lower of two of the format's
+# numbers goes to the upper one where f + u reaches one, u in [0, 1) from the element's index and the step.
+E4M3 = dict(type=torch.float8_e4m3fn, digits=3, least=-6, top=8, shift=0)
+E5M2 = dict(type=torch.float8_e5m2, digits=2, least=-14, top=15, shift=16)
 
 
-def _offset(i, t, words):
-    return ((((i * words[0]) & 0xFFFFFFFF) + t * words[1] & 0xFFFFFFFF) >> 16).float() * 2.0 ** -16
+def _offset(i, t, form):
+    x = i * 0xC2B2AE35 + t * 0x9E3779B9 & 0xFFFFFFFF
+    x = (x ^ x >> 16) * 0x2C1B3C6D & 0xFFFFFFFF
+    return (x >> form["shift"] & 0xFFFF).float() * 2.0 ** -16
 
 
 def _scale(most, form):
@@ -254,8 +255,8 @@ def _adamw_one(w, t, h, c1, c2):
     done = dict(param=new, m=m, v=v)
     if w["m_scale"] is not None:
         i = torch.arange(p.numel(), device=p.device).view_as(p)
-        done["m"], done["m_scale"] = _encode(m, E4M3, _offset(i, t, OFFSET_M))
-        done["v"], done["v_scale"] = _encode(v, E5M2, _offset(i, t, OFFSET_V))
+        done["m"], done["m_scale"] = _encode(m, E4M3, _offset(i, t, E4M3))
+        done["v"], done["v_scale"] = _encode(v, E5M2, _offset(i, t, E5M2))
     if w["copy"] is not None:
         done["copy"] = new.to(torch.bfloat16)
     for name, value in done.items():
@@ -367,8 +368,8 @@ def _exact_norm(case, x):
     return out
 
 
-def _exact_moment(x, digits, least, top, largest, words, t, scales, keep):
-    """(numbers, scales) that a moment x of 64 bits is held as; rows outside `keep` from the state they had."""
+def _exact_moment(x, digits, least, largest, half, t, scales):
+    """(numbers, scales) that a moment x of 64 bits is held as; `half`: the half of the offset's 32 bits."""
     rows, d = x.shape
     blocks = scales.shape[1]
     a = torch.zeros((rows, blocks * BLOCK), dtype=torch.float64, device=DEV)
@@ -381,7 +382,9 @@ def _exact_moment(x, digits, least, top, largest, words, t, scales, keep):
     e = torch.floor(torch.log2(torch.where(a > 0, a, torch.ones_like(a)))).clamp(min=least) - digits
     unit = torch.exp2(torch.where(a > 0, e, torch.full_like(e, least - digits)))
     i = torch.arange(rows * d, device=DEV).view(rows, d)
-    u = torch.remainder(i * words[0] + t * words[1], 1 << 32).div(1 << 16, rounding_mode="floor") / 65536.0
+    w = torch.remainder(i * 3266489909 + t * 2654435769, 1 << 32)
+    w = torch.remainder(torch.bitwise_xor(w, w.div(1 << 16, rounding_mode="floor")) * 739982445, 1 << 32)
+    u = (w.div(1 << 16, rounding_mode="floor") if half else torch.remainder(w, 1 << 16)).double() / 65536.0
     return torch.floor(a / unit + u) * unit, s
 
 
@@ -403,9 +406,9 @@ def _exact_adamw(case, x):
         out = dict(param=p - step, m=m, v=v)
         if eight:
             del step
-            q, out["m_scale"] = _exact_moment(m, 3, -6, 8, 448.0, OFFSET_M, t, w["m_scale"], on)
+            q, out["m_scale"] = _exact_moment(m, 3, -6, 448.0, 0, t, w["m_scale"])
             out["m"] = torch.where(m < 0, -q, q)
-            q, out["v_scale"] = _exact_moment(v, 2, -14, 15, 57344.0, OFFSET_V, t, w["v_scale"], on)
+            q, out["v_scale"] = _exact_moment(v, 2, -14, 57344.0, 1, t, w["v_scale"])
             out["v"] = torch.where(v > 0, q.clamp(min=2.0 ** -16), q)
         if w["copy"] is not None:
             out["copy"] = out["param"]
