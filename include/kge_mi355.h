@@ -17,6 +17,8 @@
  *                            the gradients with respect to embeddings and M_r
  *   kge_rgcn_backward        chain rule on Eq. 1-2 (Algorithm 1, "backward")
  *   kge_optimizer_step       Algorithm 1, "optimizer.step()"
+ *   kge_dense_*, kge_layer_norm_*   a learned block in front of the encoder, for vertices with features
+ *   kge_adamw_step           the update of all parameters in one launch, moments in 32 or 8 bits
  *
  * General rules
  *  - Every function returns KGE_OK (0) or a negative kge_status; on error no
@@ -330,6 +332,110 @@ int kge_optimizer_step(const kge_opt *opt, float *param, const float *grad, floa
                        int64_t n, void *stream);
 int kge_optimizer_step_rows(const kge_opt *opt, float *param, const float *grad, float *m, float *v,
                             int64_t n_rows, int32_t d, const uint8_t *row_mask, void *stream);
+
+/*
+ * Vertex-feature block: what stands between a fixed feature matrix and the encoder's input,
+ *   H_0 = norm(act(X W + b) + R),
+ * as a dense layer and a layer norm, each with its backward pass.  Rows (X, R, Y, pre, dY, dX, add) and W are
+ * matrices of `dtype`; row strides (ld*, in elements, at least the row's width) may be larger than the rows, and
+ * nothing between rows is read or written; any alignment to whole elements is taken.  W is dense.  Biases, norm
+ * weights, statistics and the parameters' gradients are float.  Outputs may not overlap inputs, except where it
+ * says so.  All calls are asynchronous on `stream`, allocate nothing, never synchronise, use no atomics (results repeat
+ * bit for bit), and can be captured into a HIP graph; calls on different streams need different workspaces.
+ */
+enum { KGE_DT_F32 = 0, KGE_DT_BF16 = 1 };
+
+/*
+ * Dense layer:  pre = X W + b;  Y = act(pre) + R.   n_rows may be anything from 0 to 2^31 - 1, widths 1 to 65536.
+ *   act: KGE_ACT_IDENTITY, KGE_ACT_RELU or KGE_ACT_SILU (z / (1 + e^-z), this layer only)
+ *   W : DEVICE dtype [d_in][d_out]      b : DEVICE float [d_out] or NULL
+ * Sums are fp32; bf16 results are rounded once, at the end.  fp32 products have fp32 accuracy (they run as bf16
+ * products of exact three-way splits).
+ *
+ * kge_dense_forward: X [n_rows][d_in]; R [n_rows][d_out] or NULL (may be X when d_in == d_out, may be Y); Y [n_rows][d_out];
+ *   pre [n_rows][d_out] or NULL: act's argument rounded to dtype, for the backward pass.
+ * kge_dense_backward: dP = dY * act'(pre), with act' at pre as it was stored (ReLU: 0 at 0; a ReLU layer without R may pass Y);
+ *   dX [n_rows][d_in] = dP W^T + add, or NULL;  add [n_rows][d_in] or NULL (may be dX): a gradient that reaches X past the layer,
+ *     for a residual R = X that is dY
+ *   dW [d_in][d_out] = X^T dP, db [d_out] = column sums of dP: float, overwritten, each may be NULL (the gradient of R is dY itself)
+ *   pre may be NULL for KGE_ACT_IDENTITY, X when neither dW nor db is asked for, W when dX is not
+ *   workspace: 256-byte aligned, at least kge_dense_workspace_bytes(layer, n_rows) bytes; NULL with dW and db NULL.
+ */
+enum { KGE_ACT_SILU = 2 };
+typedef struct kge_dense {
+    int32_t d_in, d_out, act, dtype;
+    const void *W;
+    const float *b;
+} kge_dense;
+int kge_dense_forward(const kge_dense *layer, int64_t n_rows, const void *X, int64_t ldx, const void *R, int64_t ldr,
+                      void *Y, int64_t ldy, void *pre, int64_t ldp, void *stream);
+size_t kge_dense_workspace_bytes(const kge_dense *layer, int64_t n_rows);      /* 0 on invalid arguments */
+int kge_dense_backward(const kge_dense *layer, int64_t n_rows, const void *X, int64_t ldx, const void *pre, int64_t ldp,
+                       const void *dY, int64_t lddy, const void *add, int64_t ldadd, void *dX, int64_t lddx, float *dW,
+                       float *db, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Layer norm of rows:  y = (x - mean) rstd gamma + beta,  rstd = 1 / sqrt(var + eps),  var the mean squared deviation.
+ *   d 1 to 16384; x_dtype is X's and dX's, y_dtype Y's and dY's type; gamma, beta: DEVICE float [d] or NULL (ones, zeros)
+ * kge_layer_norm_forward: mean, rstd DEVICE float [n_rows] or NULL: what the backward pass takes.
+ * kge_layer_norm_backward: dX [n_rows][d], dgamma, dbeta [d] float: overwritten, each may be NULL.
+ *   workspace: 256-byte aligned, at least kge_layer_norm_workspace_bytes(norm, n_rows) bytes; NULL with dgamma and dbeta NULL.
+ */
+typedef struct kge_norm {
+    int32_t d, x_dtype, y_dtype;
+    float eps;
+    const float *gamma, *beta;
+} kge_norm;
+int kge_layer_norm_forward(const kge_norm *norm, int64_t n_rows, const void *X, int64_t ldx, void *Y, int64_t ldy,
+                           float *mean, float *rstd, void *stream);
+size_t kge_layer_norm_workspace_bytes(const kge_norm *norm, int64_t n_rows);   /* 0 on invalid arguments */
+int kge_layer_norm_backward(const kge_norm *norm, int64_t n_rows, const void *X, int64_t ldx, const float *mean,
+                            const float *rstd, const void *dY, int64_t lddy, void *dX, int64_t lddx, float *dgamma,
+                            float *dbeta, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * AdamW over a list of tensors, in one launch per 28 tensors (Adam with decoupled weight decay):
+ *   m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
+ *   p <- p - lr (weight_decay p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)),  t = 1, 2, ...
+ * Each tensor is n_rows rows of d elements, dense.  Only the rows that `rows` takes are read and written:
+ *   KGE_ROWS_ALL      all;  KGE_ROWS_MASK  those with row_mask[row] != 0 (DEVICE uint8 [n_rows], e.g. kge_cgraph_input_rows);
+ *   KGE_ROWS_NONZERO  those whose gradient is not all zeros (d at most 65536)
+ * state_bits 32: m, v are float arrays, zero before the first step.
+ * state_bits 8:  m is e4m3, v e5m2 (OCP formats), one byte an element, with scales m_scale, v_scale: float
+ *   [n_rows][ceil(d / KGE_ADAMW_BLOCK)], one for each KGE_ADAMW_BLOCK consecutive elements of a row; a moment is its number
+ *   times its scale, a power of two (0: a block of zeros).  All zero before the first step.  Element i (its index in the tensor
+ *   modulo 2^32) whose scaled magnitude lies between two numbers of the format, a fraction f of their distance above the lower one, goes
+ *   to the upper one iff f + u >= 1,
+ *     x = (i * 0xC2B2AE35 + t * 0x9E3779B9) mod 2^32;  x = ((x xor (x >> 16)) * 0x2C1B3C6D) mod 2^32
+ *     u = (x mod 2^16) / 2^16 for m, (x >> 16) / 2^16 for v
+ *   (t modulo 2^32): the mean over steps is the number itself, so that averages are kept whose steps are far below the formats'
+ *   distances.  What this costs v is a spread of at most sqrt(1/8) of it (an eighth is half the largest distance).  A v above zero is never
+ *   stored as zero.  The update takes the moments before they are rounded.  A block that meets an infinity or a NaN reads as
+ *   NaN from then on.  3 to 4 times less memory for the state, 4/7 of the traffic of a step.
+ * copy: NULL, or DEVICE bf16 [n_rows][d] that gets the updated parameters rounded (weights of a bf16 dense layer).
+ * t_dev: NULL, or DEVICE int64: the step number is read from there when the launch runs and t is ignored; a call captured into
+ *   a HIP graph repeats its arguments, and with t_dev the caller advances the step between replays.
+ * No two arrays may overlap.
+ */
+#define KGE_ADAMW_BLOCK 256
+enum { KGE_ROWS_ALL = 0, KGE_ROWS_MASK = 1, KGE_ROWS_NONZERO = 2 };
+typedef struct kge_adamw_tensor {
+    float *param;
+    const float *grad;
+    void *m, *v;
+    float *m_scale, *v_scale;      /* NULL with state_bits 32 */
+    uint16_t *copy;
+    const uint8_t *row_mask;       /* NULL unless rows is KGE_ROWS_MASK */
+    int64_t n_rows, d;
+    int32_t state_bits, rows;
+    float weight_decay;
+} kge_adamw_tensor;
+typedef struct kge_adamw {
+    float lr, beta1, beta2, eps;
+    int64_t t;
+    const int64_t *t_dev;
+} kge_adamw;
+int kge_adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tensors, int32_t n_tensors, void *stream);
 
 /*
  * Link-prediction evaluation ("Evaluation Metrics" section: filtered setting, MRR Eq. 5, Hits@k Eq. 6).

@@ -24,12 +24,17 @@ EXPORTED = ["kge_build_partition", "kge_partition_info", "kge_partition_export",
             "kge_optimizer_step_rows", "kge_eval_filter_create", "kge_eval_filter_destroy",
             "kge_eval_workspace_bytes", "kge_eval_rank_all", "kge_eval_rank_candidates", "kge_eval_metrics",
             "kge_eval_debug_scores", "kge_eval_rank_all_static", "kge_cgraph_input_rows", "kge_score_index_create", "kge_score_index_destroy",
-            "kge_partition_bad_ids", "kge_test_set_rel_slab", "kge_test_pair_query"]
+            "kge_partition_bad_ids", "kge_test_set_rel_slab", "kge_test_pair_query", "kge_dense_forward",
+            "kge_dense_workspace_bytes", "kge_dense_backward", "kge_layer_norm_forward", "kge_layer_norm_workspace_bytes",
+            "kge_layer_norm_backward", "kge_adamw_step"]
 
-ACT_IDENTITY, ACT_RELU = 0, 1
+ACT_IDENTITY, ACT_RELU, ACT_SILU = 0, 1, 2       # ACT_SILU: dense layers only
 ORDER_PROJECT_FIRST, ORDER_RELATION_WEIGHTS = 0, 2
 OPT_SGD, OPT_ADAM = 0, 1
 MSG_F32, MSG_BF16 = 0, 1
+DT_F32, DT_BF16 = 0, 1
+ROWS_ALL, ROWS_MASK, ROWS_NONZERO = 0, 1, 2
+ADAMW_BLOCK = 256                 # KGE_ADAMW_BLOCK
 NEG_TAIL, NEG_HEAD_OR_TAIL = 0, 1
 DOMAIN_CORE, DOMAIN_ALL = 0, 1
 EVAL_STATIC_BYTES = 32 << 20      # KGE_EVAL_STATIC_BYTES
@@ -74,6 +79,28 @@ class _Opt(C.Structure):
                 ("eps", C.c_float), ("t", C.c_int64)]
 
 
+class _Dense(C.Structure):
+    _fields_ = [("d_in", C.c_int32), ("d_out", C.c_int32), ("act", C.c_int32), ("dtype", C.c_int32),
+                ("W", C.c_void_p), ("b", C.c_void_p)]
+
+
+class _Norm(C.Structure):
+    _fields_ = [("d", C.c_int32), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32), ("eps", C.c_float),
+                ("gamma", C.c_void_p), ("beta", C.c_void_p)]
+
+
+class _AdamWTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("row_mask", C.c_void_p),
+                ("n_rows", C.c_int64), ("d", C.c_int64), ("state_bits", C.c_int32), ("rows", C.c_int32),
+                ("weight_decay", C.c_float)]
+
+
+class _AdamW(C.Structure):
+    _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
+                ("t", C.c_int64), ("t_dev", C.c_void_p)]
+
+
 class _ProfEntry(C.Structure):
     _fields_ = [("name", C.c_char * 32), ("total_ms", C.c_double), ("calls", C.c_int64)]
 
@@ -96,6 +123,8 @@ def load():
         lib.kge_score_index_destroy.restype = None
         lib.kge_eval_filter_destroy.restype = None
         lib.kge_eval_workspace_bytes.restype = C.c_size_t
+        lib.kge_dense_workspace_bytes.restype = C.c_size_t
+        lib.kge_layer_norm_workspace_bytes.restype = C.c_size_t
         _lib = lib
     return _lib
 
@@ -375,6 +404,263 @@ def optimizer_step(kind: int, param, grad, m=None, v=None, lr=0.01, beta1=0.9, b
     else:
         _check(load().kge_optimizer_step(C.byref(o), _ptr(param), _ptr(grad), _ptr(m), _ptr(v),
                                          C.c_int64(param.numel()), _stream(stream)))
+
+
+# ---- vertex-feature block (dense layer, layer norm) and AdamW over a list of tensors ------------
+
+def _need(ok, msg: str):
+    """An argument check of this layer: the library's own status for it (KGE_EINVAL)."""
+    if not ok:
+        raise KgeError(-1, msg)
+
+
+def _rows(t, name: str, width=None, n=None, dtypes=None):
+    """(address, row stride) of a 2-D device tensor whose rows are dense; None is no tensor."""
+    if t is None:
+        return C.c_void_p(0), C.c_int64(0)
+    _need(t.dim() == 2, "%s: a matrix of rows is wanted, not %d dimensions" % (name, t.dim()))
+    _need(width is None or t.shape[1] == width, "%s: rows of %s elements are wanted, not %d" % (name, width, t.shape[1]))
+    _need(n is None or t.shape[0] == n, "%s: %s rows are wanted, not %d" % (name, n, t.shape[0]))
+    _need(dtypes is None or t.dtype in dtypes, "%s: bad type %s" % (name, t.dtype))
+    _need(t.shape[1] <= 1 or t.stride(1) == 1, "%s: a row's elements must lie side by side" % name)
+    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    _need(ld >= t.shape[1], "%s: rows overlap" % name)
+    return C.c_void_p(t.data_ptr()), C.c_int64(ld)
+
+
+def _vector(t, name: str, width: int, need=False):
+    import torch
+    _need(t is not None or not need, "%s is missing" % name)
+    if t is not None:
+        _need(t.dtype == torch.float32 and t.numel() == width and t.is_contiguous(),
+              "%s: %d contiguous floats are wanted" % (name, width))
+    return C.c_void_p(0 if t is None else t.data_ptr())
+
+
+def _workspace(t, need: int, device):
+    """The caller's workspace, or one from torch's allocator."""
+    import torch
+    if t is None:
+        return torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+    _need(t.is_contiguous(), "workspace: contiguous memory is wanted")
+    return t
+
+
+class _On:
+    """The device that all of a call's tensors are on is the current one while it runs (stream None: that device's
+    current stream)."""
+
+    def __init__(self, first, others):
+        import torch
+        _need(first.is_cuda, "device tensors are wanted (there is no CPU fallback)")
+        for t in others:
+            _need(t is None or t.device == first.device, "all tensors of a call must be on one device")
+        self.guard = torch.cuda.device(first.device) if first.device.index != torch.cuda.current_device() else None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *e):
+        if self.guard is not None:
+            self.guard.__exit__(*e)
+
+
+def _type_of(dtype, name: str) -> int:
+    import torch
+    _need(dtype in (torch.float32, torch.bfloat16), "%s: float32 or bfloat16 is wanted, not %s" % (name, dtype))
+    return DT_F32 if dtype == torch.float32 else DT_BF16
+
+
+def _dense(layer: dict, X):
+    W, b = layer["W"], layer.get("b")
+    _need(W.dim() == 2 and W.is_contiguous(), "W: a contiguous matrix is wanted")
+    dt = _type_of(X.dtype, "X")
+    _need(W.dtype == X.dtype, "W and X must be of one type")
+    return _Dense(W.shape[0], W.shape[1], int(layer["act"]), dt, W.data_ptr(), _vector(b, "b", W.shape[1]).value)
+
+
+def dense_workspace_bytes(layer: dict, n_rows: int) -> int:
+    W = layer["W"]
+    d = _Dense(W.shape[0], W.shape[1], int(layer["act"]), _type_of(W.dtype, "W"), None, None)
+    n = load().kge_dense_workspace_bytes(C.byref(d), C.c_int64(n_rows))
+    if n == 0:
+        raise KgeError(-1, load().kge_last_error().decode())
+    return int(n)
+
+
+def dense_forward(layer: dict, X, R=None, keep_pre: bool = False, Y=None, pre=None, stream=None):
+    """(Y, pre): Y = act(X W + b) + R on the rows of X; layer = dict(W=, b= or None, act=).  pre (keep_pre, or a tensor to
+    write it to): act's argument, which dense_backward takes; otherwise None."""
+    import torch
+    d, types = _dense(layer, X), (X.dtype,)
+    n, wide = X.shape[0], d.d_out
+    x, ldx = _rows(X, "X", d.d_in)
+    r, ldr = _rows(R, "R", wide, n, types)
+    Y = torch.empty((n, wide), dtype=X.dtype, device=X.device) if Y is None else Y
+    if pre is None and keep_pre:
+        pre = torch.empty((n, wide), dtype=X.dtype, device=X.device)
+    y, ldy = _rows(Y, "Y", wide, n, types)
+    z, ldz = _rows(pre, "pre", wide, n, types)
+    with _On(X, (layer["W"], layer.get("b"), R, Y, pre)):
+        _check(load().kge_dense_forward(C.byref(d), C.c_int64(n), x, ldx, r, ldr, y, ldy, z, ldz, _stream(stream)))
+    return Y, pre
+
+
+def dense_backward(layer: dict, X, pre, dY, add=None, need_dX: bool = True, need_dW: bool = True, dX=None, dW=None, db=None,
+                   workspace=None, stream=None) -> dict:
+    """dict(dX=, dW=, db=) of dense_forward (dX: need_dX; dW, db: need_dW); add: a gradient that reaches X past the layer."""
+    import torch
+    d, types = _dense(layer, X), (X.dtype,)
+    n = X.shape[0]
+    x, ldx = _rows(X, "X", d.d_in)
+    z, ldz = _rows(pre, "pre", d.d_out, n, types)
+    g, ldg = _rows(dY, "dY", d.d_out, n, types)
+    if need_dX and dX is None:
+        dX = torch.empty((n, d.d_in), dtype=X.dtype, device=X.device)
+    if need_dW:
+        dW = torch.empty((d.d_in, d.d_out), dtype=torch.float32, device=X.device) if dW is None else dW
+        db = torch.empty(d.d_out, dtype=torch.float32, device=X.device) if db is None else db
+        _need(dW.dim() == 2 and tuple(dW.shape) == (d.d_in, d.d_out), "dW: %d x %d is wanted" % (d.d_in, d.d_out))
+        workspace = _workspace(workspace, dense_workspace_bytes(layer, n), X.device)
+    else:
+        dW = db = workspace = None
+    dX = dX if need_dX else None
+    o, ldo = _rows(dX, "dX", d.d_in, n, types)
+    a, lda = _rows(add, "add", d.d_in, n, types)
+    pw, pb = _vector(dW, "dW", d.d_in * d.d_out), _vector(db, "db", d.d_out)
+    with _On(X, (layer["W"], pre, dY, add, dX, dW, db, workspace)):
+        _check(load().kge_dense_backward(C.byref(d), C.c_int64(n), x, ldx, z, ldz, g, ldg, a, lda, o, ldo, pw, pb, _ptr(workspace),
+                                         C.c_size_t(0 if workspace is None else workspace.numel() * workspace.element_size()),
+                                         _stream(stream)))
+    return dict(dX=dX, dW=dW, db=db)
+
+
+def _norm(norm: dict, d: int, x_dtype, y_dtype):
+    return _Norm(d, _type_of(x_dtype, "X"), _type_of(y_dtype, "Y"), float(norm.get("eps", 1e-5)),
+                 _vector(norm.get("gamma"), "gamma", d).value, _vector(norm.get("beta"), "beta", d).value)
+
+
+def layer_norm_workspace_bytes(d: int, n_rows: int) -> int:
+    p = _Norm(d, DT_F32, DT_F32, 0.0, None, None)
+    n = load().kge_layer_norm_workspace_bytes(C.byref(p), C.c_int64(n_rows))
+    if n == 0:
+        raise KgeError(-1, load().kge_last_error().decode())
+    return int(n)
+
+
+def layer_norm_forward(norm: dict, X, out_dtype=None, Y=None, mean=None, rstd=None, stream=None):
+    """(Y, mean, rstd) of X's rows; norm = dict(gamma= or None, beta= or None, eps=); Y in out_dtype (X's by default)."""
+    import torch
+    _need(X.dim() == 2, "X: a matrix of rows is wanted, not %d dimensions" % X.dim())
+    n, d = X.shape
+    Y = torch.empty((n, d), dtype=out_dtype or X.dtype, device=X.device) if Y is None else Y
+    mean = torch.empty(n, dtype=torch.float32, device=X.device) if mean is None else mean
+    rstd = torch.empty(n, dtype=torch.float32, device=X.device) if rstd is None else rstd
+    p = _norm(norm, d, X.dtype, Y.dtype)
+    x, ldx = _rows(X, "X")
+    y, ldy = _rows(Y, "Y", d, n)
+    pm, pr = _vector(mean, "mean", n), _vector(rstd, "rstd", n)
+    with _On(X, (norm.get("gamma"), norm.get("beta"), Y, mean, rstd)):
+        _check(load().kge_layer_norm_forward(C.byref(p), C.c_int64(n), x, ldx, y, ldy, pm, pr, _stream(stream)))
+    return Y, mean, rstd
+
+
+def layer_norm_backward(norm: dict, X, mean, rstd, dY, need_dX: bool = True, dX=None, dgamma=None, dbeta=None, workspace=None,
+                        stream=None) -> dict:
+    """dict(dX=, dgamma=, dbeta=) of layer_norm_forward (dX: need_dX)."""
+    import torch
+    _need(X.dim() == 2, "X: a matrix of rows is wanted, not %d dimensions" % X.dim())
+    n, d = X.shape
+    p = _norm(norm, d, X.dtype, dY.dtype)
+    x, ldx = _rows(X, "X")
+    g, ldg = _rows(dY, "dY", d, n)
+    if not need_dX:
+        dX = None
+    elif dX is None:
+        dX = torch.empty((n, d), dtype=X.dtype, device=X.device)
+    o, ldo = _rows(dX, "dX", d, n, (X.dtype,))
+    dgamma = torch.empty(d, dtype=torch.float32, device=X.device) if dgamma is None else dgamma
+    dbeta = torch.empty(d, dtype=torch.float32, device=X.device) if dbeta is None else dbeta
+    pm, pr = _vector(mean, "mean", n, True), _vector(rstd, "rstd", n, True)
+    pg, pb = _vector(dgamma, "dgamma", d), _vector(dbeta, "dbeta", d)
+    workspace = _workspace(workspace, layer_norm_workspace_bytes(d, n), X.device)
+    with _On(X, (norm.get("gamma"), norm.get("beta"), mean, rstd, dY, dX, dgamma, dbeta, workspace)):
+        _check(load().kge_layer_norm_backward(C.byref(p), C.c_int64(n), x, ldx, pm, pr, g, ldg, o, ldo, pg, pb, _ptr(workspace),
+                                              C.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream)))
+    return dict(dX=dX, dgamma=dgamma, dbeta=dbeta)
+
+
+class AdamWTensors:
+    """The descriptions of the tensors that adamw_step updates, laid out once (the tensors are kept alive).  Each is a dict:
+    param, grad; m, v and, for moments of 8 bits, m_scale, v_scale (adamw_state makes them); and, as wanted, weight_decay (0),
+    rows ("all", "mask", "nonzero"), row_mask (a tensor or a device address), copy (bf16).  A parameter of two dimensions is held
+    by rows, any other as one row."""
+
+    def __init__(self, tensors: Sequence[dict]):
+        import torch
+        self.tensors = [dict(t) for t in tensors]
+        self.array = (_AdamWTensor * max(len(self.tensors), 1))()
+        for i, t in enumerate(self.tensors):
+            a, p = self.array[i], t["param"]
+            name = "tensor %d: " % i
+            rows, d = _row_shape(p)
+            _need(p.dtype == torch.float32 and p.is_contiguous(), name + "param: contiguous floats are wanted")
+            _need(t["grad"].dtype == torch.float32 and t["grad"].is_contiguous() and t["grad"].numel() == p.numel(),
+                  name + "grad: contiguous floats are wanted, as many as param's")
+            eight = t.get("m_scale") is not None
+            for k, dt in (("m", torch.float8_e4m3fn if eight else torch.float32), ("v", torch.float8_e5m2 if eight else torch.float32)):
+                _need(t[k].dtype == dt and t[k].is_contiguous() and t[k].numel() == p.numel(),
+                      name + "%s: contiguous %s is wanted, as many as param's" % (k, dt))
+            if eight:
+                for k in ("m_scale", "v_scale"):
+                    _need(t.get(k) is not None and t[k].dtype == torch.float32 and t[k].is_contiguous() and
+                          t[k].numel() == rows * -(-d // ADAMW_BLOCK), name + "%s: a float for each block of %d is wanted" % (k, ADAMW_BLOCK))
+            else:
+                _need(t.get("v_scale") is None, name + "v_scale without m_scale")
+            copy, mask, how = t.get("copy"), t.get("row_mask"), t.get("rows", "all")
+            _need(copy is None or (copy.dtype == torch.bfloat16 and copy.is_contiguous() and copy.numel() == p.numel()),
+                  name + "copy: contiguous bfloat16 is wanted, as many as param's")
+            _need(how in ("all", "mask", "nonzero"), name + "rows: all, mask or nonzero is wanted")
+            if mask is not None and not isinstance(mask, int):
+                _need(mask.dtype in (torch.uint8, torch.bool) and mask.is_contiguous() and mask.numel() == rows,
+                      name + "row_mask: a byte for each row is wanted")
+            on = [x for x in (t["grad"], t["m"], t["v"], t.get("m_scale"), t.get("v_scale"), copy, mask) if hasattr(x, "device")]
+            _need(all(x.device == self.tensors[0]["param"].device for x in on + [p]), "all tensors of a call must be on one device")
+            a.param, a.grad, a.m, a.v = (t[k].data_ptr() for k in ("param", "grad", "m", "v"))
+            a.m_scale, a.v_scale, a.copy = (_ptr(t.get(k)).value for k in ("m_scale", "v_scale", "copy"))
+            a.row_mask = mask if isinstance(mask, int) else _ptr(mask).value
+            a.n_rows, a.d, a.state_bits = rows, d, 8 if eight else 32
+            a.rows, a.weight_decay = dict(all=ROWS_ALL, mask=ROWS_MASK, nonzero=ROWS_NONZERO)[how], float(t.get("weight_decay", 0.0))
+
+
+def _row_shape(p):
+    return (p.shape[0], p.shape[1]) if p.dim() == 2 else (1, p.numel())
+
+
+def adamw_state(param, bits: int = 32) -> dict:
+    """Zeroed moments of a parameter: dict(m=, v=, m_scale=, v_scale=), the scales None with 32 bits."""
+    import torch
+    _need(bits in (8, 32), "moments have 32 or 8 bits")
+    if bits == 32:
+        return dict(m=torch.zeros_like(param), v=torch.zeros_like(param), m_scale=None, v_scale=None)
+    rows, d = _row_shape(param)
+    scales = lambda: torch.zeros((rows, -(-d // ADAMW_BLOCK)), dtype=torch.float32, device=param.device)
+    codes = lambda dt: torch.zeros(param.shape, dtype=torch.uint8, device=param.device).view(dt)
+    return dict(m=codes(torch.float8_e4m3fn), v=codes(torch.float8_e5m2), m_scale=scales(), v_scale=scales())
+
+
+def adamw_step(tensors, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, t=1, t_dev=None, stream=None):
+    """One AdamW step in place on all tensors: an AdamWTensors or a list of its dicts.  t_dev: the step number as a device
+    int64 tensor of one element, in place of t."""
+    import torch
+    plan = tensors if isinstance(tensors, AdamWTensors) else AdamWTensors(tensors)
+    _need(t_dev is None or (t_dev.dtype == torch.int64 and t_dev.numel() == 1), "t_dev: one int64 is wanted")
+    o = _AdamW(lr, beta1, beta2, eps, int(t), _ptr(t_dev).value)
+    if not plan.tensors:
+        return
+    with _On(plan.tensors[0]["param"], (t_dev,)):
+        _check(load().kge_adamw_step(C.byref(o), plan.array, C.c_int32(len(plan.tensors)), _stream(stream)))
 
 
 # ---- link-prediction evaluation (filtered ranks, MRR, Hits@k) ----------------------------------

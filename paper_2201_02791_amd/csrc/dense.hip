@@ -1,0 +1,546 @@
+// Dense layer on the rows of a feature matrix, with everything around the product in its epilogue, and its backward pass.
+//
+//   forward    pre = X W + b;  Y = act(pre) + R
+//   backward   dP = dY * act'(pre);  dX = dP W^T + add;  dW = X^T dP;  db = sum over rows of dP
+//
+// One kernel for the three products C[i][j] = sum_k A[i][k] B[k][j]; they differ in how an operand lies in memory:
+//
+//   forward     A = X: terms k side by side          B = W: columns j side by side
+//   input       A = dP: terms side by side           B = W^T: terms side by side
+//   weights     A = X^T: columns i side by side      B = dP: columns side by side       (terms: the rows of X)
+//
+// A tile of 128 x 128 results per block of four wavefronts, 64 x 64 each on v_mfma_f32_32x32x16_bf16.  Tiles reach LDS
+// through registers, where they become bf16 and where dY turns into dP: act' is never stored, and the next tile is
+// loaded while one is multiplied.  An operand whose terms lie side by side is read back with ds_read_b128 from rows of
+// terms, one whose columns do with the transposing ds_read_b64_tr_b16 from rows of columns; the chunks of 16 bytes of a
+// row are XOR-ed with its number so that neither meets a bank twice.
+//
+// fp32 numbers become three bf16 parts and six products (split_bf16.h): 417 TFLOP/s where the fp32 instruction has 157.
+// bf16 numbers enter as they are, and so does dP of bf16 rows under identity and ReLU; under SiLU dP is an fp32 number:
+// two parts (2^-17) where the result is rounded to bf16, three where it is a weights' gradient in fp32.  Sums that are
+// not finite come again from fp32 products: infinities do not survive a split.
+//
+// The weights' gradient sums over as many rows as there are: they are cut into chunks so that about as many blocks run as
+// the chip holds, each writes its sums to the workspace and a second launch adds them in a fixed order.
+#include "common.h"
+#include "split_bf16.h"
+
+#include <math.h>
+
+#include <type_traits>
+
+namespace {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int BM = 128, BN = 128, NT = 256;
+enum { FORWARD = 0, INPUT = 1, WEIGHTS = 2 };
+
+__device__ __forceinline__ float bf(uint32_t w16) { return __uint_as_float(w16 << 16); }
+
+// 8 consecutive elements from a (n of them exist; the others read as zeros).  Rows may start at any element: the loads ask
+// for no more alignment than an element has
+struct __attribute__((packed, aligned(4))) F8 { float x[8]; };
+struct __attribute__((packed, aligned(2))) H8 { uint32_t w[4]; };
+__device__ __forceinline__ void load8(const float *a, int n, float x[8])
+{
+    if (n >= 8) {
+        const F8 q = *reinterpret_cast<const F8 *>(a);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = q.x[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = k < n ? a[k] : 0.f;
+    }
+}
+__device__ __forceinline__ uint4 load8(const uint16_t *a, int n)
+{
+    if (n >= 8) {
+        const H8 q = *reinterpret_cast<const H8 *>(a);
+        return make_uint4(q.w[0], q.w[1], q.w[2], q.w[3]);
+    }
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = (2 * k < n ? a[2 * k] : 0u) | (2 * k + 1 < n ? (uint32_t)a[2 * k + 1] << 16 : 0u);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void spread(uint4 q, float x[8])
+{
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { x[2 * k] = bf(w[k] & 0xffffu); x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_of(float z)
+{
+    return ACT == KGE_ACT_RELU ? (z < 0.f ? 0.f : z) : ACT == KGE_ACT_SILU ? z / (1.f + __expf(-z)) : z;
+}
+template <int ACT>
+__device__ __forceinline__ float act_grad(float z)
+{
+    if (ACT == KGE_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+    if (ACT == KGE_ACT_SILU) {
+        const float s = 1.f / (1.f + __expf(-z));
+        return s * (1.f + z * (1.f - s));
+    }
+    return 1.f;
+}
+
+__device__ __forceinline__ float elem(const float *a) { return *a; }
+__device__ __forceinline__ float elem(const uint16_t *a) { return bf(*a); }
+__device__ __forceinline__ void put(float *a, float x) { *a = x; }
+__device__ __forceinline__ void put(uint16_t *a, float x) { *a = __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+template <class T>
+struct Args {
+    const T *A, *B;                // as stored (see the table above)
+    int64_t lda, ldb;
+    const T *pre;                  // laid out like the operand that is dP (A of INPUT, B of WEIGHTS)
+    int64_t ldpre;
+    int64_t M;                     // rows of the result
+    int32_t N;                     // its columns
+    int64_t K;                     // terms
+    int64_t chunk;                 // terms per block (WEIGHTS; K otherwise)
+    int32_t tiles_n;
+    int64_t tiles_m;
+    T *C, *pre_out;                // FORWARD: Y, pre;  INPUT: dX
+    int64_t ldc, ldp;
+    const T *add;                  // FORWARD: R;  INPUT: add
+    int64_t ldadd;
+    const float *bias;
+    float *part, *part_b;          // WEIGHTS: [chunks][M][N] sums, [chunks][N] sums of dP's columns (or null)
+};
+
+// what a thread holds of an operand's next tile: chunks of 8 elements, as fp32 numbers or as bf16 as they lie
+template <bool RAW, int CH>
+struct Held {
+    uint4 q[RAW ? CH : 1];
+    float x[RAW ? 1 : CH][8];
+};
+
+template <int PARTS>
+__device__ __forceinline__ void to_lds(const float x[8], unsigned char *at, int plane)
+{
+    uint32_t w[3][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const Split3 s = split_pair(x[2 * k], x[2 * k + 1]);
+        w[0][k] = s.w[0]; w[1][k] = s.w[1]; w[2][k] = s.w[2];
+    }
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) *reinterpret_cast<uint4 *>(at + p * plane) = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+}
+
+template <int MODE, class T, int ACT>
+struct Shape {
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr bool SOFT = !F32 && ACT == KGE_ACT_SILU;          // dP of bf16 rows that is no bf16 number
+    static constexpr int PA = F32 ? 3 : MODE == INPUT && SOFT ? 2 : 1;
+    static constexpr int PB = F32 ? 3 : MODE == WEIGHTS && SOFT ? 3 : 1;
+    static constexpr bool ROWA = MODE != WEIGHTS, ROWB = MODE == INPUT;    // terms side by side
+    static constexpr int BK = PA + PB > 2 ? 32 : 64;
+    static constexpr int LDS = (PA * BM + PB * BN) * BK * 2;
+    static constexpr int CH = BM * BK / 8 / NT;                        // chunks of 8 per thread and operand
+};
+
+// The place of chunk (r, c) of a tile: rows of BK terms (a row is 64 or 128 bytes), or rows of 128 columns (256 bytes)
+template <int BK>
+__device__ __forceinline__ int term_place(int r, int c)
+{
+    constexpr int PER = BK / 8;
+    return r * (2 * BK) + ((c ^ (PER == 4 ? (r >> 1) & 3 : r & 7)) << 4);
+}
+__device__ __forceinline__ int column_place(int k, int c) { return k * 256 + ((c ^ (4 * (k & 3))) << 4); }
+
+template <int MODE, class T, int ACT>
+__global__ __launch_bounds__(NT) void k_dense(Args<T> a)
+{
+    typedef Shape<MODE, T, ACT> S;
+    constexpr int BK = S::BK, PA = S::PA, PB = S::PB, CH = S::CH;
+    constexpr bool RAWA = PA == 1, RAWB = PB == 1;
+    constexpr int PLANE = BM * BK * 2;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[S::LDS];
+    unsigned char *const la = smem, *const lb = smem + PA * PLANE;
+
+    // block -> (tile of rows, tile of columns, chunk of terms).  Workgroup i runs on XCD i % 8, each with its own L2: the
+    // tiles that read the same long rows follow one another on one XCD
+    int64_t tm, chunk = 0;
+    int32_t tn;
+    if (MODE == WEIGHTS) {
+        const int64_t tiles = a.tiles_m * a.tiles_n, chunks = cdiv(a.K, a.chunk);
+        if (chunks >= 8) {
+            const int64_t seq = blockIdx.x >> 3;
+            chunk = (seq / tiles) * 8 + (blockIdx.x & 7);
+            const int64_t t = seq % tiles;
+            tm = t / a.tiles_n; tn = (int32_t)(t % a.tiles_n);
+        } else {
+            chunk = blockIdx.x / tiles;
+            const int64_t t = blockIdx.x % tiles;
+            tm = t / a.tiles_n; tn = (int32_t)(t % a.tiles_n);
+        }
+        if (chunk >= chunks) return;
+    } else if (a.tiles_m >= 64) {
+        const int64_t seq = blockIdx.x >> 3;
+        tm = (seq / a.tiles_n) * 8 + (blockIdx.x & 7);
+        tn = (int32_t)(seq % a.tiles_n);
+        if (tm >= a.tiles_m) return;
+    } else {
+        tm = blockIdx.x / a.tiles_n;
+        tn = (int32_t)(blockIdx.x % a.tiles_n);
+    }
+    const int64_t m0 = tm * BM, k_beg = chunk * a.chunk, k_end = min(k_beg + a.chunk, a.K);
+    const int32_t n0 = tn * BN;
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w >> 1, wn = w & 1;
+
+    Held<RAWA, CH> ha, hp;
+    Held<RAWB, CH> hb, hq;         // hp, hq: pre of the operand that is dP
+    constexpr bool GRAD = MODE != FORWARD && ACT != KGE_ACT_IDENTITY;
+
+    // chunk j of this thread in a tile of terms / of columns: (row, chunk in the row)
+    auto term_at = [&](int j, int &r, int &c) { const int i = j * NT + t; r = i / (BK / 8); c = i % (BK / 8); };
+    auto column_at = [&](int j, int &r, int &c) { const int i = j * NT + t; r = i / 16; c = i % 16; };
+
+    auto fetch = [&](int64_t k0) __attribute__((always_inline)) {
+        auto one = [&](auto &h, auto raw, int j, const T *base, int64_t ld, bool rows, int64_t outer0, int64_t outer_n) __attribute__((always_inline)) {
+            int r, c;
+            const T *p;
+            int n;
+            if (rows) {            // terms side by side: row outer0 + r, terms k0 + 8 c
+                term_at(j, r, c);
+                p = base + (outer0 + r) * ld + k0 + 8 * c;
+                n = outer0 + r < outer_n ? (int)min((int64_t)8, k_end - k0 - 8 * c) : 0;
+            } else {               // columns side by side: term k0 + r, columns outer0 + 8 c
+                column_at(j, r, c);
+                p = base + (k0 + r) * ld + outer0 + 8 * c;
+                n = k0 + r < k_end ? (int)min((int64_t)8, outer_n - outer0 - 8 * c) : 0;
+            }
+            if constexpr (S::F32) load8(p, n, h.x[j]);
+            else if constexpr (decltype(raw)::value) h.q[j] = load8(p, n);
+            else spread(load8(p, n), h.x[j]);
+        };
+        const std::integral_constant<bool, RAWA> rawa{};
+        const std::integral_constant<bool, RAWB> rawb{};
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            one(ha, rawa, j, a.A, a.lda, S::ROWA, m0, a.M);
+            if constexpr (MODE == INPUT && GRAD) one(hp, rawa, j, a.pre, a.ldpre, true, m0, a.M);
+            one(hb, rawb, j, a.B, a.ldb, S::ROWB, n0, a.N);
+            if constexpr (MODE == WEIGHTS && GRAD) one(hq, rawb, j, a.pre, a.ldpre, false, n0, a.N);
+        }
+    };
+
+    floatx16 acc[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    float col[8];                  // WEIGHTS: sums of dP over this thread's rows, its 8 columns (the same in every chunk)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) col[k] = 0.f;
+    const bool sum_columns = MODE == WEIGHTS && a.part_b && tm == 0;
+
+    // registers -> LDS, dY -> dP on the way
+    auto stage = [&]() __attribute__((always_inline)) {
+        auto one = [&](auto &h, auto &hg, int j, unsigned char *lds, bool rows, auto parts, bool grad, bool columns) __attribute__((always_inline)) {
+            constexpr int P = decltype(parts)::value;
+            int r, c;
+            if (rows) term_at(j, r, c);
+            else column_at(j, r, c);
+            unsigned char *at = lds + (rows ? term_place<BK>(r, c) : column_place(r, c));
+            if constexpr (P == 1) {
+                uint4 q = h.q[j];
+                if (grad) {        // ReLU: dY where pre is above zero (sign clear and not zero; a NaN is not above)
+                    uint32_t d[4] = {q.x, q.y, q.z, q.w};
+                    const uint32_t z[4] = {hg.q[j].x, hg.q[j].y, hg.q[j].z, hg.q[j].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float lo = bf(z[k] & 0xffffu), hi = __uint_as_float(z[k] & 0xffff0000u);
+                        d[k] = (lo > 0.f ? d[k] & 0xffffu : 0u) | (hi > 0.f ? d[k] & 0xffff0000u : 0u);
+                    }
+                    q = make_uint4(d[0], d[1], d[2], d[3]);
+                }
+                *reinterpret_cast<uint4 *>(at) = q;
+                if (columns) {
+                    float x[8];
+                    spread(q, x);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) col[k] += x[k];
+                }
+            } else {
+                float x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = grad ? h.x[j][k] * act_grad<ACT>(hg.x[j][k]) : h.x[j][k];
+                to_lds<P>(x, at, PLANE);
+                if (columns)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) col[k] += x[k];
+            }
+        };
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            one(ha, hp, j, la, S::ROWA, std::integral_constant<int, PA>(), MODE == INPUT && GRAD, false);
+            one(hb, hq, j, lb, S::ROWB, std::integral_constant<int, PB>(), MODE == WEIGHTS && GRAD, sum_columns);
+        }
+    };
+
+    // operand of the matrix instruction: row (or column) lane % 32 of block `blk` of 32, terms ks + 8 (lane / 32) ..
+    const int l16 = lane & 15, kr0 = 8 * (lane >> 5) + (l16 >> 2);
+    const int cb = (16 * ((lane >> 4) & 1) + 4 * (l16 & 3)) * 2, sw = ((l16 >> 2) & 3) << 6;
+    auto frag = [&](const unsigned char *lds, bool rows, int blk, int ks) __attribute__((always_inline)) -> uint4 {
+        if (rows) return *reinterpret_cast<const uint4 *>(lds + term_place<BK>(32 * blk + (lane & 31), ks / 8 + (lane >> 5)));
+        const unsigned char *p = lds + (ks + kr0) * 256 + (((blk * 64) ^ sw) + cb);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)p);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)(p + 4 * 256));
+        return __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+
+    fetch(k_beg);
+    for (int64_t k0 = k_beg; k0 < k_end; k0 += BK) {
+        stage();
+        __syncthreads();
+        if (k0 + BK < k_end) fetch(k0 + BK);
+#pragma unroll
+        for (int ks = 0; ks < BK; ks += 16) {
+            uint4 fa[PA][2], fb[PB][2];
+#pragma unroll
+            for (int p = 0; p < PA; ++p)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) fa[p][i] = frag(la + p * PLANE, S::ROWA, 2 * wm + i, ks);
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) fb[p][j] = frag(lb + p * PLANE, S::ROWB, 2 * wn + j, ks);
+            // smallest products first; of three parts each, those of 2^-24 of the product and below are left out
+#pragma unroll
+            for (int s = PA + PB - 2; s >= 0; --s) {
+                if (PA == 3 && PB == 3 && s > 2) continue;
+#pragma unroll
+                for (int pa = 0; pa < PA; ++pa) {
+                    const int pb = s - pa;
+                    if (pb < 0 || pb >= PB) continue;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) acc[i][j] = split_mfma(fa[pa][i], fb[pb][j], acc[i][j]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+
+    // a sum that is not finite: once more from fp32 products, term by term
+    auto again = [&](int64_t m, int64_t n) -> float {
+        float s = 0.f;
+        for (int64_t k = k_beg; k < k_end; ++k) {
+            float x = elem(S::ROWA ? a.A + m * a.lda + k : a.A + k * a.lda + m);
+            float y = elem(S::ROWB ? a.B + n * a.ldb + k : a.B + k * a.ldb + n);
+            if (MODE == INPUT && GRAD) x *= act_grad<ACT>(elem(a.pre + m * a.ldpre + k));
+            if (MODE == WEIGHTS && GRAD) y *= act_grad<ACT>(elem(a.pre + k * a.ldpre + n));
+            s = fmaf(x, y, s);
+        }
+        return s;
+    };
+
+    // register v of lane l: row 8 (v / 4) + 4 (l / 32) + v % 4 and column l % 32 of the 32 x 32 block
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int64_t n = n0 + 64 * wn + 32 * j + (lane & 31);
+            if (n >= a.N) continue;
+            const float b = MODE == FORWARD && a.bias ? a.bias[n] : 0.f;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int64_t m = m0 + 64 * wm + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
+                if (m >= a.M) continue;
+                float x = acc[i][j][v];
+                if (PA + PB > 2 && split_not_finite(x)) x = again(m, n);
+                if (MODE == FORWARD) {
+                    x += b;
+                    if (a.pre_out) put(a.pre_out + m * a.ldp + n, x);
+                    x = act_of<ACT>(x);
+                    if (a.add) x += elem(a.add + m * a.ldadd + n);
+                    put(a.C + m * a.ldc + n, x);
+                } else if (MODE == INPUT) {
+                    if (a.add) x += elem(a.add + m * a.ldadd + n);
+                    put(a.C + m * a.ldc + n, x);
+                } else {
+                    a.part[(chunk * a.M + m) * a.N + n] = x;
+                }
+            }
+        }
+    if (MODE == WEIGHTS && sum_columns) {        // 16 threads hold the same columns: added in their order
+        float *s = reinterpret_cast<float *>(smem);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[(t >> 4) * 128 + (t & 15) * 8 + k] = col[k];
+        __syncthreads();
+        if (t < 128 && n0 + t < a.N) {
+            float x = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x += s[r * 128 + t];
+            a.part_b[chunk * a.N + n0 + t] = x;
+        }
+    }
+}
+
+// dW and db from the chunks' sums, in the chunks' order: 64 elements a block, 4 chunks side by side
+__global__ __launch_bounds__(256) void k_dense_sum(const float *__restrict__ part, const float *__restrict__ part_b, int64_t chunks, int64_t nw,
+                                                   int64_t nb, float *__restrict__ dW, float *__restrict__ db)
+{
+    __shared__ float s[4][64];
+    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+    const int64_t i = (int64_t)blockIdx.x * 64 + x;
+    const bool w = i < nw;
+    const float *from = w ? part + i : part_b + (i - nw);
+    const int64_t step = w ? nw : nb;
+    float v = 0.f;
+    if (i < nw + nb)
+        for (int64_t c = y; c < chunks; c += 4) v += from[c * step];
+    s[y][x] = v;
+    __syncthreads();
+    if (y == 0 && i < nw + nb) (w ? dW + i : db + (i - nw))[0] = (s[0][x] + s[1][x]) + (s[2][x] + s[3][x]);
+}
+
+constexpr int32_t MAX_D = 65536;
+
+int check(const kge_dense *L, int64_t n_rows)
+{
+    KGE_REQUIRE(L, KGE_EINVAL, "NULL argument");
+    KGE_REQUIRE(L->d_in >= 1 && L->d_out >= 1 && L->d_in <= MAX_D && L->d_out <= MAX_D, KGE_EINVAL, "dense: widths are 1 to %d", MAX_D);
+    KGE_REQUIRE(L->dtype == KGE_DT_F32 || L->dtype == KGE_DT_BF16, KGE_EINVAL, "dense: bad type");
+    KGE_REQUIRE(L->act == KGE_ACT_IDENTITY || L->act == KGE_ACT_RELU || L->act == KGE_ACT_SILU, KGE_EINVAL, "dense: bad act");
+    KGE_REQUIRE(n_rows >= 0, KGE_EINVAL, "dense: negative number of rows");
+    KGE_REQUIRE(n_rows <= 0x7fffffffLL, KGE_ERANGE, "dense: at most 2^31 - 1 rows");
+    return KGE_OK;
+}
+
+// chunks of rows of the weights' gradient: about three blocks for each of the 256 compute units, at least 512 rows each
+int64_t chunk_rows(const kge_dense *L, int64_t n_rows)
+{
+    const int64_t tiles = cdiv(L->d_in, BM) * cdiv(L->d_out, BN);
+    int64_t chunks = cdiv(768, tiles);
+    if (chunks > cdiv(n_rows, 512)) chunks = cdiv(n_rows, 512);
+    if (chunks < 1) chunks = 1;
+    return align_up((size_t)cdiv(n_rows > 0 ? n_rows : 1, chunks), 64);
+}
+
+template <class T, class F>
+void with_act(int act, F f)
+{
+    if (act == KGE_ACT_RELU) f(std::integral_constant<int, KGE_ACT_RELU>());
+    else if (act == KGE_ACT_SILU) f(std::integral_constant<int, KGE_ACT_SILU>());
+    else f(std::integral_constant<int, KGE_ACT_IDENTITY>());
+}
+
+template <int MODE, class T>
+int launch(const kge_dense *L, Args<T> a, hipStream_t st)
+{
+    a.tiles_m = cdiv(a.M, BM);
+    a.tiles_n = (int32_t)cdiv(a.N, BN);
+    int64_t blocks = a.tiles_m * a.tiles_n;
+    if (MODE == WEIGHTS) {
+        const int64_t chunks = cdiv(a.K, a.chunk);
+        blocks *= chunks >= 8 ? (int64_t)align_up((size_t)chunks, 8) : chunks;
+    } else if (a.tiles_m >= 64) blocks = (int64_t)align_up((size_t)a.tiles_m, 8) * a.tiles_n;
+    KGE_REQUIRE(blocks <= 0x7fffffffLL, KGE_ERANGE, "dense: too large for one launch");
+    KGE_PROF(MODE == FORWARD ? "dense" : MODE == INPUT ? "dense_input_grad" : "dense_weight_grad", st);
+    with_act<T>(L->act, [&](auto act) { k_dense<MODE, T, act.value><<<(unsigned)blocks, NT, 0, st>>>(a); });
+    KGE_LAUNCH_CHECK();
+    return KGE_OK;
+}
+
+bool at_element(const void *p, int32_t dtype) { return ((uintptr_t)p % (dtype == KGE_DT_BF16 ? 2 : 4)) == 0; }
+
+template <class T>
+int forward(const kge_dense *L, int64_t n, const void *X, int64_t ldx, const void *R, int64_t ldr, void *Y, int64_t ldy, void *pre, int64_t ldp,
+            hipStream_t st)
+{
+    Args<T> a{};
+    a.A = (const T *)X; a.lda = ldx; a.B = (const T *)L->W; a.ldb = L->d_out;
+    a.M = n; a.N = L->d_out; a.K = a.chunk = L->d_in;
+    a.C = (T *)Y; a.ldc = ldy; a.pre_out = (T *)pre; a.ldp = ldp; a.add = (const T *)R; a.ldadd = ldr; a.bias = L->b;
+    return launch<FORWARD, T>(L, a, st);
+}
+
+template <class T>
+int backward(const kge_dense *L, int64_t n, const void *X, int64_t ldx, const void *pre, int64_t ldp, const void *dY, int64_t lddy, const void *add,
+             int64_t ldadd, void *dX, int64_t lddx, float *dW, float *db, void *ws, hipStream_t st)
+{
+    if (dX && n > 0) {
+        Args<T> a{};
+        a.A = (const T *)dY; a.lda = lddy; a.pre = (const T *)pre; a.ldpre = ldp; a.B = (const T *)L->W; a.ldb = L->d_out;
+        a.M = n; a.N = L->d_in; a.K = a.chunk = L->d_out;
+        a.C = (T *)dX; a.ldc = lddx; a.add = (const T *)add; a.ldadd = ldadd;
+        int rc = launch<INPUT, T>(L, a, st);
+        if (rc != KGE_OK) return rc;
+    }
+    if (dW || db) {
+        const int64_t chunk = chunk_rows(L, n), chunks = cdiv(n, chunk), nw = (int64_t)L->d_in * L->d_out;
+        Args<T> a{};
+        a.part = (float *)ws;
+        a.part_b = db ? a.part + chunks * nw : nullptr;
+        if (n > 0) {
+            a.A = (const T *)X; a.lda = ldx; a.B = (const T *)dY; a.ldb = lddy; a.pre = (const T *)pre; a.ldpre = ldp;
+            a.M = L->d_in; a.N = L->d_out; a.K = n; a.chunk = chunk;
+            int rc = launch<WEIGHTS, T>(L, a, st);
+            if (rc != KGE_OK) return rc;
+        }
+        KGE_PROF("dense_sum", st);             // without rows: sums of nothing, zeros
+        const int64_t w = dW ? nw : 0, b = db ? L->d_out : 0;
+        k_dense_sum<<<(unsigned)cdiv(w + b, 64), 256, 0, st>>>(a.part, a.part_b, chunks, w, b, dW, db);
+        KGE_LAUNCH_CHECK();
+    }
+    return KGE_OK;
+}
+
+}  // namespace
+
+extern "C" int kge_dense_forward(const kge_dense *L, int64_t n_rows, const void *X, int64_t ldx, const void *R, int64_t ldr, void *Y, int64_t ldy,
+                                 void *pre, int64_t ldp, void *stream)
+{
+    int rc = check(L, n_rows);
+    if (rc != KGE_OK) return rc;
+    KGE_REQUIRE(ldx >= L->d_in && ldy >= L->d_out && (!R || ldr >= L->d_out) && (!pre || ldp >= L->d_out), KGE_EINVAL,
+                "dense: a row stride is smaller than the row");
+    if (n_rows == 0) return KGE_OK;
+    KGE_REQUIRE(L->W && X && Y, KGE_EINVAL, "NULL argument");
+    KGE_REQUIRE(at_element(L->W, L->dtype) && at_element(X, L->dtype) && at_element(R, L->dtype) && at_element(Y, L->dtype) &&
+                    at_element(pre, L->dtype) && at_element(L->b, KGE_DT_F32), KGE_EINVAL, "dense: an array is not aligned to its elements");
+    hipStream_t st = (hipStream_t)stream;
+    return L->dtype == KGE_DT_F32 ? forward<float>(L, n_rows, X, ldx, R, ldr, Y, ldy, pre, ldp, st)
+                                  : forward<uint16_t>(L, n_rows, X, ldx, R, ldr, Y, ldy, pre, ldp, st);
+}
+
+extern "C" size_t kge_dense_workspace_bytes(const kge_dense *L, int64_t n_rows)
+{
+    if (check(L, n_rows) != KGE_OK) return 0;
+    const int64_t chunks = n_rows > 0 ? cdiv(n_rows, chunk_rows(L, n_rows)) : 1;
+    return align_up((size_t)chunks * ((size_t)L->d_in * L->d_out + L->d_out) * sizeof(float), 256);
+}
+
+extern "C" int kge_dense_backward(const kge_dense *L, int64_t n_rows, const void *X, int64_t ldx, const void *pre, int64_t ldp, const void *dY,
+                                  int64_t lddy, const void *add, int64_t ldadd, void *dX, int64_t lddx, float *dW, float *db, void *workspace,
+                                  size_t ws_bytes, void *stream)
+{
+    int rc = check(L, n_rows);
+    if (rc != KGE_OK) return rc;
+    KGE_REQUIRE(n_rows == 0 || ((L->W || !dX) && (X || !(dW || db)) && dY && (pre || L->act == KGE_ACT_IDENTITY)), KGE_EINVAL, "NULL argument");
+    KGE_REQUIRE((!X || ldx >= L->d_in) && (!dY || lddy >= L->d_out) && (!pre || ldp >= L->d_out) && (!add || ldadd >= L->d_in) && (!dX || lddx >= L->d_in),
+                KGE_EINVAL, "dense: a row stride is smaller than the row");
+    KGE_REQUIRE(!add || dX, KGE_EINVAL, "dense: a gradient to add needs dX");
+    KGE_REQUIRE(at_element(L->W, L->dtype) && at_element(X, L->dtype) && at_element(pre, L->dtype) && at_element(dY, L->dtype) &&
+                    at_element(add, L->dtype) && at_element(dX, L->dtype) && at_element(dW, KGE_DT_F32) && at_element(db, KGE_DT_F32),
+                KGE_EINVAL, "dense: an array is not aligned to its elements");
+    if (dW || db) {
+        KGE_REQUIRE(workspace && ((uintptr_t)workspace % 256) == 0, KGE_EINVAL, "dense: the workspace must be 256-byte aligned");
+        KGE_REQUIRE(ws_bytes >= kge_dense_workspace_bytes(L, n_rows), KGE_ENOMEM, "dense: workspace too small");
+    }
+    hipStream_t st = (hipStream_t)stream;
+    return L->dtype == KGE_DT_F32
+               ? backward<float>(L, n_rows, X, ldx, pre, ldp, dY, lddy, add, ldadd, dX, lddx, dW, db, workspace, st)
+               : backward<uint16_t>(L, n_rows, X, ldx, pre, ldp, dY, lddy, add, ldadd, dX, lddx, dW, db, workspace, st);
+}

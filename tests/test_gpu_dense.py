@@ -1,0 +1,263 @@
+"""Dense layer (forward and backward pass) against its formula in 64 bits: types, odd and ragged sizes, strides, activations,
+residuals, rows of nothing, infinities, other streams, graphs."""
+import sys
+
+import numpy as np
+import pytest
+
+import block_ref as ref
+
+pytestmark = pytest.mark.gpu
+ACTS = {"identity": ref.IDENTITY, "relu": ref.RELU, "silu": ref.SILU}
+
+
+def say(*a):
+    print("[case]", *a, file=sys.stderr, flush=True)
+
+
+@pytest.fixture(scope="module")
+def kb():
+    import torch
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_2201_02791_amd import binding
+    binding.load()
+    return binding
+
+
+def tt(kind):
+    import torch
+    return torch.float32 if kind == "f32" else torch.bfloat16
+
+
+def dev(x, kind="f32", wide=0, shift=0):
+    """The matrix on the device in a type (rounded to it); wide > 0: as columns shift .. of a wider matrix of 7s."""
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(tt(kind)).cuda()
+    if not wide or x.ndim != 2:
+        return t
+    buf = torch.full((x.shape[0], x.shape[1] + wide), 7.0, dtype=tt(kind), device="cuda")
+    buf[:, shift:shift + x.shape[1]] = t
+    return buf[:, shift:shift + x.shape[1]]
+
+
+def host(t):
+    return t.detach().cpu().double().numpy()
+
+
+def inputs(n, di, do, seed, std=1.0):
+    rng = np.random.default_rng(seed)
+    return (rng.normal(0, std, (n, di)), rng.normal(0, 1.0 / np.sqrt(di), (di, do)), rng.normal(0, 0.3, do).astype(np.float32),
+            rng.normal(0, std, (n, do)), rng.normal(0, 0.1, (n, do)), rng.normal(0, 0.1, (n, di)))
+
+
+SIZES = [(1, 1, 1), (1, 1000, 517), (2, 7, 3), (3, 64, 32), (17, 256, 129), (128, 128, 128), (129, 33, 127), (255, 200, 200),
+         (300, 203, 517), (1000, 32, 31), (2049, 130, 258), (5, 4100, 20)]
+
+
+def within(got, want, bound, what):
+    bad = np.abs(got - want) > bound
+    assert not bad.any(), "%s: %d of %d are off, worst %g of its bound" % (
+        what, bad.sum(), bad.size, float(np.max(np.abs(got - want) / np.maximum(bound, 1e-300))))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("n,di,do", SIZES)
+def test_forward(kb, kind, act, n, di, do):
+    say("dense forward", kind, act, n, di, do)
+    X, W, b, R, _, _ = inputs(n, di, do, n + di + do)
+    dX, dW, dR, db = dev(X, kind), dev(W, kind), dev(R, kind), dev(b)
+    for res, bias in ((False, True), (True, True), (True, False)):
+        layer = dict(W=dW, b=db if bias else None, act=ACTS[act])
+        Y, pre = kb.dense_forward(layer, dX, R=dR if res else None, keep_pre=True)
+        x, w, r = host(dX), host(dW), host(dR) if res else None
+        y, z = ref.dense_forward(x, w, b.astype(np.float64) if bias else None, ACTS[act], r)
+        by, bz = ref.dense_forward_bound(x, w, b.astype(np.float64) if bias else None, ACTS[act], r, kind)
+        within(host(pre), z, bz, "pre")
+        within(host(Y), y, by, "Y")
+        again, none = kb.dense_forward(layer, dX, R=dR if res else None)
+        assert none is None and bool((again == Y).all()), "the same call gives the same bits"
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("n,di,do", SIZES)
+def test_backward(kb, kind, act, n, di, do):
+    say("dense backward", kind, act, n, di, do)
+    X, W, b, R, G, A = inputs(n, di, do, 3 * n + di + do)
+    dX, dW, dG, dA = dev(X, kind), dev(W, kind), dev(G, kind), dev(A, kind)
+    layer = dict(W=dW, b=dev(b), act=ACTS[act])
+    pre = kb.dense_forward(layer, dX, keep_pre=True)[1]
+    x, w, z, g = host(dX), host(dW), host(pre), host(dG)
+    for add in (None, dA):
+        got = kb.dense_backward(layer, dX, pre if act != "identity" else None, dG, add=add)
+        a = None if add is None else host(add)
+        want = ref.dense_backward(x, w, z, g, ACTS[act], a)
+        bound = ref.dense_backward_bound(x, w, z, g, ACTS[act], a, kind)
+        for k, name in enumerate(("dX", "dW", "db")):
+            within(host(got[name]), want[k], bound[k], name)
+        again = kb.dense_backward(layer, dX, pre, dG, add=add)
+        assert all(bool((again[k] == got[k]).all()) for k in got), "the same call gives the same bits"
+    part = kb.dense_backward(layer, dX, pre, dG, need_dX=False)
+    assert part["dX"] is None and bool((part["dW"] == got["dW"]).all()) and bool((part["db"] == got["db"]).all())
+    part = kb.dense_backward(layer, dX, pre, dG, need_dW=False)
+    assert part["dW"] is None and part["db"] is None
+    within(host(part["dX"]), host(kb.dense_backward(layer, dX, pre, dG)["dX"]), 0.0, "dX alone")
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_many_rows_in_chunks(kb, kind):
+    """The weights' gradient over more rows than a chunk holds, the last chunk a short one."""
+    n, di, do = 70001, 40, 24
+    say("dense chunks", kind)
+    X, W, b, _, G, _ = inputs(n, di, do, 5)
+    dX, dG = dev(X, kind), dev(G, kind)
+    layer = dict(W=dev(W, kind), b=dev(b), act=ref.SILU)
+    Y, pre = kb.dense_forward(layer, dX, keep_pre=True)
+    got = kb.dense_backward(layer, dX, pre, dG)
+    args = host(dX), host(layer["W"]), host(pre), host(dG), ref.SILU, None
+    for k, name in enumerate(("dX", "dW", "db")):
+        within(host(got[name]), ref.dense_backward(*args)[k], ref.dense_backward_bound(*args, kind)[k], name)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n,di,do,wide,shift", [(70, 37, 45, 3, 1), (260, 128, 64, 8, 8), (131, 96, 100, 1, 0)])
+def test_strided_rows_keep_what_lies_between(kb, kind, n, di, do, wide, shift):
+    import torch
+    say("dense strides", kind, n, di, do, wide, shift)
+    X, W, b, R, G, A = inputs(n, di, do, 9)
+    flat = [dev(z, kind) for z in (X, R, G, A)]
+    views = [dev(z, kind, wide, shift) for z in (X, R, G, A)]
+    layer = dict(W=dev(W, kind), b=dev(b), act=ref.SILU)
+    Y, pre = kb.dense_forward(layer, flat[0], R=flat[1], keep_pre=True)
+    out = [torch.full((n + 2, w + wide), 5.0, dtype=tt(kind), device="cuda") for w in (do, do, di)]
+    vY, vpre, vdX = (o[1:n + 1, shift:shift + w] for o, w in zip(out, (do, do, di)))
+    kb.dense_forward(layer, views[0], R=views[1], Y=vY, pre=vpre)
+    assert bool((vY == Y).all()) and bool((vpre == pre).all())
+    want = kb.dense_backward(layer, flat[0], pre, flat[2], add=flat[3])
+    got = kb.dense_backward(layer, views[0], vpre, views[2], add=views[3], dX=vdX)
+    assert all(bool((got[k] == want[k]).all()) for k in want)
+    for o, v in zip(out, (vY, vpre, vdX)):
+        v.fill_(5.0)
+        assert bool((o == 5.0).all()), "what lies around the rows stays as it was"
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_in_place_residual_and_added_gradient(kb, kind):
+    n, d = 300, 72
+    X, W, b, R, G, A = inputs(n, d, d, 4)
+    layer = dict(W=dev(W, kind), b=dev(b), act=ref.RELU)
+    x, r, g, a = (dev(z, kind) for z in (X, R, G, A))
+    Y, pre = kb.dense_forward(layer, x, R=r, keep_pre=True)
+    kb.dense_forward(layer, x, R=r, Y=r)
+    assert bool((r == Y).all())
+    own, _ = kb.dense_forward(layer, x, R=x)
+    y, _ = ref.dense_forward(host(x), host(layer["W"]), b.astype(np.float64), ref.RELU, host(x))
+    within(host(own), y, ref.dense_forward_bound(host(x), host(layer["W"]), b.astype(np.float64), ref.RELU, host(x), kind)[0], "R = X")
+    want = kb.dense_backward(layer, x, pre, g, add=a)["dX"]
+    kb.dense_backward(layer, x, pre, g, add=a, dX=a)
+    assert bool((a == want).all())
+
+
+def test_no_rows(kb):
+    import torch
+    layer = dict(W=torch.ones((5, 6), device="cuda"), b=None, act=ref.RELU)
+    X, none = torch.empty((0, 5), device="cuda"), torch.empty((0, 6), device="cuda")
+    Y, pre = kb.dense_forward(layer, X, keep_pre=True)
+    assert tuple(Y.shape) == (0, 6) and tuple(pre.shape) == (0, 6)
+    g = kb.dense_backward(layer, X, none, none)
+    assert tuple(g["dX"].shape) == (0, 5) and not bool(g["dW"].any()) and not bool(g["db"].any())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_numbers_that_are_not_finite(kb, kind):
+    """Infinities, NaN and numbers near the type's largest reach the results that fp32 products of them have, and no others."""
+    import torch
+    n, di, do = 150, 40, 33
+    X, W, b, _, G, _ = inputs(n, di, do, 8)
+    W[3] = np.abs(W[3]) + 0.1
+    X[5, 3], X[7, 3], X[9, 2], X[11, 3] = np.inf, -np.inf, np.nan, 3.3e38 / 64
+    X[13, 3], X[13, 4] = np.inf, np.inf                      # of either sign where W[4] is negative
+    layer = dict(W=dev(W, kind), b=dev(b), act=ref.IDENTITY)
+    x = dev(X, kind)
+    Y, _ = kb.dense_forward(layer, x)
+    with np.errstate(all="ignore"):
+        want = host(x) @ host(layer["W"]) + b
+    got = host(Y)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    inf = np.isinf(want)
+    assert inf.any() and np.array_equal(got[inf], want[inf]) and np.array_equal(np.isinf(got), inf)
+    fine = np.isfinite(want)
+    assert np.abs(got[fine] / want[fine] - 1).max() < 1.0    # and the huge ones are no infinities
+    G[3, 5], G[4, 6] = np.inf, np.nan
+    g = kb.dense_backward(layer, dev(np.ones((n, di)), kind), None, dev(G, kind))
+    with np.errstate(all="ignore"):
+        dX, dW, db = ref.dense_backward(np.ones((n, di)), host(layer["W"]), None, host(dev(G, kind)), ref.IDENTITY)
+    for a, w in ((g["dX"], dX), (g["dW"], dW), (g["db"], db)):
+        a = host(a)
+        assert np.array_equal(np.isnan(a), np.isnan(w)) and np.array_equal(a[np.isinf(w)], w[np.isinf(w)])
+        assert np.array_equal(np.isinf(a), np.isinf(w))
+    relu = dict(layer, act=ref.RELU)
+    y, pre = kb.dense_forward(relu, x, keep_pre=True)
+    assert np.array_equal(np.isnan(host(y)), np.isnan(want)), "ReLU keeps a NaN"
+    assert not bool(torch.isnan(kb.dense_backward(relu, dev(np.ones((n, di)), kind), pre, dev(np.ones((n, do)), kind))["dW"]).any())
+
+
+def test_gradients_against_differences(kb):
+    """L = <C, Y> moved by +-h along a random direction of each input.  Central differences are off by h^2 / 6 of the third
+    derivative (|silu'''| < 0.4, and L is linear else) and by fp32's rounding of Y (about 2^-22 of sum |C Y|) over 2 h."""
+    import torch
+    n, di, do, h = 200, 24, 40, 2.0 ** -6
+    X, W, b, R, C, _ = inputs(n, di, do, 12)
+    rng = np.random.default_rng(3)
+    x, w, bb = dev(X), dev(W), dev(b)
+    layer = dict(W=w, b=bb, act=ref.SILU)
+    c = dev(C)
+    _, pre = kb.dense_forward(layer, x, keep_pre=True)
+    g = kb.dense_backward(layer, x, pre, c)
+    L = lambda X_, W_, b_: float((kb.dense_forward(dict(W=W_, b=b_, act=ref.SILU), X_)[0].double() * c.double()).sum())
+    size = float((kb.dense_forward(layer, x)[0].double() * c.double()).abs().sum())
+    for name, at, grad in (("X", 0, g["dX"]), ("W", 1, g["dW"]), ("b", 2, g["db"])):
+        base = [x, w, bb]
+        step = dev(rng.normal(0, 1, tuple(base[at].shape)))
+        up, down = list(base), list(base)
+        up[at], down[at] = base[at] + h * step, base[at] - h * step
+        got = (L(*up) - L(*down)) / (2 * h)
+        want = float((grad.double() * step.double()).sum())
+        moved = host(step) @ host(w) if at == 0 else host(x) @ host(step) if at == 1 else np.broadcast_to(host(step), (n, do))
+        bound = h * h / 6 * 0.4 * float(np.abs(host(c) * moved ** 3).sum()) + 2.0 ** -22 * size / h + 2.0 ** -20 * float((grad.abs() * step.abs()).sum())
+        assert abs(got - want) <= bound, (name, got, want, bound)
+        assert bound < 0.2 * float((grad.double() ** 2).sum().sqrt() * (step.double() ** 2).sum().sqrt()), "the bound says something"
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_another_stream_and_a_graph(kb, kind):
+    import torch
+    n, di, do = 700, 96, 80
+    X, W, b, R, G, _ = inputs(n, di, do, 2)
+    layer = dict(W=dev(W, kind), b=dev(b), act=ref.SILU)
+    x, r, c = dev(X, kind), dev(R, kind), dev(G, kind)
+    Y, pre = kb.dense_forward(layer, x, R=r, keep_pre=True)
+    g = kb.dense_backward(layer, x, pre, c)
+    want = [Y, pre, g["dX"], g["dW"], g["db"]]
+    out = [torch.zeros_like(t) for t in want]
+    ws = torch.empty(kb.dense_workspace_bytes(layer, n), dtype=torch.uint8, device="cuda")
+
+    def call(stream=None):
+        kb.dense_forward(layer, x, R=r, Y=out[0], pre=out[1], stream=stream)
+        kb.dense_backward(layer, x, out[1], c, dX=out[2], dW=out[3], db=out[4], workspace=ws, stream=stream)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    call(side)
+    side.synchronize()
+    assert all(bool((a == b_).all()) for a, b_ in zip(out, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for rep in range(3):
+        for o in out + [ws]:
+            o.fill_(3)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(bool((a == b_).all()) for a, b_ in zip(out, want)), rep
