@@ -1,0 +1,150 @@
+// What the dense layer's kernels share: accesses of eight elements at any element's address, the activations, and the
+// arguments of a product C[i][j] = sum_k A[i][k] B[k][j].
+#pragma once
+#include "common.h"
+#include "split_bf16.h"
+
+#include <type_traits>
+
+namespace dense {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+enum { FORWARD = 0, INPUT = 1, WEIGHTS = 2 };
+
+__device__ __forceinline__ float bf(uint32_t w16) { return __uint_as_float(w16 << 16); }
+
+// 8 consecutive elements from a (n of them exist; the others read as zeros).  Rows may start at any element: the loads ask
+// for no more alignment than an element has
+struct __attribute__((packed, aligned(4))) F8 { float x[8]; };
+struct __attribute__((packed, aligned(2))) H8 { uint32_t w[4]; };
+__device__ __forceinline__ void load8(const float *a, int n, float x[8])
+{
+    if (n >= 8) {
+        const F8 q = *reinterpret_cast<const F8 *>(a);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = q.x[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = k < n ? a[k] : 0.f;
+    }
+}
+__device__ __forceinline__ uint4 load8(const uint16_t *a, int n)
+{
+    if (n >= 8) {
+        const H8 q = *reinterpret_cast<const H8 *>(a);
+        return make_uint4(q.w[0], q.w[1], q.w[2], q.w[3]);
+    }
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = (2 * k < n ? a[2 * k] : 0u) | (2 * k + 1 < n ? (uint32_t)a[2 * k + 1] << 16 : 0u);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void spread(uint4 q, float x[8])
+{
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { x[2 * k] = bf(w[k] & 0xffffu); x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_of(float z)
+{
+    return ACT == KGE_ACT_RELU ? (z < 0.f ? 0.f : z) : ACT == KGE_ACT_SILU ? z * __builtin_amdgcn_rcpf(1.f + __expf(-z)) : z;
+}
+template <int ACT>
+__device__ __forceinline__ float act_grad(float z)
+{
+    if (ACT == KGE_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+    if (ACT == KGE_ACT_SILU) {
+        const float s = __builtin_amdgcn_rcpf(1.f + __expf(-z));
+        return s * (1.f + z * (1.f - s));
+    }
+    return 1.f;
+}
+
+// the same with the activation as a number (uniform over the launch)
+__device__ __forceinline__ float act_of(float z, int act)
+{
+    return act == KGE_ACT_RELU ? act_of<KGE_ACT_RELU>(z) : act == KGE_ACT_SILU ? act_of<KGE_ACT_SILU>(z) : z;
+}
+__device__ __forceinline__ float act_grad(float z, int act)
+{
+    return act == KGE_ACT_RELU ? act_grad<KGE_ACT_RELU>(z) : act == KGE_ACT_SILU ? act_grad<KGE_ACT_SILU>(z) : 1.f;
+}
+// dY where pre is above zero, two bf16 numbers (a NaN is not above)
+__device__ __forceinline__ uint32_t relu_pair(uint32_t dy, uint32_t z)
+{
+    return (bf(z & 0xffffu) > 0.f ? dy & 0xffffu : 0u) | (__uint_as_float(z & 0xffff0000u) > 0.f ? dy & 0xffff0000u : 0u);
+}
+
+// the first n of 8 numbers to a (n >= 8: all)
+__device__ __forceinline__ void store8(float *a, int n, const float x[8])
+{
+    if (n >= 8) {
+        F8 q;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) q.x[k] = x[k];
+        *reinterpret_cast<F8 *>(a) = q;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) if (k < n) a[k] = x[k];
+    }
+}
+__device__ __forceinline__ void store8(uint16_t *a, int n, const float x[8])
+{
+    H8 q;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q.w[k] = split_round(x[2 * k], x[2 * k + 1]);
+    if (n >= 8) *reinterpret_cast<H8 *>(a) = q;
+    else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) if (k < n) a[k] = (uint16_t)(q.w[k >> 1] >> (16 * (k & 1)));
+    }
+}
+
+__device__ __forceinline__ float elem(const float *a) { return *a; }
+__device__ __forceinline__ float elem(const uint16_t *a) { return bf(*a); }
+__device__ __forceinline__ void put(float *a, float x) { *a = x; }
+__device__ __forceinline__ void put(uint16_t *a, float x) { *a = __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+template <class T>
+struct Args {
+    const T *A, *B;                // as stored (see the table above)
+    int64_t lda, ldb;
+    const T *pre;                  // laid out like the operand that is dP (A of INPUT, B of WEIGHTS)
+    int64_t ldpre;
+    int64_t M;                     // rows of the result
+    int32_t N;                     // its columns
+    int64_t K;                     // terms
+    int64_t chunk;                 // terms per block (WEIGHTS; K otherwise)
+    int32_t tiles_n;
+    int64_t tiles_m;
+    T *C, *pre_out;                // FORWARD: Y, pre;  INPUT: dX
+    int64_t ldc, ldp;
+    const T *add;                  // FORWARD: R;  INPUT: add
+    int64_t ldadd;
+    const float *bias;
+    float *part, *part_b;          // WEIGHTS: [chunks][M][N] sums, [chunks][N] sums of dP's columns (or null)
+};
+
+template <int PARTS>
+__device__ __forceinline__ void to_lds(const float x[8], unsigned char *at, int plane)
+{
+    uint32_t w[3][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const Split3 s = split_pair(x[2 * k], x[2 * k + 1]);
+        w[0][k] = s.w[0]; w[1][k] = s.w[1]; w[2][k] = s.w[2];
+    }
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) *reinterpret_cast<uint4 *>(at + p * plane) = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+}
+
+// dense_rows.hip: FORWARD and INPUT for long matrices of at most ROWS_TERMS terms
+template <class T> constexpr int32_t ROWS_TERMS = sizeof(T) == 4 ? 128 : 256;
+constexpr int64_t ROWS_LONG = 4096;
+template <int MODE, class T> int launch_rows(const Args<T> &a, int act, hipStream_t st);
+
+}  // namespace dense

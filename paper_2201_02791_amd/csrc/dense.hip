@@ -22,96 +22,13 @@
 //
 // The weights' gradient sums over as many rows as there are: they are cut into chunks so that about as many blocks run as
 // the chip holds, each writes its sums to the workspace and a second launch adds them in a fixed order.
-#include "common.h"
-#include "split_bf16.h"
+#include "dense.h"
 
-#include <math.h>
-
-#include <type_traits>
+using namespace dense;
 
 namespace {
 
-typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-
 constexpr int BM = 128, BN = 128, NT = 256;
-enum { FORWARD = 0, INPUT = 1, WEIGHTS = 2 };
-
-__device__ __forceinline__ float bf(uint32_t w16) { return __uint_as_float(w16 << 16); }
-
-// 8 consecutive elements from a (n of them exist; the others read as zeros).  Rows may start at any element: the loads ask
-// for no more alignment than an element has
-struct __attribute__((packed, aligned(4))) F8 { float x[8]; };
-struct __attribute__((packed, aligned(2))) H8 { uint32_t w[4]; };
-__device__ __forceinline__ void load8(const float *a, int n, float x[8])
-{
-    if (n >= 8) {
-        const F8 q = *reinterpret_cast<const F8 *>(a);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = q.x[k];
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = k < n ? a[k] : 0.f;
-    }
-}
-__device__ __forceinline__ uint4 load8(const uint16_t *a, int n)
-{
-    if (n >= 8) {
-        const H8 q = *reinterpret_cast<const H8 *>(a);
-        return make_uint4(q.w[0], q.w[1], q.w[2], q.w[3]);
-    }
-    uint32_t w[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = (2 * k < n ? a[2 * k] : 0u) | (2 * k + 1 < n ? (uint32_t)a[2 * k + 1] << 16 : 0u);
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void spread(uint4 q, float x[8])
-{
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) { x[2 * k] = bf(w[k] & 0xffffu); x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
-}
-
-template <int ACT>
-__device__ __forceinline__ float act_of(float z)
-{
-    return ACT == KGE_ACT_RELU ? (z < 0.f ? 0.f : z) : ACT == KGE_ACT_SILU ? z / (1.f + __expf(-z)) : z;
-}
-template <int ACT>
-__device__ __forceinline__ float act_grad(float z)
-{
-    if (ACT == KGE_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-    if (ACT == KGE_ACT_SILU) {
-        const float s = 1.f / (1.f + __expf(-z));
-        return s * (1.f + z * (1.f - s));
-    }
-    return 1.f;
-}
-
-__device__ __forceinline__ float elem(const float *a) { return *a; }
-__device__ __forceinline__ float elem(const uint16_t *a) { return bf(*a); }
-__device__ __forceinline__ void put(float *a, float x) { *a = x; }
-__device__ __forceinline__ void put(uint16_t *a, float x) { *a = __builtin_bit_cast(uint16_t, (__bf16)x); }
-
-template <class T>
-struct Args {
-    const T *A, *B;                // as stored (see the table above)
-    int64_t lda, ldb;
-    const T *pre;                  // laid out like the operand that is dP (A of INPUT, B of WEIGHTS)
-    int64_t ldpre;
-    int64_t M;                     // rows of the result
-    int32_t N;                     // its columns
-    int64_t K;                     // terms
-    int64_t chunk;                 // terms per block (WEIGHTS; K otherwise)
-    int32_t tiles_n;
-    int64_t tiles_m;
-    T *C, *pre_out;                // FORWARD: Y, pre;  INPUT: dX
-    int64_t ldc, ldp;
-    const T *add;                  // FORWARD: R;  INPUT: add
-    int64_t ldadd;
-    const float *bias;
-    float *part, *part_b;          // WEIGHTS: [chunks][M][N] sums, [chunks][N] sums of dP's columns (or null)
-};
 
 // what a thread holds of an operand's next tile: chunks of 8 elements, as fp32 numbers or as bf16 as they lie
 template <bool RAW, int CH>
@@ -119,19 +36,6 @@ struct Held {
     uint4 q[RAW ? CH : 1];
     float x[RAW ? 1 : CH][8];
 };
-
-template <int PARTS>
-__device__ __forceinline__ void to_lds(const float x[8], unsigned char *at, int plane)
-{
-    uint32_t w[3][4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const Split3 s = split_pair(x[2 * k], x[2 * k + 1]);
-        w[0][k] = s.w[0]; w[1][k] = s.w[1]; w[2][k] = s.w[2];
-    }
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) *reinterpret_cast<uint4 *>(at + p * plane) = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
-}
 
 template <int MODE, class T, int ACT>
 struct Shape {
@@ -254,14 +158,8 @@ __global__ __launch_bounds__(NT) void k_dense(Args<T> a)
             if constexpr (P == 1) {
                 uint4 q = h.q[j];
                 if (grad) {        // ReLU: dY where pre is above zero (sign clear and not zero; a NaN is not above)
-                    uint32_t d[4] = {q.x, q.y, q.z, q.w};
-                    const uint32_t z[4] = {hg.q[j].x, hg.q[j].y, hg.q[j].z, hg.q[j].w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float lo = bf(z[k] & 0xffffu), hi = __uint_as_float(z[k] & 0xffff0000u);
-                        d[k] = (lo > 0.f ? d[k] & 0xffffu : 0u) | (hi > 0.f ? d[k] & 0xffff0000u : 0u);
-                    }
-                    q = make_uint4(d[0], d[1], d[2], d[3]);
+                    const uint4 z = hg.q[j];
+                    q = make_uint4(relu_pair(q.x, z.x), relu_pair(q.y, z.y), relu_pair(q.z, z.z), relu_pair(q.w, z.w));
                 }
                 *reinterpret_cast<uint4 *>(at) = q;
                 if (columns) {
@@ -439,6 +337,12 @@ void with_act(int act, F f)
 template <int MODE, class T>
 int launch(const kge_dense *L, Args<T> a, hipStream_t st)
 {
+    if constexpr (MODE != WEIGHTS) {
+        if (a.M >= ROWS_LONG && a.K <= ROWS_TERMS<T>) {
+            KGE_PROF(MODE == FORWARD ? "dense_rows" : "dense_rows_input_grad", st);
+            return launch_rows<MODE, T>(a, L->act, st);
+        }
+    }
     a.tiles_m = cdiv(a.M, BM);
     a.tiles_n = (int32_t)cdiv(a.N, BN);
     int64_t blocks = a.tiles_m * a.tiles_n;
