@@ -28,45 +28,50 @@ using namespace dense;
 
 namespace {
 
-constexpr int BM = 128, BN = 128, NT = 256;
-
-// what a thread holds of an operand's next tile: chunks of 8 elements, as fp32 numbers or as bf16 as they lie
-template <bool RAW, int CH>
+// what a thread holds of an operand's next tile: chunks of 8 elements as they lie in memory
+template <bool F32, int CH>
 struct Held {
-    uint4 q[RAW ? CH : 1];
-    float x[RAW ? 1 : CH][8];
+    uint4 q[F32 ? 1 : CH];
+    float x[F32 ? CH : 1][8];
 };
 
-template <int MODE, class T, int ACT>
+// A block's tile of BM x BN results, WM x WN wavefronts, (BM / WM) x (BN / WN) each
+template <int MODE, class T, int ACT, int BM, int BN, int WM, int WN>
 struct Shape {
     static constexpr bool F32 = sizeof(T) == 4;
     static constexpr bool SOFT = !F32 && ACT == KGE_ACT_SILU;          // dP of bf16 rows that is no bf16 number
     static constexpr int PA = F32 ? 3 : MODE == INPUT && SOFT ? 2 : 1;
     static constexpr int PB = F32 ? 3 : MODE == WEIGHTS && SOFT ? 3 : 1;
     static constexpr bool ROWA = MODE != WEIGHTS, ROWB = MODE == INPUT;    // terms side by side
-    static constexpr int BK = PA + PB > 2 ? 32 : 64;
-    static constexpr int LDS = (PA * BM + PB * BN) * BK * 2;
-    static constexpr int CH = BM * BK / 8 / NT;                        // chunks of 8 per thread and operand
+    static constexpr int NT = 64 * WM * WN, MI = BM / 32 / WM, NJ = BN / 32 / WN;
+    static constexpr int BK = (PA + PB > 2 && BM > 32 && BN > 32) || BM == 256 ? 32 : 64;
+    static constexpr int CHA = BM * BK / 8 / NT, CHB = BN * BK / 8 / NT;   // chunks of 8 per thread
+    static constexpr int PLANEA = BM * BK * 2, PLANEB = BN * BK * 2;
+    static constexpr int LDS = PA * PLANEA + PB * PLANEB;
+    static_assert(CHA * 8 * NT == BM * BK && CHB * 8 * NT == BN * BK, "whole chunks");
+    static_assert(LDS >= NT * 32, "the columns' sums");
 };
 
-// The place of chunk (r, c) of a tile: rows of BK terms (a row is 64 or 128 bytes), or rows of 128 columns (256 bytes)
+// The place of chunk (r, c) of a tile: rows of BK terms (a row is 64 or 128 bytes), or rows of W columns, whose blocks of 64
+// bytes are what a transposing read takes from four rows at a time
 template <int BK>
 __device__ __forceinline__ int term_place(int r, int c)
 {
     constexpr int PER = BK / 8;
     return r * (2 * BK) + ((c ^ (PER == 4 ? (r >> 1) & 3 : r & 7)) << 4);
 }
-__device__ __forceinline__ int column_place(int k, int c) { return k * 256 + ((c ^ (4 * (k & 3))) << 4); }
+template <int W>
+__device__ __forceinline__ int column_swap(int k) { return W >= 128 ? k & 3 : W == 64 ? (k >> 1) & 1 : 0; }
+template <int W>
+__device__ __forceinline__ int column_place(int k, int c) { return k * (2 * W) + ((c ^ (4 * column_swap<W>(k))) << 4); }
 
-template <int MODE, class T, int ACT>
-__global__ __launch_bounds__(NT) void k_dense(Args<T> a)
+template <int MODE, class T, int ACT, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
 {
-    typedef Shape<MODE, T, ACT> S;
-    constexpr int BK = S::BK, PA = S::PA, PB = S::PB, CH = S::CH;
-    constexpr bool RAWA = PA == 1, RAWB = PB == 1;
-    constexpr int PLANE = BM * BK * 2;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[S::LDS];
-    unsigned char *const la = smem, *const lb = smem + PA * PLANE;
+    typedef Shape<MODE, T, ACT, BM, BN, WM, WN> S;
+    constexpr int BK = S::BK, PA = S::PA, PB = S::PB, NT = S::NT, MI = S::MI, NJ = S::NJ;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    unsigned char *const la = smem, *const lb = smem + PA * S::PLANEA;
 
     // block -> (tile of rows, tile of columns, chunk of terms).  Workgroup i runs on XCD i % 8, each with its own L2: the
     // tiles that read the same long rows follow one another on one XCD
@@ -96,68 +101,73 @@ __global__ __launch_bounds__(NT) void k_dense(Args<T> a)
     }
     const int64_t m0 = tm * BM, k_beg = chunk * a.chunk, k_end = min(k_beg + a.chunk, a.K);
     const int32_t n0 = tn * BN;
-    const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w >> 1, wn = w & 1;
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w / WN, wn = w % WN;
 
-    Held<RAWA, CH> ha, hp;
-    Held<RAWB, CH> hb, hq;         // hp, hq: pre of the operand that is dP
+    Held<S::F32, S::CHA> ha, hp;
+    Held<S::F32, S::CHB> hb, hq;   // hp, hq: pre of the operand that is dP
     constexpr bool GRAD = MODE != FORWARD && ACT != KGE_ACT_IDENTITY;
 
-    // chunk j of this thread in a tile of terms / of columns: (row, chunk in the row)
-    auto term_at = [&](int j, int &r, int &c) { const int i = j * NT + t; r = i / (BK / 8); c = i % (BK / 8); };
-    auto column_at = [&](int j, int &r, int &c) { const int i = j * NT + t; r = i / 16; c = i % 16; };
-
+    // chunk j of this thread in a tile of terms: row (j NT + t) / (BK / 8); of W columns: term (j NT + t) / (W / 8).  The chunk
+    // in the row is the same for every j
+    constexpr int TC = BK / 8, AC = BM / 8, BC = BN / 8;
+    static_assert(NT % TC == 0 && NT % AC == 0 && NT % BC == 0, "one chunk of a row per thread");
     auto fetch = [&](int64_t k0) __attribute__((always_inline)) {
-        auto one = [&](auto &h, auto raw, int j, const T *base, int64_t ld, bool rows, int64_t outer0, int64_t outer_n) __attribute__((always_inline)) {
-            int r, c;
+        const int left = (int)min((int64_t)BK, k_end - k0);
+        auto one = [&](auto &h, int j, const T *base, int64_t ld, auto terms, auto per, int64_t outer0, int64_t outer_n) __attribute__((always_inline)) {
+            constexpr int PER = decltype(per)::value;
+            const int r = (j * NT + t) / PER, c = t % PER;
             const T *p;
             int n;
-            if (rows) {            // terms side by side: row outer0 + r, terms k0 + 8 c
-                term_at(j, r, c);
+            if constexpr (decltype(terms)::value) {      // row outer0 + r, terms k0 + 8 c
                 p = base + (outer0 + r) * ld + k0 + 8 * c;
-                n = outer0 + r < outer_n ? (int)min((int64_t)8, k_end - k0 - 8 * c) : 0;
-            } else {               // columns side by side: term k0 + r, columns outer0 + 8 c
-                column_at(j, r, c);
+                n = outer0 + r < outer_n ? left - 8 * c : 0;
+            } else {                                     // term k0 + r, columns outer0 + 8 c
                 p = base + (k0 + r) * ld + outer0 + 8 * c;
-                n = k0 + r < k_end ? (int)min((int64_t)8, outer_n - outer0 - 8 * c) : 0;
+                n = r < left ? (int)min((int64_t)8, outer_n - outer0 - 8 * c) : 0;
             }
             if constexpr (S::F32) load8(p, n, h.x[j]);
-            else if constexpr (decltype(raw)::value) h.q[j] = load8(p, n);
-            else spread(load8(p, n), h.x[j]);
+            else h.q[j] = load8(p, n);
         };
-        const std::integral_constant<bool, RAWA> rawa{};
-        const std::integral_constant<bool, RAWB> rawb{};
+        const std::integral_constant<bool, S::ROWA> ra{};
+        const std::integral_constant<bool, S::ROWB> rb{};
+        const std::integral_constant<int, S::ROWA ? TC : AC> ca{};
+        const std::integral_constant<int, S::ROWB ? TC : BC> cb{};
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
-            one(ha, rawa, j, a.A, a.lda, S::ROWA, m0, a.M);
-            if constexpr (MODE == INPUT && GRAD) one(hp, rawa, j, a.pre, a.ldpre, true, m0, a.M);
-            one(hb, rawb, j, a.B, a.ldb, S::ROWB, n0, a.N);
-            if constexpr (MODE == WEIGHTS && GRAD) one(hq, rawb, j, a.pre, a.ldpre, false, n0, a.N);
+        for (int j = 0; j < S::CHA; ++j) {
+            one(ha, j, a.A, a.lda, ra, ca, m0, a.M);
+            if constexpr (MODE == INPUT && GRAD) one(hp, j, a.pre, a.ldpre, ra, ca, m0, a.M);
+        }
+#pragma unroll
+        for (int j = 0; j < S::CHB; ++j) {
+            one(hb, j, a.B, a.ldb, rb, cb, n0, a.N);
+            if constexpr (MODE == WEIGHTS && GRAD) one(hq, j, a.pre, a.ldpre, rb, cb, n0, a.N);
         }
     };
 
-    floatx16 acc[2][2];
+    floatx16 acc[MI][NJ];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-    float col[8];                  // WEIGHTS: sums of dP over this thread's rows, its 8 columns (the same in every chunk)
+    float col[8];                  // WEIGHTS: sums of dP over this thread's rows, its 8 columns
 #pragma unroll
     for (int k = 0; k < 8; ++k) col[k] = 0.f;
     const bool sum_columns = MODE == WEIGHTS && a.part_b && tm == 0;
 
     // registers -> LDS, dY -> dP on the way
     auto stage = [&]() __attribute__((always_inline)) {
-        auto one = [&](auto &h, auto &hg, int j, unsigned char *lds, bool rows, auto parts, bool grad, bool columns) __attribute__((always_inline)) {
-            constexpr int P = decltype(parts)::value;
-            int r, c;
-            if (rows) term_at(j, r, c);
-            else column_at(j, r, c);
-            unsigned char *at = lds + (rows ? term_place<BK>(r, c) : column_place(r, c));
+        auto one = [&](const auto &h, const auto &hg, int j, unsigned char *lds, auto terms, auto per, auto parts, int plane, auto grad,
+                       bool columns) __attribute__((always_inline)) {
+            constexpr int PER = decltype(per)::value, P = decltype(parts)::value;
+            const int r = (j * NT + t) / PER, c = t % PER;
+            unsigned char *at = lds;
+            if constexpr (decltype(terms)::value) at += term_place<BK>(r, c);
+            else at += column_place<PER * 8>(r, c);
             if constexpr (P == 1) {
                 uint4 q = h.q[j];
-                if (grad) {        // ReLU: dY where pre is above zero (sign clear and not zero; a NaN is not above)
+                if constexpr (decltype(grad)::value) {   // ReLU
                     const uint4 z = hg.q[j];
                     q = make_uint4(relu_pair(q.x, z.x), relu_pair(q.y, z.y), relu_pair(q.z, z.z), relu_pair(q.w, z.w));
                 }
@@ -169,31 +179,52 @@ __global__ __launch_bounds__(NT) void k_dense(Args<T> a)
                     for (int k = 0; k < 8; ++k) col[k] += x[k];
                 }
             } else {
-                float x[8];
+                float x[8], z[8];
+                if constexpr (S::F32) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = grad ? h.x[j][k] * act_grad<ACT>(hg.x[j][k]) : h.x[j][k];
-                to_lds<P>(x, at, PLANE);
+                    for (int k = 0; k < 8; ++k) x[k] = h.x[j][k];
+                } else spread(h.q[j], x);
+                if constexpr (decltype(grad)::value) {
+                    if constexpr (S::F32) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) z[k] = hg.x[j][k];
+                    } else spread(hg.q[j], z);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] *= act_grad<ACT>(z[k]);
+                }
+                to_lds<P>(x, at, plane);
                 if (columns)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) col[k] += x[k];
             }
         };
+        const std::integral_constant<bool, S::ROWA> ra{};
+        const std::integral_constant<bool, S::ROWB> rb{};
+        const std::integral_constant<int, S::ROWA ? TC : AC> ca{};
+        const std::integral_constant<int, S::ROWB ? TC : BC> cb{};
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
-            one(ha, hp, j, la, S::ROWA, std::integral_constant<int, PA>(), MODE == INPUT && GRAD, false);
-            one(hb, hq, j, lb, S::ROWB, std::integral_constant<int, PB>(), MODE == WEIGHTS && GRAD, sum_columns);
-        }
+        for (int j = 0; j < S::CHA; ++j)
+            one(ha, hp, j, la, ra, ca, std::integral_constant<int, PA>(), S::PLANEA, std::integral_constant<bool, MODE == INPUT && GRAD>(), false);
+#pragma unroll
+        for (int j = 0; j < S::CHB; ++j)
+            one(hb, hq, j, lb, rb, cb, std::integral_constant<int, PB>(), S::PLANEB, std::integral_constant<bool, MODE == WEIGHTS && GRAD>(),
+                sum_columns);
     };
 
     // operand of the matrix instruction: row (or column) lane % 32 of block `blk` of 32, terms ks + 8 (lane / 32) ..
     const int l16 = lane & 15, kr0 = 8 * (lane >> 5) + (l16 >> 2);
-    const int cb = (16 * ((lane >> 4) & 1) + 4 * (l16 & 3)) * 2, sw = ((l16 >> 2) & 3) << 6;
-    auto frag = [&](const unsigned char *lds, bool rows, int blk, int ks) __attribute__((always_inline)) -> uint4 {
-        if (rows) return *reinterpret_cast<const uint4 *>(lds + term_place<BK>(32 * blk + (lane & 31), ks / 8 + (lane >> 5)));
-        const unsigned char *p = lds + (ks + kr0) * 256 + (((blk * 64) ^ sw) + cb);
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)p);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)(p + 4 * 256));
-        return __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    const int cb = (16 * ((lane >> 4) & 1) + 4 * (l16 & 3)) * 2;
+    auto frag = [&](const unsigned char *lds, auto terms, auto width, int blk, int ks) __attribute__((always_inline)) -> uint4 {
+        if constexpr (decltype(terms)::value)
+            return *reinterpret_cast<const uint4 *>(lds + term_place<BK>(32 * blk + (lane & 31), ks / 8 + (lane >> 5)));
+        else {
+            constexpr int W = decltype(width)::value;
+            // rows kr0 and kr0 + 4 of a step, and those of later steps, are swapped alike
+            const unsigned char *p = lds + (ks + kr0) * (2 * W) + (((blk ^ column_swap<W>(kr0)) << 6) + cb);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)p);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)(p + 4 * 2 * W));
+            return __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
     };
 
     fetch(k_beg);
@@ -203,15 +234,17 @@ __global__ __launch_bounds__(NT) void k_dense(Args<T> a)
         if (k0 + BK < k_end) fetch(k0 + BK);
 #pragma unroll
         for (int ks = 0; ks < BK; ks += 16) {
-            uint4 fa[PA][2], fb[PB][2];
+            uint4 fa[PA][MI], fb[PB][NJ];
 #pragma unroll
             for (int p = 0; p < PA; ++p)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) fa[p][i] = frag(la + p * PLANE, S::ROWA, 2 * wm + i, ks);
+                for (int i = 0; i < MI; ++i)
+                    fa[p][i] = frag(la + p * S::PLANEA, std::integral_constant<bool, S::ROWA>(), std::integral_constant<int, BM>(), MI * wm + i, ks);
 #pragma unroll
             for (int p = 0; p < PB; ++p)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) fb[p][j] = frag(lb + p * PLANE, S::ROWB, 2 * wn + j, ks);
+                for (int j = 0; j < NJ; ++j)
+                    fb[p][j] = frag(lb + p * S::PLANEB, std::integral_constant<bool, S::ROWB>(), std::integral_constant<int, BN>(), NJ * wn + j, ks);
             // smallest products first; of three parts each, those of 2^-24 of the product and below are left out
 #pragma unroll
             for (int s = PA + PB - 2; s >= 0; --s) {
@@ -221,9 +254,9 @@ __global__ __launch_bounds__(NT) void k_dense(Args<T> a)
                     const int pb = s - pa;
                     if (pb < 0 || pb >= PB) continue;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                    for (int i = 0; i < MI; ++i)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) acc[i][j] = split_mfma(fa[pa][i], fb[pb][j], acc[i][j]);
+                        for (int j = 0; j < NJ; ++j) acc[i][j] = split_mfma(fa[pa][i], fb[pb][j], acc[i][j]);
                 }
             }
         }
@@ -245,15 +278,15 @@ __global__ __launch_bounds__(NT) void k_dense(Args<T> a)
 
     // register v of lane l: row 8 (v / 4) + 4 (l / 32) + v % 4 and column l % 32 of the 32 x 32 block
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t n = n0 + 64 * wn + 32 * j + (lane & 31);
+        for (int j = 0; j < NJ; ++j) {
+            const int64_t n = n0 + 32 * (NJ * wn + j) + (lane & 31);
             if (n >= a.N) continue;
             const float b = MODE == FORWARD && a.bias ? a.bias[n] : 0.f;
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                const int64_t m = m0 + 64 * wm + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
+                const int64_t m = m0 + 32 * (MI * wm + i) + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
                 if (m >= a.M) continue;
                 float x = acc[i][j][v];
                 if (PA + PB > 2 && split_not_finite(x)) x = again(m, n);
@@ -271,36 +304,41 @@ __global__ __launch_bounds__(NT) void k_dense(Args<T> a)
                 }
             }
         }
-    if (MODE == WEIGHTS && sum_columns) {        // 16 threads hold the same columns: added in their order
+    if (MODE == WEIGHTS && sum_columns) {        // NT / BC threads hold the same columns: added in their order
         float *s = reinterpret_cast<float *>(smem);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s[(t >> 4) * 128 + (t & 15) * 8 + k] = col[k];
+        for (int k = 0; k < 8; ++k) s[(t / BC) * BN + (t % BC) * 8 + k] = col[k];
         __syncthreads();
-        if (t < 128 && n0 + t < a.N) {
+        if (t < BN && n0 + t < a.N) {
             float x = 0.f;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) x += s[r * 128 + t];
+#pragma unroll 16
+            for (int r = 0; r < NT / BC; ++r) x += s[r * BN + t];
             a.part_b[chunk * a.N + n0 + t] = x;
         }
     }
 }
 
-// dW and db from the chunks' sums, in the chunks' order: 64 elements a block, 4 chunks side by side
-__global__ __launch_bounds__(256) void k_dense_sum(const float *__restrict__ part, const float *__restrict__ part_b, int64_t chunks, int64_t nw,
-                                                   int64_t nb, float *__restrict__ dW, float *__restrict__ db)
+// dW and db from the chunks' sums: 32 elements a block, 32 runs of chunks side by side, then these in their order
+__global__ __launch_bounds__(1024) void k_dense_sum(const float *__restrict__ part, const float *__restrict__ part_b, int64_t chunks, int64_t nw,
+                                                    int64_t nb, float *__restrict__ dW, float *__restrict__ db)
 {
-    __shared__ float s[4][64];
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-    const int64_t i = (int64_t)blockIdx.x * 64 + x;
+    __shared__ float s[32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t i = (int64_t)blockIdx.x * 32 + x;
     const bool w = i < nw;
     const float *from = w ? part + i : part_b + (i - nw);
     const int64_t step = w ? nw : nb;
     float v = 0.f;
     if (i < nw + nb)
-        for (int64_t c = y; c < chunks; c += 4) v += from[c * step];
+        for (int64_t c = y; c < chunks; c += 32) v += from[c * step];
     s[y][x] = v;
     __syncthreads();
-    if (y == 0 && i < nw + nb) (w ? dW + i : db + (i - nw))[0] = (s[0][x] + s[1][x]) + (s[2][x] + s[3][x]);
+    if (y == 0 && i < nw + nb) {
+        v = 0.f;
+#pragma unroll
+        for (int r = 0; r < 32; ++r) v += s[r][x];
+        (w ? dW + i : db + (i - nw))[0] = v;
+    }
 }
 
 constexpr int32_t MAX_D = 65536;
@@ -316,17 +354,30 @@ int check(const kge_dense *L, int64_t n_rows)
     return KGE_OK;
 }
 
-// chunks of rows of the weights' gradient: about three blocks for each of the 256 compute units, at least 512 rows each
+// The weights' gradient has the smallest tile that takes a narrow side whole: what is empty of a tile is multiplied all the same.  bf16
+// results of 129 columns and more on both sides take a tile of 256 x 256, whose rows are read, and turned into dP, half as often.
+struct Tile { int bm, bn; };
+Tile weights_tile(const kge_dense *L)
+{
+    if (L->d_out <= 32) return {128, 32};
+    if (L->d_out <= 64) return {128, 64};
+    if (L->d_in <= 32) return {32, 128};
+    if (L->dtype == KGE_DT_BF16 && L->d_in > 128 && L->d_out > 128) return {256, 256};
+    return {128, 128};
+}
+
+// chunks of rows of the weights' gradient: about as many blocks as run at once, at least 512 rows each
 int64_t chunk_rows(const kge_dense *L, int64_t n_rows)
 {
-    const int64_t tiles = cdiv(L->d_in, BM) * cdiv(L->d_out, BN);
-    int64_t chunks = cdiv(768, tiles);
+    const Tile tile = weights_tile(L);
+    const int64_t tiles = cdiv(L->d_in, tile.bm) * cdiv(L->d_out, tile.bn);
+    int64_t chunks = cdiv(tile.bm == 256 ? 256 : 512, tiles);
     if (chunks > cdiv(n_rows, 512)) chunks = cdiv(n_rows, 512);
     if (chunks < 1) chunks = 1;
     return align_up((size_t)cdiv(n_rows > 0 ? n_rows : 1, chunks), 64);
 }
 
-template <class T, class F>
+template <class F>
 void with_act(int act, F f)
 {
     if (act == KGE_ACT_RELU) f(std::integral_constant<int, KGE_ACT_RELU>());
@@ -334,15 +385,9 @@ void with_act(int act, F f)
     else f(std::integral_constant<int, KGE_ACT_IDENTITY>());
 }
 
-template <int MODE, class T>
-int launch(const kge_dense *L, Args<T> a, hipStream_t st)
+template <int MODE, class T, int BM, int BN, int WM, int WN>
+int launch_tile(int act, Args<T> a, hipStream_t st)
 {
-    if constexpr (MODE != WEIGHTS) {
-        if (a.M >= ROWS_LONG && a.K <= ROWS_TERMS<T>) {
-            KGE_PROF(MODE == FORWARD ? "dense_rows" : "dense_rows_input_grad", st);
-            return launch_rows<MODE, T>(a, L->act, st);
-        }
-    }
     a.tiles_m = cdiv(a.M, BM);
     a.tiles_n = (int32_t)cdiv(a.N, BN);
     int64_t blocks = a.tiles_m * a.tiles_n;
@@ -351,10 +396,39 @@ int launch(const kge_dense *L, Args<T> a, hipStream_t st)
         blocks *= chunks >= 8 ? (int64_t)align_up((size_t)chunks, 8) : chunks;
     } else if (a.tiles_m >= 64) blocks = (int64_t)align_up((size_t)a.tiles_m, 8) * a.tiles_n;
     KGE_REQUIRE(blocks <= 0x7fffffffLL, KGE_ERANGE, "dense: too large for one launch");
-    KGE_PROF(MODE == FORWARD ? "dense" : MODE == INPUT ? "dense_input_grad" : "dense_weight_grad", st);
-    with_act<T>(L->act, [&](auto act) { k_dense<MODE, T, act.value><<<(unsigned)blocks, NT, 0, st>>>(a); });
+    hipError_t e = hipSuccess;
+    with_act(act, [&](auto act_c) {
+        constexpr int ACT = decltype(act_c)::value, LDS = Shape<MODE, T, ACT, BM, BN, WM, WN>::LDS;
+        auto kernel = k_dense<MODE, T, ACT, BM, BN, WM, WN>;
+        if (LDS > 64 * 1024) e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+        if (e == hipSuccess) kernel<<<(unsigned)blocks, 64 * WM * WN, LDS, st>>>(a);
+    });
+    KGE_HIP(e);
     KGE_LAUNCH_CHECK();
     return KGE_OK;
+}
+
+template <int MODE, class T>
+int launch(const kge_dense *L, const Args<T> &a, hipStream_t st)
+{
+    if constexpr (MODE == WEIGHTS) {
+        KGE_PROF("dense_weight_grad", st);
+        const Tile tile = weights_tile(L);
+        if (tile.bn == 32) return launch_tile<MODE, T, 128, 32, 4, 1>(L->act, a, st);
+        if (tile.bn == 64) return launch_tile<MODE, T, 128, 64, 2, 2>(L->act, a, st);
+        if (tile.bm == 32) return launch_tile<MODE, T, 32, 128, 1, 4>(L->act, a, st);
+        if constexpr (sizeof(T) == 2) {
+            if (tile.bm == 256) return launch_tile<MODE, T, 256, 256, 4, 2>(L->act, a, st);
+        }
+        return launch_tile<MODE, T, 128, 128, 2, 2>(L->act, a, st);
+    } else {
+        if (a.M >= ROWS_LONG && a.K <= ROWS_TERMS<T>) {
+            KGE_PROF(MODE == FORWARD ? "dense_rows" : "dense_rows_input_grad", st);
+            return launch_rows<MODE, T>(a, L->act, st);
+        }
+        KGE_PROF(MODE == FORWARD ? "dense" : "dense_input_grad", st);
+        return launch_tile<MODE, T, 128, 128, 2, 2>(L->act, a, st);
+    }
 }
 
 bool at_element(const void *p, int32_t dtype) { return ((uintptr_t)p % (dtype == KGE_DT_BF16 ? 2 : 4)) == 0; }
@@ -395,7 +469,7 @@ int backward(const kge_dense *L, int64_t n, const void *X, int64_t ldx, const vo
         }
         KGE_PROF("dense_sum", st);             // without rows: sums of nothing, zeros
         const int64_t w = dW ? nw : 0, b = db ? L->d_out : 0;
-        k_dense_sum<<<(unsigned)cdiv(w + b, 64), 256, 0, st>>>(a.part, a.part_b, chunks, w, b, dW, db);
+        k_dense_sum<<<(unsigned)cdiv(w + b, 32), 1024, 0, st>>>(a.part, a.part_b, chunks, w, b, dW, db);
         KGE_LAUNCH_CHECK();
     }
     return KGE_OK;
