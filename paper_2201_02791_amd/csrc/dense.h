@@ -19,26 +19,37 @@ __device__ __forceinline__ float bf(uint32_t w16) { return __uint_as_float(w16 <
 // for no more alignment than an element has
 struct __attribute__((packed, aligned(4))) F8 { float x[8]; };
 struct __attribute__((packed, aligned(2))) H8 { uint32_t w[4]; };
+__device__ __forceinline__ void load8(const float *a, float x[8])
+{
+    const F8 q = *reinterpret_cast<const F8 *>(a);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = q.x[k];
+}
+__device__ __forceinline__ uint4 load8(const uint16_t *a)
+{
+    const H8 q = *reinterpret_cast<const H8 *>(a);
+    return make_uint4(q.w[0], q.w[1], q.w[2], q.w[3]);
+}
 __device__ __forceinline__ void load8(const float *a, int n, float x[8])
 {
-    if (n >= 8) {
-        const F8 q = *reinterpret_cast<const F8 *>(a);
+    if (n >= 8) load8(a, x);
+    else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = q.x[k];
-    } else {
+        for (int k = 0; k < 8; ++k) x[k] = 0.f;
+        if (n > 0) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = k < n ? a[k] : 0.f;
+            for (int k = 0; k < 7; ++k) if (k < n) x[k] = a[k];
+        }
     }
 }
 __device__ __forceinline__ uint4 load8(const uint16_t *a, int n)
 {
-    if (n >= 8) {
-        const H8 q = *reinterpret_cast<const H8 *>(a);
-        return make_uint4(q.w[0], q.w[1], q.w[2], q.w[3]);
-    }
-    uint32_t w[4];
+    if (n >= 8) return load8(a);
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    if (n > 0) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = (2 * k < n ? a[2 * k] : 0u) | (2 * k + 1 < n ? (uint32_t)a[2 * k + 1] << 16 : 0u);
+        for (int k = 0; k < 7; ++k) if (k < n) w[k >> 1] |= (uint32_t)a[k] << (16 * (k & 1));
+    }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ void spread(uint4 q, float x[8])
@@ -48,17 +59,19 @@ __device__ __forceinline__ void spread(uint4 q, float x[8])
     for (int k = 0; k < 4; ++k) { x[2 * k] = bf(w[k] & 0xffffu); x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
 }
 
+// e^-z; below 2^-126 it is zero beside the one that it is added to
+__device__ __forceinline__ float exp_minus(float z) { return __builtin_amdgcn_exp2f(z * -1.44269504f); }
 template <int ACT>
 __device__ __forceinline__ float act_of(float z)
 {
-    return ACT == KGE_ACT_RELU ? (z < 0.f ? 0.f : z) : ACT == KGE_ACT_SILU ? z * __builtin_amdgcn_rcpf(1.f + __expf(-z)) : z;
+    return ACT == KGE_ACT_RELU ? (z < 0.f ? 0.f : z) : ACT == KGE_ACT_SILU ? z * __builtin_amdgcn_rcpf(1.f + exp_minus(z)) : z;
 }
 template <int ACT>
 __device__ __forceinline__ float act_grad(float z)
 {
     if (ACT == KGE_ACT_RELU) return z > 0.f ? 1.f : 0.f;
     if (ACT == KGE_ACT_SILU) {
-        const float s = __builtin_amdgcn_rcpf(1.f + __expf(-z));
+        const float s = __builtin_amdgcn_rcpf(1.f + exp_minus(z));
         return s * (1.f + z * (1.f - s));
     }
     return 1.f;

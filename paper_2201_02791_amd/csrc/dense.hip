@@ -47,7 +47,10 @@ struct Shape {
     static constexpr int BK = (PA + PB > 2 && BM > 32 && BN > 32) || BM == 256 ? 32 : 64;
     static constexpr int CHA = BM * BK / 8 / NT, CHB = BN * BK / 8 / NT;   // chunks of 8 per thread
     static constexpr int PLANEA = BM * BK * 2, PLANEB = BN * BK * 2;
-    static constexpr int LDS = PA * PLANEA + PB * PLANEB;
+    static constexpr int BUFFER = PA * PLANEA + PB * PLANEB;
+    // a block that has its compute unit to itself stages one tile while it multiplies another
+    static constexpr bool TWO = BM == 256;
+    static constexpr int LDS = (TWO ? 2 : 1) * BUFFER;
     static_assert(CHA * 8 * NT == BM * BK && CHB * 8 * NT == BN * BK, "whole chunks");
     static_assert(LDS >= NT * 32, "the columns' sums");
 };
@@ -71,7 +74,6 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
     typedef Shape<MODE, T, ACT, BM, BN, WM, WN> S;
     constexpr int BK = S::BK, PA = S::PA, PB = S::PB, NT = S::NT, MI = S::MI, NJ = S::NJ;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    unsigned char *const la = smem, *const lb = smem + PA * S::PLANEA;
 
     // block -> (tile of rows, tile of columns, chunk of terms).  Workgroup i runs on XCD i % 8, each with its own L2: the
     // tiles that read the same long rows follow one another on one XCD
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
     }
     const int64_t m0 = tm * BM, k_beg = chunk * a.chunk, k_end = min(k_beg + a.chunk, a.K);
     const int32_t n0 = tn * BN;
-    const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w / WN, wn = w % WN;
+    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), wm = w / WN, wn = w % WN;
 
     Held<S::F32, S::CHA> ha, hp;
     Held<S::F32, S::CHB> hb, hq;   // hp, hq: pre of the operand that is dP
@@ -111,37 +113,55 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
     // in the row is the same for every j
     constexpr int TC = BK / 8, AC = BM / 8, BC = BN / 8;
     static_assert(NT % TC == 0 && NT % AC == 0 && NT % BC == 0, "one chunk of a row per thread");
+    // where this thread's first chunk lies when k0 = k_beg, and how far apart its chunks and the tiles are
+    struct Walk { const T *p; int64_t row, tile; int n; };      // n: elements of a chunk that exist, as far as the tile's place goes
+    auto walk = [&](const T *base, int64_t ld, auto terms, auto per, int64_t outer0, int64_t outer_n) __attribute__((always_inline)) -> Walk {
+        constexpr int PER = decltype(per)::value;
+        const int r = t / PER, c = t % PER;
+        if constexpr (decltype(terms)::value) return {base + (outer0 + r) * ld + k_beg + 8 * c, NT / PER * ld, BK, 8};
+        else return {base + (k_beg + r) * ld + outer0 + 8 * c, NT / PER * ld, BK * ld, (int)max((int64_t)0, min((int64_t)8, outer_n - outer0 - 8 * c))};
+    };
+    const std::integral_constant<bool, S::ROWA> ra{};
+    const std::integral_constant<bool, S::ROWB> rb{};
+    const std::integral_constant<int, S::ROWA ? TC : AC> ca{};
+    const std::integral_constant<int, S::ROWB ? TC : BC> cb{};
+    Walk wa = walk(a.A, a.lda, ra, ca, m0, a.M), wb = walk(a.B, a.ldb, rb, cb, n0, a.N), wp{};
+    if constexpr (GRAD) wp = MODE == INPUT ? walk(a.pre, a.ldpre, ra, ca, m0, a.M) : walk(a.pre, a.ldpre, rb, cb, n0, a.N);
+    const bool inside = m0 + BM <= a.M && n0 + BN <= a.N;
+
     auto fetch = [&](int64_t k0) __attribute__((always_inline)) {
         const int left = (int)min((int64_t)BK, k_end - k0);
-        auto one = [&](auto &h, int j, const T *base, int64_t ld, auto terms, auto per, int64_t outer0, int64_t outer_n) __attribute__((always_inline)) {
+        auto one = [&](auto &h, int j, const Walk &x, auto terms, auto per, int64_t outer0, int64_t outer_n, auto whole) __attribute__((always_inline)) {
             constexpr int PER = decltype(per)::value;
-            const int r = (j * NT + t) / PER, c = t % PER;
-            const T *p;
-            int n;
-            if constexpr (decltype(terms)::value) {      // row outer0 + r, terms k0 + 8 c
-                p = base + (outer0 + r) * ld + k0 + 8 * c;
-                n = outer0 + r < outer_n ? left - 8 * c : 0;
-            } else {                                     // term k0 + r, columns outer0 + 8 c
-                p = base + (k0 + r) * ld + outer0 + 8 * c;
-                n = r < left ? (int)min((int64_t)8, outer_n - outer0 - 8 * c) : 0;
+            const T *p = x.p + j * x.row;
+            if constexpr (decltype(whole)::value) {
+                if constexpr (S::F32) load8(p, h.x[j]);
+                else h.q[j] = load8(p);
+            } else {
+                const int r = (j * NT + t) / PER, c = t % PER;
+                int n;
+                if constexpr (decltype(terms)::value) n = outer0 + r < outer_n ? left - 8 * c : 0;
+                else n = r < left ? x.n : 0;
+                if constexpr (S::F32) load8(p, n, h.x[j]);
+                else h.q[j] = load8(p, n);
             }
-            if constexpr (S::F32) load8(p, n, h.x[j]);
-            else h.q[j] = load8(p, n);
         };
-        const std::integral_constant<bool, S::ROWA> ra{};
-        const std::integral_constant<bool, S::ROWB> rb{};
-        const std::integral_constant<int, S::ROWA ? TC : AC> ca{};
-        const std::integral_constant<int, S::ROWB ? TC : BC> cb{};
+        auto all = [&](auto whole) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < S::CHA; ++j) {
-            one(ha, j, a.A, a.lda, ra, ca, m0, a.M);
-            if constexpr (MODE == INPUT && GRAD) one(hp, j, a.pre, a.ldpre, ra, ca, m0, a.M);
-        }
+            for (int j = 0; j < S::CHA; ++j) {
+                one(ha, j, wa, ra, ca, m0, a.M, whole);
+                if constexpr (MODE == INPUT && GRAD) one(hp, j, wp, ra, ca, m0, a.M, whole);
+            }
 #pragma unroll
-        for (int j = 0; j < S::CHB; ++j) {
-            one(hb, j, a.B, a.ldb, rb, cb, n0, a.N);
-            if constexpr (MODE == WEIGHTS && GRAD) one(hq, j, a.pre, a.ldpre, rb, cb, n0, a.N);
-        }
+            for (int j = 0; j < S::CHB; ++j) {
+                one(hb, j, wb, rb, cb, n0, a.N, whole);
+                if constexpr (MODE == WEIGHTS && GRAD) one(hq, j, wp, rb, cb, n0, a.N, whole);
+            }
+        };
+        if (inside && left == BK) all(std::true_type());
+        else all(std::false_type());
+        wa.p += wa.tile; wb.p += wb.tile;
+        if constexpr (GRAD) wp.p += wp.tile;
     };
 
     floatx16 acc[MI][NJ];
@@ -157,7 +177,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
     const bool sum_columns = MODE == WEIGHTS && a.part_b && tm == 0;
 
     // registers -> LDS, dY -> dP on the way
-    auto stage = [&]() __attribute__((always_inline)) {
+    auto stage = [&](unsigned char *la) __attribute__((always_inline)) {
+        unsigned char *const lb = la + PA * S::PLANEA;
         auto one = [&](const auto &h, const auto &hg, int j, unsigned char *lds, auto terms, auto per, auto parts, int plane, auto grad,
                        bool columns) __attribute__((always_inline)) {
             constexpr int PER = decltype(per)::value, P = decltype(parts)::value;
@@ -198,10 +219,6 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
                     for (int k = 0; k < 8; ++k) col[k] += x[k];
             }
         };
-        const std::integral_constant<bool, S::ROWA> ra{};
-        const std::integral_constant<bool, S::ROWB> rb{};
-        const std::integral_constant<int, S::ROWA ? TC : AC> ca{};
-        const std::integral_constant<int, S::ROWB ? TC : BC> cb{};
 #pragma unroll
         for (int j = 0; j < S::CHA; ++j)
             one(ha, hp, j, la, ra, ca, std::integral_constant<int, PA>(), S::PLANEA, std::integral_constant<bool, MODE == INPUT && GRAD>(), false);
@@ -213,25 +230,22 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
 
     // operand of the matrix instruction: row (or column) lane % 32 of block `blk` of 32, terms ks + 8 (lane / 32) ..
     const int l16 = lane & 15, kr0 = 8 * (lane >> 5) + (l16 >> 2);
-    const int cb = (16 * ((lane >> 4) & 1) + 4 * (l16 & 3)) * 2;
+    const int lc = (16 * ((lane >> 4) & 1) + 4 * (l16 & 3)) * 2;
     auto frag = [&](const unsigned char *lds, auto terms, auto width, int blk, int ks) __attribute__((always_inline)) -> uint4 {
         if constexpr (decltype(terms)::value)
             return *reinterpret_cast<const uint4 *>(lds + term_place<BK>(32 * blk + (lane & 31), ks / 8 + (lane >> 5)));
         else {
             constexpr int W = decltype(width)::value;
             // rows kr0 and kr0 + 4 of a step, and those of later steps, are swapped alike
-            const unsigned char *p = lds + (ks + kr0) * (2 * W) + (((blk ^ column_swap<W>(kr0)) << 6) + cb);
+            const unsigned char *p = lds + (ks + kr0) * (2 * W) + (((blk ^ column_swap<W>(kr0)) << 6) + lc);
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)p);
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)(p + 4 * 2 * W));
             return __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
     };
 
-    fetch(k_beg);
-    for (int64_t k0 = k_beg; k0 < k_end; k0 += BK) {
-        stage();
-        __syncthreads();
-        if (k0 + BK < k_end) fetch(k0 + BK);
+    auto multiply = [&](const unsigned char *la) __attribute__((always_inline)) {
+        const unsigned char *const lb = la + PA * S::PLANEA;
 #pragma unroll
         for (int ks = 0; ks < BK; ks += 16) {
             uint4 fa[PA][MI], fb[PB][NJ];
@@ -260,7 +274,30 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
                 }
             }
         }
+    };
+
+    fetch(k_beg);
+    if constexpr (S::TWO) {
+        stage(smem);
+        if (k_beg + BK < k_end) fetch(k_beg + BK);
         __syncthreads();
+        int side = 0;
+        for (int64_t k0 = k_beg; k0 < k_end; k0 += BK, side ^= 1) {
+            // of the two wavefronts that share a SIMD one stages while the other multiplies, and then the other way round
+            if (w < WM * WN / 2) multiply(smem + side * S::BUFFER);
+            if (k0 + BK < k_end) stage(smem + (side ^ 1) * S::BUFFER);       // last read a barrier ago
+            if (k0 + 2 * BK < k_end) fetch(k0 + 2 * BK);
+            if (w >= WM * WN / 2) multiply(smem + side * S::BUFFER);
+            __syncthreads();
+        }
+    } else {
+        for (int64_t k0 = k_beg; k0 < k_end; k0 += BK) {
+            stage(smem);
+            __syncthreads();
+            if (k0 + BK < k_end) fetch(k0 + BK);
+            multiply(smem);
+            __syncthreads();
+        }
     }
 
     // a sum that is not finite: once more from fp32 products, term by term

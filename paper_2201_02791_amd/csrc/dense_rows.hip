@@ -30,7 +30,7 @@ struct Rows {
     static constexpr int WM = WN >= 4 ? 1 : 4 / WN, NW = WN * WM, NT = 64 * NW, TR = 32 * RB * WM;
     static constexpr int STRIDE = KS * 32 + 16, PLANE = TR * STRIDE;
     static constexpr int OUT = 32 * WN + 8;                        // floats per row of sums: 4 rows further, 32 banks further
-    static constexpr int CH = (TR * KS * 2 + NT - 1) / NT;         // chunks of 8 terms per thread and tile
+    static constexpr int CH = TR * KS * 2 / NT;         // chunks of 8 terms per thread and tile
     static constexpr int LDS = P * PLANE > TR * OUT * 4 ? P * PLANE : TR * OUT * 4;
 };
 
@@ -92,29 +92,45 @@ __global__ __launch_bounds__((Rows<MODE, T, SOFT, KS, WN, RB>::NT), 2) void k_de
     const bool grad = MODE == INPUT && r.act != KGE_ACT_IDENTITY;
     Chunks<!F32, CH> hx, hg;
     Chunks<!F32, 2 * RB> hr;
-    auto place = [&](int j, int &row, int &c) { const int i = j * NT + t; row = i / (2 * KS); c = i % (2 * KS); };
     auto load = [&](auto &h, int j, const T *p, int n) __attribute__((always_inline)) {
         if constexpr (F32) load8(p, n, h.x[j]);
         else h.q[j] = load8(p, n);
     };
+    // a thread's chunks: the same one of every (NT / 2 KS)th row
+    static_assert(NT % (2 * KS) == 0 && CH * NT == TR * KS * 2, "whole rows");
+    const int tr = t / (2 * KS), tc = t % (2 * KS);
+    const int tn = K - 8 * tc;
+    const T *pa = a.A + (tile * TR + tr) * a.lda + 8 * tc, *pg = grad ? a.pre + (tile * TR + tr) * a.ldpre + 8 * tc : nullptr;
+    const int64_t step_a = NT / (2 * KS) * a.lda, step_g = NT / (2 * KS) * a.ldpre;
     auto fetch = [&](int64_t ti) __attribute__((always_inline)) {
+        if (K == 16 * KS && ti * TR + TR <= a.M) {
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
-            int row, c;
-            place(j, row, c);
-            const int64_t m = ti * TR + row;
-            const int n = row < TR && m < a.M ? K - 8 * c : 0;
-            load(hx, j, a.A + m * a.lda + 8 * c, n);
-            if (grad) load(hg, j, a.pre + m * a.ldpre + 8 * c, n);
+            for (int j = 0; j < CH; ++j) {
+                if constexpr (F32) load8(pa + j * step_a, hx.x[j]);
+                else hx.q[j] = load8(pa + j * step_a);
+            }
+            if (grad) {
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    if constexpr (F32) load8(pg + j * step_g, hg.x[j]);
+                    else hg.q[j] = load8(pg + j * step_g);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const int n = ti * TR + j * (NT / (2 * KS)) + tr < a.M ? tn : 0;
+                load(hx, j, pa + j * step_a, n);
+                if (grad) load(hg, j, pg + j * step_g, n);
+            }
         }
+        pa += r.lanes * TR * a.lda;
+        if (grad) pg += r.lanes * TR * a.ldpre;
     };
     auto stage = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            int row, c;
-            place(j, row, c);
-            if (CH * NT != TR * KS * 2 && row >= TR) continue;
-            unsigned char *at = smem + row * S::STRIDE + 16 * c;
+            unsigned char *at = smem + (j * (NT / (2 * KS)) + tr) * S::STRIDE + 16 * tc;
             if constexpr (P == 1) {
                 uint4 q = hx.q[j];
                 if (grad) {        // ReLU
