@@ -36,9 +36,11 @@ __device__ __forceinline__ void load8(const float *a, int n, float x[8])
     else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = 0.f;
-        if (n > 0) {
+        if (n > 0) {               // past the end the last element again: no branch parts the loads
 #pragma unroll
-            for (int k = 0; k < 7; ++k) if (k < n) x[k] = a[k];
+            for (int k = 0; k < 7; ++k) x[k] = a[min(k, n - 1)];
+#pragma unroll
+            for (int k = 1; k < 7; ++k) x[k] = k < n ? x[k] : 0.f;
         }
     }
 }
@@ -47,8 +49,11 @@ __device__ __forceinline__ uint4 load8(const uint16_t *a, int n)
     if (n >= 8) return load8(a);
     uint32_t w[4] = {0u, 0u, 0u, 0u};
     if (n > 0) {
+        uint32_t x[7];
 #pragma unroll
-        for (int k = 0; k < 7; ++k) if (k < n) w[k >> 1] |= (uint32_t)a[k] << (16 * (k & 1));
+        for (int k = 0; k < 7; ++k) x[k] = a[min(k, n - 1)];
+#pragma unroll
+        for (int k = 0; k < 7; ++k) w[k >> 1] |= k < n ? x[k] << (16 * (k & 1)) : 0u;
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
@@ -155,9 +160,13 @@ __device__ __forceinline__ void to_lds(const float x[8], unsigned char *at, int 
     for (int p = 0; p < PARTS; ++p) *reinterpret_cast<uint4 *>(at + p * plane) = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
 }
 
-// dense_rows.hip: FORWARD and INPUT for long matrices of at most ROWS_TERMS terms
+// dense_rows_*.hip: FORWARD and INPUT for long matrices of at most ROWS_TERMS terms
 template <class T> constexpr int32_t ROWS_TERMS = sizeof(T) == 4 ? 128 : 256;
 constexpr int64_t ROWS_LONG = 4096;
 template <int MODE, class T> int launch_rows(const Args<T> &a, int act, hipStream_t st);
+template <> int launch_rows<FORWARD, float>(const Args<float> &a, int act, hipStream_t st);
+template <> int launch_rows<FORWARD, uint16_t>(const Args<uint16_t> &a, int act, hipStream_t st);
+template <> int launch_rows<INPUT, float>(const Args<float> &a, int act, hipStream_t st);
+template <> int launch_rows<INPUT, uint16_t>(const Args<uint16_t> &a, int act, hipStream_t st);
 
 }  // namespace dense
