@@ -50,7 +50,9 @@ struct Shape {
     static constexpr int BUFFER = PA * PLANEA + PB * PLANEB;
     // a block that has its compute unit to itself stages one tile while it multiplies another
     static constexpr bool TWO = BM == 256;
-    static constexpr int LDS = (TWO ? 2 : 1) * BUFFER;
+    static constexpr int OUT = 32 * NJ + 8;                            // floats per row of results in LDS: 4 rows further, 32 banks further
+    static constexpr int TILES = (TWO ? 2 : 1) * BUFFER, RESULTS = WM * WN * 32 * OUT * 4;
+    static constexpr int LDS = TILES > RESULTS ? TILES : RESULTS;
     static_assert(CHA * 8 * NT == BM * BK && CHB * 8 * NT == BN * BK, "whole chunks");
     static_assert(LDS >= NT * 32, "the columns' sums");
 };
@@ -105,63 +107,86 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
     const int32_t n0 = tn * BN;
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), wm = w / WN, wn = w % WN;
 
-    Held<S::F32, S::CHA> ha, hp;
-    Held<S::F32, S::CHB> hb, hq;   // hp, hq: pre of the operand that is dP
+    struct Set {
+        Held<S::F32, S::CHA> a, p;
+        Held<S::F32, S::CHB> b, q; // p, q: pre of the operand that is dP
+    };
+    Set set;
     constexpr bool GRAD = MODE != FORWARD && ACT != KGE_ACT_IDENTITY;
 
     // chunk j of this thread in a tile of terms: row (j NT + t) / (BK / 8); of W columns: term (j NT + t) / (W / 8).  The chunk
     // in the row is the same for every j
     constexpr int TC = BK / 8, AC = BM / 8, BC = BN / 8;
     static_assert(NT % TC == 0 && NT % AC == 0 && NT % BC == 0, "one chunk of a row per thread");
-    // where this thread's first chunk lies when k0 = k_beg, and how far apart its chunks and the tiles are
-    struct Walk { const T *p; int64_t row, tile; int n; };      // n: elements of a chunk that exist, as far as the tile's place goes
-    auto walk = [&](const T *base, int64_t ld, auto terms, auto per, int64_t outer0, int64_t outer_n) __attribute__((always_inline)) -> Walk {
+    // Where this thread's chunks lie when k0 = k_beg, and how far apart the tiles are.  Rows and columns past the result's read the
+    // last row or the first chunk in their place: what they add up to is not stored.  Only terms past the end have to be zeros.
+    struct Walk { const T *p[(S::CHA > S::CHB ? S::CHA : S::CHB)]; int64_t tile; };
+    auto walk = [&](const T *base, int64_t ld, auto terms, auto per, auto chunks, int64_t outer0, int64_t outer_n) __attribute__((always_inline)) -> Walk {
         constexpr int PER = decltype(per)::value;
-        const int r = t / PER, c = t % PER;
-        if constexpr (decltype(terms)::value) return {base + (outer0 + r) * ld + k_beg + 8 * c, NT / PER * ld, BK, 8};
-        else return {base + (k_beg + r) * ld + outer0 + 8 * c, NT / PER * ld, BK * ld, (int)max((int64_t)0, min((int64_t)8, outer_n - outer0 - 8 * c))};
+        Walk x;
+#pragma unroll
+        for (int j = 0; j < decltype(chunks)::value; ++j) {
+            const int r = (j * NT + t) / PER, c = t % PER;
+            if constexpr (decltype(terms)::value) x.p[j] = base + min(outer0 + r, outer_n - 1) * ld + k_beg + 8 * c;
+            else x.p[j] = base + (k_beg + r) * ld + (outer0 + 8 * c < outer_n ? outer0 + 8 * c : 0);
+        }
+        x.tile = decltype(terms)::value ? BK : BK * ld;
+        return x;
     };
     const std::integral_constant<bool, S::ROWA> ra{};
     const std::integral_constant<bool, S::ROWB> rb{};
     const std::integral_constant<int, S::ROWA ? TC : AC> ca{};
     const std::integral_constant<int, S::ROWB ? TC : BC> cb{};
-    Walk wa = walk(a.A, a.lda, ra, ca, m0, a.M), wb = walk(a.B, a.ldb, rb, cb, n0, a.N), wp{};
-    if constexpr (GRAD) wp = MODE == INPUT ? walk(a.pre, a.ldpre, ra, ca, m0, a.M) : walk(a.pre, a.ldpre, rb, cb, n0, a.N);
-    const bool inside = m0 + BM <= a.M && n0 + BN <= a.N;
+    const std::integral_constant<int, S::CHA> na{};
+    const std::integral_constant<int, S::CHB> nb{};
+    Walk wa = walk(a.A, a.lda, ra, ca, na, m0, a.M), wb = walk(a.B, a.ldb, rb, cb, nb, n0, a.N), wp{};
+    if constexpr (GRAD) wp = MODE == INPUT ? walk(a.pre, a.ldpre, ra, ca, na, m0, a.M) : walk(a.pre, a.ldpre, rb, cb, nb, n0, a.N);
+    // Tiles up to here load whole chunks: their terms all exist, and a chunk that the end of a row of columns cuts reads on into the
+    // next row, which the last one (the last eight, should they be narrower than a chunk) does not have
+    const bool cut = (!S::ROWA && a.M % 8 != 0) || (!S::ROWB && a.N % 8 != 0);
+    const int64_t k_whole = min(k_end, cut ? a.K - 8 : a.K) - BK;
 
-    auto fetch = [&](int64_t k0) __attribute__((always_inline)) {
-        const int left = (int)min((int64_t)BK, k_end - k0);
+    auto fetch = [&](Set &h, int64_t k0, auto counted) __attribute__((always_inline)) {
         auto one = [&](auto &h, int j, const Walk &x, auto terms, auto per, int64_t outer0, int64_t outer_n, auto whole) __attribute__((always_inline)) {
             constexpr int PER = decltype(per)::value;
-            const T *p = x.p + j * x.row;
             if constexpr (decltype(whole)::value) {
-                if constexpr (S::F32) load8(p, h.x[j]);
-                else h.q[j] = load8(p);
+                if constexpr (S::F32) load8(x.p[j], h.x[j]);
+                else h.q[j] = load8(x.p[j]);
             } else {
+                const int left = (int)min((int64_t)BK, k_end - k0);
                 const int r = (j * NT + t) / PER, c = t % PER;
                 int n;
                 if constexpr (decltype(terms)::value) n = outer0 + r < outer_n ? left - 8 * c : 0;
-                else n = r < left ? x.n : 0;
-                if constexpr (S::F32) load8(p, n, h.x[j]);
-                else h.q[j] = load8(p, n);
+                else n = r < left ? (int)max((int64_t)0, min((int64_t)8, outer_n - outer0 - 8 * c)) : 0;
+                if constexpr (S::F32) load8(x.p[j], n, h.x[j]);
+                else h.q[j] = load8(x.p[j], n);
             }
         };
         auto all = [&](auto whole) __attribute__((always_inline)) {
 #pragma unroll
             for (int j = 0; j < S::CHA; ++j) {
-                one(ha, j, wa, ra, ca, m0, a.M, whole);
-                if constexpr (MODE == INPUT && GRAD) one(hp, j, wp, ra, ca, m0, a.M, whole);
+                one(h.a, j, wa, ra, ca, m0, a.M, whole);
+                if constexpr (MODE == INPUT && GRAD) one(h.p, j, wp, ra, ca, m0, a.M, whole);
             }
 #pragma unroll
             for (int j = 0; j < S::CHB; ++j) {
-                one(hb, j, wb, rb, cb, n0, a.N, whole);
-                if constexpr (MODE == WEIGHTS && GRAD) one(hq, j, wp, rb, cb, n0, a.N, whole);
+                one(h.b, j, wb, rb, cb, n0, a.N, whole);
+                if constexpr (MODE == WEIGHTS && GRAD) one(h.q, j, wp, rb, cb, n0, a.N, whole);
             }
         };
-        if (inside && left == BK) all(std::true_type());
+        if constexpr (decltype(counted)::value) all(std::true_type());
+        else if (k0 <= k_whole) all(std::true_type());
         else all(std::false_type());
-        wa.p += wa.tile; wb.p += wb.tile;
-        if constexpr (GRAD) wp.p += wp.tile;
+#pragma unroll
+        for (int j = 0; j < S::CHA; ++j) {
+            wa.p[j] += wa.tile;
+            if constexpr (MODE == INPUT && GRAD) wp.p[j] += wp.tile;
+        }
+#pragma unroll
+        for (int j = 0; j < S::CHB; ++j) {
+            wb.p[j] += wb.tile;
+            if constexpr (MODE == WEIGHTS && GRAD) wp.p[j] += wp.tile;
+        }
     };
 
     floatx16 acc[MI][NJ];
@@ -177,7 +202,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
     const bool sum_columns = MODE == WEIGHTS && a.part_b && tm == 0;
 
     // registers -> LDS, dY -> dP on the way
-    auto stage = [&](unsigned char *la) __attribute__((always_inline)) {
+    auto stage = [&](const Set &set, unsigned char *la) __attribute__((always_inline)) {
         unsigned char *const lb = la + PA * S::PLANEA;
         auto one = [&](const auto &h, const auto &hg, int j, unsigned char *lds, auto terms, auto per, auto parts, int plane, auto grad,
                        bool columns) __attribute__((always_inline)) {
@@ -221,10 +246,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
         };
 #pragma unroll
         for (int j = 0; j < S::CHA; ++j)
-            one(ha, hp, j, la, ra, ca, std::integral_constant<int, PA>(), S::PLANEA, std::integral_constant<bool, MODE == INPUT && GRAD>(), false);
+            one(set.a, set.p, j, la, ra, ca, std::integral_constant<int, PA>(), S::PLANEA, std::integral_constant<bool, MODE == INPUT && GRAD>(), false);
 #pragma unroll
         for (int j = 0; j < S::CHB; ++j)
-            one(hb, hq, j, lb, rb, cb, std::integral_constant<int, PB>(), S::PLANEB, std::integral_constant<bool, MODE == WEIGHTS && GRAD>(),
+            one(set.b, set.q, j, lb, rb, cb, std::integral_constant<int, PB>(), S::PLANEB, std::integral_constant<bool, MODE == WEIGHTS && GRAD>(),
                 sum_columns);
     };
 
@@ -276,72 +301,116 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
         }
     };
 
-    fetch(k_beg);
+    const std::true_type counted{};
+    const std::false_type guarded{};
     if constexpr (S::TWO) {
-        stage(smem);
-        if (k_beg + BK < k_end) fetch(k_beg + BK);
+        // Tile i is multiplied out of buffer i mod 2 while tile i + 1 goes from registers to the other buffer and the loads of tile i + 2
+        // are issued into these.  Of the two wavefronts that share a SIMD one stages while the other multiplies, and then the other
+        // way round.  (Loads another tile ahead need 24 more registers, which 128 sums a lane do not leave: 439 us for 408.)
+        const int64_t tiles = cdiv(k_end - k_beg, BK);
+        const bool late = w >= WM * WN / 2;
+        fetch(set, k_beg, guarded);
+        stage(set, smem);
+        if (tiles > 1) fetch(set, k_beg + BK, guarded);
         __syncthreads();
         int side = 0;
-        for (int64_t k0 = k_beg; k0 < k_end; k0 += BK, side ^= 1) {
-            // of the two wavefronts that share a SIMD one stages while the other multiplies, and then the other way round
-            if (w < WM * WN / 2) multiply(smem + side * S::BUFFER);
-            if (k0 + BK < k_end) stage(smem + (side ^ 1) * S::BUFFER);       // last read a barrier ago
-            if (k0 + 2 * BK < k_end) fetch(k0 + 2 * BK);
-            if (w >= WM * WN / 2) multiply(smem + side * S::BUFFER);
+        auto step = [&](int64_t i, auto how) __attribute__((always_inline)) {
+            constexpr bool COUNTED = decltype(how)::value;
+            const unsigned char *const now = smem + side * S::BUFFER;
+            side ^= 1;
+            if (!late) multiply(now);
+            if (COUNTED || i + 1 < tiles) stage(set, smem + side * S::BUFFER);       // last read a barrier ago
+            if (COUNTED || i + 2 < tiles) fetch(set, k_beg + (i + 2) * BK, how);
+            if (late) multiply(now);
             __syncthreads();
-        }
+        };
+        int64_t i = 0;
+        for (; k_beg + (i + 2) * BK <= k_whole; ++i) step(i, counted);
+        for (; i < tiles; ++i) step(i, guarded);
     } else {
+        fetch(set, k_beg, guarded);
         for (int64_t k0 = k_beg; k0 < k_end; k0 += BK) {
-            stage(smem);
+            stage(set, smem);
             __syncthreads();
-            if (k0 + BK < k_end) fetch(k0 + BK);
+            if (k0 + BK < k_end) fetch(set, k0 + BK, guarded);
             multiply(smem);
             __syncthreads();
         }
     }
 
-    // a sum that is not finite: once more from fp32 products, term by term
-    auto again = [&](int64_t m, int64_t n) -> float {
-        float s = 0.f;
-        for (int64_t k = k_beg; k < k_end; ++k) {
-            float x = elem(S::ROWA ? a.A + m * a.lda + k : a.A + k * a.lda + m);
-            float y = elem(S::ROWB ? a.B + n * a.ldb + k : a.B + k * a.ldb + n);
-            if (MODE == INPUT && GRAD) x *= act_grad<ACT>(elem(a.pre + m * a.ldpre + k));
-            if (MODE == WEIGHTS && GRAD) y *= act_grad<ACT>(elem(a.pre + k * a.ldpre + n));
-            s = fmaf(x, y, s);
-        }
-        return s;
-    };
-
-    // register v of lane l: row 8 (v / 4) + 4 (l / 32) + v % 4 and column l % 32 of the 32 x 32 block
+    // Results pass through LDS, a wavefront's 32 rows at a time in a place of its own, so that bias, activation, residual and stores
+    // work on 8 consecutive columns a lane
+    float *const out = reinterpret_cast<float *>(smem) + w * (32 * S::OUT);
+    constexpr int OC = 4 * NJ;
+    const int oc = lane % OC;
+    const int64_t n = n0 + 32 * NJ * wn + 8 * oc;
+    const int count = (int)max((int64_t)0, min((int64_t)8, a.N - n));
+    float bias[8];
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
+    for (int k = 0; k < 8; ++k) bias[k] = MODE == FORWARD && a.bias && k < count ? a.bias[n + k] : 0.f;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int64_t n = n0 + 32 * (NJ * wn + j) + (lane & 31);
-            if (n >= a.N) continue;
-            const float b = MODE == FORWARD && a.bias ? a.bias[n] : 0.f;
+    for (int i = 0; i < MI; ++i) {
+        __builtin_amdgcn_wave_barrier();
+        // register v of lane l: row 8 (v / 4) + 4 (l / 32) + v % 4 and column l % 32 of the 32 x 32 block
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int64_t m = m0 + 32 * (MI * wm + i) + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
-                if (m >= a.M) continue;
-                float x = acc[i][j][v];
-                if (PA + PB > 2 && split_not_finite(x)) x = again(m, n);
-                if (MODE == FORWARD) {
-                    x += b;
-                    if (a.pre_out) put(a.pre_out + m * a.ldp + n, x);
-                    x = act_of<ACT>(x);
-                    if (a.add) x += elem(a.add + m * a.ldadd + n);
-                    put(a.C + m * a.ldc + n, x);
-                } else if (MODE == INPUT) {
-                    if (a.add) x += elem(a.add + m * a.ldadd + n);
-                    put(a.C + m * a.ldc + n, x);
-                } else {
-                    a.part[(chunk * a.M + m) * a.N + n] = x;
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) out[(8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * S::OUT + 32 * j + (lane & 31)] = acc[i][j][v];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int q = 0; q < 2 * NJ; ++q) {
+            const int r = q * (64 / OC) + lane / OC;
+            const int64_t m = m0 + 32 * (MI * wm + i) + r;
+            float *from = out + r * S::OUT + 8 * oc;
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = from[k];
+            if (m >= a.M || count == 0) continue;
+            if (PA + PB > 2) {     // a sum that is not finite: once more from fp32 products, term by term
+                bool bad = false;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) bad |= k < count && split_not_finite(x[k]);
+                if (bad) {
+                    for (int c = 0; c < count; ++c) {
+                        if (!split_not_finite(from[c])) continue;
+                        float s = 0.f;
+                        for (int64_t k = k_beg; k < k_end; ++k) {
+                            float y = elem(S::ROWA ? a.A + m * a.lda + k : a.A + k * a.lda + m);
+                            float z = elem(S::ROWB ? a.B + (n + c) * a.ldb + k : a.B + k * a.ldb + n + c);
+                            if (MODE == INPUT && GRAD) y *= act_grad<ACT>(elem(a.pre + m * a.ldpre + k));
+                            if (MODE == WEIGHTS && GRAD) z *= act_grad<ACT>(elem(a.pre + k * a.ldpre + n + c));
+                            s = fmaf(y, z, s);
+                        }
+                        from[c] = s;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] = from[k];
                 }
             }
+            if (MODE == WEIGHTS) {
+                store8(a.part + (chunk * a.M + m) * a.N + n, count, x);
+                continue;
+            }
+            if (MODE == FORWARD) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] += bias[k];
+                if (a.pre_out) store8(a.pre_out + m * a.ldp + n, count, x);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = act_of<ACT>(x[k]);
+            }
+            if (a.add) {
+                float y[8];
+                if constexpr (S::F32) load8(a.add + m * a.ldadd + n, count, y);
+                else spread(load8(a.add + m * a.ldadd + n, count), y);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] += y[k];
+            }
+            store8(a.C + m * a.ldc + n, count, x);
         }
+    }
     if (MODE == WEIGHTS && sum_columns) {        // NT / BC threads hold the same columns: added in their order
+        __syncthreads();
         float *s = reinterpret_cast<float *>(smem);
 #pragma unroll
         for (int k = 0; k < 8; ++k) s[(t / BC) * BN + (t % BC) * 8 + k] = col[k];
