@@ -160,13 +160,38 @@ __device__ __forceinline__ void to_lds(const float x[8], unsigned char *at, int 
     for (int p = 0; p < PARTS; ++p) *reinterpret_cast<uint4 *>(at + p * plane) = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
 }
 
-// dense_rows_*.hip: FORWARD and INPUT for long matrices of at most ROWS_TERMS terms
+// dense_rows_*.hip: FORWARD and INPUT for long matrices of narrow rows, at most ROWS_TERMS terms
 template <class T> constexpr int32_t ROWS_TERMS = sizeof(T) == 4 ? 128 : 256;
-constexpr int64_t ROWS_LONG = 4096;
+// whether whole tiles of 32 rows may go through that kernel's loop without branches: chunks of 8 elements that exist or do not, and
+// rows of the result at words of 4 bytes that 31 bits reach
+template <class T>
+bool rows_counted(const Args<T> &a)
+{
+    auto words = [](const T *p, int64_t ld) { return ((uintptr_t)p % 4) == 0 && (ld * (int64_t)sizeof(T)) % 4 == 0 && ld * 32 * (int64_t)sizeof(T) < 0x7fff0000; };
+    return a.K % 8 == 0 && a.N % 8 == 0 && words(a.C, a.ldc) && (!a.pre_out || words(a.pre_out, a.ldp));
+}
+// Where it pays (us against the tiled kernel's, forward / input gradient).  fp32, 65 terms and more, 16384 rows and more: 16.9 / 13.8
+// against 20.5 / 18.7 at 16000 x 128 x 128, 298 / 301 against 402 / 343 at 10^6; with 64 terms 207 / 220 against 214 / 181.  bf16: the tiles
+// split nothing, and loading all of B into every block costs about 20 us: 51.7 / 58.1 against 42.4 / 66.0 at 128000 x 256 x 256,
+// 315 / 421 against 358 / 505 at 10^6, and 99 / 155 against 83 / 109 with 64 terms; 777 / 705 against 646 / 687 at 10^6 x 100 x 500, in the
+// loop with branches.
+template <class T>
+bool rows_pay(const Args<T> &a)
+{
+    if (a.K <= 64 || a.K > ROWS_TERMS<T>) return false;
+    return sizeof(T) == 4 ? a.M >= 16384 : a.M >= 200000 && rows_counted(a);
+}
 template <int MODE, class T> int launch_rows(const Args<T> &a, int act, hipStream_t st);
 template <> int launch_rows<FORWARD, float>(const Args<float> &a, int act, hipStream_t st);
 template <> int launch_rows<FORWARD, uint16_t>(const Args<uint16_t> &a, int act, hipStream_t st);
 template <> int launch_rows<INPUT, float>(const Args<float> &a, int act, hipStream_t st);
 template <> int launch_rows<INPUT, uint16_t>(const Args<uint16_t> &a, int act, hipStream_t st);
+
+// dense_few.hip: FORWARD and INPUT of few results.  Its time grows with blocks x terms where the tiled kernel's grows with the terms
+// alone: at 1024 blocks of 32 x 32, 18.9 / 28.2 us against 22.7 / 46.9 (1000 terms, bf16) and 29.6 / 42.9 against 63.0 / 78.3 (fp32); at
+// 2048, 31.5 / 51.3 against 21.8 / 49.4 and 51.8 / 79.0 against 67.4 / 81.0.
+template <class T>
+bool few_pay(const Args<T> &a) { return cdiv(a.M, 32) * cdiv(a.N, 32) <= (sizeof(T) == 4 ? 2048 : 1024); }
+template <int MODE, class T> int launch_few(Args<T> a, int act, hipStream_t st);
 
 }  // namespace dense

@@ -528,7 +528,11 @@ int launch(const kge_dense *L, const Args<T> &a, hipStream_t st)
         }
         return launch_tile<MODE, T, 128, 128, 2, 2>(L->act, a, st);
     } else {
-        if (a.M >= ROWS_LONG && a.K <= ROWS_TERMS<T>) {
+        if (few_pay(a)) {
+            KGE_PROF(MODE == FORWARD ? "dense_few" : "dense_few_input_grad", st);
+            return launch_few<MODE, T>(a, L->act, st);
+        }
+        if (rows_pay(a)) {
             KGE_PROF(MODE == FORWARD ? "dense_rows" : "dense_rows_input_grad", st);
             return launch_rows<MODE, T>(a, L->act, st);
         }

@@ -346,9 +346,7 @@ int launch_one(const Args<T> &a, int act, hipStream_t st)
     r.groups = (int32_t)cdiv(a.N, 32 * WN);
     r.tiles = cdiv(a.M, S::TR);
     r.whole = a.M / S::TR;
-    // chunks of 8 elements that exist or do not, and rows of the result at words of 4 bytes that 31 bits reach
-    auto words = [&](const T *p, int64_t ld) { return ((uintptr_t)p % 4) == 0 && (ld * (int64_t)sizeof(T)) % 4 == 0 && ld * S::TR * (int64_t)sizeof(T) < 0x7fff0000; };
-    r.counted = a.K % 8 == 0 && a.N % 8 == 0 && words(a.C, a.ldc) && (!PRE || words(a.pre_out, a.ldp));
+    r.counted = rows_counted(a);
     // one block of 8 wavefronts or two of 4 per compute unit, as LDS allows
     const int64_t at_once = WN == 8 || 2 * S::LDS > 160 * 1024 ? 256 : 512;
     static_assert(S::LDS <= 160 * 1024, "LDS of a compute unit");
@@ -386,8 +384,7 @@ int launch_shape(const Args<T> &a, int act, hipStream_t st)
 {
     // groups of 256 columns unless groups of 128 leave fewer empty
     const bool wide = cdiv(a.N, 128) * 128 >= cdiv(a.N, 256) * 256;
-    // fp32, B in registers: 12 a step of 16 terms, 96 of them at 128 terms.  156 for 208 terms left too few: the next tile's rows went to
-    // scratch memory, and 14541 rows of 203 took 95 us where the tiled kernel took 55
+    // fp32, B in registers: 12 a step of 16 terms, 96 of them at 128 terms; 156 for 208 terms left too few for the rows on their way
     if constexpr (sizeof(T) == 2) {
         if (a.K > 128) return wide ? launch_options<MODE, T, ACT, 16, 8>(a, act, st) : launch_options<MODE, T, ACT, 16, 4>(a, act, st);
     }

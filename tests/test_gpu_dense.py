@@ -108,7 +108,9 @@ def test_backward(kb, kind, act, n, di, do):
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("n,di,do,act", [(4100, 60, 64, "silu"), (4096, 64, 100, "relu"), (4173, 33, 200, "identity"), (4101, 128, 31, "relu"),
                                          (4255, 100, 128, "silu"), (4127, 127, 257, "relu"), (4100, 250, 64, "silu"), (5000, 200, 128, "relu"),
-                                         (4300, 256, 256, "silu"), (4129, 255, 515, "identity"), (33000, 96, 96, "silu"), (4100, 300, 40, "silu")])
+                                         (4300, 256, 256, "silu"), (4129, 255, 515, "identity"), (33000, 96, 96, "silu"), (4100, 300, 40, "silu"),
+                                         (16387, 128, 128, "silu"), (16400, 66, 200, "relu"), (17000, 120, 72, "identity"),
+                                         (20001, 100, 257, "silu"), (200003, 256, 96, "silu"), (200000, 72, 136, "relu")])
 def test_long_matrices_of_narrow_rows(kb, kind, n, di, do, act):
     """Every width class of the kernels that keep W in registers, both ways round, beside widths that they do not take."""
     say("dense rows", kind, n, di, do, act)
@@ -119,6 +121,11 @@ def test_long_matrices_of_narrow_rows(kb, kind, n, di, do, act):
     args = host(x), host(layer["W"]), b.astype(np.float64), ACTS[act], host(r)
     for got, want, bound, what in zip((Y, pre), ref.dense_forward(*args), ref.dense_forward_bound(*args, kind), ("Y", "pre")):
         within(host(got), want, bound, what)
+    if di == do:
+        own = kb.dense_forward(layer, x, R=x, keep_pre=True)
+        args = (*args[:4], host(x))
+        within(host(own[0]), ref.dense_forward(*args)[0], ref.dense_forward_bound(*args, kind)[0], "R = X")
+        assert bool((own[1] == pre).all()) and bool((kb.dense_forward(layer, x, R=x)[0] == own[0]).all())
     bare = kb.dense_forward(dict(layer, b=None), x)[0]
     within(host(bare), ref.dense_forward(args[0], args[1], None, ACTS[act])[0],
            ref.dense_forward_bound(args[0], args[1], None, ACTS[act], None, kind)[0], "Y alone")
@@ -193,11 +200,11 @@ def test_no_rows(kb):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
-@pytest.mark.parametrize("n", [150, 4200])
+@pytest.mark.parametrize("n", [150, 4200, 16500])
 def test_numbers_that_are_not_finite(kb, kind, n):
     """Infinities, NaN and numbers near the type's largest reach the results that fp32 products of them have, and no others."""
     import torch
-    di, do = 40, 33
+    di, do = (72, 33) if n > 10000 else (40, 33)
     X, W, b, _, G, _ = inputs(n, di, do, 8)
     W[3] = np.abs(W[3]) + 0.1
     X[5, 3], X[7, 3], X[9, 2], X[11, 3] = np.inf, -np.inf, np.nan, 3.3e38 / 64
