@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import sys
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -31,6 +32,7 @@ EXPORTED = ["kge_build_partition", "kge_partition_info", "kge_partition_export",
 ACT_IDENTITY, ACT_RELU, ACT_SILU = 0, 1, 2       # ACT_SILU: dense layers only
 ORDER_PROJECT_FIRST, ORDER_RELATION_WEIGHTS = 0, 2
 OPT_SGD, OPT_ADAM = 0, 1
+OPT_ADAMW = 2                     # TrainStep: adamw_step over all parameters (not a kind of optimizer_step)
 MSG_F32, MSG_BF16 = 0, 1
 DT_F32, DT_BF16 = 0, 1
 ROWS_ALL, ROWS_MASK, ROWS_NONZERO = 0, 1, 2
@@ -125,6 +127,15 @@ def load():
         lib.kge_eval_workspace_bytes.restype = C.c_size_t
         lib.kge_dense_workspace_bytes.restype = C.c_size_t
         lib.kge_layer_norm_workspace_bytes.restype = C.c_size_t
+        # with argument types ctypes takes plain integers: a call of the block costs half the time on the host
+        p, i64, size = C.c_void_p, C.c_int64, C.c_size_t
+        lib.kge_dense_forward.argtypes = [p, i64] + [p, i64] * 4 + [p]
+        lib.kge_dense_workspace_bytes.argtypes = [p, i64]
+        lib.kge_dense_backward.argtypes = [p, i64] + [p, i64] * 5 + [p, p, p, size, p]
+        lib.kge_layer_norm_forward.argtypes = [p, i64] + [p, i64] * 2 + [p, p, p]
+        lib.kge_layer_norm_workspace_bytes.argtypes = [p, i64]
+        lib.kge_layer_norm_backward.argtypes = [p, i64, p, i64, p, p, p, i64, p, i64, p, p, p, size, p]
+        lib.kge_adamw_step.argtypes = [p, p, C.c_int32, p]
         _lib = lib
     return _lib
 
@@ -408,82 +419,105 @@ def optimizer_step(kind: int, param, grad, m=None, v=None, lr=0.01, beta1=0.9, b
 
 # ---- vertex-feature block (dense layer, layer norm) and AdamW over a list of tensors ------------
 
+# These calls are short enough for the host's time to count: a caller's tensors mean that torch is loaded, and looking it up is
+# cheaper than importing it again.
+
 def _need(ok, msg: str):
     """An argument check of this layer: the library's own status for it (KGE_EINVAL)."""
     if not ok:
         raise KgeError(-1, msg)
 
 
-def _rows(t, name: str, width=None, n=None, dtypes=None):
+def _rows(t, name: str, width=None, n=None, dtype=None):
     """(address, row stride) of a 2-D device tensor whose rows are dense; None is no tensor."""
     if t is None:
-        return C.c_void_p(0), C.c_int64(0)
-    _need(t.dim() == 2, "%s: a matrix of rows is wanted, not %d dimensions" % (name, t.dim()))
-    _need(width is None or t.shape[1] == width, "%s: rows of %s elements are wanted, not %d" % (name, width, t.shape[1]))
-    _need(n is None or t.shape[0] == n, "%s: %s rows are wanted, not %d" % (name, n, t.shape[0]))
-    _need(dtypes is None or t.dtype in dtypes, "%s: bad type %s" % (name, t.dtype))
-    _need(t.shape[1] <= 1 or t.stride(1) == 1, "%s: a row's elements must lie side by side" % name)
-    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    _need(ld >= t.shape[1], "%s: rows overlap" % name)
-    return C.c_void_p(t.data_ptr()), C.c_int64(ld)
+        return 0, 0
+    if t.dim() != 2:
+        raise KgeError(-1, "%s: a matrix of rows is wanted, not %d dimensions" % (name, t.dim()))
+    rows, cols = t.shape
+    if (width is not None and cols != width) or (n is not None and rows != n):
+        raise KgeError(-1, "%s: %s x %s is wanted, not %d x %d" % (name, "any" if n is None else n, "any" if width is None else width, rows, cols))
+    if dtype is not None and t.dtype != dtype:
+        raise KgeError(-1, "%s: %s is wanted, not %s" % (name, dtype, t.dtype))
+    ld, one = t.stride()
+    if (cols > 1 and one != 1) or (rows > 1 and ld < cols):
+        raise KgeError(-1, "%s: a row's elements must lie side by side, and rows apart" % name)
+    return t.data_ptr(), ld if rows > 1 else cols
 
 
 def _vector(t, name: str, width: int, need=False):
-    import torch
-    _need(t is not None or not need, "%s is missing" % name)
-    if t is not None:
-        _need(t.dtype == torch.float32 and t.numel() == width and t.is_contiguous(),
-              "%s: %d contiguous floats are wanted" % (name, width))
-    return C.c_void_p(0 if t is None else t.data_ptr())
+    """Address of `width` contiguous floats; None is no tensor unless it is needed."""
+    torch = sys.modules["torch"]
+    if t is None:
+        _need(not need, "%s is missing" % name)
+        return 0
+    if t.dtype != torch.float32 or t.numel() != width or not t.is_contiguous():
+        raise KgeError(-1, "%s: %d contiguous floats are wanted" % (name, width))
+    return t.data_ptr()
 
 
 def _workspace(t, need: int, device):
     """The caller's workspace, or one from torch's allocator."""
-    import torch
+    torch = sys.modules["torch"]
     if t is None:
         return torch.empty(max(need, 1), dtype=torch.uint8, device=device)
     _need(t.is_contiguous(), "workspace: contiguous memory is wanted")
     return t
 
 
-class _On:
-    """The device that all of a call's tensors are on is the current one while it runs (stream None: that device's
-    current stream)."""
-
-    def __init__(self, first, others):
-        import torch
-        _need(first.is_cuda, "device tensors are wanted (there is no CPU fallback)")
-        for t in others:
-            _need(t is None or t.device == first.device, "all tensors of a call must be on one device")
-        self.guard = torch.cuda.device(first.device) if first.device.index != torch.cuda.current_device() else None
+class _Here:
+    """No change of device."""
 
     def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
+        pass
 
     def __exit__(self, *e):
-        if self.guard is not None:
-            self.guard.__exit__(*e)
+        pass
+
+
+_HERE = _Here()
+
+
+def _on(first, *others):
+    """The device that all of a call's tensors are on is the current one while it runs (stream None: that device's
+    current stream)."""
+    torch = sys.modules["torch"]
+    if not first.is_cuda:
+        raise KgeError(-1, "device tensors are wanted (there is no CPU fallback)")
+    at = first.get_device()
+    for t in others:
+        if t is not None and (not t.is_cuda or t.get_device() != at):
+            raise KgeError(-1, "all tensors of a call must be on one device")
+    return _HERE if at == torch.cuda.current_device() else torch.cuda.device(at)
+
+
+def _stream_at(stream, t):
+    """The stream's address; None: the current one of t's device, asked for by number (a search for the current device takes
+    longer than the rest of the call)."""
+    if stream is None:
+        stream = sys.modules["torch"].cuda.current_stream(t.get_device())
+    return getattr(stream, "cuda_stream", stream)
 
 
 def _type_of(dtype, name: str) -> int:
-    import torch
+    torch = sys.modules["torch"]
     _need(dtype in (torch.float32, torch.bfloat16), "%s: float32 or bfloat16 is wanted, not %s" % (name, dtype))
     return DT_F32 if dtype == torch.float32 else DT_BF16
 
 
 def _dense(layer: dict, X):
-    W, b = layer["W"], layer.get("b")
-    _need(W.dim() == 2 and W.is_contiguous(), "W: a contiguous matrix is wanted")
+    W = layer["W"]
+    if W.dim() != 2 or not W.is_contiguous():
+        raise KgeError(-1, "W: a contiguous matrix is wanted")
     dt = _type_of(X.dtype, "X")
     _need(W.dtype == X.dtype, "W and X must be of one type")
-    return _Dense(W.shape[0], W.shape[1], int(layer["act"]), dt, W.data_ptr(), _vector(b, "b", W.shape[1]).value)
+    return _Dense(W.shape[0], W.shape[1], int(layer["act"]), dt, W.data_ptr(), _vector(layer.get("b"), "b", W.shape[1]))
 
 
 def dense_workspace_bytes(layer: dict, n_rows: int) -> int:
     W = layer["W"]
     d = _Dense(W.shape[0], W.shape[1], int(layer["act"]), _type_of(W.dtype, "W"), None, None)
-    n = load().kge_dense_workspace_bytes(C.byref(d), C.c_int64(n_rows))
+    n = load().kge_dense_workspace_bytes(C.byref(d), n_rows)
     if n == 0:
         raise KgeError(-1, load().kge_last_error().decode())
     return int(n)
@@ -492,58 +526,61 @@ def dense_workspace_bytes(layer: dict, n_rows: int) -> int:
 def dense_forward(layer: dict, X, R=None, keep_pre: bool = False, Y=None, pre=None, stream=None):
     """(Y, pre): Y = act(X W + b) + R on the rows of X; layer = dict(W=, b= or None, act=).  pre (keep_pre, or a tensor to
     write it to): act's argument, which dense_backward takes; otherwise None."""
-    import torch
-    d, types = _dense(layer, X), (X.dtype,)
-    n, wide = X.shape[0], d.d_out
+    torch = sys.modules["torch"]
+    d, dtype = _dense(layer, X), X.dtype
     x, ldx = _rows(X, "X", d.d_in)
-    r, ldr = _rows(R, "R", wide, n, types)
-    Y = torch.empty((n, wide), dtype=X.dtype, device=X.device) if Y is None else Y
+    n, wide = X.shape[0], d.d_out
+    r, ldr = _rows(R, "R", wide, n, dtype)
+    if Y is None:
+        Y = torch.empty((n, wide), dtype=dtype, device=X.device)
     if pre is None and keep_pre:
-        pre = torch.empty((n, wide), dtype=X.dtype, device=X.device)
-    y, ldy = _rows(Y, "Y", wide, n, types)
-    z, ldz = _rows(pre, "pre", wide, n, types)
-    with _On(X, (layer["W"], layer.get("b"), R, Y, pre)):
-        _check(load().kge_dense_forward(C.byref(d), C.c_int64(n), x, ldx, r, ldr, y, ldy, z, ldz, _stream(stream)))
+        pre = torch.empty((n, wide), dtype=dtype, device=X.device)
+    y, ldy = _rows(Y, "Y", wide, n, dtype)
+    z, ldz = _rows(pre, "pre", wide, n, dtype)
+    with _on(X, layer["W"], layer.get("b"), R, Y, pre):
+        _check(load().kge_dense_forward(C.byref(d), n, x, ldx, r, ldr, y, ldy, z, ldz, _stream_at(stream, X)))
     return Y, pre
 
 
 def dense_backward(layer: dict, X, pre, dY, add=None, need_dX: bool = True, need_dW: bool = True, dX=None, dW=None, db=None,
                    workspace=None, stream=None) -> dict:
     """dict(dX=, dW=, db=) of dense_forward (dX: need_dX; dW, db: need_dW); add: a gradient that reaches X past the layer."""
-    import torch
-    d, types = _dense(layer, X), (X.dtype,)
-    n = X.shape[0]
+    torch = sys.modules["torch"]
+    d, dtype = _dense(layer, X), X.dtype
     x, ldx = _rows(X, "X", d.d_in)
-    z, ldz = _rows(pre, "pre", d.d_out, n, types)
-    g, ldg = _rows(dY, "dY", d.d_out, n, types)
-    if need_dX and dX is None:
-        dX = torch.empty((n, d.d_in), dtype=X.dtype, device=X.device)
+    n = X.shape[0]
+    z, ldz = _rows(pre, "pre", d.d_out, n, dtype)
+    g, ldg = _rows(dY, "dY", d.d_out, n, dtype)
+    if not need_dX:
+        dX = None
+    elif dX is None:
+        dX = torch.empty((n, d.d_in), dtype=dtype, device=X.device)
+    ws_bytes = 0
     if need_dW:
         dW = torch.empty((d.d_in, d.d_out), dtype=torch.float32, device=X.device) if dW is None else dW
         db = torch.empty(d.d_out, dtype=torch.float32, device=X.device) if db is None else db
-        _need(dW.dim() == 2 and tuple(dW.shape) == (d.d_in, d.d_out), "dW: %d x %d is wanted" % (d.d_in, d.d_out))
+        _need(dW.dim() == 2 and dW.shape[0] == d.d_in, "dW: %d x %d is wanted" % (d.d_in, d.d_out))
         workspace = _workspace(workspace, dense_workspace_bytes(layer, n), X.device)
+        ws_bytes = workspace.numel() * workspace.element_size()
     else:
         dW = db = workspace = None
-    dX = dX if need_dX else None
-    o, ldo = _rows(dX, "dX", d.d_in, n, types)
-    a, lda = _rows(add, "add", d.d_in, n, types)
+    o, ldo = _rows(dX, "dX", d.d_in, n, dtype)
+    a, lda = _rows(add, "add", d.d_in, n, dtype)
     pw, pb = _vector(dW, "dW", d.d_in * d.d_out), _vector(db, "db", d.d_out)
-    with _On(X, (layer["W"], pre, dY, add, dX, dW, db, workspace)):
-        _check(load().kge_dense_backward(C.byref(d), C.c_int64(n), x, ldx, z, ldz, g, ldg, a, lda, o, ldo, pw, pb, _ptr(workspace),
-                                         C.c_size_t(0 if workspace is None else workspace.numel() * workspace.element_size()),
-                                         _stream(stream)))
+    with _on(X, layer["W"], pre, dY, add, dX, dW, db, workspace):
+        _check(load().kge_dense_backward(C.byref(d), n, x, ldx, z, ldz, g, ldg, a, lda, o, ldo, pw, pb,
+                                         0 if workspace is None else workspace.data_ptr(), ws_bytes, _stream_at(stream, X)))
     return dict(dX=dX, dW=dW, db=db)
 
 
 def _norm(norm: dict, d: int, x_dtype, y_dtype):
     return _Norm(d, _type_of(x_dtype, "X"), _type_of(y_dtype, "Y"), float(norm.get("eps", 1e-5)),
-                 _vector(norm.get("gamma"), "gamma", d).value, _vector(norm.get("beta"), "beta", d).value)
+                 _vector(norm.get("gamma"), "gamma", d), _vector(norm.get("beta"), "beta", d))
 
 
 def layer_norm_workspace_bytes(d: int, n_rows: int) -> int:
     p = _Norm(d, DT_F32, DT_F32, 0.0, None, None)
-    n = load().kge_layer_norm_workspace_bytes(C.byref(p), C.c_int64(n_rows))
+    n = load().kge_layer_norm_workspace_bytes(C.byref(p), n_rows)
     if n == 0:
         raise KgeError(-1, load().kge_last_error().decode())
     return int(n)
@@ -551,43 +588,41 @@ def layer_norm_workspace_bytes(d: int, n_rows: int) -> int:
 
 def layer_norm_forward(norm: dict, X, out_dtype=None, Y=None, mean=None, rstd=None, stream=None):
     """(Y, mean, rstd) of X's rows; norm = dict(gamma= or None, beta= or None, eps=); Y in out_dtype (X's by default)."""
-    import torch
-    _need(X.dim() == 2, "X: a matrix of rows is wanted, not %d dimensions" % X.dim())
+    torch = sys.modules["torch"]
+    x, ldx = _rows(X, "X")
     n, d = X.shape
     Y = torch.empty((n, d), dtype=out_dtype or X.dtype, device=X.device) if Y is None else Y
     mean = torch.empty(n, dtype=torch.float32, device=X.device) if mean is None else mean
     rstd = torch.empty(n, dtype=torch.float32, device=X.device) if rstd is None else rstd
     p = _norm(norm, d, X.dtype, Y.dtype)
-    x, ldx = _rows(X, "X")
     y, ldy = _rows(Y, "Y", d, n)
     pm, pr = _vector(mean, "mean", n), _vector(rstd, "rstd", n)
-    with _On(X, (norm.get("gamma"), norm.get("beta"), Y, mean, rstd)):
-        _check(load().kge_layer_norm_forward(C.byref(p), C.c_int64(n), x, ldx, y, ldy, pm, pr, _stream(stream)))
+    with _on(X, norm.get("gamma"), norm.get("beta"), Y, mean, rstd):
+        _check(load().kge_layer_norm_forward(C.byref(p), n, x, ldx, y, ldy, pm, pr, _stream_at(stream, X)))
     return Y, mean, rstd
 
 
 def layer_norm_backward(norm: dict, X, mean, rstd, dY, need_dX: bool = True, dX=None, dgamma=None, dbeta=None, workspace=None,
                         stream=None) -> dict:
     """dict(dX=, dgamma=, dbeta=) of layer_norm_forward (dX: need_dX)."""
-    import torch
-    _need(X.dim() == 2, "X: a matrix of rows is wanted, not %d dimensions" % X.dim())
+    torch = sys.modules["torch"]
+    x, ldx = _rows(X, "X")
     n, d = X.shape
     p = _norm(norm, d, X.dtype, dY.dtype)
-    x, ldx = _rows(X, "X")
     g, ldg = _rows(dY, "dY", d, n)
     if not need_dX:
         dX = None
     elif dX is None:
         dX = torch.empty((n, d), dtype=X.dtype, device=X.device)
-    o, ldo = _rows(dX, "dX", d, n, (X.dtype,))
+    o, ldo = _rows(dX, "dX", d, n, X.dtype)
     dgamma = torch.empty(d, dtype=torch.float32, device=X.device) if dgamma is None else dgamma
     dbeta = torch.empty(d, dtype=torch.float32, device=X.device) if dbeta is None else dbeta
     pm, pr = _vector(mean, "mean", n, True), _vector(rstd, "rstd", n, True)
     pg, pb = _vector(dgamma, "dgamma", d), _vector(dbeta, "dbeta", d)
     workspace = _workspace(workspace, layer_norm_workspace_bytes(d, n), X.device)
-    with _On(X, (norm.get("gamma"), norm.get("beta"), mean, rstd, dY, dX, dgamma, dbeta, workspace)):
-        _check(load().kge_layer_norm_backward(C.byref(p), C.c_int64(n), x, ldx, pm, pr, g, ldg, o, ldo, pg, pb, _ptr(workspace),
-                                              C.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream)))
+    with _on(X, norm.get("gamma"), norm.get("beta"), mean, rstd, dY, dX, dgamma, dbeta, workspace):
+        _check(load().kge_layer_norm_backward(C.byref(p), n, x, ldx, pm, pr, g, ldg, o, ldo, pg, pb, workspace.data_ptr(),
+                                              workspace.numel() * workspace.element_size(), _stream_at(stream, X)))
     return dict(dX=dX, dgamma=dgamma, dbeta=dbeta)
 
 
@@ -598,7 +633,7 @@ class AdamWTensors:
     by rows, any other as one row."""
 
     def __init__(self, tensors: Sequence[dict]):
-        import torch
+        torch = sys.modules["torch"]
         self.tensors = [dict(t) for t in tensors]
         self.array = (_AdamWTensor * max(len(self.tensors), 1))()
         for i, t in enumerate(self.tensors):
@@ -640,7 +675,7 @@ def _row_shape(p):
 
 def adamw_state(param, bits: int = 32) -> dict:
     """Zeroed moments of a parameter: dict(m=, v=, m_scale=, v_scale=), the scales None with 32 bits."""
-    import torch
+    torch = sys.modules["torch"]
     _need(bits in (8, 32), "moments have 32 or 8 bits")
     if bits == 32:
         return dict(m=torch.zeros_like(param), v=torch.zeros_like(param), m_scale=None, v_scale=None)
@@ -653,14 +688,14 @@ def adamw_state(param, bits: int = 32) -> dict:
 def adamw_step(tensors, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, t=1, t_dev=None, stream=None):
     """One AdamW step in place on all tensors: an AdamWTensors or a list of its dicts.  t_dev: the step number as a device
     int64 tensor of one element, in place of t."""
-    import torch
+    torch = sys.modules["torch"]
     plan = tensors if isinstance(tensors, AdamWTensors) else AdamWTensors(tensors)
     _need(t_dev is None or (t_dev.dtype == torch.int64 and t_dev.numel() == 1), "t_dev: one int64 is wanted")
     o = _AdamW(lr, beta1, beta2, eps, int(t), _ptr(t_dev).value)
     if not plan.tensors:
         return
-    with _On(plan.tensors[0]["param"], (t_dev,)):
-        _check(load().kge_adamw_step(C.byref(o), plan.array, C.c_int32(len(plan.tensors)), _stream(stream)))
+    with _on(plan.tensors[0]["param"], t_dev):
+        _check(load().kge_adamw_step(C.byref(o), plan.array, len(plan.tensors), _stream_at(stream, plan.tensors[0]["param"])))
 
 
 # ---- link-prediction evaluation (filtered ranks, MRR, Hits@k) ----------------------------------
