@@ -50,6 +50,8 @@ struct Shape {
     static constexpr int BUFFER = PA * PLANEA + PB * PLANEB;
     // a block that has its compute unit to itself stages one tile while it multiplies another
     static constexpr bool TWO = BM == 256;
+    // per SIMD: 168 registers, so that three blocks share a compute unit where one of fp32 numbers alone would leave it for two
+    static constexpr int WAVES = F32 && MODE != WEIGHTS ? (BM == 64 ? 4 : MODE == FORWARD ? 3 : 2) : 1;
     static constexpr int OUT = 32 * NJ + 8;                            // floats per row of results in LDS: 4 rows further, 32 banks further
     static constexpr int TILES = (TWO ? 2 : 1) * BUFFER, RESULTS = WM * WN * 32 * OUT * 4;
     static constexpr int LDS = TILES > RESULTS ? TILES : RESULTS;
@@ -71,7 +73,7 @@ template <int W>
 __device__ __forceinline__ int column_place(int k, int c) { return k * (2 * W) + ((c ^ (4 * column_swap<W>(k))) << 4); }
 
 template <int MODE, class T, int ACT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
+__global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>::WAVES)) void k_dense(Args<T> a)
 {
     typedef Shape<MODE, T, ACT, BM, BN, WM, WN> S;
     constexpr int BK = S::BK, PA = S::PA, PB = S::PB, NT = S::NT, MI = S::MI, NJ = S::NJ;
@@ -269,7 +271,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
         }
     };
 
+    // a wavefront whose results all lie past the end leaves the matrix cores to the others
+    const bool idle = BM == 64 && n0 + 32 * NJ * wn >= a.N;
     auto multiply = [&](const unsigned char *la) __attribute__((always_inline)) {
+        if (idle) return;
         const unsigned char *const lb = la + PA * S::PLANEA;
 #pragma unroll
         for (int ks = 0; ks < BK; ks += 16) {
@@ -304,29 +309,35 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
     const std::true_type counted{};
     const std::false_type guarded{};
     if constexpr (S::TWO) {
-        // Tile i is multiplied out of buffer i mod 2 while tile i + 1 goes from registers to the other buffer and the loads of tile i + 2
-        // are issued into these.  Of the two wavefronts that share a SIMD one stages while the other multiplies, and then the other
-        // way round.  (Loads another tile ahead need 24 more registers, which 128 sums a lane do not leave: 439 us for 408.)
+        // Tile i is multiplied out of buffer i mod 2 while tile i + 1 goes from its registers to the other buffer and the loads of
+        // tile i + 3 are issued into these; those of tile i + 2 are on their way.  Of the two wavefronts that share a SIMD one
+        // stages while the other multiplies, and then the other way round.
         const int64_t tiles = cdiv(k_end - k_beg, BK);
         const bool late = w >= WM * WN / 2;
+        Set other;
         fetch(set, k_beg, guarded);
+        if (tiles > 1) fetch(other, k_beg + BK, guarded);
         stage(set, smem);
-        if (tiles > 1) fetch(set, k_beg + BK, guarded);
+        if (tiles > 2) fetch(set, k_beg + 2 * BK, guarded);
         __syncthreads();
-        int side = 0;
-        auto step = [&](int64_t i, auto how) __attribute__((always_inline)) {
+        auto step = [&](int64_t i, Set &next, int side, auto how) __attribute__((always_inline)) {
             constexpr bool COUNTED = decltype(how)::value;
             const unsigned char *const now = smem + side * S::BUFFER;
-            side ^= 1;
             if (!late) multiply(now);
-            if (COUNTED || i + 1 < tiles) stage(set, smem + side * S::BUFFER);       // last read a barrier ago
-            if (COUNTED || i + 2 < tiles) fetch(set, k_beg + (i + 2) * BK, how);
+            if (COUNTED || i + 1 < tiles) stage(next, smem + (side ^ 1) * S::BUFFER);       // last read a barrier ago
+            if (COUNTED || i + 3 < tiles) fetch(next, k_beg + (i + 3) * BK, how);
             if (late) multiply(now);
             __syncthreads();
         };
         int64_t i = 0;
-        for (; k_beg + (i + 2) * BK <= k_whole; ++i) step(i, counted);
-        for (; i < tiles; ++i) step(i, guarded);
+        for (; k_beg + (i + 4) * BK <= k_whole; i += 2) {
+            step(i, other, 0, counted);
+            step(i + 1, set, 1, counted);
+        }
+        for (; i < tiles; i += 2) {
+            step(i, other, 0, guarded);
+            if (i + 1 < tiles) step(i + 1, set, 1, guarded);
+        }
     } else {
         fetch(set, k_beg, guarded);
         for (int64_t k0 = k_beg; k0 < k_end; k0 += BK) {
@@ -350,6 +361,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_dense(Args<T> a)
     for (int k = 0; k < 8; ++k) bias[k] = MODE == FORWARD && a.bias && k < count ? a.bias[n + k] : 0.f;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
+        if (idle) break;
         __builtin_amdgcn_wave_barrier();
         // register v of lane l: row 8 (v / 4) + 4 (l / 32) + v % 4 and column l % 32 of the 32 x 32 block
 #pragma unroll
@@ -461,24 +473,26 @@ int check(const kge_dense *L, int64_t n_rows)
 }
 
 // The weights' gradient has the smallest tile that takes a narrow side whole: what is empty of a tile is multiplied all the same.  bf16
-// results of 129 columns and more on both sides take a tile of 256 x 256, whose rows are read, and turned into dP, half as often.
+// results of 129 rows and 65 columns and more take a tile of 256 x 128, so that dY becomes dP in one block alone for up to 256 rows (a
+// million rows of 256 x 256, SiLU: 781 us with tiles of 128 x 128, 474 with 256 x 256, whose 128 sums a lane leave no registers for
+// loads two tiles ahead, 460 with these)
 struct Tile { int bm, bn; };
 Tile weights_tile(const kge_dense *L)
 {
     if (L->d_out <= 32) return {128, 32};
     if (L->d_out <= 64) return {128, 64};
     if (L->d_in <= 32) return {32, 128};
-    if (L->dtype == KGE_DT_BF16 && L->d_in > 128 && L->d_out > 128) return {256, 256};
+    if (L->dtype == KGE_DT_BF16 && L->d_in > 128 && L->d_out > 64) return {256, 128};
     return {128, 128};
 }
 
-// chunks of rows of the weights' gradient: about as many blocks as run at once, at least 512 rows each
+// chunks of rows of the weights' gradient: about as many blocks as run at once, at least 256 rows each
 int64_t chunk_rows(const kge_dense *L, int64_t n_rows)
 {
     const Tile tile = weights_tile(L);
     const int64_t tiles = cdiv(L->d_in, tile.bm) * cdiv(L->d_out, tile.bn);
     int64_t chunks = cdiv(tile.bm == 256 ? 256 : 512, tiles);
-    if (chunks > cdiv(n_rows, 512)) chunks = cdiv(n_rows, 512);
+    if (chunks > cdiv(n_rows, 256)) chunks = cdiv(n_rows, 256);
     if (chunks < 1) chunks = 1;
     return align_up((size_t)cdiv(n_rows > 0 ? n_rows : 1, chunks), 64);
 }
@@ -524,7 +538,7 @@ int launch(const kge_dense *L, const Args<T> &a, hipStream_t st)
         if (tile.bn == 64) return launch_tile<MODE, T, 128, 64, 2, 2>(L->act, a, st);
         if (tile.bm == 32) return launch_tile<MODE, T, 32, 128, 1, 4>(L->act, a, st);
         if constexpr (sizeof(T) == 2) {
-            if (tile.bm == 256) return launch_tile<MODE, T, 256, 256, 4, 2>(L->act, a, st);
+            if (tile.bm == 256) return launch_tile<MODE, T, 256, 128, 4, 2>(L->act, a, st);
         }
         return launch_tile<MODE, T, 128, 128, 2, 2>(L->act, a, st);
     } else {
@@ -537,6 +551,12 @@ int launch(const kge_dense *L, const Args<T> &a, hipStream_t st)
             return launch_rows<MODE, T>(a, L->act, st);
         }
         KGE_PROF(MODE == FORWARD ? "dense" : "dense_input_grad", st);
+        // fp32, tiles that all run at once: half as tall, four to a compute unit in place of three, they start, end and store less in
+        // step (14541 x 203 x 517, 570 tiles of 128 x 128: 51.7 / 44.7 us against 53.0 / 54.2 forward / input gradient); with more
+        // of them, W is split and read twice as often for nothing (10^5 x 512 x 512: 5 % more)
+        if constexpr (sizeof(T) == 4) {
+            if (cdiv(a.M, 128) * cdiv(a.N, 128) <= 640) return launch_tile<MODE, T, 64, 128, 1, 4>(L->act, a, st);
+        }
         return launch_tile<MODE, T, 128, 128, 2, 2>(L->act, a, st);
     }
 }

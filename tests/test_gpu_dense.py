@@ -51,7 +51,7 @@ def inputs(n, di, do, seed, std=1.0):
 
 
 SIZES = [(1, 1, 1), (1, 1000, 517), (2, 7, 3), (3, 64, 32), (17, 256, 129), (128, 128, 128), (129, 33, 127), (255, 200, 200),
-         (300, 203, 517), (1000, 32, 31), (600, 70, 50), (700, 30, 129), (2049, 130, 258), (5, 4100, 20)]
+         (300, 203, 517), (1000, 32, 31), (600, 70, 50), (700, 30, 129), (1500, 140, 70), (2049, 130, 258), (5, 4100, 20)]
 
 
 def within(got, want, bound, what):
