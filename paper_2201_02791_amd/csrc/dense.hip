@@ -447,8 +447,17 @@ __global__ __launch_bounds__(1024) void k_dense_sum(const float *__restrict__ pa
     const float *from = w ? part + i : part_b + (i - nw);
     const int64_t step = w ? nw : nb;
     float v = 0.f;
-    if (i < nw + nb)
-        for (int64_t c = y; c < chunks; c += 32) v += from[c * step];
+    if (i < nw + nb) {
+        int64_t c = y;
+        for (; c + 3 * 32 < chunks; c += 4 * 32) {       // four loads on their way, added in the chunks' order
+            float z[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) z[k] = from[(c + 32 * k) * step];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v += z[k];
+        }
+        for (; c < chunks; c += 32) v += from[c * step];
+    }
     s[y][x] = v;
     __syncthreads();
     if (y == 0 && i < nw + nb) {

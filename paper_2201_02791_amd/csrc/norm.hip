@@ -86,58 +86,69 @@ __device__ __forceinline__ float group_sum(float v, float (*lds)[16], int side)
     return v;
 }
 
+// rows that a group has in flight: what one lane's loads leave of the memory's rate
+constexpr int rows_at_once(int V) { return V == 1 ? 4 : V == 2 ? 2 : 1; }
+
 template <int G, int V, bool VEC, class TX, class TY>
 __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_forward(const TX *__restrict__ X, int64_t ldx, int64_t n, int32_t d,
                                                                      const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
                                                                      TY *__restrict__ Y, int64_t ldy, float *__restrict__ mean_out,
                                                                      float *__restrict__ rstd_out)
 {
-    constexpr int NT = G > 256 ? G : 256;
+    constexpr int NT = G > 256 ? G : 256, ROWS = NT / G, U = rows_at_once(V);
     __shared__ float lds[3][16];
     const int l = threadIdx.x & (G - 1);
-    const int64_t row = (int64_t)blockIdx.x * (NT / G) + threadIdx.x / G;
-    const bool in = row < n;                     // uniform over the group; the exchanges below stay inside it
-    float x[V][4];
-    float s = 0.f;
+    const int64_t row0 = (int64_t)blockIdx.x * (ROWS * U) + threadIdx.x / G;
+    float x[U][V][4];
 #pragma unroll
-    for (int c = 0; c < V; ++c) {
-        const int at = (c * G + l) * 4;
-        get4<VEC>(X + row * ldx + at, in ? d - at : 0, x[c]);
-        s += (x[c][0] + x[c][1]) + (x[c][2] + x[c][3]);
-    }
-    const float inv_d = 1.f / (float)d;
-    float mean = group_sum<G>(s, lds, 0) * inv_d;
-    // the deviations' own mean is what rounding left of the row's: it is taken out of them and of their mean square, so that a row
-    // of one value has neither
-    float s1 = 0.f, s2 = 0.f;
+    for (int u = 0; u < U; ++u) {
+        const int64_t row = row0 + u * ROWS;     // whether it exists is uniform over the group; the exchanges below stay inside it
 #pragma unroll
-    for (int c = 0; c < V; ++c) {
-        const int left = d - (c * G + l) * 4;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            x[c][k] -= mean;
-            if (k < left) { s1 += x[c][k]; s2 += x[c][k] * x[c][k]; }
+        for (int c = 0; c < V; ++c) {
+            const int at = (c * G + l) * 4;
+            get4<VEC>(X + row * ldx + at, row < n ? d - at : 0, x[u][c]);
         }
     }
-    const float rest = group_sum<G>(s1, lds, 1) * inv_d;
-    const float square = group_sum<G>(s2, lds, 2) * inv_d;
-    const float var = square - rest * rest;
-    const float rstd = 1.f / sqrtf((var < 0.f ? 0.f : var) + eps);      // a NaN stays one
-    mean += rest;
-    if (!in) return;
+    const float inv_d = 1.f / (float)d;
 #pragma unroll
-    for (int c = 0; c < V; ++c) {
-        const int at = (c * G + l) * 4, left = d - at;
-        float g[4] = {1.f, 1.f, 1.f, 1.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
-        if (gamma) get4<VEC>(gamma + at, left, g);
-        if (beta) get4<VEC>(beta + at, left, b);
+    for (int u = 0; u < U; ++u) {
+        const int64_t row = row0 + u * ROWS;
+        float s = 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[c][k] = (x[c][k] - rest) * rstd * g[k] + b[k];
-        put4<VEC>(Y + row * ldy + at, left, x[c]);
-    }
-    if (l == 0) {
-        if (mean_out) mean_out[row] = mean;
-        if (rstd_out) rstd_out[row] = rstd;
+        for (int c = 0; c < V; ++c) s += (x[u][c][0] + x[u][c][1]) + (x[u][c][2] + x[u][c][3]);
+        float mean = group_sum<G>(s, lds, 0) * inv_d;
+        // the deviations' own mean is what rounding left of the row's: it is taken out of them and of their mean square, so that a
+        // row of one value has neither
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+            const int left = d - (c * G + l) * 4;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                x[u][c][k] -= mean;
+                if (k < left) { s1 += x[u][c][k]; s2 += x[u][c][k] * x[u][c][k]; }
+            }
+        }
+        const float rest = group_sum<G>(s1, lds, 1) * inv_d;
+        const float square = group_sum<G>(s2, lds, 2) * inv_d;
+        const float var = square - rest * rest;
+        const float rstd = 1.f / sqrtf((var < 0.f ? 0.f : var) + eps);      // a NaN stays one
+        mean += rest;
+        if (row >= n) continue;
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+            const int at = (c * G + l) * 4, left = d - at;
+            float g[4] = {1.f, 1.f, 1.f, 1.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
+            if (gamma) get4<VEC>(gamma + at, left, g);
+            if (beta) get4<VEC>(beta + at, left, b);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[u][c][k] = (x[u][c][k] - rest) * rstd * g[k] + b[k];
+            put4<VEC>(Y + row * ldy + at, left, x[u][c]);
+        }
+        if (l == 0) {
+            if (mean_out) mean_out[row] = mean;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
     }
 }
 
@@ -163,33 +174,42 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_backward(const TX *_
             dg[c][k] = db[c][k] = 0.f;
         }
     }
+    constexpr int U = rows_at_once(V);
     int side = 0;
-    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < n; row0 += (int64_t)gridDim.x * ROWS, side ^= 1) {
-        const int64_t row = row0 + sub;
-        const bool in = row < n;
-        const float mean = in ? mean_in[row] : 0.f, rstd = in ? rstd_in[row] : 0.f;
-        float x[V][4], u[V][4];
-        float su = 0.f, sx = 0.f;
+    for (int64_t row0 = (int64_t)blockIdx.x * (ROWS * U); row0 < n; row0 += (int64_t)gridDim.x * (ROWS * U)) {
+        float x[U][V][4], g_y[U][V][4], mean[U], rstd[U];
 #pragma unroll
-        for (int c = 0; c < V; ++c) {
-            const int at = (c * G + l) * 4;
-            get4<VEC>(X + row * ldx + at, in ? d - at : 0, x[c]);
-            get4<VEC>(dY + row * lddy + at, in ? d - at : 0, u[c]);
-        }
+        for (int q = 0; q < U; ++q) {
+            const int64_t row = row0 + q * ROWS + sub;
+            const bool in = row < n;
+            mean[q] = in ? mean_in[row] : 0.f;
+            rstd[q] = in ? rstd_in[row] : 0.f;
 #pragma unroll
-        for (int c = 0; c < V; ++c) {
-            const int left = d - (c * G + l) * 4;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                x[c][k] = k < left ? (x[c][k] - mean) * rstd : 0.f;
-                dg[c][k] += u[c][k] * x[c][k];
-                db[c][k] += u[c][k];
-                u[c][k] *= g[c][k];
-                su += u[c][k];
-                sx += u[c][k] * x[c][k];
+            for (int c = 0; c < V; ++c) {
+                const int at = (c * G + l) * 4;
+                get4<VEC>(X + row * ldx + at, in ? d - at : 0, x[q][c]);
+                get4<VEC>(dY + row * lddy + at, in ? d - at : 0, g_y[q][c]);
             }
         }
-        if (dX) {                                // uniform over the grid
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            const int64_t row = row0 + q * ROWS + sub;
+            float su = 0.f, sx = 0.f;
+#pragma unroll
+            for (int c = 0; c < V; ++c) {
+                const int left = d - (c * G + l) * 4;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float &xh = x[q][c][k], &u = g_y[q][c][k];
+                    xh = k < left ? (xh - mean[q]) * rstd[q] : 0.f;
+                    dg[c][k] += u * xh;
+                    db[c][k] += u;
+                    u *= g[c][k];
+                    su += u;
+                    sx += u * xh;
+                }
+            }
+            if (!dX) continue;                   // uniform over the grid
             if constexpr (G > 64) {
                 // two sums, one barrier: they travel in the two halves of the row that `side` names
                 for (int off = 32; off > 0; off >>= 1) { su += __shfl_xor(su, off, 64); sx += __shfl_xor(sx, off, 64); }
@@ -199,19 +219,19 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_backward(const TX *_
                 su = sx = 0.f;
 #pragma unroll
                 for (int w = 0; w < G / 64; ++w) { su += two[side][0][w]; sx += two[side][1][w]; }
+                side ^= 1;
             } else {
                 su = group_sum<G>(su, nullptr, 0);
                 sx = group_sum<G>(sx, nullptr, 0);
             }
             su *= inv_d; sx *= inv_d;
-            if (in) {
+            if (row >= n) continue;
 #pragma unroll
-                for (int c = 0; c < V; ++c) {
-                    const int at = (c * G + l) * 4;
+            for (int c = 0; c < V; ++c) {
+                const int at = (c * G + l) * 4;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) x[c][k] = rstd * (u[c][k] - su - x[c][k] * sx);
-                    put4<VEC>(dX + row * lddx + at, d - at, x[c]);
-                }
+                for (int k = 0; k < 4; ++k) x[q][c][k] = rstd[q] * (g_y[q][c][k] - su - x[q][c][k] * sx);
+                put4<VEC>(dX + row * lddx + at, d - at, x[q][c]);
             }
         }
     }
@@ -254,8 +274,17 @@ __global__ __launch_bounds__(1024) void k_norm_sum(const float *__restrict__ par
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + x;
     float v = 0.f;
-    if (c < 2 * d)
-        for (int r = y; r < blocks; r += 32) v += part[(int64_t)r * 2 * d + c];
+    if (c < 2 * d) {
+        int r = y;
+        for (; r + 7 * 32 < blocks; r += 8 * 32) {       // eight loads on their way, added in the rows' order
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = part[(int64_t)(r + 32 * k) * 2 * d + c];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v += x[k];
+        }
+        for (; r < blocks; r += 32) v += part[(int64_t)r * 2 * d + c];
+    }
     s[y][x] = v;
     __syncthreads();
     if (y == 0 && c < 2 * d) {
@@ -273,7 +302,7 @@ constexpr int32_t MAX_D = 16384;
 int rows_of(int32_t d) { return d <= 64 ? 16 : d <= 128 ? 8 : d <= 2048 ? 4 : 1; }
 int64_t backward_blocks(int64_t n, int32_t d)
 {
-    const int64_t most = d <= 2048 ? 1024 : 512, want = cdiv(n, rows_of(d));
+    const int64_t most = d <= 2048 ? 1024 : 512, want = cdiv(n, rows_of(d) * rows_at_once(d <= 256 ? 1 : d <= 512 ? 2 : 4));
     return want < most ? want : most;
 }
 
@@ -344,8 +373,8 @@ extern "C" int kge_layer_norm_forward(const kge_norm *L, int64_t n_rows, const v
         with_types(L, vec, [&](auto v, auto tx, auto ty) {
             typedef decltype(tx) TX;
             typedef decltype(ty) TY;
-            constexpr int nt = G.value > 256 ? G.value : 256;
-            k_norm_forward<G.value, V.value, v.value, TX, TY><<<(unsigned)cdiv(n_rows, nt / G.value), nt, 0, st>>>(
+            constexpr int nt = G.value > 256 ? G.value : 256, rows = nt / G.value * rows_at_once(V.value);
+            k_norm_forward<G.value, V.value, v.value, TX, TY><<<(unsigned)cdiv(n_rows, rows), nt, 0, st>>>(
                 (const TX *)X, ldx, n_rows, d, L->gamma, L->beta, L->eps, (TY *)Y, ldy, mean, rstd);
         });
     });
