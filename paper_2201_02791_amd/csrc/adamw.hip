@@ -167,7 +167,8 @@ __device__ __forceinline__ void update(const List &o, const Tensor &T, int64_t a
     for (int k = 0; k < 4; ++k) {
         m.x[k] = o.b1 * m.x[k] + o.omb1 * g.x[k];
         v.x[k] = o.b2 * v.x[k] + (o.omb2 * g.x[k]) * g.x[k];
-        const float step_k = m.x[k] * inv_c1 / (sqrtf(v.x[k] * inv_c2) + o.eps);
+        // the reciprocal is off by a unit in its last place, of the step and not of the parameter
+        const float step_k = m.x[k] * inv_c1 * __builtin_amdgcn_rcpf(sqrtf(v.x[k] * inv_c2) + o.eps);
         p.x[k] -= o.lr * (T.wd * p.x[k] + step_k);
         if (EIGHT && any && (VEC || k < n)) {
             most_m = max(most_m, __float_as_uint(m.x[k]) & 0x7fffffffu);

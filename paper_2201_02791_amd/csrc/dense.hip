@@ -436,11 +436,12 @@ __global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>:
     }
 }
 
-// dW and db from the chunks' sums: 32 elements a block, 32 runs of chunks side by side, then these in their order
-__global__ __launch_bounds__(1024) void k_dense_sum(const float *__restrict__ part, const float *__restrict__ part_b, int64_t chunks, int64_t nw,
+// dW and db from the chunks' sums: 32 elements a block, Y runs of chunks side by side, then these in their order
+template <int Y>
+__global__ __launch_bounds__(32 * Y) void k_dense_sum(const float *__restrict__ part, const float *__restrict__ part_b, int64_t chunks, int64_t nw,
                                                     int64_t nb, float *__restrict__ dW, float *__restrict__ db)
 {
-    __shared__ float s[32][33];
+    __shared__ float s[Y][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int64_t i = (int64_t)blockIdx.x * 32 + x;
     const bool w = i < nw;
@@ -449,21 +450,21 @@ __global__ __launch_bounds__(1024) void k_dense_sum(const float *__restrict__ pa
     float v = 0.f;
     if (i < nw + nb) {
         int64_t c = y;
-        for (; c + 3 * 32 < chunks; c += 4 * 32) {       // four loads on their way, added in the chunks' order
+        for (; c + 3 * Y < chunks; c += 4 * Y) {       // four loads on their way, added in the chunks' order
             float z[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) z[k] = from[(c + 32 * k) * step];
+            for (int k = 0; k < 4; ++k) z[k] = from[(c + Y * k) * step];
 #pragma unroll
             for (int k = 0; k < 4; ++k) v += z[k];
         }
-        for (; c < chunks; c += 32) v += from[c * step];
+        for (; c < chunks; c += Y) v += from[c * step];
     }
     s[y][x] = v;
     __syncthreads();
     if (y == 0 && i < nw + nb) {
         v = 0.f;
 #pragma unroll
-        for (int r = 0; r < 32; ++r) v += s[r][x];
+        for (int r = 0; r < Y; ++r) v += s[r][x];
         (w ? dW + i : db + (i - nw))[0] = v;
     }
 }
@@ -608,7 +609,9 @@ int backward(const kge_dense *L, int64_t n, const void *X, int64_t ldx, const vo
         }
         KGE_PROF("dense_sum", st);             // without rows: sums of nothing, zeros
         const int64_t w = dW ? nw : 0, b = db ? L->d_out : 0;
-        k_dense_sum<<<(unsigned)cdiv(w + b, 32), 1024, 0, st>>>(a.part, a.part_b, chunks, w, b, dW, db);
+        const unsigned blocks = (unsigned)cdiv(w + b, 32);
+        if (chunks > 96) k_dense_sum<32><<<blocks, 1024, 0, st>>>(a.part, a.part_b, chunks, w, b, dW, db);
+        else k_dense_sum<8><<<blocks, 256, 0, st>>>(a.part, a.part_b, chunks, w, b, dW, db);
         KGE_LAUNCH_CHECK();
     }
     return KGE_OK;
