@@ -105,9 +105,24 @@ __device__ __forceinline__ void store_codes(uint8_t *a, uint32_t r, int n)
     }
 }
 
-// largest of the magnitudes' bit patterns over the unit's lanes (a NaN is larger than all)
+// largest of the magnitudes' bit patterns over the unit's lanes (a NaN is larger than all): rotations inside a row of 16 lanes,
+// which cost one instruction each, then the rows
+template <int N>
+__device__ __forceinline__ uint32_t most_rotated(uint32_t v)
+{
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 | N, 0xf, 0xf, false));
+}
 __device__ __forceinline__ uint32_t most_of(uint32_t v, int lanes)
 {
+    if (lanes >= 16) {
+        v = most_rotated<8>(v);
+        v = most_rotated<4>(v);
+        v = most_rotated<2>(v);
+        v = most_rotated<1>(v);
+        if (lanes >= 32) v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
+        if (lanes == 64) v = max(v, (uint32_t)__shfl_xor((int)v, 32, 64));
+        return v;
+    }
     for (int off = lanes >> 1; off > 0; off >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, off, 64));
     return v;
 }
@@ -123,13 +138,14 @@ __device__ __forceinline__ uint32_t scale_bits(uint32_t most)
     return (uint32_t)max(e, 1) << 23;
 }
 
-// a scaled magnitude, to a number of the format with DIGITS bits behind the point and normal numbers from 2^LEAST on
+// a scaled magnitude, to a number of the format with DIGITS bits behind the point and normal numbers from 2^LEAST on; the offset
+// in units of 2^-16.  Both products are by powers of two: the sum is what rounds, whether it is fused or not
 template <int DIGITS, int LEAST>
-__device__ __forceinline__ float round_up_by(float y, float u)
+__device__ __forceinline__ float round_up_by(float y, float offset)
 {
     const uint32_t e = max(__float_as_uint(y) & 0x7f800000u, (uint32_t)(127 + LEAST) << 23);
     const float per = __uint_as_float(((uint32_t)(254 + DIGITS) << 23) - e);
-    return floorf(y * per + u) * __uint_as_float(e - ((uint32_t)DIGITS << 23));
+    return floorf(__builtin_fmaf(offset, 0x1p-16f, y * per)) * __uint_as_float(e - ((uint32_t)DIGITS << 23));
 }
 
 // the two offsets of an element, 16 bits each, from its index and the step (times their multipliers)
@@ -167,8 +183,10 @@ __device__ __forceinline__ void update(const List &o, const Tensor &T, int64_t a
     for (int k = 0; k < 4; ++k) {
         m.x[k] = o.b1 * m.x[k] + o.omb1 * g.x[k];
         v.x[k] = o.b2 * v.x[k] + (o.omb2 * g.x[k]) * g.x[k];
-        // the reciprocal is off by a unit in its last place, of the step and not of the parameter
-        const float step_k = m.x[k] * inv_c1 * __builtin_amdgcn_rcpf(sqrtf(v.x[k] * inv_c2) + o.eps);
+        // root and reciprocal are off by a unit in the last place, of the step and not of the parameter.  The instruction for the root
+        // need not keep numbers below 2^-126, which count only beside an eps of no size
+        const float w = v.x[k] * inv_c2;
+        const float step_k = m.x[k] * inv_c1 * __builtin_amdgcn_rcpf((o.eps >= 0x1p-40f ? __builtin_amdgcn_sqrtf(w) : sqrtf(w)) + o.eps);
         p.x[k] -= o.lr * (T.wd * p.x[k] + step_k);
         if (EIGHT && any && (VEC || k < n)) {
             most_m = max(most_m, __float_as_uint(m.x[k]) & 0x7fffffffu);
@@ -182,10 +200,8 @@ __device__ __forceinline__ void update(const List &o, const Tensor &T, int64_t a
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const uint32_t x = offsets_of(((uint32_t)at + (uint32_t)k) * 0xC2B2AE35u + step * 0x9E3779B9u);
-            q[k] = round_up_by<3, -6>(fabsf(m.x[k]) * im, (float)(x & 0xffffu) * 0x1p-16f);
-            q[k] = copysignf(fminf(q[k], 448.f), m.x[k]);
-            r[k] = round_up_by<2, -14>(v.x[k] * iv, (float)(x >> 16) * 0x1p-16f);
-            r[k] = fminf(v.x[k] > 0.f ? fmaxf(r[k], 0x1p-16f) : 0.f, 57344.f);
+            q[k] = copysignf(round_up_by<3, -6>(fabsf(m.x[k]) * im, (float)(x & 0xffffu)), m.x[k]);
+            r[k] = fmaxf(round_up_by<2, -14>(v.x[k] * iv, (float)(x >> 16)), v.x[k] > 0.f ? 0x1p-16f : 0.f);
         }
         cm = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false), true);
         cv = (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(r[2], r[3], __builtin_amdgcn_cvt_pk_bf8_f32(r[0], r[1], 0, false), true);
