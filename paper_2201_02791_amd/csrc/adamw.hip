@@ -46,7 +46,7 @@ struct Tensor {
     float wd;
     int32_t how;                   // lanes of a unit (low byte), HOW_*
 };
-enum { HOW_VEC = 1 << 8, HOW_8BIT = 1 << 9, HOW_NONZERO = 1 << 10 };
+enum { HOW_WHOLE = 1 << 8, HOW_8BIT = 1 << 9, HOW_NONZERO = 1 << 10 };
 
 struct List {
     Tensor t[LIST_MAX];
@@ -60,48 +60,54 @@ static_assert(sizeof(List) <= 4096, "launch arguments");
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 
 struct Four { float x[4]; };
+// four elements at any element's address
+struct __attribute__((packed, aligned(4))) F4 { float x[4]; };
+struct __attribute__((packed, aligned(1))) C4 { uint32_t w; };
+struct __attribute__((packed, aligned(2))) H4 { uint32_t w[2]; };
 
-template <bool VEC>
+// n elements of four; WHOLE: rows are a multiple of four, n is four
+template <bool WHOLE>
 __device__ __forceinline__ Four load4(const float *a, int n)
 {
-    Four r;
-    if (VEC) {
-        const float4 q = *reinterpret_cast<const float4 *>(a);
-        r.x[0] = q.x; r.x[1] = q.y; r.x[2] = q.z; r.x[3] = q.w;
+    Four r{};
+    if (WHOLE || n >= 4) {
+        const F4 q = *reinterpret_cast<const F4 *>(a);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r.x[k] = q.x[k];
     } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) r.x[k] = k < n ? a[k] : 0.f;
+        for (int k = 0; k < 3; ++k) r.x[k] = k < n ? a[k] : 0.f;
     }
     return r;
 }
 
-template <bool VEC>
+template <bool WHOLE>
 __device__ __forceinline__ void store4(float *a, const Four &r, int n)
 {
-    if (VEC) *reinterpret_cast<float4 *>(a) = make_float4(r.x[0], r.x[1], r.x[2], r.x[3]);
+    if (WHOLE || n >= 4) *reinterpret_cast<F4 *>(a) = F4{{r.x[0], r.x[1], r.x[2], r.x[3]}};
     else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) if (k < n) a[k] = r.x[k];
+        for (int k = 0; k < 3; ++k) if (k < n) a[k] = r.x[k];
     }
 }
 
-template <bool VEC>
+template <bool WHOLE>
 __device__ __forceinline__ uint32_t load_codes(const uint8_t *a, int n)
 {
-    if (VEC) return *reinterpret_cast<const uint32_t *>(a);
+    if (WHOLE || n >= 4) return reinterpret_cast<const C4 *>(a)->w;
     uint32_t r = 0u;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) if (k < n) r |= (uint32_t)a[k] << (8 * k);
+    for (int k = 0; k < 3; ++k) if (k < n) r |= (uint32_t)a[k] << (8 * k);
     return r;
 }
 
-template <bool VEC>
+template <bool WHOLE>
 __device__ __forceinline__ void store_codes(uint8_t *a, uint32_t r, int n)
 {
-    if (VEC) *reinterpret_cast<uint32_t *>(a) = r;
+    if (WHOLE || n >= 4) reinterpret_cast<C4 *>(a)->w = r;
     else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) if (k < n) a[k] = (uint8_t)(r >> (8 * k));
+        for (int k = 0; k < 3; ++k) if (k < n) a[k] = (uint8_t)(r >> (8 * k));
     }
 }
 
@@ -152,7 +158,7 @@ __device__ __forceinline__ float round_up_by(float y, float offset)
 __device__ __forceinline__ uint32_t offsets_of(uint32_t x) { return (x ^ (x >> 16)) * 0x2C1B3C6Du; }
 
 // One block of a row by the `lanes` lanes of a unit: element i0 + 4 lane .., n of its four inside the row (n <= 0: none).
-template <bool VEC, bool EIGHT>
+template <bool WHOLE, bool EIGHT>
 __device__ __forceinline__ void update(const List &o, const Tensor &T, int64_t at, int n, int64_t scale_at, int lanes, float inv_c1,
                                        float inv_c2, uint32_t step, bool on)
 {
@@ -161,15 +167,15 @@ __device__ __forceinline__ void update(const List &o, const Tensor &T, int64_t a
     uint32_t cm = 0u, cv = 0u;
     float sm = 0.f, sv = 0.f;
     if (any) {
-        p = load4<VEC>(T.p + at, n);
-        g = load4<VEC>(T.g + at, n);
+        p = load4<WHOLE>(T.p + at, n);
+        g = load4<WHOLE>(T.g + at, n);
         if (EIGHT) {
-            cm = load_codes<VEC>((const uint8_t *)T.m + at, n);
-            cv = load_codes<VEC>((const uint8_t *)T.v + at, n);
+            cm = load_codes<WHOLE>((const uint8_t *)T.m + at, n);
+            cv = load_codes<WHOLE>((const uint8_t *)T.v + at, n);
             sm = T.ms[scale_at]; sv = T.vs[scale_at];
         } else {
-            m = load4<VEC>((const float *)T.m + at, n);
-            v = load4<VEC>((const float *)T.v + at, n);
+            m = load4<WHOLE>((const float *)T.m + at, n);
+            v = load4<WHOLE>((const float *)T.v + at, n);
         }
     }
     if (EIGHT) {
@@ -188,7 +194,7 @@ __device__ __forceinline__ void update(const List &o, const Tensor &T, int64_t a
         const float w = v.x[k] * inv_c2;
         const float step_k = m.x[k] * inv_c1 * __builtin_amdgcn_rcpf((o.eps >= 0x1p-40f ? __builtin_amdgcn_sqrtf(w) : sqrtf(w)) + o.eps);
         p.x[k] -= o.lr * (T.wd * p.x[k] + step_k);
-        if (EIGHT && any && (VEC || k < n)) {
+        if (EIGHT && any && (WHOLE || k < n)) {
             most_m = max(most_m, __float_as_uint(m.x[k]) & 0x7fffffffu);
             most_v = max(most_v, __float_as_uint(v.x[k]) & 0x7fffffffu);
         }
@@ -206,30 +212,30 @@ __device__ __forceinline__ void update(const List &o, const Tensor &T, int64_t a
         cm = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false), true);
         cv = (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(r[2], r[3], __builtin_amdgcn_cvt_pk_bf8_f32(r[0], r[1], 0, false), true);
         if (any) {
-            store_codes<VEC>((uint8_t *)T.m + at, cm, n);
-            store_codes<VEC>((uint8_t *)T.v + at, cv, n);
+            store_codes<WHOLE>((uint8_t *)T.m + at, cm, n);
+            store_codes<WHOLE>((uint8_t *)T.v + at, cv, n);
             if ((threadIdx.x & (lanes - 1)) == 0) { T.ms[scale_at] = __uint_as_float(km); T.vs[scale_at] = __uint_as_float(kv); }
         }
     }
     if (!any) return;
-    store4<VEC>(T.p + at, p, n);
+    store4<WHOLE>(T.p + at, p, n);
     if (!EIGHT) {
-        store4<VEC>((float *)T.m + at, m, n);
-        store4<VEC>((float *)T.v + at, v, n);
+        store4<WHOLE>((float *)T.m + at, m, n);
+        store4<WHOLE>((float *)T.v + at, v, n);
     }
     if (T.copy) {
         uint16_t c[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) c[k] = __builtin_bit_cast(uint16_t, (__bf16)p.x[k]);
-        if (VEC) *reinterpret_cast<uint2 *>(T.copy + at) = make_uint2(c[0] | (uint32_t)c[1] << 16, c[2] | (uint32_t)c[3] << 16);
+        if (WHOLE || n >= 4) *reinterpret_cast<H4 *>(T.copy + at) = H4{{c[0] | (uint32_t)c[1] << 16, c[2] | (uint32_t)c[3] << 16}};
         else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) if (k < n) T.copy[at + k] = c[k];
+            for (int k = 0; k < 3; ++k) if (k < n) T.copy[at + k] = c[k];
         }
     }
 }
 
-template <bool VEC, bool EIGHT>
+template <bool WHOLE, bool EIGHT>
 __device__ __forceinline__ void unit(const List &o, const Tensor &T, int64_t w, float inv_c1, float inv_c2, uint32_t step)
 {
     const int lane = threadIdx.x & 63, lanes = T.how & 0xff;
@@ -241,7 +247,7 @@ __device__ __forceinline__ void unit(const List &o, const Tensor &T, int64_t w, 
         for (int64_t b = 0; b < T.nb; ++b) {
             const int64_t c = b * BLOCK + 4 * l;
             if (in && c < T.d) {
-                const Four g = load4<VEC>(T.g + row * T.d + c, (int)min((int64_t)4, T.d - c));
+                const Four g = load4<WHOLE>(T.g + row * T.d + c, (int)min((int64_t)4, T.d - c));
                 some |= (g.x[0] != 0.f) | (g.x[1] != 0.f) | (g.x[2] != 0.f) | (g.x[3] != 0.f);
             }
         }
@@ -249,7 +255,7 @@ __device__ __forceinline__ void unit(const List &o, const Tensor &T, int64_t w, 
         const bool on = (__ballot(some) & mine) != 0ull;
         for (int64_t b = 0; b < T.nb; ++b) {
             const int64_t c = b * BLOCK + 4 * l;
-            update<VEC, EIGHT>(o, T, row * T.d + c, in ? (int)min((int64_t)4, T.d - c) : 0, row * T.nb + b, lanes, inv_c1, inv_c2,
+            update<WHOLE, EIGHT>(o, T, row * T.d + c, in ? (int)min((int64_t)4, T.d - c) : 0, row * T.nb + b, lanes, inv_c1, inv_c2,
                                step, on);
         }
         return;
@@ -262,7 +268,7 @@ __device__ __forceinline__ void unit(const List &o, const Tensor &T, int64_t w, 
     const bool in = row < T.n_rows;
     const int64_t c = b * BLOCK + 4 * l;
     const bool on = in && (!T.mask || T.mask[row]);
-    update<VEC, EIGHT>(o, T, row * T.d + c, in ? (int)min((int64_t)4, T.d - c) : 0, row * T.nb + b, lanes, inv_c1, inv_c2, step, on);
+    update<WHOLE, EIGHT>(o, T, row * T.d + c, in ? (int)min((int64_t)4, T.d - c) : 0, row * T.nb + b, lanes, inv_c1, inv_c2, step, on);
 }
 
 __global__ __launch_bounds__(256) void k_adamw(List o)
@@ -285,10 +291,10 @@ __global__ __launch_bounds__(256) void k_adamw(List o)
     const Tensor &T = o.t[i];
     const int64_t mine = w - T.first;
     if (T.how & HOW_8BIT) {
-        if (T.how & HOW_VEC) unit<true, true>(o, T, mine, inv_c1, inv_c2, (uint32_t)step);
+        if (T.how & HOW_WHOLE) unit<true, true>(o, T, mine, inv_c1, inv_c2, (uint32_t)step);
         else unit<false, true>(o, T, mine, inv_c1, inv_c2, (uint32_t)step);
     } else {
-        if (T.how & HOW_VEC) unit<true, false>(o, T, mine, inv_c1, inv_c2, (uint32_t)step);
+        if (T.how & HOW_WHOLE) unit<true, false>(o, T, mine, inv_c1, inv_c2, (uint32_t)step);
         else unit<false, false>(o, T, mine, inv_c1, inv_c2, (uint32_t)step);
     }
 }
@@ -349,9 +355,7 @@ extern "C" int kge_adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tens
             T.nb = cdiv(T.d, BLOCK);
             int lanes = 1;
             while (lanes < 64 && 4 * lanes < T.d) lanes *= 2;
-            const bool vec = T.d % 4 == 0 && aligned(x.param, 16) && aligned(x.grad, 16) && aligned(x.copy, 8) &&
-                             (eight ? aligned(x.m, 4) && aligned(x.v, 4) : aligned(x.m, 16) && aligned(x.v, 16));
-            T.how = lanes | (vec ? HOW_VEC : 0) | (eight ? HOW_8BIT : 0) | (x.rows == KGE_ROWS_NONZERO ? HOW_NONZERO : 0);
+            T.how = lanes | (T.d % 4 == 0 ? HOW_WHOLE : 0) | (eight ? HOW_8BIT : 0) | (x.rows == KGE_ROWS_NONZERO ? HOW_NONZERO : 0);
             const int64_t units = x.rows == KGE_ROWS_NONZERO || T.nb == 1 ? cdiv(T.n_rows, 64 / lanes) : T.n_rows * T.nb;
             if (o.n > 0 && waves + units > 4 * 0x7ffffff0LL) break;
             T.first = waves;

@@ -17,55 +17,61 @@
 
 namespace {
 
+// four elements at any element's address
+struct __attribute__((packed, aligned(4))) F4 { float x[4]; };
+struct __attribute__((packed, aligned(2))) H4 { uint32_t w[2]; };
+
 template <class T> struct Elem;
 template <> struct Elem<float> {
     static __device__ __forceinline__ void load(const float *a, float x[4])
     {
-        const float4 q = *reinterpret_cast<const float4 *>(a);
-        x[0] = q.x; x[1] = q.y; x[2] = q.z; x[3] = q.w;
+        const F4 q = *reinterpret_cast<const F4 *>(a);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = q.x[k];
     }
-    static __device__ __forceinline__ void store(float *a, const float x[4]) { *reinterpret_cast<float4 *>(a) = make_float4(x[0], x[1], x[2], x[3]); }
+    static __device__ __forceinline__ void store(float *a, const float x[4]) { *reinterpret_cast<F4 *>(a) = F4{{x[0], x[1], x[2], x[3]}}; }
     static __device__ __forceinline__ float one(const float *a) { return *a; }
     static __device__ __forceinline__ void put(float *a, float x) { *a = x; }
 };
 template <> struct Elem<__bf16> {
     static __device__ __forceinline__ void load(const __bf16 *a, float x[4])
     {
-        const uint2 q = *reinterpret_cast<const uint2 *>(a);
-        x[0] = __uint_as_float(q.x << 16); x[1] = __uint_as_float(q.x & 0xffff0000u);
-        x[2] = __uint_as_float(q.y << 16); x[3] = __uint_as_float(q.y & 0xffff0000u);
+        const H4 q = *reinterpret_cast<const H4 *>(a);
+        x[0] = __uint_as_float(q.w[0] << 16); x[1] = __uint_as_float(q.w[0] & 0xffff0000u);
+        x[2] = __uint_as_float(q.w[1] << 16); x[3] = __uint_as_float(q.w[1] & 0xffff0000u);
     }
     static __device__ __forceinline__ void store(__bf16 *a, const float x[4])
     {
         typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
         const bf16x4 q = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
-        *reinterpret_cast<uint2 *>(a) = __builtin_bit_cast(uint2, q);
+        *reinterpret_cast<H4 *>(a) = __builtin_bit_cast(H4, q);
     }
     static __device__ __forceinline__ float one(const __bf16 *a) { return (float)*a; }
     static __device__ __forceinline__ void put(__bf16 *a, float x) { *a = (__bf16)x; }
 };
 
-// VEC: rows start at a multiple of four elements' bytes and d is a multiple of 4, so a lane's four elements are all inside
-// the row or all outside
-template <bool VEC, class T>
+// WHOLE: d is a multiple of 4, so that a lane's four elements are all inside the row or all outside
+template <bool WHOLE, class T>
 __device__ __forceinline__ void get4(const T *a, int n, float x[4])
 {
-    if (VEC) {
-        if (n > 0) Elem<T>::load(a, x);
-        else x[0] = x[1] = x[2] = x[3] = 0.f;
-    } else {
+    if (WHOLE ? n > 0 : n >= 4) Elem<T>::load(a, x);
+    else {
+        x[0] = x[1] = x[2] = x[3] = 0.f;
+        if (!WHOLE && n > 0) {                   // past the end the last element again: no branch parts the loads
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = k < n ? Elem<T>::one(a + k) : 0.f;
+            for (int k = 0; k < 3; ++k) x[k] = Elem<T>::one(a + min(k, n - 1));
+            x[1] = n > 1 ? x[1] : 0.f;
+            x[2] = n > 2 ? x[2] : 0.f;
+        }
     }
 }
-template <bool VEC, class T>
+template <bool WHOLE, class T>
 __device__ __forceinline__ void put4(T *a, int n, const float x[4])
 {
-    if (VEC) {
-        if (n > 0) Elem<T>::store(a, x);
-    } else {
+    if (WHOLE ? n > 0 : n >= 4) Elem<T>::store(a, x);
+    else if (!WHOLE) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) if (k < n) Elem<T>::put(a + k, x[k]);
+        for (int k = 0; k < 3; ++k) if (k < n) Elem<T>::put(a + k, x[k]);
     }
 }
 
@@ -89,7 +95,7 @@ __device__ __forceinline__ float group_sum(float v, float (*lds)[16], int side)
 // rows that a group has in flight: what one lane's loads leave of the memory's rate
 constexpr int rows_at_once(int V) { return V == 1 ? 4 : V == 2 ? 2 : 1; }
 
-template <int G, int V, bool VEC, class TX, class TY>
+template <int G, int V, bool WHOLE, class TX, class TY>
 __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_forward(const TX *__restrict__ X, int64_t ldx, int64_t n, int32_t d,
                                                                      const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
                                                                      TY *__restrict__ Y, int64_t ldy, float *__restrict__ mean_out,
@@ -106,7 +112,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_forward(const TX *__
 #pragma unroll
         for (int c = 0; c < V; ++c) {
             const int at = (c * G + l) * 4;
-            get4<VEC>(X + row * ldx + at, row < n ? d - at : 0, x[u][c]);
+            get4<WHOLE>(X + row * ldx + at, row < n ? d - at : 0, x[u][c]);
         }
     }
     const float inv_d = 1.f / (float)d;
@@ -139,11 +145,11 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_forward(const TX *__
         for (int c = 0; c < V; ++c) {
             const int at = (c * G + l) * 4, left = d - at;
             float g[4] = {1.f, 1.f, 1.f, 1.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
-            if (gamma) get4<VEC>(gamma + at, left, g);
-            if (beta) get4<VEC>(beta + at, left, b);
+            if (gamma) get4<WHOLE>(gamma + at, left, g);
+            if (beta) get4<WHOLE>(beta + at, left, b);
 #pragma unroll
             for (int k = 0; k < 4; ++k) x[u][c][k] = (x[u][c][k] - rest) * rstd * g[k] + b[k];
-            put4<VEC>(Y + row * ldy + at, left, x[u][c]);
+            put4<WHOLE>(Y + row * ldy + at, left, x[u][c]);
         }
         if (l == 0) {
             if (mean_out) mean_out[row] = mean;
@@ -153,7 +159,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_forward(const TX *__
 }
 
 // part (if wanted): [blocks][2][d], the block's sums of dy xh and of dy
-template <int G, int V, bool VEC, class TX, class TY>
+template <int G, int V, bool WHOLE, class TX, class TY>
 __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_backward(const TX *__restrict__ X, int64_t ldx, int64_t n, int32_t d,
                                                                       const float *__restrict__ gamma, const float *__restrict__ mean_in,
                                                                       const float *__restrict__ rstd_in, const TY *__restrict__ dY,
@@ -167,7 +173,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_backward(const TX *_
 #pragma unroll
     for (int c = 0; c < V; ++c) {
         const int at = (c * G + l) * 4;
-        if (gamma) get4<VEC>(gamma + at, d - at, g[c]);
+        if (gamma) get4<WHOLE>(gamma + at, d - at, g[c]);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (!gamma) g[c][k] = 1.f;
@@ -187,8 +193,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_backward(const TX *_
 #pragma unroll
             for (int c = 0; c < V; ++c) {
                 const int at = (c * G + l) * 4;
-                get4<VEC>(X + row * ldx + at, in ? d - at : 0, x[q][c]);
-                get4<VEC>(dY + row * lddy + at, in ? d - at : 0, g_y[q][c]);
+                get4<WHOLE>(X + row * ldx + at, in ? d - at : 0, x[q][c]);
+                get4<WHOLE>(dY + row * lddy + at, in ? d - at : 0, g_y[q][c]);
             }
         }
 #pragma unroll
@@ -231,7 +237,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_backward(const TX *_
                 const int at = (c * G + l) * 4;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) x[q][c][k] = rstd[q] * (g_y[q][c][k] - su - x[q][c][k] * sx);
-                put4<VEC>(dX + row * lddx + at, d - at, x[q][c]);
+                put4<WHOLE>(dX + row * lddx + at, d - at, x[q][c]);
             }
         }
     }
@@ -319,7 +325,6 @@ int check(const kge_norm *L, int64_t n_rows)
 }
 
 size_t bytes_of(int32_t dtype) { return dtype == KGE_DT_BF16 ? 2 : 4; }
-bool four(const void *p, int64_t ld, int32_t dtype) { return ((uintptr_t)p % (4 * bytes_of(dtype))) == 0 && ld % 4 == 0; }
 
 // calls f(G, V) with the group and the steps that rows of d elements take
 template <class F>
@@ -336,7 +341,7 @@ void with_shape(int32_t d, F f)
     else f(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
 }
 template <class F>
-void with_types(const kge_norm *L, bool vec, F f)
+void with_types(const kge_norm *L, bool whole, F f)
 {
     auto types = [&](auto v) {
         if (L->x_dtype == KGE_DT_F32) {
@@ -347,7 +352,7 @@ void with_types(const kge_norm *L, bool vec, F f)
             else f(v, __bf16{}, __bf16{});
         }
     };
-    if (vec) types(std::true_type());
+    if (whole) types(std::true_type());
     else types(std::false_type());
 }
 
@@ -365,12 +370,10 @@ extern "C" int kge_layer_norm_forward(const kge_norm *L, int64_t n_rows, const v
     KGE_REQUIRE(((uintptr_t)X % bytes_of(L->x_dtype)) == 0 && ((uintptr_t)Y % bytes_of(L->y_dtype)) == 0 &&
                     ((uintptr_t)L->gamma % 4) == 0 && ((uintptr_t)L->beta % 4) == 0 && ((uintptr_t)mean % 4) == 0 && ((uintptr_t)rstd % 4) == 0,
                 KGE_EINVAL, "layer norm: an array is not aligned to its elements");
-    const bool vec = d % 4 == 0 && four(X, ldx, L->x_dtype) && four(Y, ldy, L->y_dtype) && four(L->gamma, 4, KGE_DT_F32) &&
-                     four(L->beta, 4, KGE_DT_F32);
     hipStream_t st = (hipStream_t)stream;
     KGE_PROF("layer_norm", st);
     with_shape(d, [&](auto G, auto V) {
-        with_types(L, vec, [&](auto v, auto tx, auto ty) {
+        with_types(L, d % 4 == 0, [&](auto v, auto tx, auto ty) {
             typedef decltype(tx) TX;
             typedef decltype(ty) TY;
             constexpr int nt = G.value > 256 ? G.value : 256, rows = nt / G.value * rows_at_once(V.value);
@@ -409,11 +412,9 @@ extern "C" int kge_layer_norm_backward(const kge_norm *L, int64_t n_rows, const 
     }
     const int64_t blocks = backward_blocks(n_rows, d);
     if (n_rows > 0 && (want || dX)) {
-        const bool vec = d % 4 == 0 && four(X, ldx, L->x_dtype) && four(dY, lddy, L->y_dtype) && (!dX || four(dX, lddx, L->x_dtype)) &&
-                         four(L->gamma, 4, KGE_DT_F32);
         KGE_PROF("layer_norm_bwd", st);
         with_shape(d, [&](auto G, auto V) {
-            with_types(L, vec, [&](auto v, auto tx, auto ty) {
+            with_types(L, d % 4 == 0, [&](auto v, auto tx, auto ty) {
                 typedef decltype(tx) TX;
                 typedef decltype(ty) TY;
                 constexpr int nt = G.value > 256 ? G.value : 256;
