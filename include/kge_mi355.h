@@ -337,8 +337,8 @@ int kge_optimizer_step_rows(const kge_opt *opt, float *param, const float *grad,
  * Vertex-feature block: what stands between a fixed feature matrix and the encoder's input,
  *   H_0 = norm(act(X W + b) + R),
  * as a dense layer and a layer norm, each with its backward pass.  Rows (X, R, Y, pre, dY, dX, add) and W are
- * matrices of `dtype`; row strides (ld*, in elements, at least the row's width) may be larger than the rows, and
- * nothing between rows is read or written; any alignment to whole elements is taken.  W is dense.  Biases, norm
+ * matrices of `dtype`; row strides (ld*, in elements, at least the row's width) may be larger than the rows: what
+ * lies between two rows may be read but not used, and is never written; any alignment to whole elements is taken.  W is dense.  Biases, norm
  * weights, statistics and the parameters' gradients are float.  Outputs may not overlap inputs, except where it
  * says so.  All calls are asynchronous on `stream`, allocate nothing, never synchronise, use no atomics (results repeat
  * bit for bit), and can be captured into a HIP graph; calls on different streams need different workspaces.
@@ -346,13 +346,14 @@ int kge_optimizer_step_rows(const kge_opt *opt, float *param, const float *grad,
 enum { KGE_DT_F32 = 0, KGE_DT_BF16 = 1 };
 
 /*
- * Dense layer:  pre = X W + b;  Y = act(pre) + R.   n_rows may be anything from 0 to 2^31 - 1, widths 1 to 65536.
+ * Dense layer:  pre = X W + b;  Y = act(pre) + R.   n_rows is 0 to 2^31 - 1, widths are 1 to 65536; KGE_ERANGE beyond 2^24 tiles of
+ * 128 x 128 results, and for a dW of more than 2^28 elements.
  *   act: KGE_ACT_IDENTITY, KGE_ACT_RELU or KGE_ACT_SILU (z / (1 + e^-z), this layer only)
  *   W : DEVICE dtype [d_in][d_out]      b : DEVICE float [d_out] or NULL
  * Sums are fp32; bf16 results are rounded once, at the end.  fp32 products have fp32 accuracy (they run as bf16
  * products of exact three-way splits).
  *
- * kge_dense_forward: X [n_rows][d_in]; R [n_rows][d_out] or NULL (may be X when d_in == d_out, may be Y); Y [n_rows][d_out];
+ * kge_dense_forward: X [n_rows][d_in]; R [n_rows][d_out] or NULL (may be X when d_in == d_out, or Y, which may not be X); Y [n_rows][d_out];
  *   pre [n_rows][d_out] or NULL: act's argument rounded to dtype, for the backward pass.
  * kge_dense_backward: dP = dY * act'(pre), with act' at pre as it was stored (ReLU: 0 at 0; a ReLU layer without R may pass Y);
  *   dX [n_rows][d_in] = dP W^T + add, or NULL;  add [n_rows][d_in] or NULL (may be dX): a gradient that reaches X past the layer,

@@ -32,6 +32,7 @@ namespace {
 
 constexpr int BLOCK = KGE_ADAMW_BLOCK;        // 64 lanes x 4 elements
 static_assert(BLOCK == 256, "one wavefront holds a block, 4 elements a lane");
+constexpr int64_t MOST_WAVES = (1ll << 32) / 64 - 4;      // a launch has fewer than 2^32 threads
 constexpr int LIST_MAX = 28;                  // tensors per launch: their descriptions are launch arguments, below 4 KB
 
 struct Tensor {
@@ -309,6 +310,7 @@ extern "C" int kge_adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tens
     KGE_REQUIRE(n_tensors >= 0, KGE_EINVAL, "negative number of tensors");
     KGE_REQUIRE(opt->beta1 >= 0.f && opt->beta1 < 1.f && opt->beta2 >= 0.f && opt->beta2 < 1.f, KGE_EINVAL,
                 "beta1 and beta2 must be in [0, 1)");
+    KGE_REQUIRE(aligned(opt->t_dev, 8), KGE_EINVAL, "t_dev is not aligned to its type");
     KGE_REQUIRE(opt->t_dev || opt->t >= 1, KGE_EINVAL, "AdamW's step number t starts at 1");
     for (int32_t i = 0; i < n_tensors; ++i) {
         const kge_adamw_tensor &x = tensors[i];
@@ -357,13 +359,13 @@ extern "C" int kge_adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tens
             while (lanes < 64 && 4 * lanes < T.d) lanes *= 2;
             T.how = lanes | (T.d % 4 == 0 ? HOW_WHOLE : 0) | (eight ? HOW_8BIT : 0) | (x.rows == KGE_ROWS_NONZERO ? HOW_NONZERO : 0);
             const int64_t units = x.rows == KGE_ROWS_NONZERO || T.nb == 1 ? cdiv(T.n_rows, 64 / lanes) : T.n_rows * T.nb;
-            if (o.n > 0 && waves + units > 4 * 0x7ffffff0LL) break;
+            if (o.n > 0 && waves + units > MOST_WAVES) break;
             T.first = waves;
             waves += units;
             o.t[o.n++] = T;
         }
         if (o.n == 0) continue;
-        KGE_REQUIRE(cdiv(waves, 4) <= 0x7fffffffLL, KGE_ERANGE, "tensors too large for one launch");
+        KGE_REQUIRE(waves <= MOST_WAVES, KGE_ERANGE, "tensor %d: too large for one launch", i - 1);
         k_adamw<<<(unsigned)cdiv(waves, 4), 256, 0, st>>>(o);
         KGE_LAUNCH_CHECK();
     }

@@ -525,7 +525,7 @@ int launch_tile(int act, Args<T> a, hipStream_t st)
         const int64_t chunks = cdiv(a.K, a.chunk);
         blocks *= chunks >= 8 ? (int64_t)align_up((size_t)chunks, 8) : chunks;
     } else if (a.tiles_m >= 64) blocks = (int64_t)align_up((size_t)a.tiles_m, 8) * a.tiles_n;
-    KGE_REQUIRE(blocks <= 0x7fffffffLL, KGE_ERANGE, "dense: too large for one launch");
+    KGE_REQUIRE(blocks < (1ll << 32) / (64 * WM * WN), KGE_ERANGE, "dense: too large for one launch");
     hipError_t e = hipSuccess;
     with_act(act, [&](auto act_c) {
         constexpr int ACT = decltype(act_c)::value, LDS = Shape<MODE, T, ACT, BM, BN, WM, WN>::LDS;
@@ -656,6 +656,7 @@ extern "C" int kge_dense_backward(const kge_dense *L, int64_t n_rows, const void
                     at_element(add, L->dtype) && at_element(dX, L->dtype) && at_element(dW, KGE_DT_F32) && at_element(db, KGE_DT_F32),
                 KGE_EINVAL, "dense: an array is not aligned to its elements");
     if (dW || db) {
+        KGE_REQUIRE((int64_t)L->d_in * L->d_out <= 1ll << 28, KGE_ERANGE, "dense: a weights' gradient has at most 2^28 elements");
         KGE_REQUIRE(workspace && ((uintptr_t)workspace % 256) == 0, KGE_EINVAL, "dense: the workspace must be 256-byte aligned");
         KGE_REQUIRE(ws_bytes >= kge_dense_workspace_bytes(L, n_rows), KGE_ENOMEM, "dense: workspace too small");
     }

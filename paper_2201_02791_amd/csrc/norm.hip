@@ -377,8 +377,13 @@ extern "C" int kge_layer_norm_forward(const kge_norm *L, int64_t n_rows, const v
             typedef decltype(tx) TX;
             typedef decltype(ty) TY;
             constexpr int nt = G.value > 256 ? G.value : 256, rows = nt / G.value * rows_at_once(V.value);
-            k_norm_forward<G.value, V.value, v.value, TX, TY><<<(unsigned)cdiv(n_rows, rows), nt, 0, st>>>(
-                (const TX *)X, ldx, n_rows, d, L->gamma, L->beta, L->eps, (TY *)Y, ldy, mean, rstd);
+            constexpr int64_t most = (int64_t)rows * (0x7fffffff / nt);      // a launch has fewer than 2^32 threads
+            for (int64_t r = 0; r < n_rows; r += most) {
+                const int64_t n = n_rows - r < most ? n_rows - r : most;
+                k_norm_forward<G.value, V.value, v.value, TX, TY><<<(unsigned)cdiv(n, rows), nt, 0, st>>>(
+                    (const TX *)X + r * ldx, ldx, n, d, L->gamma, L->beta, L->eps, (TY *)Y + r * ldy, ldy, mean ? mean + r : nullptr,
+                    rstd ? rstd + r : nullptr);
+            }
         });
     });
     KGE_LAUNCH_CHECK();

@@ -77,6 +77,7 @@ class TrainStep:
             self.block = FeatureBlock(params["block"], bf16=msg_dtype == kb.MSG_BF16, device=device, **block)
             need_dH0 = True
             self.H0 = torch.empty((self.block.X.shape[0], self.block.W.shape[1]), dtype=torch.float32, device=self.dev)
+            assert self.H0.shape[1] == self.layers[0]["V"].shape[1]
         else:
             self.H0 = t(params["H0"])
         assert self.H0.shape[0] == N

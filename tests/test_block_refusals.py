@@ -52,6 +52,8 @@ def test_dense_backward(kb):
                         (call(ws=N0), EINVAL), (call(ws=C.c_void_p(4096 + 64)), EINVAL), (call(size=16), ENOMEM),
                         (call(d=kb._Dense(8, 4, 1, 0, None, None)), EINVAL)):
         assert got == status
+    wide = kb._Dense(65536, 65536, 0, 0, 1 << 12, None)
+    assert lib.kge_dense_backward(C.byref(wide), L(5), P, L(65536), N0, L(0), P, L(65536), N0, L(0), N0, L(0), P, P, P, C.c_size_t(1 << 62), N0) == ERANGE
     assert lib.kge_dense_backward(None, L(5), P, L(8), P, L(4), P, L(4), N0, L(8), P, L(8), P, P, P, C.c_size_t(1 << 20), N0) == EINVAL
 
 
@@ -74,7 +76,7 @@ def test_layer_norm(kb):
     (dict(n_rows=-1), EINVAL), (dict(d=-1), EINVAL), (dict(state_bits=16), EINVAL), (dict(rows=3), EINVAL), (dict(param=None), EINVAL),
     (dict(m=None), EINVAL), (dict(state_bits=8), EINVAL), (dict(m_scale=1 << 12), EINVAL), (dict(rows=1), EINVAL),
     (dict(row_mask=1 << 12), EINVAL), (dict(rows=2, d=70000), EINVAL), (dict(n_rows=1 << 40, d=1 << 30), ERANGE),
-    (dict(param=(1 << 12) + 2), EINVAL), (dict(copy=(1 << 12) + 1), EINVAL)])
+    (dict(n_rows=1, d=1 << 36), ERANGE), (dict(param=(1 << 12) + 2), EINVAL), (dict(copy=(1 << 12) + 1), EINVAL)])
 def test_adamw(kb, change, status):
     a = dict(param=1 << 12, grad=1 << 12, m=1 << 12, v=1 << 12, n_rows=3, d=8, state_bits=32, rows=0, weight_decay=0.0)
     a.update(change)
@@ -89,6 +91,7 @@ def test_adamw_hyper_parameters(kb):
     assert call(0.01, 0.9, 0.999, 1e-8, 1, None) == 0                 # nothing to update: nothing runs
     assert call(0.01, 1.0, 0.999, 1e-8, 1, None) == EINVAL and call(0.01, 0.9, -0.1, 1e-8, 1, None) == EINVAL
     assert call(0.01, 0.9, 0.999, 1e-8, 0, None) == EINVAL and call(0.01, 0.9, 0.999, 1e-8, 1, None, n=-1) == EINVAL
+    assert call(0.01, 0.9, 0.999, 1e-8, 1, (1 << 12) + 4) == EINVAL
     assert kb.load().kge_adamw_step(None, C.byref(t), C.c_int32(1), N0) == EINVAL
 
 

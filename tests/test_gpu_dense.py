@@ -262,9 +262,9 @@ def test_gradients_against_differences(kb):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
-def test_another_stream_and_a_graph(kb, kind):
+@pytest.mark.parametrize("n,di,do", [(700, 96, 80), (17000, 128, 96), (3000, 256, 200), (200000, 136, 72)])
+def test_another_stream_and_a_graph(kb, kind, n, di, do):
     import torch
-    n, di, do = 700, 96, 80
     X, W, b, R, G, _ = inputs(n, di, do, 2)
     layer = dict(W=dev(W, kind), b=dev(b), act=ref.SILU)
     x, r, c = dev(X, kind), dev(R, kind), dev(G, kind)
