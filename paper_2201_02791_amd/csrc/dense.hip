@@ -601,11 +601,12 @@ int backward(const kge_dense *L, int64_t n, const void *X, int64_t ldx, const vo
         Args<T> a{};
         a.part = (float *)ws;
         a.part_b = db ? a.part + chunks * nw : nullptr;
+        if (chunks == 1 && dW) { a.part = dW; a.part_b = db; }      // one chunk's sums are the result
         if (n > 0) {
             a.A = (const T *)X; a.lda = ldx; a.B = (const T *)dY; a.ldb = lddy; a.pre = (const T *)pre; a.ldpre = ldp;
             a.M = L->d_in; a.N = L->d_out; a.K = n; a.chunk = chunk;
             int rc = launch<WEIGHTS, T>(L, a, st);
-            if (rc != KGE_OK) return rc;
+            if (rc != KGE_OK || a.part == dW) return rc;
         }
         KGE_PROF("dense_sum", st);             // without rows: sums of nothing, zeros
         const int64_t w = dW ? nw : 0, b = db ? L->d_out : 0;

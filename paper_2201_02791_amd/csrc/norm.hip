@@ -158,12 +158,13 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_forward(const TX *__
     }
 }
 
-// part (if wanted): [blocks][2][d], the block's sums of dy xh and of dy
+// sums_g, sums_b (each if wanted): the block's sums of dy xh and of dy, `step` elements behind those of the block before
 template <int G, int V, bool WHOLE, class TX, class TY>
 __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_backward(const TX *__restrict__ X, int64_t ldx, int64_t n, int32_t d,
                                                                       const float *__restrict__ gamma, const float *__restrict__ mean_in,
                                                                       const float *__restrict__ rstd_in, const TY *__restrict__ dY,
-                                                                      int64_t lddy, TX *__restrict__ dX, int64_t lddx, float *__restrict__ part)
+                                                                      int64_t lddy, TX *__restrict__ dX, int64_t lddx, float *__restrict__ sums_g,
+                                                                      float *__restrict__ sums_b, int64_t step)
 {
     constexpr int NT = G > 256 ? G : 256, ROWS = NT / G;
     __shared__ float sums[ROWS > 1 ? NT * 4 * V : 1];
@@ -241,7 +242,9 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_backward(const TX *_
             }
         }
     }
-    if (!part) return;
+    if (!sums_g && !sums_b) return;
+    if (sums_g) sums_g += blockIdx.x * step;
+    if (sums_b) sums_b += blockIdx.x * step;
     if constexpr (ROWS > 1) {                    // the block's groups, in their order
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
@@ -251,11 +254,12 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_backward(const TX *_
 #pragma unroll
                 for (int k = 0; k < 4; ++k) sums[sub * 4 * V * G + (c * G + l) * 4 + k] = which ? db[c][k] : dg[c][k];
             __syncthreads();
-            for (int i = threadIdx.x; i < d; i += NT) {
+            float *const to = which ? sums_b : sums_g;
+            for (int i = threadIdx.x; to && i < d; i += NT) {
                 float s = 0.f;
 #pragma unroll
                 for (int r = 0; r < ROWS; ++r) s += sums[r * 4 * V * G + i];
-                part[((int64_t)blockIdx.x * 2 + which) * d + i] = s;
+                to[i] = s;
             }
         }
     } else {
@@ -265,8 +269,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_backward(const TX *_
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (at + k < d) {
-                    part[(int64_t)blockIdx.x * 2 * d + at + k] = dg[c][k];
-                    part[(int64_t)blockIdx.x * 2 * d + d + at + k] = db[c][k];
+                    if (sums_g) sums_g[at + k] = dg[c][k];
+                    if (sums_b) sums_b[at + k] = db[c][k];
                 }
         }
     }
@@ -416,6 +420,9 @@ extern "C" int kge_layer_norm_backward(const kge_norm *L, int64_t n_rows, const 
         KGE_REQUIRE(ws_bytes >= kge_layer_norm_workspace_bytes(L, n_rows), KGE_ENOMEM, "layer norm: workspace too small");
     }
     const int64_t blocks = backward_blocks(n_rows, d);
+    // one block's sums are the result
+    float *const sums_g = !want ? nullptr : blocks == 1 ? dgamma : (float *)workspace;
+    float *const sums_b = !want ? nullptr : blocks == 1 ? dbeta : (float *)workspace + d;
     if (n_rows > 0 && (want || dX)) {
         KGE_PROF("layer_norm_bwd", st);
         with_shape(d, [&](auto G, auto V) {
@@ -424,12 +431,12 @@ extern "C" int kge_layer_norm_backward(const kge_norm *L, int64_t n_rows, const 
                 typedef decltype(ty) TY;
                 constexpr int nt = G.value > 256 ? G.value : 256;
                 k_norm_backward<G.value, V.value, v.value, TX, TY><<<(unsigned)blocks, nt, 0, st>>>(
-                    (const TX *)X, ldx, n_rows, d, L->gamma, mean, rstd, (const TY *)dY, lddy, (TX *)dX, lddx, want ? (float *)workspace : nullptr);
+                    (const TX *)X, ldx, n_rows, d, L->gamma, mean, rstd, (const TY *)dY, lddy, (TX *)dX, lddx, sums_g, sums_b, 2 * (int64_t)d);
             });
         });
         KGE_LAUNCH_CHECK();
     }
-    if (want) {                                  // without rows: sums of nothing, zeros
+    if (want && blocks != 1) {                   // without rows: sums of nothing, zeros
         KGE_PROF("layer_norm_sum", st);
         k_norm_sum<<<(unsigned)cdiv(2 * (int64_t)d, 32), 1024, 0, st>>>((const float *)workspace, (int32_t)blocks, d, dgamma, dbeta);
         KGE_LAUNCH_CHECK();
