@@ -12,7 +12,8 @@
 // where no branch decides whether one is issued, so a tile that is all there goes through a loop without such branches: what is
 // optional (R or `add`, pre) is a template argument, and the lanes whose columns lie past the result store through a buffer
 // descriptor that drops them.  With branches in the loop it waited for everything, stores included: a million rows of 256
-// bf16 numbers, input gradient with SiLU, took 546 us.
+// bf16 numbers, input gradient with SiLU, took 546 us, and 465 so.  Measured: 2.9 million fp32 rows of 128 to 128 with R = X and pre
+// 900 us, 4.9 TB/s (1134 us with branches and R read again); a million bf16 rows of 256 to 256 with pre 307 us, 5.0 TB/s.
 //
 // LDS rows are 16 bytes longer than their terms: an odd number of 16-byte chunks apart, eight rows meet all banks.
 // Blocks of the several column groups of a wide result run on one XCD in step, so that the rows come from HBM once.

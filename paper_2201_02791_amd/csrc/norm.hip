@@ -10,7 +10,10 @@
 // columns in registers over all their rows, 2 x 4 V per lane; a second launch adds the blocks' rows in a fixed order, so
 // that the result repeats bit for bit.  Statistics and sums are fp32 whatever the rows' type.
 //
-// Bandwidth bound: forward a row is read and written once, backward two rows are read and one is written.
+// Bandwidth bound: forward a row is read and written once, backward two rows are read and one is written.  Rows of up to 256
+// elements are taken four at a time per group, of up to 512 two, so that a lane's loads cover the memory's latency: 2.9 million
+// fp32 rows of 128 forward 566 us, 5.3 TB/s (589 us one at a time); a million bf16 rows of 256 with fp32 gradients backward
+// 380 us, 5.4 TB/s (455 us).
 #include "common.h"
 
 #include <type_traits>
