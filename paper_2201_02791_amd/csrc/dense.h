@@ -71,27 +71,18 @@ __device__ __forceinline__ float act_of(float z)
 {
     return ACT == KGE_ACT_RELU ? (z < 0.f ? 0.f : z) : ACT == KGE_ACT_SILU ? z * __builtin_amdgcn_rcpf(1.f + exp_minus(z)) : z;
 }
+// dP = dy act'(z).  ReLU chooses: where z is not above zero nothing of dy is left, an infinity or NaN neither (a NaN is not above)
 template <int ACT>
-__device__ __forceinline__ float act_grad(float z)
+__device__ __forceinline__ float through_act(float dy, float z)
 {
-    if (ACT == KGE_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+    if (ACT == KGE_ACT_RELU) return z > 0.f ? dy : 0.f;
     if (ACT == KGE_ACT_SILU) {
         const float s = __builtin_amdgcn_rcpf(1.f + exp_minus(z));
-        return s * (1.f + z * (1.f - s));
+        return dy * (s * (1.f + z * (1.f - s)));
     }
-    return 1.f;
+    return dy;
 }
-
-// the same with the activation as a number (uniform over the launch)
-__device__ __forceinline__ float act_of(float z, int act)
-{
-    return act == KGE_ACT_RELU ? act_of<KGE_ACT_RELU>(z) : act == KGE_ACT_SILU ? act_of<KGE_ACT_SILU>(z) : z;
-}
-__device__ __forceinline__ float act_grad(float z, int act)
-{
-    return act == KGE_ACT_RELU ? act_grad<KGE_ACT_RELU>(z) : act == KGE_ACT_SILU ? act_grad<KGE_ACT_SILU>(z) : 1.f;
-}
-// dY where pre is above zero, two bf16 numbers (a NaN is not above)
+// the same of two bf16 numbers under ReLU
 __device__ __forceinline__ uint32_t relu_pair(uint32_t dy, uint32_t z)
 {
     return (bf(z & 0xffffu) > 0.f ? dy & 0xffffu : 0u) | (__uint_as_float(z & 0xffff0000u) > 0.f ? dy & 0xffff0000u : 0u);

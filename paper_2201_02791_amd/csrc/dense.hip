@@ -243,7 +243,7 @@ __global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>:
                         for (int k = 0; k < 8; ++k) z[k] = hg.x[j][k];
                     } else spread(hg.q[j], z);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] *= act_grad<ACT>(z[k]);
+                    for (int k = 0; k < 8; ++k) x[k] = through_act<ACT>(x[k], z[k]);
                 }
                 to_lds<P>(x, at, plane);
                 if (columns)
@@ -395,8 +395,8 @@ __global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>:
                         for (int64_t k = k_beg; k < k_end; ++k) {
                             float y = elem(S::ROWA ? a.A + m * a.lda + k : a.A + k * a.lda + m);
                             float z = elem(S::ROWB ? a.B + (n + c) * a.ldb + k : a.B + k * a.ldb + n + c);
-                            if (MODE == INPUT && GRAD) y *= act_grad<ACT>(elem(a.pre + m * a.ldpre + k));
-                            if (MODE == WEIGHTS && GRAD) z *= act_grad<ACT>(elem(a.pre + k * a.ldpre + n + c));
+                            if (MODE == INPUT && GRAD) y = through_act<ACT>(y, elem(a.pre + m * a.ldpre + k));
+                            if (MODE == WEIGHTS && GRAD) z = through_act<ACT>(z, elem(a.pre + k * a.ldpre + n + c));
                             s = fmaf(y, z, s);
                         }
                         from[c] = s;

@@ -55,7 +55,7 @@ __global__ __launch_bounds__(NT) void k_dense_few(Args<T> a)
     auto multiply = [&](Step &h) __attribute__((always_inline)) {
         if (GRAD) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h.x[i] *= act_grad<ACT>(h.z[i]);
+            for (int i = 0; i < 8; ++i) h.x[i] = through_act<ACT>(h.x[i], h.z[i]);
         }
         uint32_t fx[3][4], fy[3][4];
 #pragma unroll
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(NT) void k_dense_few(Args<T> a)
             x = 0.f;
             for (int32_t i = 0; i < K; ++i) {
                 float y = elem(a.A + mi * a.lda + i);
-                if (GRAD) y *= act_grad<ACT>(elem(a.pre + mi * a.ldpre + i));
+                if (GRAD) y = through_act<ACT>(y, elem(a.pre + mi * a.ldpre + i));
                 x = fmaf(y, elem(MODE == FORWARD ? a.B + (int64_t)i * a.ldb + ni : a.B + (int64_t)ni * a.ldb + i), x);
             }
         }

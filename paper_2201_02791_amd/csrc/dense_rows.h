@@ -183,8 +183,8 @@ __global__ __launch_bounds__(64 * WN, 2) void k_dense_rows(RowArgs<T> r)
                 if (GRAD) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        x[k] *= act_grad<ACT>(z[k]);
-                        if (F32 || ACT == KGE_ACT_SILU) x[k] = __uint_as_float(__float_as_uint(x[k]) & keep);      // 0 times the pre of a row's first chunk
+                        x[k] = through_act<ACT>(x[k], z[k]);
+                        if (ACT == KGE_ACT_SILU) x[k] = __uint_as_float(__float_as_uint(x[k]) & keep);      // 0 times the pre of a row's first chunk
                     }
                 }
                 to_lds<P>(x, at, S::PLANE);
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(64 * WN, 2) void k_dense_rows(RowArgs<T> r)
                         float s = 0.f;
                         for (int32_t i = 0; i < K; ++i) {
                             float y = elem(a.A + m * a.lda + i);
-                            if (GRAD) y *= act_grad<ACT>(elem(a.pre + m * a.ldpre + i));
+                            if (GRAD) y = through_act<ACT>(y, elem(a.pre + m * a.ldpre + i));
                             s = fmaf(y, elem(MODE == FORWARD ? a.B + (int64_t)i * a.ldb + on + k : a.B + (int64_t)(on + k) * a.ldb + i), s);
                         }
                         from[k] = s;

@@ -292,3 +292,73 @@ def test_another_stream_and_a_graph(kb, kind, n, di, do):
         graph.replay()
         torch.cuda.synchronize()
         assert all(bool((a == b_).all()) for a, b_ in zip(out, want)), rep
+
+
+# one size for each kernel: few results; tiles of 64 x 128 (fp32); tiles of 128 x 128; rows past W in registers (fp32, bf16)
+KERNELS = [(150, 40, 33), (12000, 200, 200), (50000, 136, 136), (17000, 128, 128), (200000, 136, 72)]
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n,di,do", KERNELS)
+def test_relu_hides_what_is_not_finite(kb, kind, n, di, do):
+    """Where pre is not above zero, dY counts for nothing, whatever it is: bit for bit what zeros there give."""
+    import torch
+    say("relu hides", kind, n, di, do)
+    X, W, b, Z, G, _ = inputs(n, di, do, 21)
+    Z[2], Z[5, ::2], Z[6, ::3] = np.nan, 0.0, -np.inf
+    layer = dict(W=dev(W, kind), b=dev(b), act=ref.RELU)
+    x, pre, clean = dev(X, kind), dev(Z, kind), dev(G, kind)
+    hidden = ~(pre > 0)
+    clean[hidden] = 0.0
+    for what in (float("inf"), float("nan"), -3.3e38):
+        dirty = clean.clone()
+        dirty[hidden] = what
+        want, got = (kb.dense_backward(layer, x, pre, g) for g in (clean, dirty))
+        for k in want:
+            assert bool((got[k] == want[k]).all()), (k, what)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n,di,do", KERNELS[1:])
+def test_numbers_that_are_not_finite_in_long_matrices(kb, kind, n, di, do):
+    say("dense not finite", kind, n, di, do)
+    X, W, b, _, G, _ = inputs(n, di, do, 22)
+    W[3] = np.abs(W[3]) + 0.1
+    at = n - 40                                              # in the last tiles and in the first
+    for r in (0, at):
+        X[r + 5, 3], X[r + 7, 3], X[r + 9, 2], X[r + 11, 3] = np.inf, -np.inf, np.nan, 3.3e38 / 64
+        X[r + 13, 3], X[r + 13, 4] = np.inf, np.inf
+        G[r + 3, 5], G[r + 4, 6] = np.inf, np.nan
+    layer = dict(W=dev(W, kind), b=dev(b), act=ref.IDENTITY)
+    x, g = dev(X, kind), dev(G, kind)
+    ones = dev(np.ones((n, di)), kind)
+    back = kb.dense_backward(layer, ones, None, g)
+    with np.errstate(all="ignore"):
+        want = host(x) @ host(layer["W"]) + b
+        dX, dW, db = ref.dense_backward(host(ones), host(layer["W"]), None, host(g), ref.IDENTITY)
+    for a, w in ((kb.dense_forward(layer, x)[0], want), (back["dX"], dX), (back["dW"], dW), (back["db"], db)):
+        a = host(a)
+        assert np.isinf(w).any() and np.isnan(w).any()
+        assert np.array_equal(np.isnan(a), np.isnan(w)) and np.array_equal(np.isinf(a), np.isinf(w))
+        assert np.array_equal(a[np.isinf(w)], w[np.isinf(w)])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n,di,do", [(70, 37, 45), (4000, 203, 150), (12000, 200, 200), (17000, 128, 128), (200000, 136, 72)])
+def test_nothing_between_the_rows_counts(kb, kind, n, di, do):
+    """Rows apart by columns of NaN: bit for bit what the same rows without them give."""
+    import torch
+    say("dense gaps of NaN", kind, n, di, do)
+    X, W, b, Z, G, _ = inputs(n, di, do, 23)
+    apart = lambda t, wide: torch.cat([t, torch.full((n, wide), float("nan"), dtype=t.dtype, device="cuda")], 1)[:, :t.shape[1]]
+    layer = dict(W=dev(W, kind), b=dev(b), act=ref.SILU)
+    x, z, g = dev(X, kind), dev(Z, kind), dev(G, kind)
+    want = kb.dense_backward(layer, x, z, g, add=x)
+    Y, pre = kb.dense_forward(layer, x, R=g, keep_pre=True)
+    for wide in (1, 8):
+        xs, zs, gs = (apart(t, wide) for t in (x, z, g))
+        got = kb.dense_backward(layer, xs, zs, gs, add=xs)
+        for k in want:
+            assert bool((got[k] == want[k]).all()), (k, wide)
+        Ys, pres = kb.dense_forward(layer, xs, R=gs, keep_pre=True)
+        assert bool((Ys == Y).all()) and bool((pres == pre).all()), wide
