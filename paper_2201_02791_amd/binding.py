@@ -456,47 +456,47 @@ def _vector(t, name: str, width: int, need=False):
     return t.data_ptr()
 
 
-def _workspace(t, need: int, device):
-    """The caller's workspace, or one from torch's allocator."""
+def _new(X, shape, dtype, stream):
+    """What a call makes by itself is memory of the stream that it runs on: the current one's may still be in use there, and would
+    be given away again in the current one's order."""
+    if stream is None or not X.is_cuda:
+        return X.new_empty(shape, dtype=dtype)
     torch = sys.modules["torch"]
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(stream, X.device) if stream else torch.cuda.default_stream(X.device)
+    with torch.cuda.stream(stream):
+        return X.new_empty(shape, dtype=dtype)
+
+
+def _workspace(t, need: int, X, stream):
+    """The caller's workspace, or one from torch's allocator."""
     if t is None:
-        return torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+        return _new(X, max(need, 1), sys.modules["torch"].uint8, stream)
     _need(t.is_contiguous(), "workspace: contiguous memory is wanted")
     return t
 
 
-class _Here:
-    """No change of device."""
-
-    def __enter__(self):
-        pass
-
-    def __exit__(self, *e):
-        pass
-
-
-_HERE = _Here()
-
-
-def _on(first, *others):
-    """The device that all of a call's tensors are on is the current one while it runs (stream None: that device's
-    current stream)."""
+def _call(function, stream, first, others, *args):
+    """One library call on the device that all of its tensors are on, on `stream` or that device's current one.  Asked of torch by
+    number and without its wrappers, device and stream cost a tenth of what they do otherwise."""
     torch = sys.modules["torch"]
     if not first.is_cuda:
         raise KgeError(-1, "device tensors are wanted (there is no CPU fallback)")
     at = first.get_device()
     for t in others:
-        if t is not None and (not t.is_cuda or t.get_device() != at):
+        if t is not None and t.get_device() != at:
             raise KgeError(-1, "all tensors of a call must be on one device")
-    return _HERE if at == torch.cuda.current_device() else torch.cuda.device(at)
-
-
-def _stream_at(stream, t):
-    """The stream's address; None: the current one of t's device, asked for by number (a search for the current device takes
-    longer than the rest of the call)."""
     if stream is None:
-        stream = sys.modules["torch"].cuda.current_stream(t.get_device())
-    return getattr(stream, "cuda_stream", stream)
+        stream = torch._C._cuda_getCurrentRawStream(at)
+    else:
+        stream = getattr(stream, "cuda_stream", stream)
+    if torch._C._cuda_getDevice() == at:
+        rc = function(*args, stream)
+    else:
+        with torch.cuda.device(at):
+            rc = function(*args, stream)
+    if rc != 0:
+        _check(rc)
 
 
 def _type_of(dtype, name: str) -> int:
@@ -526,19 +526,17 @@ def dense_workspace_bytes(layer: dict, n_rows: int) -> int:
 def dense_forward(layer: dict, X, R=None, keep_pre: bool = False, Y=None, pre=None, stream=None):
     """(Y, pre): Y = act(X W + b) + R on the rows of X; layer = dict(W=, b= or None, act=).  pre (keep_pre, or a tensor to
     write it to): act's argument, which dense_backward takes; otherwise None."""
-    torch = sys.modules["torch"]
     d, dtype = _dense(layer, X), X.dtype
     x, ldx = _rows(X, "X", d.d_in)
     n, wide = X.shape[0], d.d_out
     r, ldr = _rows(R, "R", wide, n, dtype)
     if Y is None:
-        Y = torch.empty((n, wide), dtype=dtype, device=X.device)
+        Y = _new(X, (n, wide), dtype, stream)
     if pre is None and keep_pre:
-        pre = torch.empty((n, wide), dtype=dtype, device=X.device)
+        pre = _new(X, (n, wide), dtype, stream)
     y, ldy = _rows(Y, "Y", wide, n, dtype)
     z, ldz = _rows(pre, "pre", wide, n, dtype)
-    with _on(X, layer["W"], layer.get("b"), R, Y, pre):
-        _check(load().kge_dense_forward(C.byref(d), n, x, ldx, r, ldr, y, ldy, z, ldz, _stream_at(stream, X)))
+    _call(load().kge_dense_forward, stream, X, (layer["W"], layer.get("b"), R, Y, pre), C.byref(d), n, x, ldx, r, ldr, y, ldy, z, ldz)
     return Y, pre
 
 
@@ -554,22 +552,21 @@ def dense_backward(layer: dict, X, pre, dY, add=None, need_dX: bool = True, need
     if not need_dX:
         dX = None
     elif dX is None:
-        dX = torch.empty((n, d.d_in), dtype=dtype, device=X.device)
+        dX = _new(X, (n, d.d_in), dtype, stream)
     ws_bytes = 0
     if need_dW:
-        dW = torch.empty((d.d_in, d.d_out), dtype=torch.float32, device=X.device) if dW is None else dW
-        db = torch.empty(d.d_out, dtype=torch.float32, device=X.device) if db is None else db
+        dW = _new(X, (d.d_in, d.d_out), torch.float32, stream) if dW is None else dW
+        db = _new(X, d.d_out, torch.float32, stream) if db is None else db
         _need(dW.dim() == 2 and dW.shape[0] == d.d_in, "dW: %d x %d is wanted" % (d.d_in, d.d_out))
-        workspace = _workspace(workspace, dense_workspace_bytes(layer, n), X.device)
+        workspace = _workspace(workspace, dense_workspace_bytes(layer, n), X, stream)
         ws_bytes = workspace.numel() * workspace.element_size()
     else:
         dW = db = workspace = None
     o, ldo = _rows(dX, "dX", d.d_in, n, dtype)
     a, lda = _rows(add, "add", d.d_in, n, dtype)
     pw, pb = _vector(dW, "dW", d.d_in * d.d_out), _vector(db, "db", d.d_out)
-    with _on(X, layer["W"], pre, dY, add, dX, dW, db, workspace):
-        _check(load().kge_dense_backward(C.byref(d), n, x, ldx, z, ldz, g, ldg, a, lda, o, ldo, pw, pb,
-                                         0 if workspace is None else workspace.data_ptr(), ws_bytes, _stream_at(stream, X)))
+    _call(load().kge_dense_backward, stream, X, (layer["W"], pre, dY, add, dX, dW, db, workspace), C.byref(d), n, x, ldx, z, ldz, g, ldg,
+          a, lda, o, ldo, pw, pb, 0 if workspace is None else workspace.data_ptr(), ws_bytes)
     return dict(dX=dX, dW=dW, db=db)
 
 
@@ -591,14 +588,14 @@ def layer_norm_forward(norm: dict, X, out_dtype=None, Y=None, mean=None, rstd=No
     torch = sys.modules["torch"]
     x, ldx = _rows(X, "X")
     n, d = X.shape
-    Y = torch.empty((n, d), dtype=out_dtype or X.dtype, device=X.device) if Y is None else Y
-    mean = torch.empty(n, dtype=torch.float32, device=X.device) if mean is None else mean
-    rstd = torch.empty(n, dtype=torch.float32, device=X.device) if rstd is None else rstd
+    Y = _new(X, (n, d), out_dtype or X.dtype, stream) if Y is None else Y
+    mean = _new(X, n, torch.float32, stream) if mean is None else mean
+    rstd = _new(X, n, torch.float32, stream) if rstd is None else rstd
     p = _norm(norm, d, X.dtype, Y.dtype)
     y, ldy = _rows(Y, "Y", d, n)
     pm, pr = _vector(mean, "mean", n), _vector(rstd, "rstd", n)
-    with _on(X, norm.get("gamma"), norm.get("beta"), Y, mean, rstd):
-        _check(load().kge_layer_norm_forward(C.byref(p), n, x, ldx, y, ldy, pm, pr, _stream_at(stream, X)))
+    _call(load().kge_layer_norm_forward, stream, X, (norm.get("gamma"), norm.get("beta"), Y, mean, rstd), C.byref(p), n, x, ldx, y, ldy,
+          pm, pr)
     return Y, mean, rstd
 
 
@@ -613,16 +610,15 @@ def layer_norm_backward(norm: dict, X, mean, rstd, dY, need_dX: bool = True, dX=
     if not need_dX:
         dX = None
     elif dX is None:
-        dX = torch.empty((n, d), dtype=X.dtype, device=X.device)
+        dX = _new(X, (n, d), X.dtype, stream)
     o, ldo = _rows(dX, "dX", d, n, X.dtype)
-    dgamma = torch.empty(d, dtype=torch.float32, device=X.device) if dgamma is None else dgamma
-    dbeta = torch.empty(d, dtype=torch.float32, device=X.device) if dbeta is None else dbeta
+    dgamma = _new(X, d, torch.float32, stream) if dgamma is None else dgamma
+    dbeta = _new(X, d, torch.float32, stream) if dbeta is None else dbeta
     pm, pr = _vector(mean, "mean", n, True), _vector(rstd, "rstd", n, True)
     pg, pb = _vector(dgamma, "dgamma", d), _vector(dbeta, "dbeta", d)
-    workspace = _workspace(workspace, layer_norm_workspace_bytes(d, n), X.device)
-    with _on(X, norm.get("gamma"), norm.get("beta"), mean, rstd, dY, dX, dgamma, dbeta, workspace):
-        _check(load().kge_layer_norm_backward(C.byref(p), n, x, ldx, pm, pr, g, ldg, o, ldo, pg, pb, workspace.data_ptr(),
-                                              workspace.numel() * workspace.element_size(), _stream_at(stream, X)))
+    workspace = _workspace(workspace, layer_norm_workspace_bytes(d, n), X, stream)
+    _call(load().kge_layer_norm_backward, stream, X, (norm.get("gamma"), norm.get("beta"), mean, rstd, dY, dX, dgamma, dbeta, workspace),
+          C.byref(p), n, x, ldx, pm, pr, g, ldg, o, ldo, pg, pb, workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return dict(dX=dX, dgamma=dgamma, dbeta=dbeta)
 
 
@@ -694,8 +690,7 @@ def adamw_step(tensors, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, t=1, t_dev=No
     o = _AdamW(lr, beta1, beta2, eps, int(t), _ptr(t_dev).value)
     if not plan.tensors:
         return
-    with _on(plan.tensors[0]["param"], t_dev):
-        _check(load().kge_adamw_step(C.byref(o), plan.array, len(plan.tensors), _stream_at(stream, plan.tensors[0]["param"])))
+    _call(load().kge_adamw_step, stream, plan.tensors[0]["param"], (t_dev,), C.byref(o), plan.array, len(plan.tensors))
 
 
 # ---- link-prediction evaluation (filtered ranks, MRR, Hits@k) ----------------------------------

@@ -5,7 +5,7 @@
 // order of the matrix instruction (8 consecutive terms of a row a lane; of W, whose columns lie side by side, 32
 // neighbours a load), without LDS and without a barrier until their eight sums meet there.  What bounds it is the latency of
 // two or three dependent loads; rows past the last repeat it, their results are not stored.  One row of 1024 by 1024 bf16: 4.7 us on
-// the device (17 us in the tiled kernel), 11 with the host's part of the call.
+// the device (17 us in the tiled kernel), 10 with the host's part of the call.
 #include "dense.h"
 
 using namespace dense;

@@ -362,3 +362,30 @@ def test_nothing_between_the_rows_counts(kb, kind, n, di, do):
             assert bool((got[k] == want[k]).all()), (k, wide)
         Ys, pres = kb.dense_forward(layer, xs, R=gs, keep_pre=True)
         assert bool((Ys == Y).all()) and bool((pres == pre).all()), wide
+
+
+def test_results_on_a_callers_stream_are_of_its_memory(kb):
+    """Memory that work on the current stream still writes is no place for another stream's results."""
+    import torch
+    X, W, b, _, G, _ = inputs(4096, 64, 512, 24)
+    layer = dict(W=dev(W), b=dev(b), act=ref.IDENTITY)
+    x, g, a = dev(X), dev(G), torch.zeros((4096, 4096), device="cuda")
+    want = kb.dense_forward(layer, x)[0].clone()
+    grads = {k: v.clone() for k, v in kb.dense_backward(layer, x, None, g).items()}
+    norm = dict(gamma=None, beta=None, eps=1e-5)
+    normed = kb.layer_norm_forward(norm, want)[0].clone()
+    side, out = torch.cuda.Stream(), torch.empty_like(a)
+    for stream in (side, side.cuda_stream):
+        torch.cuda.synchronize()
+        for _ in range(40):
+            torch.mm(a, a, out=out)                          # tens of milliseconds that the fills below wait for
+        late = [torch.empty_like(t) for t in [want, normed] + list(grads.values()) for _ in range(3)]
+        for t in late:
+            t.fill_(7.0)
+        del late, t
+        Y = kb.dense_forward(layer, x, stream=stream)[0]
+        got = kb.dense_backward(layer, x, None, g, stream=stream)
+        N = kb.layer_norm_forward(norm, want, stream=stream)[0]
+        torch.cuda.synchronize()
+        assert bool((Y == want).all()) and bool((N == normed).all())
+        assert all(bool((got[k] == grads[k]).all()) for k in grads)
