@@ -441,36 +441,51 @@ __global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>:
     }
 }
 
-// dW and db from the chunks' sums: 32 elements a block, Y runs of chunks side by side, then these in their order
+// dW and db from the chunks' sums: 64 elements of either a block, four a lane, Y runs of chunks side by side, then these in their
+// order.  One element a lane took 28 us in place of 12 at 3 chunks of 1500 x 1500, and 13.5 in place of 10 at 128 of 256 x 256
 template <int Y>
-__global__ __launch_bounds__(32 * Y) void k_dense_sum(const float *__restrict__ part, const float *__restrict__ part_b, int64_t chunks, int64_t nw,
+__global__ __launch_bounds__(16 * Y) void k_dense_sum(const float *__restrict__ part, const float *__restrict__ part_b, int64_t chunks, int64_t nw,
                                                     int64_t nb, float *__restrict__ dW, float *__restrict__ db)
 {
-    __shared__ float s[Y][33];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int64_t i = (int64_t)blockIdx.x * 32 + x;
-    const bool w = i < nw;
-    const float *from = w ? part + i : part_b + (i - nw);
-    const int64_t step = w ? nw : nb;
-    float v = 0.f;
-    if (i < nw + nb) {
+    struct __attribute__((packed, aligned(4))) F4 { float x[4]; };
+    __shared__ float s[Y][68];
+    const int x = 4 * (threadIdx.x & 15), y = threadIdx.x >> 4;
+    const int64_t blocks_w = cdiv(nw, 64);
+    const bool w = blockIdx.x < blocks_w;
+    const int64_t n = w ? nw : nb, i0 = (w ? blockIdx.x : blockIdx.x - blocks_w) * 64, left = n - i0 - x;
+    const float *const from = (w ? part : part_b) + i0 + x;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (left >= 4) {
+        auto at = [&](int64_t c) { return *reinterpret_cast<const F4 *>(from + c * n); };
         int64_t c = y;
         for (; c + 3 * Y < chunks; c += 4 * Y) {       // four loads on their way, added in the chunks' order
-            float z[4];
+            F4 z[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) z[k] = from[(c + Y * k) * step];
+            for (int k = 0; k < 4; ++k) z[k] = at(c + Y * k);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v += z[k];
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += z[k].x[e];
         }
-        for (; c < chunks; c += Y) v += from[c * step];
-    }
-    s[y][x] = v;
-    __syncthreads();
-    if (y == 0 && i < nw + nb) {
-        v = 0.f;
+        for (; c < chunks; c += Y) {
+            const F4 z = at(c);
 #pragma unroll
-        for (int r = 0; r < Y; ++r) v += s[r][x];
-        (w ? dW + i : db + (i - nw))[0] = v;
+            for (int e = 0; e < 4; ++e) v[e] += z.x[e];
+        }
+    } else {
+        for (int64_t c = y; c < chunks; c += Y)
+#pragma unroll
+            for (int e = 0; e < 3; ++e) if (e < left) v[e] += from[c * n + e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[y][x + e] = v[e];
+    __syncthreads();
+    const int t = threadIdx.x;
+    if (t < 64 && i0 + t < n) {
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < Y; ++r) sum += s[r][t];
+        (w ? dW : db)[i0 + t] = sum;
     }
 }
 
@@ -501,12 +516,14 @@ Tile weights_tile(const kge_dense *L)
     return {128, 128};
 }
 
-// chunks of rows of the weights' gradient: about as many blocks as run at once, at least 256 rows each
+// Chunks of rows of the weights' gradient: as many as run at once, at least 256 rows each.  A chunk's tiles run on one XCD: the chip
+// holds 512 blocks, but an XCD 64, and one more than that is a second round (29082 x 203 x 517 fp32, 10 tiles: 103 us with 51 chunks,
+// 7 of them on some XCDs, 73 with 48; 60000 x 384 x 384 bf16 65 and 44)
 int64_t chunk_rows(const kge_dense *L, int64_t n_rows)
 {
     const Tile tile = weights_tile(L);
-    const int64_t tiles = cdiv(L->d_in, tile.bm) * cdiv(L->d_out, tile.bn);
-    int64_t chunks = cdiv(tile.bm == 256 ? 256 : 512, tiles);
+    const int64_t tiles = cdiv(L->d_in, tile.bm) * cdiv(L->d_out, tile.bn), at_once = tile.bm == 256 ? 256 : 512;
+    int64_t chunks = tiles <= at_once / 8 ? 8 * (at_once / 8 / tiles) : at_once / tiles;
     if (chunks > cdiv(n_rows, 256)) chunks = cdiv(n_rows, 256);
     if (chunks < 1) chunks = 1;
     return align_up((size_t)cdiv(n_rows > 0 ? n_rows : 1, chunks), 64);
@@ -615,9 +632,11 @@ int backward(const kge_dense *L, int64_t n, const void *X, int64_t ldx, const vo
         }
         KGE_PROF("dense_sum", st);             // without rows: sums of nothing, zeros
         const int64_t w = dW ? nw : 0, b = db ? L->d_out : 0;
-        const unsigned blocks = (unsigned)cdiv(w + b, 32);
-        if (chunks > 96) k_dense_sum<32><<<blocks, 1024, 0, st>>>(a.part, a.part_b, chunks, w, b, dW, db);
-        else k_dense_sum<8><<<blocks, 256, 0, st>>>(a.part, a.part_b, chunks, w, b, dW, db);
+        const unsigned blocks = (unsigned)(cdiv(w, 64) + cdiv(b, 64));
+        if (chunks > 256) k_dense_sum<64><<<blocks, 1024, 0, st>>>(a.part, a.part_b, chunks, w, b, dW, db);
+        else if (chunks > 96) k_dense_sum<32><<<blocks, 512, 0, st>>>(a.part, a.part_b, chunks, w, b, dW, db);
+        else if (chunks > 16) k_dense_sum<16><<<blocks, 256, 0, st>>>(a.part, a.part_b, chunks, w, b, dW, db);
+        else k_dense_sum<4><<<blocks, 64, 0, st>>>(a.part, a.part_b, chunks, w, b, dW, db);
         KGE_LAUNCH_CHECK();
     }
     return KGE_OK;

@@ -389,3 +389,17 @@ def test_results_on_a_callers_stream_are_of_its_memory(kb):
         torch.cuda.synchronize()
         assert bool((Y == want).all()) and bool((N == normed).all())
         assert all(bool((got[k] == grads[k]).all()) for k in grads)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n,di,do", [(29082, 203, 517), (3000, 700, 129), (2600, 9, 3), (70000, 66, 65), (140000, 20, 21), (300, 1030, 1100)])
+def test_weights_gradients_of_few_and_many_chunks(kb, kind, n, di, do):
+    say("dense chunks", kind, n, di, do)
+    X, _, _, Z, G, _ = inputs(n, di, do, 25)
+    x, z, g = dev(X, kind), dev(Z, kind), dev(G, kind)
+    layer = dict(W=dev(np.zeros((di, do)), kind), b=None, act=ref.RELU)
+    got = kb.dense_backward(layer, x, z, g, need_dX=False)
+    args = (host(x), host(layer["W"]), host(z), host(g), ref.RELU)
+    want, bound = ref.dense_backward(*args), ref.dense_backward_bound(*args, None, kind)
+    within(host(got["dW"]), want[1], bound[1], "dW")
+    within(host(got["db"]), want[2], bound[2], "db")
