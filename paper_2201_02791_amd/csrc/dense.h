@@ -129,6 +129,7 @@ struct Args {
     int64_t K;                     // terms
     int64_t chunk;                 // terms per block (WEIGHTS; K otherwise)
     int32_t tiles_n;
+    uint32_t wide;                 // blocks in front of those of the last, narrow columns
     int64_t tiles_m;
     T *C, *pre_out;                // FORWARD: Y, pre;  INPUT: dX
     int64_t ldc, ldp;

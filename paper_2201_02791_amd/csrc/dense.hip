@@ -29,6 +29,8 @@
 // the chip holds, each writes its sums to the workspace and a second launch adds them in a fixed order.
 #include "dense.h"
 
+#include <algorithm>
+
 using namespace dense;
 
 namespace {
@@ -49,8 +51,9 @@ struct Shape {
     static constexpr int PB = F32 ? 3 : MODE == WEIGHTS && SOFT ? 3 : 1;
     static constexpr bool ROWA = MODE != WEIGHTS, ROWB = MODE == INPUT;    // terms side by side
     static constexpr int NT = 64 * WM * WN, MI = BM / 32 / WM, NJ = BN / 32 / WN;
-    static constexpr int BK = (PA + PB > 2 && BM > 32 && BN > 32) || BM == 256 ? 32 : 64;
-    static constexpr int CHA = BM * BK / 8 / NT, CHB = BN * BK / 8 / NT;   // chunks of 8 per thread
+    static constexpr int BK = (PA + PB > 2 && (MODE != WEIGHTS || (BM > 32 && BN > 32))) || BM == 256 ? 32 : 64;
+    static constexpr int ALLA = BM * BK / 8, ALLB = BN * BK / 8;         // chunks of 8; with fewer than threads, several hold the same one
+    static constexpr int CHA = ALLA / NT, CHB = ALLB < NT ? 1 : ALLB / NT;
     static constexpr int PLANEA = BM * BK * 2, PLANEB = BN * BK * 2;
     static constexpr int BUFFER = PA * PLANEA + PB * PLANEB;
     // a block that has its compute unit to itself stages one tile while it multiplies another
@@ -60,7 +63,7 @@ struct Shape {
     static constexpr int OUT = 32 * NJ + 8;                            // floats per row of results in LDS: 4 rows further, 32 banks further
     static constexpr int TILES = (TWO ? 2 : 1) * BUFFER, RESULTS = WM * WN * 32 * OUT * 4;
     static constexpr int LDS = TILES > RESULTS ? TILES : RESULTS;
-    static_assert(CHA * 8 * NT == BM * BK && CHB * 8 * NT == BN * BK, "whole chunks");
+    static_assert(CHA * NT == ALLA && (CHB * NT == ALLB || (MODE != WEIGHTS && NT % ALLB == 0)), "whole chunks");
     static_assert(LDS >= NT * 32, "the columns' sums");
 };
 
@@ -77,42 +80,15 @@ __device__ __forceinline__ int column_swap(int k) { return W >= 128 ? k & 3 : W 
 template <int W>
 __device__ __forceinline__ int column_place(int k, int c) { return k * (2 * W) + ((c ^ (4 * column_swap<W>(k))) << 4); }
 
+// the tile at row m0 and column n0 of the result, its terms those of a chunk
 template <int MODE, class T, int ACT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>::WAVES)) void k_dense(Args<T> a)
+__device__ __forceinline__ void tile_at(const Args<T> &a, int64_t m0, int32_t n0, int64_t chunk, unsigned char *smem)
 {
     typedef Shape<MODE, T, ACT, BM, BN, WM, WN> S;
     constexpr int BK = S::BK, PA = S::PA, PB = S::PB, NT = S::NT, MI = S::MI, NJ = S::NJ;
-    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-
-    // block -> (tile of rows, tile of columns, chunk of terms).  Workgroup i runs on XCD i % 8, each with its own L2: the
-    // tiles that read the same long rows follow one another on one XCD
-    int64_t tm, chunk = 0;
-    int32_t tn;
-    if (MODE == WEIGHTS) {
-        const int64_t tiles = a.tiles_m * a.tiles_n, chunks = cdiv(a.K, a.chunk);
-        if (chunks >= 8) {
-            const int64_t seq = blockIdx.x >> 3;
-            chunk = (seq / tiles) * 8 + (blockIdx.x & 7);
-            const int64_t t = seq % tiles;
-            tm = t / a.tiles_n; tn = (int32_t)(t % a.tiles_n);
-        } else {
-            chunk = blockIdx.x / tiles;
-            const int64_t t = blockIdx.x % tiles;
-            tm = t / a.tiles_n; tn = (int32_t)(t % a.tiles_n);
-        }
-        if (chunk >= chunks) return;
-    } else if (a.tiles_m >= 64) {
-        const int64_t seq = blockIdx.x >> 3;
-        tm = (seq / a.tiles_n) * 8 + (blockIdx.x & 7);
-        tn = (int32_t)(seq % a.tiles_n);
-        if (tm >= a.tiles_m) return;
-    } else {
-        tm = blockIdx.x / a.tiles_n;
-        tn = (int32_t)(blockIdx.x % a.tiles_n);
-    }
-    const int64_t m0 = tm * BM, k_beg = chunk * a.chunk, k_end = min(k_beg + a.chunk, a.K);
-    const int32_t n0 = tn * BN;
+    const int64_t k_beg = chunk * a.chunk, k_end = min(k_beg + a.chunk, a.K);
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), wm = w / WN, wn = w % WN;
+    const int tb = S::ALLB < NT ? t % S::ALLB : t;
 
     struct Set {
         Held<S::F32, S::CHA> a, p;
@@ -128,7 +104,7 @@ __global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>:
     // Where this thread's chunks lie when k0 = k_beg, and how far apart the tiles are.  Rows and columns past the result's read the
     // last row or the first chunk in their place: what they add up to is not stored.  Only terms past the end have to be zeros.
     struct Walk { const T *p[(S::CHA > S::CHB ? S::CHA : S::CHB)]; int64_t tile; };
-    auto walk = [&](const T *base, int64_t ld, auto terms, auto per, auto chunks, int64_t outer0, int64_t outer_n) __attribute__((always_inline)) -> Walk {
+    auto walk = [&](int t, const T *base, int64_t ld, auto terms, auto per, auto chunks, int64_t outer0, int64_t outer_n) __attribute__((always_inline)) -> Walk {
         constexpr int PER = decltype(per)::value;
         Walk x;
 #pragma unroll
@@ -146,15 +122,15 @@ __global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>:
     const std::integral_constant<int, S::ROWB ? TC : BC> cb{};
     const std::integral_constant<int, S::CHA> na{};
     const std::integral_constant<int, S::CHB> nb{};
-    Walk wa = walk(a.A, a.lda, ra, ca, na, m0, a.M), wb = walk(a.B, a.ldb, rb, cb, nb, n0, a.N), wp{};
-    if constexpr (GRAD) wp = MODE == INPUT ? walk(a.pre, a.ldpre, ra, ca, na, m0, a.M) : walk(a.pre, a.ldpre, rb, cb, nb, n0, a.N);
+    Walk wa = walk(t, a.A, a.lda, ra, ca, na, m0, a.M), wb = walk(tb, a.B, a.ldb, rb, cb, nb, n0, a.N), wp{};
+    if constexpr (GRAD) wp = MODE == INPUT ? walk(t, a.pre, a.ldpre, ra, ca, na, m0, a.M) : walk(tb, a.pre, a.ldpre, rb, cb, nb, n0, a.N);
     // Tiles up to here load whole chunks: their terms all exist, and a chunk that the end of a row of columns cuts reads on into the
     // next row, which the last one (the last eight, should they be narrower than a chunk) does not have
     const bool cut = (!S::ROWA && a.M % 8 != 0) || (!S::ROWB && a.N % 8 != 0);
     const int64_t k_whole = min(k_end, cut ? a.K - 8 : a.K) - BK;
 
     auto fetch = [&](Set &h, int64_t k0, auto counted) __attribute__((always_inline)) {
-        auto one = [&](auto &h, int j, const Walk &x, auto terms, auto per, int64_t outer0, int64_t outer_n, auto whole) __attribute__((always_inline)) {
+        auto one = [&](int t, auto &h, int j, const Walk &x, auto terms, auto per, int64_t outer0, int64_t outer_n, auto whole) __attribute__((always_inline)) {
             constexpr int PER = decltype(per)::value;
             if constexpr (decltype(whole)::value) {
                 if constexpr (S::F32) load8(x.p[j], h.x[j]);
@@ -172,13 +148,13 @@ __global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>:
         auto all = [&](auto whole) __attribute__((always_inline)) {
 #pragma unroll
             for (int j = 0; j < S::CHA; ++j) {
-                one(h.a, j, wa, ra, ca, m0, a.M, whole);
-                if constexpr (MODE == INPUT && GRAD) one(h.p, j, wp, ra, ca, m0, a.M, whole);
+                one(t, h.a, j, wa, ra, ca, m0, a.M, whole);
+                if constexpr (MODE == INPUT && GRAD) one(t, h.p, j, wp, ra, ca, m0, a.M, whole);
             }
 #pragma unroll
             for (int j = 0; j < S::CHB; ++j) {
-                one(h.b, j, wb, rb, cb, n0, a.N, whole);
-                if constexpr (MODE == WEIGHTS && GRAD) one(h.q, j, wp, rb, cb, n0, a.N, whole);
+                one(tb, h.b, j, wb, rb, cb, n0, a.N, whole);
+                if constexpr (MODE == WEIGHTS && GRAD) one(tb, h.q, j, wp, rb, cb, n0, a.N, whole);
             }
         };
         if constexpr (decltype(counted)::value) all(std::true_type());
@@ -206,12 +182,12 @@ __global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>:
     float col[8];                  // WEIGHTS: sums of dP over this thread's rows, its 8 columns
 #pragma unroll
     for (int k = 0; k < 8; ++k) col[k] = 0.f;
-    const bool sum_columns = MODE == WEIGHTS && a.part_b && tm == 0;
+    const bool sum_columns = MODE == WEIGHTS && a.part_b && m0 == 0;
 
     // registers -> LDS, dY -> dP on the way
     auto stage = [&](const Set &set, unsigned char *la) __attribute__((always_inline)) {
         unsigned char *const lb = la + PA * S::PLANEA;
-        auto one = [&](const auto &h, const auto &hg, int j, unsigned char *lds, auto terms, auto per, auto parts, int plane, auto grad,
+        auto one = [&](int t, const auto &h, const auto &hg, int j, unsigned char *lds, auto terms, auto per, auto parts, int plane, auto grad,
                        bool columns) __attribute__((always_inline)) {
             constexpr int PER = decltype(per)::value, P = decltype(parts)::value;
             const int r = (j * NT + t) / PER, c = t % PER;
@@ -253,10 +229,10 @@ __global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>:
         };
 #pragma unroll
         for (int j = 0; j < S::CHA; ++j)
-            one(set.a, set.p, j, la, ra, ca, std::integral_constant<int, PA>(), S::PLANEA, std::integral_constant<bool, MODE == INPUT && GRAD>(), false);
+            one(t, set.a, set.p, j, la, ra, ca, std::integral_constant<int, PA>(), S::PLANEA, std::integral_constant<bool, MODE == INPUT && GRAD>(), false);
 #pragma unroll
         for (int j = 0; j < S::CHB; ++j)
-            one(set.b, set.q, j, lb, rb, cb, std::integral_constant<int, PB>(), S::PLANEB, std::integral_constant<bool, MODE == WEIGHTS && GRAD>(),
+            one(tb, set.b, set.q, j, lb, rb, cb, std::integral_constant<int, PB>(), S::PLANEB, std::integral_constant<bool, MODE == WEIGHTS && GRAD>(),
                 sum_columns);
     };
 
@@ -441,6 +417,43 @@ __global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>:
     }
 }
 
+// NARROW: the last columns, 32 or fewer, have tiles of 128 x 32 behind the others
+template <int MODE, class T, int ACT, int BM, int BN, int WM, int WN, bool NARROW>
+__global__ __launch_bounds__(64 * WM * WN, (Shape<MODE, T, ACT, BM, BN, WM, WN>::WAVES)) void k_dense(Args<T> a)
+{
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    // block -> (tile of rows, tile of columns, chunk of terms).  Workgroup i runs on XCD i % 8, each with its own L2: the
+    // tiles that read the same long rows follow one another on one XCD
+    int64_t tm, chunk = 0;
+    int32_t tn;
+    if (MODE == WEIGHTS) {
+        const int64_t tiles = a.tiles_m * a.tiles_n, chunks = cdiv(a.K, a.chunk);
+        if (chunks >= 8) {
+            const int64_t seq = blockIdx.x >> 3;
+            chunk = (seq / tiles) * 8 + (blockIdx.x & 7);
+            const int64_t t = seq % tiles;
+            tm = t / a.tiles_n; tn = (int32_t)(t % a.tiles_n);
+        } else {
+            chunk = blockIdx.x / tiles;
+            const int64_t t = blockIdx.x % tiles;
+            tm = t / a.tiles_n; tn = (int32_t)(t % a.tiles_n);
+        }
+        if (chunk >= chunks) return;
+    } else if (NARROW && blockIdx.x >= a.wide) {
+        if constexpr (NARROW) tile_at<MODE, T, ACT, 128, 32, 4, 1>(a, (int64_t)(blockIdx.x - a.wide) * 128, a.tiles_n * BN, 0, smem);
+        return;
+    } else if (a.tiles_m >= 64) {
+        const int64_t seq = blockIdx.x >> 3;
+        tm = (seq / a.tiles_n) * 8 + (blockIdx.x & 7);
+        tn = (int32_t)(seq % a.tiles_n);
+        if (tm >= a.tiles_m) return;
+    } else {
+        tm = blockIdx.x / a.tiles_n;
+        tn = (int32_t)(blockIdx.x % a.tiles_n);
+    }
+    tile_at<MODE, T, ACT, BM, BN, WM, WN>(a, tm * BM, tn * BN, chunk, smem);
+}
+
 // dW and db from the chunks' sums: 64 elements of either a block, four a lane, Y runs of chunks side by side, then these in their
 // order.  One element a lane took 28 us in place of 12 at 3 chunks of 1500 x 1500, and 13.5 in place of 10 at 128 of 256 x 256
 template <int Y>
@@ -537,23 +550,38 @@ void with_act(int act, F f)
     else f(std::integral_constant<int, KGE_ACT_IDENTITY>());
 }
 
-template <int MODE, class T, int BM, int BN, int WM, int WN>
+// Up to three whole tiles of columns and 32 columns or fewer (us with a tile of 128 for these against narrow ones): fp32 112 / 119
+// against 92 / 108 (forward with 200 terms / input gradient with 200, 100000 rows, 160 columns), 137 / 160 against 128 / 149 (60000
+// rows, 288), 196 / 217 against 192 / 206 (100000, 400), but 233 against 240 with 528; bf16 forward 43 against 34, 44 against 42, 75
+// against 64.  A bf16 input gradient splits dP in either: 54 against 59 with 160 columns
+template <int MODE, class T>
+constexpr bool MAY_NARROW = MODE == FORWARD || (MODE == INPUT && sizeof(T) == 4);
+bool narrow_pays(int32_t n) { return n > 128 && n <= 416 && n % 128 >= 1 && n % 128 <= 32; }
+
+template <int MODE, class T, int BM, int BN, int WM, int WN, bool NARROW = false>
 int launch_tile(int act, Args<T> a, hipStream_t st)
 {
+    if constexpr (MAY_NARROW<MODE, T> && !NARROW) {
+        if (narrow_pays(a.N)) return launch_tile<MODE, T, BM, BN, WM, WN, true>(act, a, st);
+    }
     a.tiles_m = cdiv(a.M, BM);
-    a.tiles_n = (int32_t)cdiv(a.N, BN);
+    a.tiles_n = NARROW ? a.N / BN : (int32_t)cdiv(a.N, BN);
     int64_t blocks = a.tiles_m * a.tiles_n;
     if (MODE == WEIGHTS) {
         const int64_t chunks = cdiv(a.K, a.chunk);
         blocks *= chunks >= 8 ? (int64_t)align_up((size_t)chunks, 8) : chunks;
     } else if (a.tiles_m >= 64) blocks = (int64_t)align_up((size_t)a.tiles_m, 8) * a.tiles_n;
+    a.wide = (uint32_t)blocks;
+    if (NARROW) blocks += cdiv(a.M, 128);
     KGE_REQUIRE(blocks < (1ll << 32) / (64 * WM * WN), KGE_ERANGE, "dense: too large for one launch");
     hipError_t e = hipSuccess;
     with_act(act, [&](auto act_c) {
-        constexpr int ACT = decltype(act_c)::value, LDS = Shape<MODE, T, ACT, BM, BN, WM, WN>::LDS;
-        auto kernel = k_dense<MODE, T, ACT, BM, BN, WM, WN>;
-        if (LDS > 64 * 1024) e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-        if (e == hipSuccess) kernel<<<(unsigned)blocks, 64 * WM * WN, LDS, st>>>(a);
+        constexpr int ACT = decltype(act_c)::value, WIDE = Shape<MODE, T, ACT, BM, BN, WM, WN>::LDS;
+        int lds = WIDE;
+        if constexpr (NARROW) lds = std::max(lds, Shape<MODE, T, ACT, 128, 32, 4, 1>::LDS);
+        auto kernel = k_dense<MODE, T, ACT, BM, BN, WM, WN, NARROW>;
+        if (lds > 64 * 1024) e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e == hipSuccess) kernel<<<(unsigned)blocks, 64 * WM * WN, lds, st>>>(a);
     });
     KGE_HIP(e);
     KGE_LAUNCH_CHECK();

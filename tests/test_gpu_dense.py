@@ -403,3 +403,22 @@ def test_weights_gradients_of_few_and_many_chunks(kb, kind, n, di, do):
     want, bound = ref.dense_backward(*args), ref.dense_backward_bound(*args, None, kind)
     within(host(got["dW"]), want[1], bound[1], "dW")
     within(host(got["db"]), want[2], bound[2], "db")
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n,di,do,act", [(30000, 129, 160, "silu"), (14541, 160, 129, "relu"), (9000, 388, 416, "identity"), (12001, 260, 257, "silu")])
+def test_last_columns_of_a_wide_result(kb, kind, n, di, do, act):
+    """Results one to 32 columns wider than whole tiles."""
+    say("dense narrow", kind, n, di, do, act)
+    X, W, b, R, G, A = inputs(n, di, do, 26)
+    x, r, g, a = (dev(z, kind) for z in (X, R, G, A))
+    layer = dict(W=dev(W, kind), b=dev(b), act=ACTS[act])
+    Y, pre = kb.dense_forward(layer, x, R=r, keep_pre=True)
+    got = kb.dense_backward(layer, x, pre, g, add=a)
+    b64 = b.astype(np.float64)
+    forward = (host(x), host(layer["W"]), b64, ACTS[act], host(r))
+    for t, w, e, name in zip((Y, pre), ref.dense_forward(*forward), ref.dense_forward_bound(*forward, kind), ("Y", "pre")):
+        within(host(t), w, e, name)
+    back = (host(x), host(layer["W"]), host(pre), host(g), ACTS[act], host(a))
+    for k, w, e in zip(("dX", "dW", "db"), ref.dense_backward(*back), ref.dense_backward_bound(*back, kind)):
+        within(host(got[k]), w, e, k)
