@@ -57,6 +57,18 @@ def test_dense_backward(kb):
     assert lib.kge_dense_backward(None, L(5), P, L(8), P, L(4), P, L(4), N0, L(8), P, L(8), P, P, P, C.c_size_t(1 << 20), N0) == EINVAL
 
 
+def test_dense_outputs_that_are_inputs(kb):
+    lib, d = kb.load(), kb._Dense(8, 8, 1, 0, 1 << 12, None)
+    X, R, Y, Z = (C.c_void_p((k + 1) << 12) for k in range(4))
+    forward = lambda X, R, Y, pre: lib.kge_dense_forward(C.byref(d), L(5), X, L(8), R, L(8), Y, L(8), pre, L(8), N0)  # noqa: E731
+    for call in ((X, N0, X, N0), (X, X, X, Z), (X, R, Y, X), (X, R, Y, R), (X, R, Y, Y)):
+        assert forward(*call) == EINVAL and b"may not be" in lib.kge_last_error()
+    backward = lambda dX, ws: lib.kge_dense_backward(C.byref(d), L(5), X, L(8), Y, L(8), Z, L(8), R, L(8), dX, L(8), ws, ws, ws,  # noqa: E731
+                                                     C.c_size_t(1 << 20), N0)
+    for dX in (X, Y, Z):
+        assert backward(dX, P) == EINVAL and b"may not be" in lib.kge_last_error()
+
+
 def test_layer_norm(kb):
     lib = kb.load()
     fwd = lambda p, n=5, X=P, Y=P, ldx=8: lib.kge_layer_norm_forward(C.byref(p), L(n), X, L(ldx), Y, L(8), N0, N0, N0)  # noqa: E731
