@@ -422,3 +422,23 @@ def test_last_columns_of_a_wide_result(kb, kind, n, di, do, act):
     back = (host(x), host(layer["W"]), host(pre), host(g), ACTS[act], host(a))
     for k, w, e in zip(("dX", "dW", "db"), ref.dense_backward(*back), ref.dense_backward_bound(*back, kind)):
         within(host(got[k]), w, e, k)
+
+
+@pytest.mark.parametrize("kind,n,di,do", [("f32", 17003, 128, 768), ("f32", 16500, 80, 384), ("f32", 17000, 640, 72), ("bf16", 200001, 72, 264),
+                                          ("bf16", 200016, 264, 72)])
+def test_several_groups_of_columns_of_a_long_matrix(kb, kind, n, di, do):
+    say("dense groups", kind, n, di, do)
+    X, W, b, R, G, _ = inputs(n, di, do, 27)
+    x, r, g = dev(X, kind), dev(R, kind), dev(G, kind)
+    layer = dict(W=dev(W, kind), b=dev(b), act=ref.RELU)
+    Y, pre = kb.dense_forward(layer, x, R=r, keep_pre=True)
+    dX = kb.dense_backward(layer, x, pre, g, need_dW=False)["dX"]
+    w, b64 = host(layer["W"]), b.astype(np.float64)
+    for part in (slice(0, 300), slice(n // 2, n // 2 + 1000), slice(n - 4000, n)):      # every group and wavefront, first and last tiles
+        forward = (host(x[part]), w, b64, ref.RELU, host(r[part]))
+        for t, want, e, name in zip((Y, pre), ref.dense_forward(*forward), ref.dense_forward_bound(*forward, kind), ("Y", "pre")):
+            within(host(t[part]), want, e, name)
+        back = (host(x[part]), w, host(pre[part]), host(g[part]), ref.RELU)
+        within(host(dX[part]), ref.dense_backward(*back)[0], ref.dense_backward_bound(*back, None, kind)[0], "dX")
+    again = kb.dense_forward(layer, x, R=r)[0]
+    assert bool((again == Y).all())
