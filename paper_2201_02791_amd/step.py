@@ -177,21 +177,33 @@ class TrainStep:
     # --- Algorithm 1, "optimizer.step()": every parameter the step has a gradient for
     def optimizer_step(self, kind: int = kb.OPT_ADAM, lr: float = 0.01, beta1: float = 0.9, beta2: float = 0.999,
                        eps: float = 1e-8, stream=None):
+        """The state is that of init_optimizer, or of the first call's kind; plain gradient descent needs none.  A call that is
+        refused is no step: the next one has its number."""
+        self._check_kind(kind)
+        if kind != kb.OPT_ADAMW and self.block is not None and self.block.W_rows is not self.block.W:
+            raise ValueError("a feature block in bf16 takes OPT_ADAMW, which writes the bf16 copy of its weight")
         if not hasattr(self, "opt_t"):
             self.init_optimizer(kind)
-        self.opt_t += 1
+        if kind not in (kb.OPT_SGD, self.opt_kind):
+            raise ValueError("the optimizer's state is of another kind: init_optimizer makes this one's")
+        t = self.opt_t + 1
         if kind == kb.OPT_ADAMW:
-            kb.adamw_step(self.opt_plan, lr, beta1, beta2, eps, self.opt_t, stream=stream)
+            kb.adamw_step(self.opt_plan, lr, beta1, beta2, eps, t, stream=stream)
+            self.opt_t = t
             return
-        if self.block is not None and self.block.W_rows is not self.block.W:
-            raise ValueError("a feature block in bf16 takes OPT_ADAMW, which writes the bf16 copy of its weight")
         # the entity table: only the rows the step read (flags of the sub-graph's input rows; without a
         # sub-graph the kernel skips rows whose gradient is all zero)
         mask = self.cg.input_rows_ptr() if self.cg is not None else None
         for name, p, g, rows in self._opt_pairs():
             m, v = self.opt_state.get(name, (None, None)) if kind == kb.OPT_ADAM else (None, None)
-            kb.optimizer_step(kind, p, g, m, v, lr, beta1, beta2, eps, self.opt_t, rows=rows,
+            kb.optimizer_step(kind, p, g, m, v, lr, beta1, beta2, eps, t, rows=rows,
                               row_mask=mask if rows else None, stream=stream)
+        self.opt_t = t
+
+    @staticmethod
+    def _check_kind(kind):
+        if kind not in (kb.OPT_SGD, kb.OPT_ADAM, kb.OPT_ADAMW):
+            raise ValueError("OPT_SGD, OPT_ADAM or OPT_ADAMW is wanted, not %r" % (kind,))
 
     def _opt_pairs(self):
         pairs = [("M", self.M, self.dM, False)]
@@ -210,7 +222,8 @@ class TrainStep:
         """Allocate (zeroed) moments for every parameter, so that no step allocates.  OPT_ADAMW: all parameters in one launch;
         moments of 32 or 8 bits (tensors of fewer than 4096 elements keep 32); weight_decay for every matrix but the entity
         table, whose rows the batches reach unevenly."""
-        self.opt_t = 0
+        self._check_kind(kind)
+        self.opt_t, self.opt_kind = 0, kind
         self.opt_state = {}
         if kind == kb.OPT_ADAM:
             for name, p, _, _ in self._opt_pairs():
