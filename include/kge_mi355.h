@@ -396,10 +396,10 @@ int kge_layer_norm_backward(const kge_norm *norm, int64_t n_rows, const void *X,
                             float *dbeta, void *workspace, size_t ws_bytes, void *stream);
 
 /*
- * AdamW over a list of tensors, in one launch per 28 tensors (Adam with decoupled weight decay):
+ * AdamW over a list of tensors, in one launch per 28 tensors or 2^26 wavefronts of 256 elements or less (Adam with decoupled weight decay):
  *   m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
  *   p <- p - lr (weight_decay p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)),  t = 1, 2, ...
- * Each tensor is n_rows rows of d elements, dense.  Only the rows that `rows` takes are read and written:
+ * Each tensor is n_rows rows of d elements, dense, fewer than 2^36 (KGE_ERANGE).  Only the rows that `rows` takes are read and written:
  *   KGE_ROWS_ALL      all;  KGE_ROWS_MASK  those with row_mask[row] != 0 (DEVICE uint8 [n_rows], e.g. kge_cgraph_input_rows);
  *   KGE_ROWS_NONZERO  those whose gradient is not all zeros (d at most 65536)
  * state_bits 32: m, v are float arrays, zero before the first step.

@@ -1,5 +1,5 @@
 // One AdamW step over a list of tensors (decoupled weight decay, Loshchilov & Hutter 2019), in one launch per
-// LIST_MAX tensors.
+// LIST_MAX tensors (of up to 2^26 wavefronts of work).
 //
 //   m <- b1 m + (1 - b1) g;  v <- b2 v + (1 - b2) g^2;  p <- p - lr (wd p + (m / c1) / (sqrt(v / c2) + eps)),  c = 1 - b^t
 //
@@ -35,7 +35,9 @@ namespace {
 
 constexpr int BLOCK = KGE_ADAMW_BLOCK;        // 64 lanes x 4 elements
 static_assert(BLOCK == 256, "one wavefront holds a block, 4 elements a lane");
-constexpr int64_t MOST_WAVES = (1ll << 32) / 64 - 4;      // a launch has fewer than 2^32 threads
+constexpr int64_t MOST_WAVES = (1ll << 32) / 64 - 4;      // a launch has fewer than 2^32 threads: a list of more takes several
+constexpr int64_t MOST_ELEMENTS = 1ll << 36;  // no card holds as many with their gradients
+static_assert(MOST_WAVES % 4 == 0, "whole blocks");
 constexpr int LIST_MAX = 28;                  // tensors per launch: their descriptions are launch arguments, below 4 KB
 
 struct Tensor {
@@ -58,6 +60,7 @@ struct List {
     float lr, b1, b2, eps, omb1, omb2, inv_c1, inv_c2;
     const int64_t *t_dev;          // the step number in device memory, or null
     int64_t step;
+    int64_t base;                  // the launch's first wavefront
 };
 static_assert(sizeof(List) <= 4096, "launch arguments");
 
@@ -289,7 +292,7 @@ __global__ __launch_bounds__(256) void k_adamw(List o)
         }
         inv_c1 = (float)(1.0 / (1.0 - p1)); inv_c2 = (float)(1.0 / (1.0 - p2));
     }
-    const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t w = o.base + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int i = 0;
     while (i + 1 < o.n && w >= o.t[i + 1].first) ++i;
     const Tensor &T = o.t[i];
@@ -321,7 +324,7 @@ extern "C" int kge_adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tens
         KGE_REQUIRE(x.state_bits == 32 || x.state_bits == 8, KGE_EINVAL, "tensor %d: moments have 32 or 8 bits", i);
         KGE_REQUIRE(x.rows == KGE_ROWS_ALL || x.rows == KGE_ROWS_MASK || x.rows == KGE_ROWS_NONZERO, KGE_EINVAL,
                     "tensor %d: bad choice of rows", i);
-        KGE_REQUIRE(x.d == 0 || x.n_rows <= INT64_MAX / 16 / x.d, KGE_ERANGE, "tensor %d: too large", i);
+        KGE_REQUIRE(x.d == 0 || x.n_rows <= (MOST_ELEMENTS - 1) / x.d, KGE_ERANGE, "tensor %d: 2^36 elements or more", i);
         if (x.n_rows == 0 || x.d == 0) continue;
         KGE_REQUIRE(x.param && x.grad && x.m && x.v, KGE_EINVAL, "tensor %d: NULL parameter, gradient or moment", i);
         KGE_REQUIRE((x.state_bits == 8) == (x.m_scale != nullptr) && (x.state_bits == 8) == (x.v_scale != nullptr), KGE_EINVAL,
@@ -362,15 +365,16 @@ extern "C" int kge_adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tens
             while (lanes < 64 && 4 * lanes < T.d) lanes *= 2;
             T.how = lanes | (T.d % 4 == 0 ? HOW_WHOLE : 0) | (eight ? HOW_8BIT : 0) | (x.rows == KGE_ROWS_NONZERO ? HOW_NONZERO : 0);
             const int64_t units = x.rows == KGE_ROWS_NONZERO || T.nb == 1 ? cdiv(T.n_rows, 64 / lanes) : T.n_rows * T.nb;
-            if (o.n > 0 && waves + units > MOST_WAVES) break;
             T.first = waves;
             waves += units;
             o.t[o.n++] = T;
         }
         if (o.n == 0) continue;
-        KGE_REQUIRE(waves <= MOST_WAVES, KGE_ERANGE, "tensor %d: too large for one launch", i - 1);
-        k_adamw<<<(unsigned)cdiv(waves, 4), 256, 0, st>>>(o);
-        KGE_LAUNCH_CHECK();
+        for (o.base = 0; o.base < waves; o.base += MOST_WAVES) {
+            const int64_t left = waves - o.base;
+            k_adamw<<<(unsigned)cdiv(left < MOST_WAVES ? left : MOST_WAVES, 4), 256, 0, st>>>(o);
+            KGE_LAUNCH_CHECK();
+        }
     }
     return KGE_OK;
 }
