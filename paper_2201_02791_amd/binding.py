@@ -626,12 +626,13 @@ class AdamWTensors:
     """The descriptions of the tensors that adamw_step updates, laid out once (the tensors are kept alive).  Each is a dict:
     param, grad; m, v and, for moments of 8 bits, m_scale, v_scale (adamw_state makes them); and, as wanted, weight_decay (0),
     rows ("all", "mask", "nonzero"), row_mask (a tensor or a device address), copy (bf16).  A parameter of two dimensions is held
-    by rows, any other as one row."""
+    by rows, any other as one row.  What a step writes may overlap nothing else in the list: a parameter in it twice is refused."""
 
     def __init__(self, tensors: Sequence[dict]):
         torch = sys.modules["torch"]
         self.tensors = [dict(t) for t in tensors]
         self.array = (_AdamWTensor * max(len(self.tensors), 1))()
+        places = []                        # (first byte, end, whether a step writes it, tensor, name)
         for i, t in enumerate(self.tensors):
             a, p = self.array[i], t["param"]
             name = "tensor %d: " % i
@@ -663,6 +664,18 @@ class AdamWTensors:
             a.row_mask = mask if isinstance(mask, int) else _ptr(mask).value
             a.n_rows, a.d, a.state_bits = rows, d, 8 if eight else 32
             a.rows, a.weight_decay = dict(all=ROWS_ALL, mask=ROWS_MASK, nonzero=ROWS_NONZERO)[how], float(t.get("weight_decay", 0.0))
+            for k in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy"):
+                if t.get(k) is not None:
+                    places.append((t[k].data_ptr(), t[k].data_ptr() + t[k].numel() * t[k].element_size(), k != "grad", i, k))
+            if a.row_mask:
+                places.append((a.row_mask, a.row_mask + rows, False, i, "row_mask"))
+        last = written = (0, 0, False, 0, "")        # of the places before: the one that ends last, and of those that are written
+        for at in sorted(p for p in places if p[1] > p[0]):
+            over = last if at[2] else written
+            _need(at[0] >= over[1], "tensor %d: its %s overlaps %s of tensor %d" % (at[3], at[4], over[4], over[3]))
+            last = max(last, at, key=lambda p: p[1])
+            if at[2]:
+                written = max(written, at, key=lambda p: p[1])
 
 
 def _row_shape(p):
