@@ -353,11 +353,11 @@ enum { KGE_DT_F32 = 0, KGE_DT_BF16 = 1 };
  * Sums are fp32; bf16 results are rounded once, at the end.  fp32 products have fp32 accuracy (they run as bf16
  * products of exact three-way splits).
  *
- * kge_dense_forward: X [n_rows][d_in]; R [n_rows][d_out] or NULL (may be X when d_in == d_out, or Y, which may not be X); Y [n_rows][d_out];
+ * kge_dense_forward: X [n_rows][d_in]; R [n_rows][d_out] or NULL (may be X when d_in == d_out, or Y with Y's row stride, which may not be X); Y [n_rows][d_out];
  *   pre [n_rows][d_out] or NULL: act's argument rounded to dtype, for the backward pass.
  * kge_dense_backward: dP = dY * act'(pre), with act' at pre as it was stored (ReLU: dY where pre > 0, else 0 whatever dY is; a ReLU layer without R may
  *   pass Y);
- *   dX [n_rows][d_in] = dP W^T + add, or NULL;  add [n_rows][d_in] or NULL (may be dX): a gradient that reaches X past the layer,
+ *   dX [n_rows][d_in] = dP W^T + add, or NULL;  add [n_rows][d_in] or NULL (may be dX with its row stride): a gradient that reaches X past the layer,
  *     for a residual R = X that is dY
  *   dW [d_in][d_out] = X^T dP, db [d_out] = column sums of dP: float, overwritten, each may be NULL (the gradient of R is dY itself)
  *   pre may be NULL for KGE_ACT_IDENTITY, X when neither dW nor db is asked for, W when dX is not

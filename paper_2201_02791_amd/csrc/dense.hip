@@ -684,6 +684,7 @@ extern "C" int kge_dense_forward(const kge_dense *L, int64_t n_rows, const void 
     KGE_REQUIRE(at_element(L->W, L->dtype) && at_element(X, L->dtype) && at_element(R, L->dtype) && at_element(Y, L->dtype) &&
                     at_element(pre, L->dtype) && at_element(L->b, KGE_DT_F32), KGE_EINVAL, "dense: an array is not aligned to its elements");
     KGE_REQUIRE(Y != X && Y != pre && (!pre || (pre != X && pre != R)), KGE_EINVAL, "dense: Y and pre may not be X or each other, nor pre R");
+    KGE_REQUIRE(R != Y || ldr == ldy || n_rows == 1, KGE_EINVAL, "dense: an R that is Y has Y's row stride");
     hipStream_t st = (hipStream_t)stream;
     return L->dtype == KGE_DT_F32 ? forward<float>(L, n_rows, X, ldx, R, ldr, Y, ldy, pre, ldp, st)
                                   : forward<uint16_t>(L, n_rows, X, ldx, R, ldr, Y, ldy, pre, ldp, st);
@@ -715,6 +716,7 @@ extern "C" int kge_dense_backward(const kge_dense *L, int64_t n_rows, const void
         KGE_REQUIRE(ws_bytes >= kge_dense_workspace_bytes(L, n_rows), KGE_ENOMEM, "dense: workspace too small");
     }
     KGE_REQUIRE(!dX || n_rows == 0 || (dX != dY && dX != pre && dX != X), KGE_EINVAL, "dense: dX may not be dY, pre or X");
+    KGE_REQUIRE(!dX || add != dX || ldadd == lddx || n_rows <= 1, KGE_EINVAL, "dense: an add that is dX has dX's row stride");
     hipStream_t st = (hipStream_t)stream;
     return L->dtype == KGE_DT_F32
                ? backward<float>(L, n_rows, X, ldx, pre, ldp, dY, lddy, add, ldadd, dX, lddx, dW, db, workspace, st)
