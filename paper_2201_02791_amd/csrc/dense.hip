@@ -374,6 +374,7 @@ __device__ __forceinline__ void tile_at(const Args<T> &a, int64_t m0, int32_t n0
                             if (MODE == INPUT && GRAD) y = through_act<ACT>(y, elem(a.pre + m * a.ldpre + k));
                             if (MODE == WEIGHTS && GRAD) z = through_act<ACT>(z, elem(a.pre + k * a.ldpre + n + c));
                             s = fmaf(y, z, s);
+                            if (s != s) break;     // a NaN stays one: of inputs that are all NaN one term is read
                         }
                         from[c] = s;
                     }

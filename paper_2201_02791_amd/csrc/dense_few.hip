@@ -111,6 +111,7 @@ __global__ __launch_bounds__(NT) void k_dense_few(Args<T> a)
                 float y = elem(a.A + mi * a.lda + i);
                 if (GRAD) y = through_act<ACT>(y, elem(a.pre + mi * a.ldpre + i));
                 x = fmaf(y, elem(MODE == FORWARD ? a.B + (int64_t)i * a.ldb + ni : a.B + (int64_t)ni * a.ldb + i), x);
+                if (x != x) break;             // a NaN stays one: of inputs that are all NaN one term is read
             }
         }
         if (MODE == FORWARD) {

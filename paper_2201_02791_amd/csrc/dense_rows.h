@@ -287,6 +287,7 @@ __global__ __launch_bounds__(64 * WN, 2) void k_dense_rows(RowArgs<T> r)
                             float y = elem(a.A + m * a.lda + i);
                             if (GRAD) y = through_act<ACT>(y, elem(a.pre + m * a.ldpre + i));
                             s = fmaf(y, elem(MODE == FORWARD ? a.B + (int64_t)i * a.ldb + on + k : a.B + (int64_t)(on + k) * a.ldb + i), s);
+                            if (s != s) break;     // a NaN stays one: of inputs that are all NaN one term is read
                         }
                         from[k] = s;
                     }
