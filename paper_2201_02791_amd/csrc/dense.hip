@@ -559,6 +559,18 @@ template <int MODE, class T>
 constexpr bool MAY_NARROW = MODE == FORWARD || (MODE == INPUT && sizeof(T) == 4);
 bool narrow_pays(int32_t n) { return n > 128 && n <= 416 && n % 128 >= 1 && n % 128 <= 32; }
 
+// fp32 tiles of 64 x 128 in place of 128 x 128, forward / input gradient, time over that of 128 x 128.  Up to 384 of these: twice as many
+// blocks of 64 rows leave no more than three on a compute unit, in place of one or two unequally: 0.81 to 0.98 from 200 to 360 tiles, at 203
+// to 768 terms and 203 to 640 columns (but 1.02 at 255 tiles of 768 terms).  Above, W is split and read twice as often for a round that is
+// no shorter: 400 tiles 1.01 to 1.05 up to 320 terms, 1.04 to 1.10 from 384 on; 512 0.92 to 1.04, 0.97 to 1.08; 570 0.93 to 1.02, 0.96 to
+// 1.05; 640 0.96 to 1.03, 0.99 to 1.06; 700 to 768 0.91 to 1.05 at 200 terms, 0.95 to 1.12 at 512.  Rows of an odd number of terms gain most:
+// 14541 x 203 x 517 with SiLU, 570 tiles, 51.7 / 44.7 us against 53.0 / 54.2.
+bool half_tall_pays(int64_t m, int32_t n, int64_t terms)
+{
+    const int64_t tiles = cdiv(m, 128) * cdiv(n, 128);
+    return tiles <= 384 || (tiles <= 640 && terms <= 320);
+}
+
 template <int MODE, class T, int BM, int BN, int WM, int WN, bool NARROW = false>
 int launch_tile(int act, Args<T> a, hipStream_t st)
 {
@@ -612,11 +624,8 @@ int launch(const kge_dense *L, const Args<T> &a, hipStream_t st)
             return launch_rows<MODE, T>(a, L->act, st);
         }
         KGE_PROF(MODE == FORWARD ? "dense" : "dense_input_grad", st);
-        // fp32, tiles that all run at once: half as tall, four to a compute unit in place of three, they start, end and store less in
-        // step (14541 x 203 x 517, 570 tiles of 128 x 128: 51.7 / 44.7 us against 53.0 / 54.2 forward / input gradient); with more
-        // of them, W is split and read twice as often for nothing (10^5 x 512 x 512: 5 % more)
         if constexpr (sizeof(T) == 4) {
-            if (cdiv(a.M, 128) * cdiv(a.N, 128) <= 640) return launch_tile<MODE, T, 64, 128, 1, 4>(L->act, a, st);
+            if (half_tall_pays(a.M, a.N, a.K)) return launch_tile<MODE, T, 64, 128, 1, 4>(L->act, a, st);
         }
         return launch_tile<MODE, T, 128, 128, 2, 2>(L->act, a, st);
     }
