@@ -350,8 +350,10 @@ enum { KGE_DT_F32 = 0, KGE_DT_BF16 = 1 };
  * 128 x 128 results, and for a dW of more than 2^28 elements.
  *   act: KGE_ACT_IDENTITY, KGE_ACT_RELU or KGE_ACT_SILU (z / (1 + e^-z), this layer only)
  *   W : DEVICE dtype [d_in][d_out]      b : DEVICE float [d_out] or NULL
- * Sums are fp32; bf16 results are rounded once, at the end.  fp32 products have fp32 accuracy (they run as bf16
- * products of exact three-way splits).
+ * Sums are fp32; bf16 results are rounded once, at the end, from operands as they are, except for dX under SiLU: there dP, which is no bf16
+ * number, is held to 2^-17 of itself (two bf16 parts) before it is multiplied.  fp32 products have fp32 accuracy: they run as bf16 products
+ * of exact three-way splits, and what is left out of a product is below 2^-24 of it, a rounding more than fp32 makes.  SiLU is within
+ * 2^-22 of the larger of one and itself, its derivative within 2^-20.
  *
  * kge_dense_forward: X [n_rows][d_in]; R [n_rows][d_out] or NULL (may be X when d_in == d_out, or Y with Y's row stride, which may not be X); Y [n_rows][d_out];
  *   pre [n_rows][d_out] or NULL: act's argument rounded to dtype, for the backward pass.

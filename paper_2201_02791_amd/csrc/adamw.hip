@@ -11,7 +11,8 @@
 // Why rounding needs an offset: v moves by 1 - b2, a thousandth, per step, and e5m2 numbers are up to a quarter apart, so
 // rounding to nearest would leave v where it is for ever.  A number between two of the format's goes to the upper one
 // where its place between them plus an offset u(element, step) in [0, 1) reaches one: over steps the mean is the number.
-// u is a hash of a multiply-add of both, one 32-bit multiplication for the two offsets of an element.  (Multiples of the
+// u is a hash of a multiply-add of both, one 32-bit multiplication for the two offsets of an element; 0x9E3779B9 is 2^32 over the golden
+// section, the other two multipliers are odd constants known from published 32-bit hashes.  (Multiples of the
 // golden section in its place, without the hash, meet [0, 1) more evenly, but an average that only falls waits for them
 // in step: it came out at half its value after three time constants, where these offsets keep its mean.)  A step's
 // variance is (1 - b2) D v^2 for numbers D v apart and is forgotten at 2 (1 - b2): v spreads by sqrt(D / 2), at most
@@ -24,7 +25,9 @@
 // Bandwidth bound: an element of 32-bit moments takes 28 bytes (16 read, 12 written), one of 8-bit moments 16.  Measured on the
 // large graph's model (a table of 10^6 x 256 of which 9 rows in 10 are taken, and 29 million other parameters): 1241 us,
 // 5.4 TB/s, and 728 us, 5.3 TB/s.  The latter was bound by its vector instructions, 105 an element and 770 us, until the blocks'
-// maxima went through rotations (a DPP instruction each) and root and reciprocal were single instructions.
+// maxima went through rotations (a DPP instruction each) and root and reciprocal were single instructions.  With the step number in device
+// memory every thread forms the corrections' powers in double: a million rows of 256, 1303 -> 1305 us at step 10 and 1301 -> 1307 at
+// step 100000 with 32 bits, 723 -> 776 and 717 -> 903 with 8, whose instructions have no time to spare.
 #include "common.h"
 
 #include <math.h>

@@ -9,16 +9,20 @@
 //   input       A = dP: terms side by side           B = W^T: terms side by side
 //   weights     A = X^T: columns i side by side      B = dP: columns side by side       (terms: the rows of X)
 //
-// A tile of 128 x 128 results per block of four wavefronts, 64 x 64 each on v_mfma_f32_32x32x16_bf16.  Tiles reach LDS
-// through registers, where they become bf16 and where dY turns into dP: act' is never stored, and the next tile is
-// loaded while one is multiplied.  An operand whose terms lie side by side is read back with ds_read_b128 from rows of
-// terms, one whose columns do with the transposing ds_read_b64_tr_b16 from rows of columns; the chunks of 16 bytes of a
-// row are XOR-ed with its number so that neither meets a bank twice.
+// A block has a tile of results: 128 x 128 on four wavefronts, 64 x 64 each on v_mfma_f32_32x32x16_bf16; 64 x 128 where 128 x 128 would
+// leave compute units with one or two (fp32 forward and input gradient); 128 x 32 for the last columns of those where few are left; and
+// for the weights' gradient what its narrow side fits, 128 x 32, 128 x 64, 32 x 128, or 256 x 128 on eight wavefronts (wide bf16 ones).
+// Operands reach LDS through registers, where they become bf16 and where dY turns into dP: act' is never stored, and the next terms are
+// loaded while some are multiplied; the 256 x 128 tile has two buffers and stages one while it multiplies the other.  An operand whose
+// terms lie side by side is read back with ds_read_b128 from rows of terms, one whose columns do with the transposing ds_read_b64_tr_b16
+// from rows of columns; the chunks of 16 bytes of a row are XOR-ed with its number so that neither meets a bank twice.
 //
 // fp32 numbers become three bf16 parts and six products (split_bf16.h): 417 TFLOP/s where the fp32 instruction has 157.
 // bf16 numbers enter as they are, and so does dP of bf16 rows under identity and ReLU; under SiLU dP is an fp32 number:
 // two parts (2^-17) where the result is rounded to bf16, three where it is a weights' gradient in fp32.  Sums that are
-// not finite come again from fp32 products: infinities do not survive a split.
+// not finite come again from fp32 products: infinities do not survive a split.  Of the nine products of three parts the three below
+// 2^-24 of the product are left out: dW of 290001 x 128 x 32, numbers of spread one, is 7.8e-7 of its root mean square off (the
+// library's fp32 product 2.9e-6).
 //
 // What bounds it: fp32, the matrix cores and the splitting beside them (128000 x 1000 x 1000 forward 1575 us, 975 TFLOP/s of bf16
 // products, 163 of fp32; the library's fp32 product alone does 153); bf16, the operands' way through LDS, a read of 1 KB per instruction
