@@ -340,8 +340,8 @@ int kge_optimizer_step_rows(const kge_opt *opt, float *param, const float *grad,
  * matrices of `dtype`; row strides (ld*, in elements, at least the row's width) may be larger than the rows: what
  * lies between two rows may be read but not used, and is never written; any alignment to whole elements is taken.  W is dense.  Biases, norm
  * weights, statistics and the parameters' gradients are float.  Outputs may not overlap inputs, except where it
- * says so.  All calls are asynchronous on `stream`, allocate nothing, never synchronise, use no atomics (results repeat
- * bit for bit), and can be captured into a HIP graph; calls on different streams need different workspaces.
+ * says so.  All calls are asynchronous on `stream`, allocate nothing, never synchronise, use no atomics (the same
+ * call's results repeat bit for bit; rows at another stride or alignment may be summed in another order), and can be captured into a HIP graph; calls on different streams need different workspaces.
  */
 enum { KGE_DT_F32 = 0, KGE_DT_BF16 = 1 };
 
