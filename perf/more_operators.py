@@ -267,8 +267,8 @@ def run(state):
         table = kb.table4_encode(state["X"])
         return dict(rows=kb.table4_decode(table), scales=table.scales)
     if kind == "scores":
-        if "table" not in state:                              # the same memory under the table's name
-            state["table"] = kb.Table4(state["codes"], state["scales"], c["d"])
+        if "table" not in state:                              # the codes as the bytes that a program holds them in
+            state["table"] = kb.Table4(state["codes"].to(torch.uint8), state["scales"], c["d"])
         return kb.table4_scores(state["table"], state["X"], fixed=state["fixed"], M=state["M"], rel=state["rel"])
     if kind == "sample":
         choice, prob = kb.sample_scores(state["scores"], state["u"], temperature=state["temperature"], top_k=state["top_k"],
