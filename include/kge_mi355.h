@@ -19,6 +19,9 @@
  *   kge_optimizer_step       Algorithm 1, "optimizer.step()"
  *   kge_dense_*, kge_layer_norm_*   a learned block in front of the encoder, for vertices with features
  *   kge_adamw_step           the update of all parameters in one launch, moments in 32 or 8 bits
+ *   kge_grad_norm, kge_clip_grads   the norm of all gradients, and their scaling to a largest norm
+ *   kge_table4_*             an embedding table in 4 bits and the scores of questions against it
+ *   kge_sample_scores        draws from rows of scores: answers, and negatives that the model takes for true
  *
  * General rules
  *  - Every function returns KGE_OK (0) or a negative kge_status; on error no
@@ -440,6 +443,35 @@ typedef struct kge_adamw {
     const int64_t *t_dev;
 } kge_adamw;
 int kge_adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tensors, int32_t n_tensors, void *stream);
+/* The same step with every gradient multiplied by *factor first (DEVICE float, read when the launch runs; e.g. what kge_grad_norm
+ * left there).  KGE_ROWS_NONZERO goes by the gradients as they are.  A factor that is NaN: nothing is written. */
+int kge_adamw_step_scaled(const kge_adamw *opt, const kge_adamw_tensor *tensors, int32_t n_tensors, const float *factor, void *stream);
+
+/*
+ * The norm of all gradients, and their scaling to a largest norm:
+ *   norm = sqrt(sum over tensors and elements of g^2);  factor = min(1, max_norm / norm), 1 where norm is 0;  g <- factor g
+ * Each tensor is n_rows rows of d elements, dense, of dtype KGE_DT_F32 or KGE_DT_BF16, fewer than 2^36 (KGE_ERANGE).  row_mask: NULL, or DEVICE
+ * uint8 [n_rows]: rows where it is 0 are neither read nor scaled (what they hold is no gradient, e.g. rows that kge_adamw_step leaves out by
+ * KGE_ROWS_MASK).  Squares and sums are in 64 bits: nothing overflows, and the result repeats bit for bit.  norm, factor: DEVICE float [1];
+ * either may be NULL, with kge_grad_norm one of them at most.  A gradient that is not finite: norm is infinite or NaN, factor NaN.
+ *   kge_grad_norm   norm and factor alone, for a step that takes the factor along (kge_adamw_step_scaled)
+ *   kge_clip_grads  the gradients are scaled as well, in place (rounded once, after fp32's product, where they are bf16); with a factor of 1
+ *                   they are not written, with a NaN they all become NaN.  No two tensors may overlap.
+ *   max_norm: zero or more; infinity scales nothing.  workspace: DEVICE, 256-byte aligned, at least kge_grad_norm_workspace_bytes(n_tensors)
+ *   bytes (0: a negative number).
+ * Asynchronous on `stream`, no allocation, no atomics, capturable; calls on different streams need different workspaces.
+ */
+typedef struct kge_grad_tensor {
+    void *grad;
+    const uint8_t *row_mask;
+    int64_t n_rows, d;
+    int32_t dtype;
+} kge_grad_tensor;
+size_t kge_grad_norm_workspace_bytes(int32_t n_tensors);
+int kge_grad_norm(const kge_grad_tensor *tensors, int32_t n_tensors, float max_norm, float *norm, float *factor, void *workspace,
+                  size_t ws_bytes, void *stream);
+int kge_clip_grads(const kge_grad_tensor *tensors, int32_t n_tensors, float max_norm, float *norm, float *factor, void *workspace,
+                   size_t ws_bytes, void *stream);
 
 /*
  * Link-prediction evaluation ("Evaluation Metrics" section: filtered setting, MRR Eq. 5, Hits@k Eq. 6).
@@ -502,6 +534,75 @@ int kge_eval_metrics(const int32_t *higher, const int32_t *equal, int64_t n_quer
 int kge_eval_rank_all_static(const kge_eval_filter *filter, const float *H, int64_t n_entities, int32_t d,
                              const float *M, int32_t n_relations, const int32_t *test_h, const int32_t *test_r,
                              const int32_t *test_t, int64_t n_test, int32_t *higher, int32_t *equal, void *stream);
+
+/*
+ * Answers: an embedding table in 4 bits, the scores of questions against all its rows, and draws from scores.
+ * All calls are asynchronous on `stream`, allocate nothing, never synchronise, use no floating-point atomics (results repeat bit for bit) and
+ * can be captured into a HIP graph.  Outputs may not overlap inputs.
+ *
+ * A table holds n_rows rows of d elements (1 to 4096; fewer than 2^31 rows).  A row is cut into ceil(d / 32) groups of 32, the last filled up with
+ * zeros.  codes: DEVICE [n_rows][groups][16] bytes, 16-byte aligned: element 2 i of a group in the low half of byte i, element 2 i + 1 in
+ * the high half; a half is a number of the format e2m1 (sign, then 0, 1/2, 1, 3/2, 2, 3, 4, 6).  scales: DEVICE bf16 [n_rows][groups].  An element
+ * is its number times its group's scale.
+ * kge_table4_encode: X [n_rows][d] of dtype, rows ldx elements apart (ldx >= d).  A group's scale is the smallest bf16 number, 2^-126 or
+ *   more, six of which reach its largest magnitude (0 for a group of zeros); each element goes to the nearest number, of two as near to the even
+ *   code.  A group with an infinity or a NaN reads as NaN.
+ * kge_table4_decode: out [n][d] of dtype, rows ldo apart: rows rows[0..n) (DEVICE int32) of the table, or with rows NULL its first n.  A
+ *   row number that the table does not have gives a row of NaN.  bf16 results are rounded once.
+ * kge_table4_scores: scores[q][i] = sum_k x_q[k] row_i[k], float, rows lds apart (lds >= n_rows), for questions q in [0, n_questions):
+ *   x_q = X[fixed[q]] * M[rel[q]], the product in fp32 (Eq. 4's question: one entity's embedding and the relation's diagonal), or X[fixed[q]]
+ *   with M NULL.  fixed NULL: X[q]; rel NULL: M[q].  X [n_x][d] of dtype, M [n_m][d] float; fixed, rel DEVICE int32.  An id outside [0, n_x)
+ *   or [0, n_m) is never an address: that question's scores are NaN.  Products are exact, sums fp32; the scale multiplies a group's sum, so
+ *   infinities in x_q give infinities or NaN.
+ */
+#define KGE_TABLE4_GROUP 32
+typedef struct kge_table4 {
+    int64_t n_rows;
+    int32_t d;
+    void *codes;
+    uint16_t *scales;
+} kge_table4;
+int kge_table4_encode(const kge_table4 *table, int32_t dtype, const void *X, int64_t ldx, void *stream);
+int kge_table4_decode(const kge_table4 *table, const int32_t *rows, int64_t n, int32_t dtype, void *out, int64_t ldo, void *stream);
+int kge_table4_scores(const kge_table4 *table, int32_t dtype, const void *X, int64_t ldx, int64_t n_x, const int32_t *fixed,
+                      const float *M, int64_t ldm, int64_t n_m, const int32_t *rel, int64_t n_questions, float *scores, int64_t lds,
+                      void *stream);
+
+/*
+ * Draws from rows of scores, from random numbers that the caller gives.  For each row of n_cols scores (dtype, rows lds apart):
+ *   weight of a score l, m the row's largest:  e^((l - m) / temperature), rounded to a multiple of 2^-b, b = min(40, 62 - ceil(log2 n_cols));
+ *     minus infinity and NaN have none, and where the largest is plus infinity, only plus infinity has one
+ *   order: descending scores, equal ones by column.  top_k leaves the first top_k, top_p of those the shortest beginning whose weights reach
+ *     top_p times theirs (one at least), min_p of those what has min_p times the largest weight or more
+ *   draw i: the first column at which the sum of the weights left, by column, exceeds u[row][i] times their total
+ * Sums are of whole multiples of 2^-b, exact in 64 bits: the result repeats bit for bit.
+ *   temperature 0: the largest score, of equal ones the first.  top_k 0, top_p 1, min_p 0: off.
+ *   row_*: NULL, or DEVICE [n_rows]: each row's own setting in place of the call's.  With row_top_k the call's top_k, unless 0, is the most that a
+ *     row has.  Settings out of range, which only the device sees: a temperature that is not above zero counts as 0, top_k below one, top_p of
+ *     one or more or NaN and a min_p that is not above zero as off; top_p below zero leaves one score, min_p above one counts as one.
+ *   u: DEVICE [n_rows][n_draws], float (u_bits 32) or double (64), in [0, 1); what is outside counts as the nearest inside, NaN as 0
+ *   choice: DEVICE int32 [n_rows][n_draws], the column; -1 for every draw of a row without weights (no columns, or only minus infinity and NaN)
+ *   prob: NULL, or DEVICE float [n_rows][n_draws]: the column's share of the weights left; 0 beside -1
+ *   n_rows, n_cols below 2^31.  workspace: DEVICE, 256-byte aligned, at least kge_sample_workspace_bytes(how, n_rows, n_cols) bytes (0: invalid
+ *   arguments); calls on different streams need different ones.
+ */
+typedef struct kge_sampling {
+    float temperature;
+    int32_t top_k;
+    float top_p, min_p;
+    const float *row_temperature;
+    const int32_t *row_top_k;
+    const float *row_top_p, *row_min_p;
+} kge_sampling;
+size_t kge_sample_workspace_bytes(const kge_sampling *how, int64_t n_rows, int64_t n_cols);
+int kge_sample_scores(const kge_sampling *how, int64_t n_rows, int64_t n_cols, const void *scores, int32_t dtype, int64_t lds,
+                      const void *u, int32_t u_bits, int32_t n_draws, int32_t *choice, float *prob, void *workspace, size_t ws_bytes,
+                      void *stream);
+/* The drawn candidates of a batch's negatives: neg_ent[q][i] = cand_ent[q][choice[q][i]], neg_side alike, for q in [0, n_pos), i in [0, n_neg).
+ * cand_ent, cand_side [n_pos][n_cand] as kge_sample_negatives writes them; choice [n_pos][n_neg] as kge_sample_scores does.  A choice outside
+ * [0, n_cand) - a row that had no weights - takes candidate i mod n_cand. */
+int kge_pick_negatives(const int32_t *cand_ent, const uint8_t *cand_side, int32_t n_cand, const int32_t *choice, int64_t n_pos, int32_t n_neg,
+                       int32_t *neg_ent, uint8_t *neg_side, void *stream);
 
 /*
  * Per-kernel timing for benchmarks (not part of the training path).  While enabled, every

@@ -27,7 +27,9 @@ EXPORTED = ["kge_build_partition", "kge_partition_info", "kge_partition_export",
             "kge_eval_debug_scores", "kge_eval_rank_all_static", "kge_cgraph_input_rows", "kge_score_index_create", "kge_score_index_destroy",
             "kge_partition_bad_ids", "kge_test_set_rel_slab", "kge_test_pair_query", "kge_dense_forward",
             "kge_dense_workspace_bytes", "kge_dense_backward", "kge_layer_norm_forward", "kge_layer_norm_workspace_bytes",
-            "kge_layer_norm_backward", "kge_adamw_step"]
+            "kge_layer_norm_backward", "kge_adamw_step", "kge_adamw_step_scaled", "kge_grad_norm_workspace_bytes", "kge_grad_norm",
+            "kge_clip_grads", "kge_table4_encode", "kge_table4_decode", "kge_table4_scores", "kge_sample_workspace_bytes",
+            "kge_sample_scores", "kge_pick_negatives"]
 
 ACT_IDENTITY, ACT_RELU, ACT_SILU = 0, 1, 2       # ACT_SILU: dense layers only
 ORDER_PROJECT_FIRST, ORDER_RELATION_WEIGHTS = 0, 2
@@ -103,6 +105,19 @@ class _AdamW(C.Structure):
                 ("t", C.c_int64), ("t_dev", C.c_void_p)]
 
 
+class _GradTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("row_mask", C.c_void_p), ("n_rows", C.c_int64), ("d", C.c_int64), ("dtype", C.c_int32)]
+
+
+class _Table4(C.Structure):
+    _fields_ = [("n_rows", C.c_int64), ("d", C.c_int32), ("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+class _Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float),
+                ("row_temperature", C.c_void_p), ("row_top_k", C.c_void_p), ("row_top_p", C.c_void_p), ("row_min_p", C.c_void_p)]
+
+
 class _ProfEntry(C.Structure):
     _fields_ = [("name", C.c_char * 32), ("total_ms", C.c_double), ("calls", C.c_int64)]
 
@@ -136,6 +151,18 @@ def load():
         lib.kge_layer_norm_workspace_bytes.argtypes = [p, i64]
         lib.kge_layer_norm_backward.argtypes = [p, i64, p, i64, p, p, p, i64, p, i64, p, p, p, size, p]
         lib.kge_adamw_step.argtypes = [p, p, C.c_int32, p]
+        lib.kge_adamw_step_scaled.argtypes = [p, p, C.c_int32, p, p]
+        for name in ("kge_grad_norm_workspace_bytes", "kge_sample_workspace_bytes"):
+            getattr(lib, name).restype = size
+        i32 = C.c_int32
+        lib.kge_grad_norm_workspace_bytes.argtypes = [i32]
+        lib.kge_grad_norm.argtypes = lib.kge_clip_grads.argtypes = [p, i32, C.c_float, p, p, p, size, p]
+        lib.kge_table4_encode.argtypes = [p, i32, p, i64, p]
+        lib.kge_table4_decode.argtypes = [p, p, i64, i32, p, i64, p]
+        lib.kge_table4_scores.argtypes = [p, i32, p, i64, i64, p, p, i64, i64, p, i64, p, i64, p]
+        lib.kge_sample_workspace_bytes.argtypes = [p, i64, i64]
+        lib.kge_sample_scores.argtypes = [p, i64, i64, p, i32, i64, p, i32, i32, p, p, p, size, p]
+        lib.kge_pick_negatives.argtypes = [p, p, i32, p, i64, i32, p, p, p]
         _lib = lib
     return _lib
 
@@ -694,16 +721,223 @@ def adamw_state(param, bits: int = 32) -> dict:
     return dict(m=codes(torch.float8_e4m3fn), v=codes(torch.float8_e5m2), m_scale=scales(), v_scale=scales())
 
 
-def adamw_step(tensors, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, t=1, t_dev=None, stream=None):
+def adamw_step(tensors, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, t=1, t_dev=None, stream=None, factor=None):
     """One AdamW step in place on all tensors: an AdamWTensors or a list of its dicts.  t_dev: the step number as a device
-    int64 tensor of one element, in place of t."""
+    int64 tensor of one element, in place of t.  factor: what gradients are multiplied by, a device float (grad_norm's);
+    one that is NaN leaves everything as it is."""
     torch = sys.modules["torch"]
     plan = tensors if isinstance(tensors, AdamWTensors) else AdamWTensors(tensors)
     _need(t_dev is None or (t_dev.dtype == torch.int64 and t_dev.numel() == 1), "t_dev: one int64 is wanted")
     o = _AdamW(lr, beta1, beta2, eps, int(t), _ptr(t_dev).value)
+    pf = _vector(factor, "factor", 1)
     if not plan.tensors:
         return
-    _call(load().kge_adamw_step, stream, plan.tensors[0]["param"], (t_dev,), C.byref(o), plan.array, len(plan.tensors))
+    first, n = plan.tensors[0]["param"], len(plan.tensors)
+    if factor is None:
+        _call(load().kge_adamw_step, stream, first, (t_dev,), C.byref(o), plan.array, n)
+    else:
+        _call(load().kge_adamw_step_scaled, stream, first, (t_dev, factor), C.byref(o), plan.array, n, pf)
+
+
+# ---- the norm of all gradients, and clipping -----------------------------------------------------
+
+class GradTensors:
+    """The gradients whose norm grad_norm and clip_grads take, laid out once (the tensors are kept alive): contiguous float32 or
+    bfloat16 tensors, or dicts of grad and row_mask (a byte for each row of a matrix, a tensor or a device address: rows where it
+    is 0 do not count).  No two may overlap."""
+
+    def __init__(self, grads: Sequence):
+        torch = sys.modules["torch"]
+        self.tensors = [dict(g) if isinstance(g, dict) else dict(grad=g) for g in grads]
+        self.array = (_GradTensor * max(len(self.tensors), 1))()
+        places = []
+        for i, t in enumerate(self.tensors):
+            g, mask, a, name = t["grad"], t.get("row_mask"), self.array[i], "gradient %d: " % i
+            _need(g.is_contiguous(), name + "a contiguous tensor is wanted")
+            a.dtype = _type_of(g.dtype, name[:-2])
+            rows, d = _row_shape(g)
+            if mask is not None and not isinstance(mask, int):
+                _need(mask.dtype in (torch.uint8, torch.bool) and mask.is_contiguous() and mask.numel() == rows,
+                      name + "row_mask: a byte for each row is wanted")
+            _need(all(x.device == self.tensors[0]["grad"].device for x in (g, mask) if hasattr(x, "device")),
+                  "all tensors of a call must be on one device")
+            a.grad, a.n_rows, a.d = g.data_ptr(), rows, d
+            a.row_mask = mask if isinstance(mask, int) else _ptr(mask).value
+            if g.numel():
+                places.append((a.grad, a.grad + g.numel() * g.element_size(), i))
+        places.sort()
+        for at, after in zip(places, places[1:]):
+            _need(after[0] >= at[1], "gradients %d and %d overlap" % (at[2], after[2]))
+
+
+def grad_norm_workspace_bytes(n_tensors: int) -> int:
+    n = load().kge_grad_norm_workspace_bytes(n_tensors)
+    if n == 0:
+        raise KgeError(-1, load().kge_last_error().decode())
+    return int(n)
+
+
+def _grad_norm(function, grads, max_norm, norm, factor, workspace, stream):
+    torch = sys.modules["torch"]
+    plan = grads if isinstance(grads, GradTensors) else GradTensors(grads)
+    _need(plan.tensors, "no gradients: there is no device to put a norm on")
+    first, n = plan.tensors[0]["grad"], len(plan.tensors)
+    norm = _new(first, (), torch.float32, stream) if norm is None else norm
+    factor = _new(first, (), torch.float32, stream) if factor is None else factor
+    pn, pf = _vector(norm, "norm", 1), _vector(factor, "factor", 1)
+    workspace = _workspace(workspace, grad_norm_workspace_bytes(n), first, stream)
+    _call(function, stream, first, (norm, factor, workspace), plan.array, n, max_norm, pn, pf, workspace.data_ptr(),
+          workspace.numel() * workspace.element_size())
+    return norm, factor
+
+
+def grad_norm(grads, max_norm: float = float("inf"), norm=None, factor=None, workspace=None, stream=None):
+    """(norm, factor), device floats: the norm of all gradients (a GradTensors or a list for one) and min(1, max_norm / norm), which
+    adamw_step takes along; the gradients stay as they are."""
+    return _grad_norm(load().kge_grad_norm, grads, max_norm, norm, factor, workspace, stream)
+
+
+def clip_grads(grads, max_norm: float, norm=None, factor=None, workspace=None, stream=None):
+    """grad_norm's (norm, factor), with the gradients scaled by the factor in place."""
+    return _grad_norm(load().kge_clip_grads, grads, max_norm, norm, factor, workspace, stream)
+
+
+# ---- answers: tables of 4 bits, their scores, draws from scores ------------------------------------
+
+TABLE4_GROUP = 32
+
+
+class Table4:
+    """An embedding table in 4 bits: codes uint8 [n][16 groups], scales bfloat16 [n][groups], groups = ceil(d / 32)."""
+
+    def __init__(self, codes, scales, d: int):
+        torch = sys.modules["torch"]
+        groups = -(-int(d) // TABLE4_GROUP)
+        _need(1 <= d <= 4096, "rows have 1 to 4096 elements")
+        _need(codes.dim() == 2 and codes.dtype == torch.uint8 and codes.is_contiguous() and codes.shape[1] == 16 * groups,
+              "codes: contiguous bytes are wanted, 16 for each group of %d elements" % TABLE4_GROUP)
+        _need(scales.dtype == torch.bfloat16 and scales.is_contiguous() and tuple(scales.shape) == (codes.shape[0], groups),
+              "scales: contiguous bfloat16 is wanted, one for each group")
+        _need(scales.device == codes.device, "all tensors of a call must be on one device")
+        self.codes, self.scales, self.n_rows, self.d = codes, scales, codes.shape[0], int(d)
+        self.struct = _Table4(self.n_rows, self.d, codes.data_ptr(), scales.data_ptr())
+
+
+def table4_encode(X, table: Table4 = None, stream=None) -> Table4:
+    """The rows of X (float32 or bfloat16) in 4 bits, in a new table or in one of their shape."""
+    torch = sys.modules["torch"]
+    dt = _type_of(X.dtype, "X")
+    x, ldx = _rows(X, "X")
+    n, d = X.shape
+    if table is None:
+        groups = -(-d // TABLE4_GROUP)
+        table = Table4(_new(X, (n, 16 * groups), torch.uint8, stream), _new(X, (n, groups), torch.bfloat16, stream), d)
+    _need((table.n_rows, table.d) == (n, d), "the table is of another shape than X")
+    _call(load().kge_table4_encode, stream, X, (table.codes, table.scales), C.byref(table.struct), dt, x, ldx)
+    return table
+
+
+def _ids(t, name: str, n=None):
+    """(address, number) of contiguous int32 ids; None is no tensor."""
+    torch = sys.modules["torch"]
+    if t is None:
+        return 0, n
+    _need(t.dtype == torch.int32 and t.is_contiguous() and t.dim() == 1, "%s: a row of contiguous int32 is wanted" % name)
+    _need(n is None or t.numel() == n, "%s: %s ids are wanted" % (name, n))
+    return t.data_ptr(), t.numel()
+
+
+def table4_decode(table: Table4, rows=None, dtype=None, out=None, stream=None):
+    """Rows of the table as float32 (or bfloat16): all, or those that rows (int32) names; a row it does not have is NaN."""
+    torch = sys.modules["torch"]
+    ids, n = _ids(rows, "rows", None if rows is not None else table.n_rows)
+    out = _new(table.codes, (n, table.d), dtype or torch.float32, stream) if out is None else out
+    o, ldo = _rows(out, "out", table.d, n)
+    _call(load().kge_table4_decode, stream, table.codes, (table.scales, rows, out), C.byref(table.struct), ids, n,
+          _type_of(out.dtype, "out"), o, ldo)
+    return out
+
+
+def table4_scores(table: Table4, X, fixed=None, M=None, rel=None, out=None, stream=None):
+    """float32 [questions][n_rows]: the scores of x_q = X[fixed[q]] * M[rel[q]] against every row of the table; without fixed the
+    questions are X's rows, without rel M's, without M there is no product."""
+    torch = sys.modules["torch"]
+    x, ldx = _rows(X, "X", table.d)
+    pf, n = _ids(fixed, "fixed", None if fixed is not None else X.shape[0])
+    pr, _ = _ids(rel, "rel", n if rel is not None else None)
+    m, ldm = _rows(M, "M", table.d, dtype=torch.float32)
+    out = _new(X, (n, table.n_rows), torch.float32, stream) if out is None else out
+    o, ldo = _rows(out, "out", table.n_rows, n, torch.float32)
+    _call(load().kge_table4_scores, stream, X, (table.codes, table.scales, fixed, M, rel, out), C.byref(table.struct),
+          _type_of(X.dtype, "X"), x, ldx, X.shape[0], pf, m, ldm, 0 if M is None else M.shape[0], pr, n, o, ldo)
+    return out
+
+
+def _setting(v, name: str, scalar, kind, n_rows: int):
+    """(the call's value, address of the rows' values, tensor or None)"""
+    if not hasattr(v, "data_ptr"):
+        return v, 0, None
+    _need(v.dtype == kind and v.is_contiguous() and v.numel() == n_rows, "%s: a number, or contiguous %s for each row" % (name, kind))
+    return scalar, v.data_ptr(), v
+
+
+def _sampling(torch, temperature, top_k, top_p, min_p, most_k, n_rows):
+    t, pt, ht = _setting(temperature, "temperature", 1.0, torch.float32, n_rows)
+    k, pk, hk = _setting(top_k, "top_k", int(most_k), torch.int32, n_rows)
+    p, pp, hp = _setting(top_p, "top_p", 1.0, torch.float32, n_rows)
+    m, pm, hm = _setting(min_p, "min_p", 0.0, torch.float32, n_rows)
+    return _Sampling(t, k, p, m, pt, pk, pp, pm), (ht, hk, hp, hm)
+
+
+def sample_workspace_bytes(n_rows: int, n_cols: int, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, most_k: int = 0) -> int:
+    how, _ = _sampling(sys.modules["torch"], temperature, top_k, top_p, min_p, most_k, n_rows)
+    n = load().kge_sample_workspace_bytes(C.byref(how), n_rows, n_cols)
+    if n == 0:
+        raise KgeError(-1, load().kge_last_error().decode())
+    return int(n)
+
+
+def sample_scores(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, most_k: int = 0, want_prob: bool = False, choice=None,
+                  prob=None, workspace=None, stream=None):
+    """(choice, prob): int32 [rows][draws], the columns drawn from each row of scores (float32 or bfloat16) by u (float32 or
+    float64 in [0, 1), [rows][draws]), -1 where a row has nothing to draw; prob (want_prob, or a tensor to write it to): their
+    shares, otherwise None.  A setting is a number, or a tensor with one for each row (float32; top_k int32, with most_k, unless
+    0, the most that a row has)."""
+    torch = sys.modules["torch"]
+    s, lds = _rows(scores, "scores")
+    dt = _type_of(scores.dtype, "scores")
+    n, cols = scores.shape
+    _need(u.dim() == 2 and u.shape[0] == n and u.is_contiguous() and u.dtype in (torch.float32, torch.float64),
+          "u: contiguous float32 or float64 is wanted, a row for each row of scores")
+    draws = u.shape[1]
+    how, kept = _sampling(torch, temperature, top_k, top_p, min_p, most_k, n)
+    choice = _new(scores, (n, draws), torch.int32, stream) if choice is None else choice
+    if prob is None and want_prob:
+        prob = _new(scores, (n, draws), torch.float32, stream)
+    _need(choice.dtype == torch.int32 and choice.is_contiguous() and choice.numel() == n * draws, "choice: contiguous int32 is wanted, one for each draw")
+    pp = _vector(prob, "prob", n * draws)
+    need = load().kge_sample_workspace_bytes(C.byref(how), n, cols)
+    if need == 0:
+        raise KgeError(-1, load().kge_last_error().decode())
+    workspace = _workspace(workspace, need, scores, stream)
+    _call(load().kge_sample_scores, stream, scores, (u, choice, prob, workspace) + kept, C.byref(how), n, cols, s, dt, lds, u.data_ptr(),
+          64 if u.dtype == torch.float64 else 32, draws, choice.data_ptr(), pp, workspace.data_ptr(),
+          workspace.numel() * workspace.element_size())
+    return choice, prob
+
+
+def pick_negatives(cand_ent, cand_side, choice, neg_ent, neg_side, stream=None):
+    """The drawn candidates: neg_ent[q][i] = cand_ent[q][choice[q][i]], neg_side alike (sample_negatives' arrays); a choice of -1
+    takes candidate i modulo their number."""
+    torch = sys.modules["torch"]
+    for t, name, kind in ((cand_ent, "cand_ent", torch.int32), (cand_side, "cand_side", torch.uint8), (choice, "choice", torch.int32),
+                          (neg_ent, "neg_ent", torch.int32), (neg_side, "neg_side", torch.uint8)):
+        _need(t.dim() == 2 and t.dtype == kind and t.is_contiguous(), "%s: a contiguous matrix of %s is wanted" % (name, kind))
+    _need(cand_side.shape == cand_ent.shape, "cand_side: of cand_ent's shape")
+    _need(choice.shape[0] == cand_ent.shape[0] and neg_ent.shape == choice.shape and neg_side.shape == choice.shape,
+          "choice, neg_ent and neg_side: of one shape, a row for each positive")
+    _call(load().kge_pick_negatives, stream, cand_ent, (cand_side, choice, neg_ent, neg_side), cand_ent.data_ptr(), cand_side.data_ptr(),
+          cand_ent.shape[1], choice.data_ptr(), choice.shape[0], choice.shape[1], neg_ent.data_ptr(), neg_side.data_ptr())
 
 
 # ---- link-prediction evaluation (filtered ranks, MRR, Hits@k) ----------------------------------

@@ -62,6 +62,7 @@ struct List {
     int32_t n;
     float lr, b1, b2, eps, omb1, omb2, inv_c1, inv_c2;
     const int64_t *t_dev;          // the step number in device memory, or null
+    const float *factor;           // what gradients are multiplied by, in device memory (k_adamw<true>)
     int64_t step;
     int64_t base;                  // the launch's first wavefront
 };
@@ -168,9 +169,9 @@ __device__ __forceinline__ float round_up_by(float y, float offset)
 __device__ __forceinline__ uint32_t offsets_of(uint32_t x) { return (x ^ (x >> 16)) * 0x2C1B3C6Du; }
 
 // One block of a row by the `lanes` lanes of a unit: element i0 + 4 lane .., n of its four inside the row (n <= 0: none).
-template <bool WHOLE, bool EIGHT>
+template <bool WHOLE, bool EIGHT, bool SCALED>
 __device__ __forceinline__ void update(const List &o, const Tensor &T, int64_t at, int n, int64_t scale_at, int lanes, float inv_c1,
-                                       float inv_c2, uint32_t step, bool on)
+                                       float inv_c2, uint32_t step, float factor, bool on)
 {
     const bool any = on && n > 0;
     Four p{}, g{}, m{}, v{};
@@ -197,6 +198,7 @@ __device__ __forceinline__ void update(const List &o, const Tensor &T, int64_t a
     uint32_t most_m = 0u, most_v = 0u;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
+        if (SCALED) g.x[k] *= factor;
         m.x[k] = o.b1 * m.x[k] + o.omb1 * g.x[k];
         v.x[k] = o.b2 * v.x[k] + (o.omb2 * g.x[k]) * g.x[k];
         // root and reciprocal are off by a unit in the last place, of the step and not of the parameter.  The instruction for the root
@@ -245,8 +247,8 @@ __device__ __forceinline__ void update(const List &o, const Tensor &T, int64_t a
     }
 }
 
-template <bool WHOLE, bool EIGHT>
-__device__ __forceinline__ void unit(const List &o, const Tensor &T, int64_t w, float inv_c1, float inv_c2, uint32_t step)
+template <bool WHOLE, bool EIGHT, bool SCALED>
+__device__ __forceinline__ void unit(const List &o, const Tensor &T, int64_t w, float inv_c1, float inv_c2, uint32_t step, float factor)
 {
     const int lane = threadIdx.x & 63, lanes = T.how & 0xff;
     const int l = lane & (lanes - 1);
@@ -265,8 +267,8 @@ __device__ __forceinline__ void unit(const List &o, const Tensor &T, int64_t w, 
         const bool on = (__ballot(some) & mine) != 0ull;
         for (int64_t b = 0; b < T.nb; ++b) {
             const int64_t c = b * BLOCK + 4 * l;
-            update<WHOLE, EIGHT>(o, T, row * T.d + c, in ? (int)min((int64_t)4, T.d - c) : 0, row * T.nb + b, lanes, inv_c1, inv_c2,
-                               step, on);
+            update<WHOLE, EIGHT, SCALED>(o, T, row * T.d + c, in ? (int)min((int64_t)4, T.d - c) : 0, row * T.nb + b, lanes, inv_c1,
+                                         inv_c2, step, factor, on);
         }
         return;
     }
@@ -278,11 +280,17 @@ __device__ __forceinline__ void unit(const List &o, const Tensor &T, int64_t w, 
     const bool in = row < T.n_rows;
     const int64_t c = b * BLOCK + 4 * l;
     const bool on = in && (!T.mask || T.mask[row]);
-    update<WHOLE, EIGHT>(o, T, row * T.d + c, in ? (int)min((int64_t)4, T.d - c) : 0, row * T.nb + b, lanes, inv_c1, inv_c2, step, on);
+    update<WHOLE, EIGHT, SCALED>(o, T, row * T.d + c, in ? (int)min((int64_t)4, T.d - c) : 0, row * T.nb + b, lanes, inv_c1, inv_c2, step,
+                                 factor, on);
 }
 
+// SCALED: gradients times a factor from device memory, which the norm of them all may have left there; one that is NaN, of
+// gradients that are not finite, leaves everything as it is
+template <bool SCALED>
 __global__ __launch_bounds__(256) void k_adamw(List o)
 {
+    const float factor = SCALED ? *o.factor : 1.f;
+    if (SCALED && factor != factor) return;
     // the bias corrections of a step number in device memory, in double like the host's
     float inv_c1 = o.inv_c1, inv_c2 = o.inv_c2;
     int64_t step = o.step;
@@ -301,11 +309,11 @@ __global__ __launch_bounds__(256) void k_adamw(List o)
     const Tensor &T = o.t[i];
     const int64_t mine = w - T.first;
     if (T.how & HOW_8BIT) {
-        if (T.how & HOW_WHOLE) unit<true, true>(o, T, mine, inv_c1, inv_c2, (uint32_t)step);
-        else unit<false, true>(o, T, mine, inv_c1, inv_c2, (uint32_t)step);
+        if (T.how & HOW_WHOLE) unit<true, true, SCALED>(o, T, mine, inv_c1, inv_c2, (uint32_t)step, factor);
+        else unit<false, true, SCALED>(o, T, mine, inv_c1, inv_c2, (uint32_t)step, factor);
     } else {
-        if (T.how & HOW_WHOLE) unit<true, false>(o, T, mine, inv_c1, inv_c2, (uint32_t)step);
-        else unit<false, false>(o, T, mine, inv_c1, inv_c2, (uint32_t)step);
+        if (T.how & HOW_WHOLE) unit<true, false, SCALED>(o, T, mine, inv_c1, inv_c2, (uint32_t)step, factor);
+        else unit<false, false, SCALED>(o, T, mine, inv_c1, inv_c2, (uint32_t)step, factor);
     }
 }
 
@@ -313,7 +321,9 @@ bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 }  // namespace
 
-extern "C" int kge_adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tensors, int32_t n_tensors, void *stream)
+namespace {
+
+int adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tensors, int32_t n_tensors, const float *factor, void *stream)
 {
     KGE_REQUIRE(opt && (tensors || n_tensors == 0), KGE_EINVAL, "NULL argument");
     KGE_REQUIRE(n_tensors >= 0, KGE_EINVAL, "negative number of tensors");
@@ -344,6 +354,7 @@ extern "C" int kge_adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tens
     List o;
     o.lr = opt->lr; o.b1 = opt->beta1; o.b2 = opt->beta2; o.eps = opt->eps;
     o.omb1 = (float)(1.0 - (double)opt->beta1); o.omb2 = (float)(1.0 - (double)opt->beta2);
+    o.factor = factor;
     o.t_dev = opt->t_dev; o.step = opt->t_dev ? 0 : opt->t;
     o.inv_c1 = o.inv_c2 = 1.f;
     if (!opt->t_dev) {
@@ -375,9 +386,22 @@ extern "C" int kge_adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tens
         if (o.n == 0) continue;
         for (o.base = 0; o.base < waves; o.base += MOST_WAVES) {
             const int64_t left = waves - o.base;
-            k_adamw<<<(unsigned)cdiv(left < MOST_WAVES ? left : MOST_WAVES, 4), 256, 0, st>>>(o);
+            (factor ? k_adamw<true> : k_adamw<false>)<<<(unsigned)cdiv(left < MOST_WAVES ? left : MOST_WAVES, 4), 256, 0, st>>>(o);
             KGE_LAUNCH_CHECK();
         }
     }
     return KGE_OK;
+}
+
+}  // namespace
+
+extern "C" int kge_adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tensors, int32_t n_tensors, void *stream)
+{
+    return adamw_step(opt, tensors, n_tensors, nullptr, stream);
+}
+
+extern "C" int kge_adamw_step_scaled(const kge_adamw *opt, const kge_adamw_tensor *tensors, int32_t n_tensors, const float *factor, void *stream)
+{
+    KGE_REQUIRE(factor && aligned(factor, 4), KGE_EINVAL, "factor: the address of a float is wanted");
+    return adamw_step(opt, tensors, n_tensors, factor, stream);
 }
