@@ -598,6 +598,12 @@ size_t kge_sample_workspace_bytes(const kge_sampling *how, int64_t n_rows, int64
 int kge_sample_scores(const kge_sampling *how, int64_t n_rows, int64_t n_cols, const void *scores, int32_t dtype, int64_t lds,
                       const void *u, int32_t u_bits, int32_t n_draws, int32_t *choice, float *prob, void *workspace, size_t ws_bytes,
                       void *stream);
+/* Negatives that the model takes for true: candidates drawn by kge_sample_negatives, scored by kge_distmult_score_loss, and of those some drawn
+ * by kge_sample_scores (the softmax weights of self-adversarial sampling, as draws).
+ * kge_hide_positives: scores[q][c] = minus infinity, rows lds apart, where candidate c makes positive q's own triple of it (the given partition's core
+ * edge pos_core_idx[q]; an index outside [0, n_core) hides nothing).  cand_ent, cand_side: [n_pos][n_cand]. */
+int kge_hide_positives(const kge_partition *p, const int32_t *pos_core_idx, int64_t n_pos, const int32_t *cand_ent, const uint8_t *cand_side,
+                       int32_t n_cand, float *scores, int64_t lds, void *stream);
 /* The drawn candidates of a batch's negatives: neg_ent[q][i] = cand_ent[q][choice[q][i]], neg_side alike, for q in [0, n_pos), i in [0, n_neg).
  * cand_ent, cand_side [n_pos][n_cand] as kge_sample_negatives writes them; choice [n_pos][n_neg] as kge_sample_scores does.  A choice outside
  * [0, n_cand) - a row that had no weights - takes candidate i mod n_cand. */

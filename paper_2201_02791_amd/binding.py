@@ -29,7 +29,7 @@ EXPORTED = ["kge_build_partition", "kge_partition_info", "kge_partition_export",
             "kge_dense_workspace_bytes", "kge_dense_backward", "kge_layer_norm_forward", "kge_layer_norm_workspace_bytes",
             "kge_layer_norm_backward", "kge_adamw_step", "kge_adamw_step_scaled", "kge_grad_norm_workspace_bytes", "kge_grad_norm",
             "kge_clip_grads", "kge_table4_encode", "kge_table4_decode", "kge_table4_scores", "kge_sample_workspace_bytes",
-            "kge_sample_scores", "kge_pick_negatives"]
+            "kge_sample_scores", "kge_hide_positives", "kge_pick_negatives"]
 
 ACT_IDENTITY, ACT_RELU, ACT_SILU = 0, 1, 2       # ACT_SILU: dense layers only
 ORDER_PROJECT_FIRST, ORDER_RELATION_WEIGHTS = 0, 2
@@ -162,6 +162,7 @@ def load():
         lib.kge_table4_scores.argtypes = [p, i32, p, i64, i64, p, p, i64, i64, p, i64, p, i64, p]
         lib.kge_sample_workspace_bytes.argtypes = [p, i64, i64]
         lib.kge_sample_scores.argtypes = [p, i64, i64, p, i32, i64, p, i32, i32, p, p, p, size, p]
+        lib.kge_hide_positives.argtypes = [p, p, i64, p, p, i32, p, i64, p]
         lib.kge_pick_negatives.argtypes = [p, p, i32, p, i64, i32, p, p, p]
         _lib = lib
     return _lib
@@ -924,6 +925,19 @@ def sample_scores(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mos
           64 if u.dtype == torch.float64 else 32, draws, choice.data_ptr(), pp, workspace.data_ptr(),
           workspace.numel() * workspace.element_size())
     return choice, prob
+
+
+def hide_positives(part: Partition, pos_core_idx, cand_ent, cand_side, scores, stream=None):
+    """scores[q][c] (a matrix of rows, in place) = minus infinity where candidate c makes positive q's own triple of it."""
+    torch = sys.modules["torch"]
+    for t, name, kind in ((cand_ent, "cand_ent", torch.int32), (cand_side, "cand_side", torch.uint8)):
+        _need(t.dim() == 2 and t.dtype == kind and t.is_contiguous(), "%s: a contiguous matrix of %s is wanted" % (name, kind))
+    n, cand = cand_ent.shape
+    _need(cand_side.shape == cand_ent.shape, "cand_side: of cand_ent's shape")
+    pos, _ = _ids(pos_core_idx, "pos_core_idx", n)
+    s, lds = _rows(scores, "scores", cand, n, torch.float32)
+    _call(load().kge_hide_positives, stream, scores, (pos_core_idx, cand_ent, cand_side), part.handle, pos, n, cand_ent.data_ptr(),
+          cand_side.data_ptr(), cand, s, lds)
 
 
 def pick_negatives(cand_ent, cand_side, choice, neg_ent, neg_side, stream=None):

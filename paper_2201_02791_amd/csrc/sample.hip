@@ -337,7 +337,38 @@ __global__ __launch_bounds__(256) void k_pick_negatives(const int32_t *__restric
     }
 }
 
+// candidates whose corrupted triple is the positive itself: their scores become minus infinity
+__global__ __launch_bounds__(256) void k_hide_positives(const int32_t *__restrict__ core_h, const int32_t *__restrict__ core_t, int32_t n_core,
+                                                        const int32_t *__restrict__ pos, int64_t n, uint32_t n_cand, const int32_t *__restrict__ cand_ent,
+                                                        const uint8_t *__restrict__ cand_side, float *__restrict__ scores, int64_t lds)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t q = i / n_cand;
+        const int32_t c = pos[q];
+        if (c < 0 || c >= n_core) continue;
+        if (cand_ent[i] == (cand_side[i] ? core_h[c] : core_t[c])) scores[q * lds + (i - q * n_cand)] = -INFINITY;
+    }
+}
+
 }  // namespace
+
+extern "C" int kge_hide_positives(const kge_partition *p, const int32_t *pos_core_idx, int64_t n_pos, const int32_t *cand_ent,
+                                  const uint8_t *cand_side, int32_t n_cand, float *scores, int64_t lds, void *stream)
+{
+    KGE_REQUIRE(p, KGE_EINVAL, "NULL partition");
+    KGE_REQUIRE(n_pos >= 0 && n_cand >= 0 && lds >= n_cand, KGE_EINVAL, "negative size, or a row stride of less than a row");
+    KGE_REQUIRE(n_pos <= 0x7fffffffll, KGE_ERANGE, "2^31 positives or more");
+    const int64_t n = n_pos * n_cand;
+    if (n == 0) return KGE_OK;
+    KGE_REQUIRE(pos_core_idx && cand_ent && cand_side && scores, KGE_EINVAL, "NULL array");
+    hipStream_t st = (hipStream_t)stream;
+    KGE_PROF("hide_positives", st);
+    const int64_t blocks = cdiv(n, 256);
+    k_hide_positives<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, st>>>(p->core_h, p->core_t, (int32_t)p->n_core, pos_core_idx, n,
+                                                                               (uint32_t)n_cand, cand_ent, cand_side, scores, lds);
+    KGE_LAUNCH_CHECK();
+    return KGE_OK;
+}
 
 extern "C" int kge_pick_negatives(const int32_t *cand_ent, const uint8_t *cand_side, int32_t n_cand, const int32_t *choice, int64_t n_pos,
                                   int32_t n_neg, int32_t *neg_ent, uint8_t *neg_side, void *stream)

@@ -114,6 +114,16 @@ class TrainStep:
         self.index = (kb.ScoreIndex(self.part, max(n_pos, 1), self.n_neg, self.H_out.shape[1])
                       if self.want_index else None)
 
+    def set_candidates(self, n_cand: int):
+        """Candidates per positive of run_hard, from which set_batch's n_neg negatives are drawn."""
+        torch, n_pos = self.torch, self.pos.numel()
+        new = lambda *shape, dtype: torch.empty(shape, dtype=dtype, device=self.dev)  # noqa: E731
+        self.cand_ent, self.cand_side = new(n_pos, n_cand, dtype=torch.int32), new(n_pos, n_cand, dtype=torch.uint8)
+        self.cand_scores = new(n_pos, 1 + n_cand, dtype=torch.float32)
+        self.choice = new(n_pos, self.n_neg, dtype=torch.int32)
+        self.cand_index = (kb.ScoreIndex(self.part, max(n_pos, 1), n_cand, self.H_out.shape[1]) if self.want_index else None)
+        self.cand_workspace = None
+
     def stage_batches(self, batches):
         """Copy several mini-batches (equal-length index arrays) to the device ahead of a loop; returns the
         tensor [n_batches, n_pos] whose rows `use_batch` takes."""
@@ -174,11 +184,36 @@ class TrainStep:
         self.score_loss(stream)
         self.backward(stream)
 
+    def run_hard(self, mode: int, seed: int, step: int, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream=None):
+        """run() with negatives that the model takes for true: of each positive's candidates (set_candidates; drawn as run()
+        draws negatives) n_neg are drawn by their scores' softmax at `temperature`, of the top_k, top_p and min_p that are
+        left, from the random numbers u ([n_pos][n_neg] in [0, 1)).  A candidate that is the positive itself is not drawn,
+        unless a positive has no other."""
+        self.set_dropout_state(seed, step)
+        n_cand = self.cand_ent.shape[1]
+        kb.sample_negatives(self.part, self.pos, n_cand, mode, seed, step, self.cand_ent, self.cand_side, stream)
+        if self.cg is not None:              # holds the negatives too: they are among the candidates
+            kb.compute_graph(self.part, self.cg, self.pos, self.cand_ent, stream)
+        self.forward(stream)
+        kb.distmult_score_loss(self.part, self.H_out, self.M, self.pos, self.cand_ent, self.cand_side, n_cand, self.cand_scores,
+                               self.loss, self.dH_out, self.dM, stream, self.cand_index)
+        scores = self.cand_scores[:, 1:]
+        kb.hide_positives(self.part, self.pos, self.cand_ent, self.cand_side, scores, stream)
+        need = kb.sample_workspace_bytes(*scores.shape, temperature, top_k, top_p, min_p)
+        if self.cand_workspace is None or self.cand_workspace.numel() < need:          # the first step of these settings
+            self.cand_workspace = self.torch.empty(need, dtype=self.torch.uint8, device=self.dev)
+        kb.sample_scores(scores, u, temperature, top_k, top_p, min_p, choice=self.choice, workspace=self.cand_workspace, stream=stream)
+        kb.pick_negatives(self.cand_ent, self.cand_side, self.choice, self.neg_ent, self.neg_side, stream)
+        self.score_loss(stream)
+        self.backward(stream)
+
     # --- Algorithm 1, "optimizer.step()": every parameter the step has a gradient for
     def optimizer_step(self, kind: int = kb.OPT_ADAM, lr: float = 0.01, beta1: float = 0.9, beta2: float = 0.999,
-                       eps: float = 1e-8, stream=None):
+                       eps: float = 1e-8, stream=None, max_norm: Optional[float] = None):
         """The state is that of init_optimizer, or of the first call's kind; plain gradient descent needs none.  A call that is
-        refused is no step: the next one has its number."""
+        refused is no step: the next one has its number.  max_norm: the gradients of all parameters together are scaled to this
+        norm where theirs is larger; self.grad_norm (device) is theirs before.  OPT_ADAMW takes the factor along and leaves the
+        gradients as they are; where they are not finite, it leaves the parameters and its state as they are."""
         self._check_kind(kind)
         if kind != kb.OPT_ADAMW and self.block is not None and self.block.W_rows is not self.block.W:
             raise ValueError("a feature block in bf16 takes OPT_ADAMW, which writes the bf16 copy of its weight")
@@ -187,8 +222,11 @@ class TrainStep:
         if kind not in (kb.OPT_SGD, self.opt_kind):
             raise ValueError("the optimizer's state is of another kind: init_optimizer makes this one's")
         t = self.opt_t + 1
+        if max_norm is not None:
+            self._clip(kb.grad_norm if kind == kb.OPT_ADAMW else kb.clip_grads, max_norm, stream)
         if kind == kb.OPT_ADAMW:
-            kb.adamw_step(self.opt_plan, lr, beta1, beta2, eps, t, stream=stream)
+            more = {} if max_norm is None else dict(factor=self.grad_factor)
+            kb.adamw_step(self.opt_plan, lr, beta1, beta2, eps, t, stream=stream, **more)
             self.opt_t = t
             return
         # the entity table: only the rows the step read (flags of the sub-graph's input rows; without a
@@ -199,6 +237,15 @@ class TrainStep:
             kb.optimizer_step(kind, p, g, m, v, lr, beta1, beta2, eps, t, rows=rows,
                               row_mask=mask if rows else None, stream=stream)
         self.opt_t = t
+
+    def _clip(self, call, max_norm: float, stream):
+        if not hasattr(self, "grad_plan"):
+            torch, mask = self.torch, self.cg.input_rows_ptr() if self.cg is not None else None
+            self.grad_plan = kb.GradTensors([dict(grad=g, row_mask=mask if rows else None) for _, _, g, rows in self._opt_pairs()])
+            n = len(self.grad_plan.tensors)
+            self.grad_norm, self.grad_factor = (torch.empty((), dtype=torch.float32, device=self.M.device) for _ in range(2))
+            self.grad_workspace = torch.empty(kb.grad_norm_workspace_bytes(n), dtype=torch.uint8, device=self.M.device)
+        call(self.grad_plan, max_norm, self.grad_norm, self.grad_factor, self.grad_workspace, stream)
 
     @staticmethod
     def _check_kind(kind):
