@@ -6,12 +6,16 @@
 //   shortest beginning whose weights reach top_p of theirs, min-p what has at least min_p times the largest weight
 //   the draw: the first column at which the sum of the weights left, in the order of columns, passes u times their total
 //
-// Weights are whole numbers below 2^63 in all, so that sums are exact: neither the order in which threads add nor the way in
-// which rows are split shows in a result.  The exponential is formed in double: a weight is off by one unit at most, and that
-// only where it lies next to a half of one.
+// Weights are whole numbers below 2^62 in all, so that sums are exact: neither the order in which threads add nor the way in
+// which rows are split shows in a result, and atomics on them change nothing.
 //
-// What top-k and top-p leave is all scores above one and, of those equal to it, the first few: that score is found digit by
-// digit of its bits (three digits), from counts or sums of weights by digit in LDS.
+// Nothing is sorted.  What top-k and top-p leave is all scores above one and, of those equal to it, the first few ("the cut").
+// That score is found digit by digit of its bits, from counts or sums of weights by digit in LDS:
+//   up to 1024 columns      a wavefront a row, digits of 8 bits, the row's keys in registers
+//   up to 65536             a block a row, digits of 11 bits; up to 16384 columns in registers, beyond read again by each pass
+//   more, a small top_k     blocks take their part of a row and leave its first k scores (k_part_top); those, in the order
+//                           of columns, are a short row for a block
+//   more                    a launch for each digit; blocks add their parts' sums by digit to the row's in memory (k_long_digit)
 #include "common.h"
 
 #include <math.h>
@@ -19,9 +23,6 @@
 namespace {
 
 typedef unsigned long long u64;
-
-constexpr int THREADS = 1024, WAVES = THREADS / 64;
-constexpr int DIGITS = 2048;                  // values of a digit: 11, 11 and 10 bits
 
 struct Sampling {
     float temperature, top_p, min_p;
@@ -37,11 +38,29 @@ struct Call {
     int32_t *choice;
     float *prob;
     int64_t n_rows, lds;
-    int32_t n_cols, n_draws, bits;
-    int32_t u64bit;
+    int32_t n_cols, n_draws, bits, u64bit;
+    const uint32_t *part_key;      // [n_rows][n_part]: a row's first scores, in the order of their columns, and the columns
+    const int32_t *part_col;
+    int32_t n_part;
 };
 
-// bits of scores in an order that whole numbers have; 0: no weight.  Both zeros are one.
+// a row's settings
+struct Setting { float t, p, low; int32_t k; };
+
+__device__ __forceinline__ Setting setting_of(const Sampling &how, int64_t r)
+{
+    Setting s;
+    s.t = how.row_temperature ? how.row_temperature[r] : how.temperature;
+    s.k = how.row_top_k ? how.row_top_k[r] : how.top_k;
+    if (how.row_top_k && how.top_k > 0) s.k = s.k > 0 ? min(s.k, how.top_k) : how.top_k;
+    s.p = how.row_top_p ? how.row_top_p[r] : how.top_p;
+    s.low = how.row_min_p ? how.row_min_p[r] : how.min_p;
+    if (!(s.t > 0.f)) { s.t = 1.f; s.k = 1; }
+    return s;
+}
+
+// ---- scores as whole numbers in their order; 0: no weight.  Both zeros are one.
+
 __device__ __forceinline__ uint32_t key_of(float l)
 {
     const uint32_t b = __float_as_uint(l + 0.f);
@@ -50,219 +69,810 @@ __device__ __forceinline__ uint32_t key_of(float l)
 }
 __device__ __forceinline__ float score_of(uint32_t key) { return __uint_as_float(key ^ ((int32_t)key < 0 ? 0x80000000u : 0xffffffffu)); }
 
-template <bool BF16>
-__device__ __forceinline__ uint32_t key_at(const void *row, int64_t c)
-{
-    return key_of(BF16 ? __uint_as_float((uint32_t)((const uint16_t *)row)[c] << 16) : ((const float *)row)[c]);
-}
+struct __attribute__((packed, aligned(4))) F4 { float x[4]; };
+struct __attribute__((packed, aligned(2))) H4 { uint16_t x[4]; };
+struct __attribute__((packed, aligned(4))) U4 { uint32_t x[4]; };
 
+// Where a row's keys come from: scores, or the first scores of its parts
+template <bool BF16>
+struct Scores {
+    const void *row;
+    int32_t n;
+    __device__ __forceinline__ void get4(int32_t c, uint32_t key[4]) const      // columns c .. c + 3
+    {
+        if (c + 4 <= n) {
+            if (BF16) {
+                const H4 q = *reinterpret_cast<const H4 *>((const uint16_t *)row + c);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) key[k] = key_of(__uint_as_float((uint32_t)q.x[k] << 16));
+            } else {
+                const F4 q = *reinterpret_cast<const F4 *>((const float *)row + c);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) key[k] = key_of(q.x[k]);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                key[k] = c + k >= n ? 0u : key_of(BF16 ? __uint_as_float((uint32_t)((const uint16_t *)row)[c + k] << 16) : ((const float *)row)[c + k]);
+        }
+    }
+    __device__ __forceinline__ int32_t column(int32_t c) const { return c; }
+};
+struct Parts {
+    const uint32_t *key_;
+    const int32_t *col;
+    int32_t n;
+    __device__ __forceinline__ void get4(int32_t c, uint32_t key[4]) const
+    {
+        if (c + 4 <= n) {
+            const U4 q = *reinterpret_cast<const U4 *>(key_ + c);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) key[k] = q.x[k];
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) key[k] = c + k < n ? key_[c + k] : 0u;
+        }
+    }
+    __device__ __forceinline__ int32_t column(int32_t c) const { return col[c]; }
+};
+
+// ---- weights
+
+// e^z, z = (l - m) / T <= 0, as 2^(x / 64): x = z 64 / ln 2 to its nearest whole number n by a table of 2^(j / 64), what is left,
+// |z'| <= ln 2 / 128, by five terms of the exponential series (the sixth is below 2^-51).  Double arithmetic throughout: a weight
+// is off by one unit at most, and that only within 2^-7 of a unit of a half of one (x carries an error of |x| 2^-53, 2^-42 at most).
+// Adding 2^52 rounds to a whole number.
 struct Weigh {
-    double most, per, unit, least;           // m, 1 / temperature, 2^b, and the exponent below which a weight rounds to zero
+    double most, per, least;           // m, 64 / (T ln 2), and the x below which a weight rounds to zero
+    const double *pow;                 // LDS: 2^(j / 64)
     uint32_t most_key;
+    int32_t bits;
+    __device__ __forceinline__ void init(uint32_t key, float t, int32_t b, const double *table)
+    {
+        most_key = key;
+        most = (double)score_of(key);
+        per = 92.332482616893656877 / (double)t;
+        least = -64.0 * (b + 2);
+        bits = b;
+        pow = table;
+    }
+    __device__ __forceinline__ u64 unit() const { return 1ull << bits; }
     __device__ __forceinline__ u64 operator()(uint32_t key) const
     {
         if (key == 0u) return 0ull;
-        if (key == most_key) return (u64)unit;
-        const double z = ((double)score_of(key) - most) * per;
-        return z > least ? (u64)rint(exp(z) * unit) : 0ull;
+        if (key == most_key) return unit();
+        const double x = ((double)score_of(key) - most) * per;
+        if (!(x > least)) return 0ull;
+        const double n = rint(x), r = (x - n) * 0.010830424696249145;
+        const double e = fma(r, fma(r, fma(r, fma(r, fma(r, 1.0 / 120.0, 1.0 / 24.0), 1.0 / 6.0), 0.5), 1.0), 1.0);
+        const int i = (int)n;
+        const double w = ldexp(pow[i & 63] * e, (i >> 6) + bits);
+        return (u64)__double_as_longlong(w + 0x1p52) & 0xfffffffffffffull;
     }
 };
 
-// ---- a block's sums
+__device__ __forceinline__ void fill_pow(double *table)
+{
+    if (threadIdx.x < 64) table[threadIdx.x] = exp2((double)threadIdx.x * (1.0 / 64.0));
+    __syncthreads();
+}
 
-__device__ __forceinline__ u64 shfl_up64(u64 v, int off) { return (u64)__shfl_up((long long)v, off, 64); }
-__device__ __forceinline__ u64 shfl_xor64(u64 v, int off) { return (u64)__shfl_xor((long long)v, off, 64); }
+// ---- sums over a wavefront and over a team of NT threads (64: a wavefront, more: the block)
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 dpp_add(u64 v)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+    return v + ((u64)hi << 32 | lo);
+}
+// inclusive sums over the lanes: within rows of 16, then the rows before
 __device__ __forceinline__ u64 wave_scan(u64 v)
 {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const u64 o = shfl_up64(v, off);
-        if ((int)(threadIdx.x & 63) >= off) v += o;
-    }
-    return v;
+    v = dpp_add<0x111, 0xf>(v);
+    v = dpp_add<0x112, 0xf>(v);
+    v = dpp_add<0x114, 0xf>(v);
+    v = dpp_add<0x118, 0xf>(v);
+    v = dpp_add<0x142, 0xa>(v);
+    return dpp_add<0x143, 0xc>(v);
 }
-
-// inclusive sums over the block's threads, and their total; s: WAVES + 1 words
-__device__ __forceinline__ u64 block_scan(u64 v, u64 *s, u64 *total)
+__device__ __forceinline__ u64 lane_of(u64 v, int lane)
 {
-    const int wave = threadIdx.x >> 6;
-    v = wave_scan(v);
-    if ((threadIdx.x & 63) == 63) s[wave] = v;
-    __syncthreads();
-    u64 before = 0ull, all = 0ull;
-    for (int i = 0; i < WAVES; ++i) {
-        if (i < wave) before += s[i];
-        all += s[i];
-    }
-    __syncthreads();
-    *total = all;
-    return before + v;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
+    return (u64)hi << 32 | lo;
 }
-
-__device__ __forceinline__ uint32_t block_max(uint32_t v, u64 *s)
+__device__ __forceinline__ u64 wave_sum(u64 v) { return lane_of(wave_scan(v), 63); }
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, off, 64));
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-    __syncthreads();
-    uint32_t all = 0u;
-    for (int i = 0; i < WAVES; ++i) all = max(all, (uint32_t)s[i]);
-    __syncthreads();
-    return all;
+    return v;
 }
 
-// The digit at which the sums, from the largest digit down, first reach `goal` (1 or more, at most their total), and the sum of
-// the digits above it.  Two digits a thread.
-__device__ __forceinline__ int digit_at(const u64 *hist, u64 goal, u64 *s, u64 *s_found, u64 *above)
-{
-    static_assert(DIGITS == 2 * THREADS, "two digits a thread");
-    const int hi = DIGITS - 1 - 2 * (int)threadIdx.x;
-    const u64 a = hist[hi], b = hist[hi - 1];
-    u64 total;
-    const u64 upto = block_scan(a + b, s, &total), before = upto - a - b;
-    if (before < goal && goal <= upto) {
-        const bool first = goal <= before + a;
-        s_found[0] = first ? hi : hi - 1;
-        s_found[1] = first ? before : before + a;
+template <int NT>
+struct Team {
+    static constexpr int WAVES = NT / 64;
+    // LDS written by the team is there for the team
+    static __device__ __forceinline__ void sync()
+    {
+        if (NT == 64) {
+            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");
+            __builtin_amdgcn_wave_barrier();
+        } else __syncthreads();
     }
-    __syncthreads();
+    static __device__ __forceinline__ int tid() { return NT == 64 ? (int)(threadIdx.x & 63) : (int)threadIdx.x; }
+    // inclusive sums over the threads, and their total; s: WAVES words of LDS
+    static __device__ __forceinline__ u64 scan(u64 v, u64 *s, u64 *total)
+    {
+        v = wave_scan(v);
+        if (NT == 64) { *total = lane_of(v, 63); return v; }
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 63) s[wave] = v;
+        __syncthreads();
+        const int at = threadIdx.x & 63;
+        const u64 sums = wave_scan(at < WAVES ? s[at] : 0ull);
+        __syncthreads();
+        *total = lane_of(sums, WAVES - 1);
+        return v + (wave ? lane_of(sums, wave - 1) : 0ull);
+    }
+    static __device__ __forceinline__ uint32_t most(uint32_t v, u64 *s)
+    {
+        v = wave_max(v);
+        if (NT == 64) return v;
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+        __syncthreads();
+        const int at = threadIdx.x & 63;
+        v = wave_max(at < WAVES ? (uint32_t)s[at] : 0u);
+        __syncthreads();
+        return v;
+    }
+};
+
+// ---- the cut
+
+struct Cut {
+    uint32_t key;                  // scores above it are left, 0: all
+    bool every;                    // all that are equal to it are, else the first `ties` of them
+    u64 ties;
+};
+
+// The search for one: which = 0 by counts (top-k), 1 by weights (top-p)
+struct Search {
+    u64 goal, above;               // sum that the scores from the cut on reach; sum of the digits above what is found
+    uint32_t found;
+};
+
+template <int BITS, int LEVEL>
+struct Digit {                     // a key's digit at a level, most significant first; the last may be shorter
+    static constexpr int LEVELS = (32 + BITS - 1) / BITS;
+    static constexpr int SHIFT = LEVEL == LEVELS - 1 ? 0 : 32 - BITS * (LEVEL + 1), WIDTH = LEVEL == LEVELS - 1 ? 32 - BITS * LEVEL : BITS;
+    static constexpr uint32_t BEFORE = LEVEL == 0 ? 0u : ~0u << (32 - BITS * LEVEL);      // the digits above
+    static __device__ __forceinline__ uint32_t of(uint32_t key) { return (key >> SHIFT) & ((1u << WIDTH) - 1u); }
+    static __device__ __forceinline__ bool in(uint32_t key, uint32_t found) { return (key & BEFORE) == found; }
+};
+
+// The digit at which the sums, from the largest digit down, first reach `goal` (1 or more, their total at most); the sum of the digits above it
+// and its own
+template <int NT, int BITS>
+__device__ __forceinline__ u64 digit_total(const u64 *hist, u64 (&v)[(1 << BITS) / NT], u64 *upto, u64 *s)
+{
+    constexpr int PER = (1 << BITS) / NT;
+    static_assert(PER >= 1, "a thread has a digit");
+    const int hi = (1 << BITS) - 1 - PER * Team<NT>::tid();
+    u64 sum = 0ull, total;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        v[k] = hist[hi - k];
+        sum += v[k];
+    }
+    *upto = Team<NT>::scan(sum, s, &total);
+    return total;
+}
+template <int NT, int BITS>
+__device__ __forceinline__ int digit_at(const u64 (&v)[(1 << BITS) / NT], u64 upto, u64 goal, u64 *s_found, u64 *above, u64 *own)
+{
+    constexpr int PER = (1 << BITS) / NT;
+    const int hi = (1 << BITS) - 1 - PER * Team<NT>::tid();
+    u64 before = upto;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) before -= v[k];
+    if (before < goal && goal <= upto) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if (before < goal && goal <= before + v[k]) { s_found[0] = hi - k; s_found[1] = before; s_found[2] = v[k]; }
+            before += v[k];
+        }
+    }
+    Team<NT>::sync();
     const int digit = (int)s_found[0];
-    *above = s_found[1];
-    __syncthreads();
+    *above = s_found[1]; *own = s_found[2];
+    Team<NT>::sync();
     return digit;
 }
 
-// One block to a row.
-template <bool BF16>
-__global__ __launch_bounds__(THREADS) void k_sample_rows(Call o)
+// what the sums have to reach, from their total; 0: nothing is cut
+__device__ __forceinline__ u64 goal_of_count(u64 all, const Setting &set) { return all <= (u64)set.k ? 0ull : (u64)set.k; }
+__device__ __forceinline__ u64 goal_of_weight(u64 all, const Setting &set)
 {
-    __shared__ u64 s_hist[DIGITS];
-    __shared__ u64 s_part[WAVES + 1], s_found[2];
-    __shared__ u64 s_sums[THREADS];
-    const int tid = threadIdx.x;
-    for (int64_t r = blockIdx.x; r < o.n_rows; r += gridDim.x) {
-        const void *row = (const char *)o.scores + r * o.lds * (BF16 ? 2 : 4);
-        const int32_t n = o.n_cols;
-        float t = o.how.row_temperature ? o.how.row_temperature[r] : o.how.temperature;
-        int32_t k = o.how.row_top_k ? o.how.row_top_k[r] : o.how.top_k;
-        if (o.how.row_top_k && o.how.top_k > 0) k = k > 0 ? min(k, o.how.top_k) : o.how.top_k;
-        const float p = o.how.row_top_p ? o.how.row_top_p[r] : o.how.top_p, low = o.how.row_min_p ? o.how.row_min_p[r] : o.how.min_p;
-        if (!(t > 0.f)) { t = 1.f; k = 1; }
-        // the largest score
-        uint32_t most = 0u;
-        for (int32_t c = tid; c < n; c += THREADS) most = max(most, key_at<BF16>(row, c));
-        most = block_max(most, s_part);
-        Weigh weigh;
-        weigh.unit = (double)(1ull << o.bits);
-        weigh.most_key = most; weigh.most = (double)score_of(most); weigh.per = 1.0 / (double)t;
-        weigh.least = -0.6931471805599453 * (o.bits + 2);
-        // what is left: keys above `cut` and, of those equal to it, the first `ties`
-        uint32_t cut = 0u;
-        u64 ties = 0ull;
-        for (int which = 0; which < 2; ++which) {                // top-k, then top-p
-            if (which == 0 ? (k <= 0 || k >= n) : !(p < 1.f)) continue;
-            u64 goal = 0ull, all = 0ull;
-            uint32_t found = 0u;
-            u64 above = 0ull;
-            const u64 cut_w = which == 1 && ties > 0ull ? weigh(cut) : 0ull;
-            for (int level = 0; level < 3; ++level) {
-                const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, width = level == 2 ? 1024 : 2048;
-                for (int i = tid; i < DIGITS; i += THREADS) s_hist[i] = 0ull;
-                __syncthreads();
-                const uint32_t same = level == 0 ? 0u : level == 1 ? 0xffe00000u : 0xfffffc00u;
-                u64 mine = 0ull;
-                for (int32_t c = tid; c < n; c += THREADS) {
-                    const uint32_t key = key_at<BF16>(row, c);
-                    if (key == 0u || (key & same) != found || (which == 1 && key <= cut)) continue;
-                    const u64 w = which == 0 ? 1ull : weigh(key);
-                    if (w) atomicAdd(&s_hist[(key >> shift) & (width - 1)], w);
-                    mine += w;
-                }
-                if (which == 1 && tid == 0 && ties > 0ull && (cut & same) == found) {
-                    atomicAdd(&s_hist[(cut >> shift) & (width - 1)], ties * cut_w);
-                    mine += ties * cut_w;
-                }
-                __syncthreads();
-                if (level == 0) {
-                    block_scan(mine, s_part, &all);
-                    if (which == 0) goal = all < (u64)k ? 0ull : (u64)k;
-                    else {
-                        const double g = ceil((double)p * (double)all);
-                        goal = g < 1.0 ? 1ull : (u64)g;
-                        if (goal > all) goal = all;
-                    }
-                    if (goal == 0ull) break;                     // fewer scores than k, or none
-                }
-                u64 more;
-                const int digit = digit_at(s_hist, goal - above, s_part, s_found, &more);
-                above += more;
-                found |= (uint32_t)digit << shift;
-            }
-            if (goal == 0ull) continue;
-            if (which == 0) { cut = found; ties = goal - above; }
-            else {
-                const u64 w = weigh(found);
-                ties = (goal - above + w - 1ull) / w;
-                cut = found;
-            }
+    const double g = ceil((double)set.p * (double)all);
+    const u64 goal = g < 1.0 ? 1ull : (u64)g;
+    return goal > all ? all : goal;
+}
+
+__device__ __forceinline__ bool cuts(int which, const Setting &set, int32_t n) { return which == 0 ? set.k > 0 && set.k < n : set.p < 1.f; }
+
+// a search ended at score `found`, whose sum is `own`, with `above` before it
+__device__ __forceinline__ Cut cut_at(int which, const Search &x, u64 own, const Cut &was, const Weigh &weigh)
+{
+    Cut c;
+    c.key = x.found;
+    if (which == 0) {
+        c.ties = x.goal - x.above;
+        c.every = c.ties == own;
+    } else {
+        const u64 w = weigh(x.found);
+        c.ties = (x.goal - x.above + w - 1ull) / w;
+        c.every = c.ties * w == own && (x.found != was.key || was.every);
+    }
+    return c;
+}
+
+// A row's keys, TILES tiles of 4 columns a thread at a time: thread t of NT has columns 4 (NT i + t) .. + 3 of tile i.  ONE: the row has no
+// more, and they stay in registers; else every pass reads them again, from the caches.
+template <int NT, int TILES, bool ONE, class Source>
+struct Keys {
+    static constexpr int V = 4 * TILES, BATCH = NT * V;
+    const Source &src;
+    uint32_t key[V];
+    __device__ __forceinline__ explicit Keys(const Source &s) : src(s) { if (ONE) load(0); }
+    __device__ __forceinline__ void load(int32_t c0)
+    {
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) src.get4(c0 + 4 * (NT * i + Team<NT>::tid()), key + 4 * i);
+    }
+    // f(first column) for each batch, whose keys are then in `key`
+    template <class F>
+    __device__ __forceinline__ void each(F f)
+    {
+        if (ONE) { f(0); return; }
+#pragma unroll 1
+        for (int32_t c0 = 0; c0 < src.n; c0 += BATCH) {
+            load(c0);
+            f(c0);
         }
-        const double least_weight = (double)(low > 1.f ? 1.f : low) * weigh.unit;
-        // the weights in the order of columns: first their total, then what the draws reach
-        u64 total = 0ull;
-        for (int pass = 0; pass < 2; ++pass) {
-            u64 base = 0ull, equal = 0ull;
-            for (int32_t c0 = 0; c0 < n; c0 += THREADS) {
-                const int32_t c = c0 + tid;
-                const uint32_t key = c < n ? key_at<BF16>(row, c) : 0u;
-                bool in = key > cut;
-                if (cut != 0u) {
-                    u64 here;
-                    const u64 before = equal + block_scan(key == cut ? 1ull : 0ull, s_part, &here);
-                    if (key == cut) in = before <= ties;
-                    equal += here;
-                }
-                u64 w = in ? weigh(key) : 0ull;
-                if ((double)w < least_weight) w = 0ull;
+    }
+};
+
+template <int NT, int BITS, int LEVEL, class K>
+__device__ __forceinline__ void search_level(int which, K &keys, const Setting &set, const Weigh &weigh, Cut &cut, Search &x, u64 *hist, u64 *s, u64 *s_found)
+{
+    typedef Digit<BITS, LEVEL> D;
+    const int tid = Team<NT>::tid();
+    if (LEVEL > 0 && x.goal == 0ull) return;
+    for (int i = tid; i < 1 << BITS; i += NT) hist[i] = 0ull;
+    Team<NT>::sync();
+    keys.each([&](int32_t) {
+#pragma unroll
+        for (int i = 0; i < K::V; ++i) {
+            const uint32_t key = keys.key[i];
+            if (key == 0u || !D::in(key, x.found) || (which == 1 && key <= cut.key)) continue;
+            const u64 w = which == 0 ? 1ull : weigh(key);
+            if (w) atomicAdd(&hist[D::of(key)], w);
+        }
+    });
+    if (which == 1 && tid == 0 && cut.key && D::in(cut.key, x.found)) atomicAdd(&hist[D::of(cut.key)], cut.ties * weigh(cut.key));
+    Team<NT>::sync();
+    u64 v[(1 << BITS) / NT], upto, more, own;
+    const u64 all = digit_total<NT, BITS>(hist, v, &upto, s);
+    if (LEVEL == 0) x.goal = which == 0 ? goal_of_count(all, set) : goal_of_weight(all, set);
+    if (x.goal == 0ull) return;
+    const int digit = digit_at<NT, BITS>(v, upto, x.goal - x.above, s_found, &more, &own);
+    x.above += more;
+    x.found |= (uint32_t)digit << D::SHIFT;
+    if (LEVEL == D::LEVELS - 1) cut = cut_at(which, x, own, cut, weigh);
+}
+
+template <int NT, int BITS, class K>
+__device__ __forceinline__ Cut find_cut(K &keys, const Setting &set, const Weigh &weigh, bool by_weight, u64 *hist, u64 *s, u64 *s_found)
+{
+    Cut cut{0u, true, 0ull};
+#pragma unroll 1
+    for (int which = 0; which < (by_weight ? 2 : 1); ++which) {
+        if (!cuts(which, set, keys.src.n)) continue;
+        Search x{0ull, 0ull, 0u};
+        search_level<NT, BITS, 0>(which, keys, set, weigh, cut, x, hist, s, s_found);
+        search_level<NT, BITS, 1>(which, keys, set, weigh, cut, x, hist, s, s_found);
+        search_level<NT, BITS, 2>(which, keys, set, weigh, cut, x, hist, s, s_found);
+        if constexpr (BITS == 8) search_level<NT, BITS, 3>(which, keys, set, weigh, cut, x, hist, s, s_found);
+    }
+    return cut;
+}
+
+// ---- draws
+
+__device__ __forceinline__ u64 goal_of_draw(const Call &o, int64_t at, u64 total)
+{
+    const double u = o.u64bit ? ((const double *)o.u)[at] : (double)((const float *)o.u)[at];
+    const double reach = u * (double)total;
+    return reach >= (double)total ? total - 1ull : reach > 0.0 ? min((u64)reach, total - 1ull) : 0ull;
+}
+
+__device__ __forceinline__ void answer(const Call &o, int64_t at, int32_t column, u64 w, u64 total)
+{
+    o.choice[at] = column;
+    if (o.prob) o.prob[at] = w ? (float)((double)w / (double)total) : 0.f;
+}
+
+// the least weight that min-p leaves
+__device__ __forceinline__ u64 least_weight(const Setting &set, const Weigh &weigh)
+{
+    const double low = set.low > 1.f ? 1.0 : set.low > 0.f ? (double)set.low : 0.0;
+    const u64 least = (u64)ceil(low * (double)weigh.unit());
+    return least ? least : 1ull;
+}
+
+// the weight of a key that is above the cut, or one of the ties left; what min-p drops has none
+__device__ __forceinline__ u64 weight_left(uint32_t key, const Weigh &weigh, u64 least)
+{
+    const u64 w = weigh(key);
+    return w >= least ? w : 0ull;
+}
+
+// The weights that are left of 4 columns a lane, 256 columns of a wavefront in order; *equal: ties of the cut before them, counted on
+__device__ __forceinline__ void left4(const uint32_t key[4], const Cut &cut, const Weigh &weigh, u64 least, u64 *equal, u64 w[4])
+{
+    if (cut.every) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = key[k] >= cut.key ? weight_left(key[k], weigh, least) : 0ull;
+        return;
+    }
+    u64 mine = 0ull;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mine += key[k] == cut.key ? 1ull : 0ull;
+    const u64 upto = wave_scan(mine);
+    u64 rank = *equal + upto - mine;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const bool tie = key[k] == cut.key;
+        w[k] = key[k] > cut.key || (tie && rank < cut.ties) ? weight_left(key[k], weigh, least) : 0ull;
+        rank += tie ? 1ull : 0ull;
+    }
+    *equal += lane_of(upto, 63);
+}
+
+__device__ __forceinline__ u64 ties_of(const uint32_t key[4], const Cut &cut)
+{
+    u64 n = 0ull;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) n += key[k] == cut.key ? 1ull : 0ull;
+    return n;
+}
+
+// The first of n sums, ascending, above the goal
+__device__ __forceinline__ int first_above(const u64 *sums, int n, u64 goal)
+{
+    int lo = 0, hi = n - 1;
+#pragma unroll 1
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (sums[mid] > goal) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo;
+}
+
+constexpr int RUN = 256;           // columns that a wavefront weighs at once
+constexpr int RUNS_MOST = 1024;    // of a row that a block takes
+constexpr int64_t ROW_MOST = RUN * RUNS_MOST;
+
+// One row.  Up to 4096 columns the sums by column are in LDS, and a thread finds a draw by halving; beyond, the sums by runs of 256
+// columns are (sums[run]: of runs 0 .. run; ties[run], where not all ties are left: their number before the run), and a wavefront
+// weighs the run of a draw again.
+template <int NT, int TILES, bool ONE, int BITS, class Source>
+__device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source &src, u64 *hist, u64 *sums, u64 *ties, u64 *s, u64 *s_found, const double *pow)
+{
+    typedef Team<NT> T;
+    typedef Keys<NT, TILES, ONE, Source> K;
+    constexpr int V = K::V, WAVES = NT / 64;
+    const int tid = T::tid(), wave = NT == 64 ? 0 : (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const Setting set = setting_of(o.how, r);
+    K keys(src);
+    uint32_t most = 0u;
+    keys.each([&](int32_t) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) most = max(most, keys.key[i]);
+    });
+    most = T::most(most, s);
+    const int64_t first = r * o.n_draws;
+    if (most == 0u) {                                            // a row without weights
+        for (int32_t i = tid; i < o.n_draws; i += NT) answer(o, first + i, -1, 0ull, 1ull);
+        return;
+    }
+    Weigh weigh;
+    weigh.init(most, set.t, o.bits, pow);
+    const Cut cut = find_cut<NT, BITS>(keys, set, weigh, true, hist, s, s_found);
+    const u64 least = least_weight(set, weigh);
+    u64 total = 0ull;
+    if constexpr (ONE && K::BATCH <= 4096) {
+        u64 equal = 0ull;                                        // ties in the tiles before and, in a block, in the wavefronts before
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            u64 w[4], before = equal;
+            if (NT > 64 && !cut.every) {                         // ties of the wavefronts before, in this tile
                 u64 here;
-                const u64 upto = block_scan(w, s_part, &here);
-                if (pass == 1 && here) {
-                    s_sums[tid] = base + upto;
-                    __syncthreads();
-                    for (int32_t i = tid; i < o.n_draws; i += THREADS) {
-                        const int64_t at = r * o.n_draws + i;
-                        const double u = o.u64bit ? ((const double *)o.u)[at] : (double)((const float *)o.u)[at];
-                        const double reach = u * (double)total;
-                        const u64 goal = reach >= (double)total ? total - 1ull : reach > 0.0 ? min((u64)reach, total - 1ull) : 0ull;
-                        if (goal < base || goal >= base + here) continue;
-                        int lo = 0, hi = THREADS - 1;            // the first of the sums above the goal
-                        while (lo < hi) {
-                            const int mid = (lo + hi) >> 1;
-                            if (s_sums[mid] > goal) hi = mid;
-                            else lo = mid + 1;
-                        }
-                        o.choice[at] = c0 + lo;
-                        if (o.prob) o.prob[at] = (float)((double)(s_sums[lo] - (lo ? s_sums[lo - 1] : base)) / (double)total);
-                    }
-                    __syncthreads();
-                }
-                base += here;
+                const u64 mine = ties_of(keys.key + 4 * i, cut), upto = T::scan(mine, s, &here);
+                before += lane_of(upto - mine, 0);
+                equal += here;
             }
-            if (pass == 0) {
-                total = base;
-                if (total == 0ull) {
-                    for (int32_t i = tid; i < o.n_draws; i += THREADS) {
-                        const int64_t at = r * o.n_draws + i;
-                        o.choice[at] = -1;
-                        if (o.prob) o.prob[at] = 0.f;
-                    }
-                    break;
+            left4(keys.key + 4 * i, cut, weigh, least, &before, w);
+            if (NT == 64) equal = before;
+            w[1] += w[0]; w[2] += w[1]; w[3] += w[2];
+            u64 all;
+            const u64 base = total + T::scan(w[3], s, &all) - w[3];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sums[4 * (NT * i + tid) + k] = base + w[k];
+            total += all;
+        }
+        T::sync();
+        for (int32_t i = tid; i < o.n_draws; i += NT) {
+            const int at = first_above(sums, K::BATCH, goal_of_draw(o, first + i, total));
+            answer(o, first + i, src.column(at), sums[at] - (at ? sums[at - 1] : 0ull), total);
+        }
+        T::sync();
+    } else {
+        static_assert(RUNS_MOST <= NT, "a thread has a run");
+        const int runs = (src.n + RUN - 1) / RUN;
+        if (!cut.every) {
+            keys.each([&](int32_t c0) {
+#pragma unroll
+                for (int i = 0; i < TILES; ++i) {
+                    const u64 mine = wave_sum(ties_of(keys.key + 4 * i, cut));
+                    const int run = c0 / RUN + i * WAVES + wave;
+                    if (lane == 0 && run < runs) ties[run] = mine;
                 }
+            });
+            T::sync();
+            const u64 mine = tid < runs ? ties[tid] : 0ull;
+            u64 all;
+            const u64 upto = T::scan(mine, s, &all);
+            if (tid < runs) ties[tid] = upto - mine;
+            T::sync();
+        }
+        keys.each([&](int32_t c0) {
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) {
+                const int run = c0 / RUN + i * WAVES + wave;
+                u64 w[4], equal = cut.every || run >= runs ? 0ull : ties[run];
+                left4(keys.key + 4 * i, cut, weigh, least, &equal, w);
+                const u64 sum = wave_sum(w[0] + w[1] + w[2] + w[3]);
+                if (lane == 0 && run < runs) sums[run] = sum;
+            }
+        });
+        T::sync();
+        const u64 mine = tid < runs ? sums[tid] : 0ull;
+        const u64 upto = T::scan(mine, s, &total);
+        if (tid < runs) sums[tid] = upto;
+        T::sync();
+        for (int32_t i = wave; i < o.n_draws; i += WAVES) {
+            const u64 goal = goal_of_draw(o, first + i, total);
+            const int run = first_above(sums, runs, goal);
+            const int32_t c = RUN * run + 4 * lane;
+            uint32_t again[4];
+            src.get4(c, again);
+            u64 w[4], equal = cut.every ? 0ull : ties[run];
+            left4(again, cut, weigh, least, &equal, w);
+            const u64 here = w[0] + w[1] + w[2] + w[3];
+            u64 before = (run ? sums[run - 1] : 0ull) + wave_scan(here) - here;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (goal >= before && goal < before + w[k]) answer(o, first + i, src.column(c + k), w[k], total);
+                before += w[k];
             }
         }
-        __syncthreads();
+        T::sync();
     }
 }
+
+// NT 64: four rows a block, a wavefront each
+template <bool BF16, int NT, int TILES, bool ONE, bool PARTS>
+__global__ __launch_bounds__(NT == 64 ? 256 : NT) void k_rows(Call o)
+{
+    constexpr int BITS = NT == 64 ? 8 : 11, TEAMS = NT == 64 ? 4 : 1, COLUMNS = 4 * TILES * NT;
+    constexpr bool BY_COLUMN = ONE && COLUMNS <= 4096;
+    __shared__ u64 s_hist[TEAMS][1 << BITS], s_sums[TEAMS][BY_COLUMN ? COLUMNS : RUNS_MOST], s_ties[BY_COLUMN ? 1 : RUNS_MOST];
+    __shared__ u64 s_part[TEAMS][16], s_found[TEAMS][4];
+    __shared__ double s_pow[64];
+    fill_pow(s_pow);
+    const int team = NT == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+    for (int64_t r = (int64_t)blockIdx.x * TEAMS + team; r < o.n_rows; r += (int64_t)gridDim.x * TEAMS) {
+        if constexpr (PARTS) {
+            const Parts src{o.part_key + r * o.n_part, o.part_col + r * o.n_part, o.n_part};
+            draw_row<NT, TILES, ONE, BITS>(o, r, src, s_hist[team], s_sums[team], s_ties, s_part[team], s_found[team], s_pow);
+        } else {
+            const Scores<BF16> src{(const char *)o.scores + r * o.lds * (BF16 ? 2 : 4), o.n_cols};
+            draw_row<NT, TILES, ONE, BITS>(o, r, src, s_hist[team], s_sums[team], s_ties, s_part[team], s_found[team], s_pow);
+        }
+    }
+}
+
+// ---- long rows, few scores left: the first k of a row are among the first k of its parts
+
+template <bool BF16, int NT, int TILES>
+__global__ __launch_bounds__(NT) void k_part_top(Call o, int64_t row0, int32_t parts, int32_t most_k, uint32_t *__restrict__ part_key, int32_t *__restrict__ part_col)
+{
+    typedef Team<NT> T;
+    __shared__ u64 s_hist[2048], s_part[16], s_found[4];
+    const int64_t r = row0 + blockIdx.x / (unsigned)parts;
+    const int32_t part = (int32_t)(blockIdx.x % (unsigned)parts);
+    constexpr int COLUMNS = 4 * TILES * NT;
+    const int32_t c0 = part * COLUMNS, n = min(COLUMNS, o.n_cols - c0);
+    const Scores<BF16> src{(const char *)o.scores + (r * o.lds + c0) * (BF16 ? 2 : 4), n};
+    Setting set = setting_of(o.how, r);
+    set.k = set.k > 0 ? min(set.k, most_k) : most_k;
+    const int tid = T::tid();
+    Keys<NT, TILES, true, Scores<BF16>> keys(src);
+    const Weigh none{};
+    const Cut cut = find_cut<NT, 11>(keys, set, none, false, s_hist, s_part, s_found);
+    uint32_t *out_key = part_key + (r * parts + part) * most_k;
+    int32_t *out_col = part_col + (r * parts + part) * most_k;
+    u64 base = 0ull;                                             // scores written, and in the upper half ties met
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+        const uint32_t *key = keys.key + 4 * i;
+        u64 mine = 0ull;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t x = key[k];
+            mine += x > cut.key ? 1ull : x == cut.key && x ? 1ull << 32 : 0ull;
+        }
+        u64 all;
+        u64 before = base + T::scan(mine, s_part, &all) - mine;
+        base += all;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t x = key[k];
+            const bool tie = x == cut.key && x;
+            const u64 ties = min(before >> 32, cut.ties);
+            if (x > cut.key || (tie && (before >> 32) < cut.ties)) {
+                const uint32_t at = (uint32_t)before + (uint32_t)ties;
+                out_key[at] = x;
+                out_col[at] = c0 + 4 * (NT * i + tid) + k;
+            }
+            before += x > cut.key ? 1ull : tie ? 1ull << 32 : 0ull;
+        }
+    }
+    const int32_t written = (int32_t)((uint32_t)base + (uint32_t)min(base >> 32, cut.ties));
+    for (int32_t i = written + tid; i < most_k; i += NT) out_key[i] = 0u;
+}
+
+// ---- long rows: a launch a digit
+
+struct State {                     // of a row, after a launch
+    Search x;
+    Cut cut;
+    uint32_t most;
+};
+
+struct Long {
+    Call o;
+    int64_t row0;                  // first row of this batch
+    int32_t parts, part;           // blocks to a row, and columns to a block (a multiple of 256)
+    uint32_t *most;                // [rows][parts]
+    u64 *hist;                     // [rows][6][2048]
+    State *state;                  // [rows][7]
+    u64 *part_sum, *part_ties;     // [rows][parts]: weights above the cut, ties of it
+    u64 *run_sum, *run_ties;       // [rows][parts][part / 256]
+};
+constexpr int LONG_T = 256, LONG_DIGITS = 2048;
+
+template <bool BF16>
+__global__ __launch_bounds__(LONG_T) void k_long_most(Long a)
+{
+    __shared__ u64 s_part[16];
+    const int64_t r = blockIdx.x / (unsigned)a.parts;
+    const int32_t part = (int32_t)(blockIdx.x % (unsigned)a.parts), c0 = part * a.part;
+    const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), min(a.o.n_cols, c0 + a.part)};
+    uint32_t most = 0u;
+    for (int32_t c = c0 + 4 * (int)threadIdx.x; c < src.n; c += 4 * LONG_T) {
+        uint32_t key[4];
+        src.get4(c, key);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) most = max(most, key[k]);
+    }
+    most = Team<LONG_T>::most(most, s_part);
+    if (threadIdx.x == 0) a.most[r * a.parts + part] = most;
+    for (int32_t i = part * LONG_T + threadIdx.x; i < 6 * LONG_DIGITS; i += a.parts * LONG_T) a.hist[r * 6 * LONG_DIGITS + i] = 0ull;
+}
+
+// The row's state after stage `prev` (3 which + level), from the sums by digit that its launch left; prev < 0: before the first
+__device__ __forceinline__ State advance(const Long &a, int64_t r, int before, int prev, const Setting &set, Weigh *weigh, const double *pow, u64 *s, u64 *s_found)
+{
+    typedef Team<LONG_T> T;
+    State st;
+    if (prev < 0) {
+        uint32_t most = 0u;
+        for (int32_t i = threadIdx.x; i < a.parts; i += LONG_T) most = max(most, a.most[r * a.parts + i]);
+        st.most = T::most(most, s);
+        st.x = Search{0ull, 0ull, 0u};
+        st.cut = Cut{0u, true, 0ull};
+    } else st = a.state[r * 7 + 1 + before];
+    weigh->init(st.most, set.t, a.o.bits, pow);
+    if (prev < 0) return st;
+    const int which = prev / 3, level = prev % 3;
+    if (cuts(which, set, a.o.n_cols) && st.most && (level == 0 || st.x.goal)) {
+        u64 v[LONG_DIGITS / LONG_T], upto, more, own;
+        const u64 all = digit_total<LONG_T, 11>(a.hist + (r * 6 + prev) * LONG_DIGITS, v, &upto, s);
+        if (level == 0) st.x.goal = which == 0 ? goal_of_count(all, set) : goal_of_weight(all, set);
+        if (st.x.goal) {
+            const int digit = digit_at<LONG_T, 11>(v, upto, st.x.goal - st.x.above, s_found, &more, &own);
+            st.x.above += more;
+            st.x.found |= (uint32_t)digit << (level == 0 ? 21 : level == 1 ? 10 : 0);
+            if (level == 2) st.cut = cut_at(which, st.x, own, st.cut, *weigh);
+        }
+    }
+    if (level == 2) st.x = Search{0ull, 0ull, 0u};
+    return st;
+}
+
+// sums by digit of stage `stage`; prev: the stage of the launch before, `before` the one before that
+template <bool BF16, int LEVEL>
+__global__ __launch_bounds__(LONG_T) void k_long_digit(Long a, int which, int before, int prev)
+{
+    typedef Digit<11, LEVEL> D;
+    __shared__ u64 s_hist[LONG_DIGITS], s_part[16], s_found[4];
+    __shared__ double s_pow[64];
+    fill_pow(s_pow);
+    const int64_t r = blockIdx.x / (unsigned)a.parts;
+    const int32_t part = (int32_t)(blockIdx.x % (unsigned)a.parts), c0 = part * a.part;
+    const Setting set = setting_of(a.o.how, a.row0 + r);
+    Weigh weigh;
+    const State st = advance(a, r, before, prev, set, &weigh, s_pow, s_part, s_found);
+    if (part == 0 && threadIdx.x == 0) a.state[r * 7 + 1 + prev] = st;
+    if (!cuts(which, set, a.o.n_cols) || st.most == 0u || (LEVEL > 0 && st.x.goal == 0ull)) return;
+    for (int i = threadIdx.x; i < LONG_DIGITS; i += LONG_T) s_hist[i] = 0ull;
+    __syncthreads();
+    const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), min(a.o.n_cols, c0 + a.part)};
+    for (int32_t c = c0 + 4 * (int)threadIdx.x; c < src.n; c += 4 * LONG_T) {
+        uint32_t key[4];
+        src.get4(c, key);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (key[k] == 0u || !D::in(key[k], st.x.found) || (which == 1 && key[k] <= st.cut.key)) continue;
+            const u64 w = which == 0 ? 1ull : weigh(key[k]);
+            if (w) atomicAdd(&s_hist[D::of(key[k])], w);
+        }
+    }
+    if (which == 1 && part == 0 && threadIdx.x == 0 && st.cut.key && D::in(st.cut.key, st.x.found))
+        atomicAdd(&s_hist[D::of(st.cut.key)], st.cut.ties * weigh(st.cut.key));
+    __syncthreads();
+    u64 *hist = a.hist + (r * 6 + which * 3 + LEVEL) * LONG_DIGITS;
+    for (int i = threadIdx.x; i < LONG_DIGITS; i += LONG_T)
+        if (s_hist[i]) atomicAdd(&hist[i], s_hist[i]);
+}
+
+// the weights above the cut and the ties of it, by runs of 256 columns and by part
+template <bool BF16>
+__global__ __launch_bounds__(LONG_T) void k_long_sums(Long a, int before, int prev)
+{
+    __shared__ u64 s_part[16], s_found[4];
+    __shared__ double s_pow[64];
+    fill_pow(s_pow);
+    const int64_t r = blockIdx.x / (unsigned)a.parts;
+    const int32_t part = (int32_t)(blockIdx.x % (unsigned)a.parts), c0 = part * a.part;
+    const Setting set = setting_of(a.o.how, a.row0 + r);
+    Weigh weigh;
+    const State st = advance(a, r, before, prev, set, &weigh, s_pow, s_part, s_found);
+    if (part == 0 && threadIdx.x == 0) a.state[r * 7 + 6] = st;      // slot 6: the last stage's own, or of stages that none of this call's are
+    const u64 least = least_weight(set, weigh);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), min(a.o.n_cols, c0 + a.part)};
+    const int32_t runs = a.part / 256;
+    u64 sum = 0ull, ties = 0ull;
+    for (int32_t i = wave; i < runs; i += LONG_T / 64) {
+        uint32_t key[4];
+        src.get4(c0 + 256 * i + 4 * lane, key);
+        u64 w = 0ull, t = 0ull;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (st.most && key[k] && (key[k] > st.cut.key || (key[k] == st.cut.key && st.cut.every))) w += weight_left(key[k], weigh, least);
+            t += key[k] == st.cut.key && !st.cut.every ? 1ull : 0ull;
+        }
+        w = wave_sum(w);
+        if (!st.cut.every) t = wave_sum(t);
+        if (lane == 0) {
+            const int64_t at = (r * a.parts + part) * runs + i;
+            a.run_sum[at] = w;
+            a.run_ties[at] = t;
+        }
+        sum += w;
+        ties += t;
+    }
+    // every lane of a wavefront has its sums
+    if (lane == 0) { s_part[wave] = sum; s_part[8 + wave] = ties; }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = ties = 0ull;
+        for (int i = 0; i < LONG_T / 64; ++i) { sum += s_part[i]; ties += s_part[8 + i]; }
+        a.part_sum[r * a.parts + part] = sum;
+        a.part_ties[r * a.parts + part] = ties;
+    }
+}
+
+// Of n items in order, with weights above the cut and ties of it, the one at which the weights left pass `goal`: its number, and what comes
+// before it (weights left, ties).  n_found 0: only the total.  All lanes of a wavefront alike.
+struct Found { int32_t item; u64 before, ties, total; };
+__device__ __forceinline__ Found find_item(const u64 *sum, const u64 *tie, int32_t n, u64 before, u64 ties, u64 left, u64 w_tie, bool search, u64 goal)
+{
+    Found f{-1, 0ull, 0ull, before};
+    const int lane = threadIdx.x & 63;
+    for (int32_t i0 = 0; i0 < n; i0 += 64) {
+        const int32_t i = i0 + lane;
+        u64 w = i < n ? sum[i] : 0ull, mine_ties = 0ull, upto_ties = 0ull;
+        if (w_tie) {
+            mine_ties = i < n ? tie[i] : 0ull;
+            upto_ties = ties + wave_scan(mine_ties);
+            const u64 first = upto_ties - mine_ties;
+            w += (min(upto_ties, left) - min(first, left)) * w_tie;
+        }
+        const u64 upto = f.total + wave_scan(w);
+        if (search && f.item < 0) {
+            const u64 hit = __ballot(upto > goal);
+            if (hit) {
+                const int at = __builtin_ctzll(hit);
+                f.item = i0 + at;
+                f.before = lane_of(upto - w, at);
+                f.ties = w_tie ? lane_of(upto_ties - mine_ties, at) : 0ull;
+                return f;
+            }
+        }
+        f.total = lane_of(upto, 63);
+        if (w_tie) ties = lane_of(upto_ties, 63);
+    }
+    return f;
+}
+
+// a wavefront a draw
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_long_draw(Long a, int64_t first, int64_t n)
+{
+    __shared__ double s_pow[64];
+    fill_pow(s_pow);
+    const int lane = threadIdx.x & 63;
+    const int64_t wave = first + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (wave >= n) return;
+    const int64_t r = wave / a.o.n_draws, at = a.row0 * a.o.n_draws + wave;
+    const State st = a.state[r * 7 + 6];
+    const Setting set = setting_of(a.o.how, a.row0 + r);
+    Weigh weigh;
+    weigh.init(st.most, set.t, a.o.bits, s_pow);
+    const u64 least = least_weight(set, weigh);
+    const u64 w_tie = st.most && !st.cut.every ? weight_left(st.cut.key, weigh, least) : 0ull;
+    const u64 *sum = a.part_sum + r * a.parts, *tie = a.part_ties + r * a.parts;
+    const u64 total = find_item(sum, tie, a.parts, 0ull, 0ull, st.cut.ties, w_tie, false, 0ull).total;
+    if (total == 0ull) {
+        if (lane == 0) answer(a.o, at, -1, 0ull, 1ull);
+        return;
+    }
+    const u64 goal = goal_of_draw(a.o, at, total);
+    const Found p = find_item(sum, tie, a.parts, 0ull, 0ull, st.cut.ties, w_tie, true, goal);
+    const int32_t runs = a.part / 256;
+    const int64_t run0 = (r * a.parts + p.item) * runs;
+    const Found f = find_item(a.run_sum + run0, a.run_ties + run0, runs, p.before, p.ties, st.cut.ties, w_tie, true, goal);
+    const int32_t c = p.item * a.part + 256 * f.item + 4 * lane;
+    const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), a.o.n_cols};
+    uint32_t key[4];
+    src.get4(c, key);
+    u64 w[4], equal = f.ties;
+    left4(key, st.cut, weigh, least, &equal, w);
+    u64 before = f.before + wave_scan(w[0] + w[1] + w[2] + w[3]) - (w[0] + w[1] + w[2] + w[3]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (goal >= before && goal < before + w[k]) answer(a.o, at, c + k, w[k], total);
+        before += w[k];
+    }
+}
+
+// ---- host
 
 int bits_of(int64_t n_cols)
 {
@@ -271,11 +881,129 @@ int bits_of(int64_t n_cols)
     return 62 - log < 40 ? 62 - log : 40;
 }
 
+constexpr int64_t LONG_BLOCKS = 1 << 22;      // of one launch
+
+// Rows that a block takes whole, however few there are, and rows enough for a block each
+constexpr int64_t BLOCK_ROW = 65536, MANY_ROWS = 256;
+
+// How a call runs, by its sizes and what the host knows of its settings
+struct Plan {
+    int32_t most_k;                // 0: rows, or digits in launches; else k_part_top's
+    int32_t parts, part, rows;     // parts of a row, columns of a part, rows a batch
+    size_t off_most, off_hist, off_state, off_sum, off_ties, off_run, off_run_ties, bytes;
+};
+
+Plan plan_of(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
+{
+    Plan p{};
+    p.bytes = 256;
+    if (n_cols <= BLOCK_ROW || (n_cols <= ROW_MOST && n_rows >= MANY_ROWS) || n_rows == 0) return p;
+    const bool greedy = !how->row_temperature && how->temperature == 0.f;
+    int64_t k = greedy ? 1 : how->top_k;
+    if (k > 0) {
+        // parts of 4096 columns where their scores left are a row of 16384 at most, else of 16384
+        for (int64_t part = 4096; part <= 16384; part *= 4) {
+            const int64_t parts = cdiv(n_cols, part);
+            if (k <= part && parts * k <= (part == 4096 ? 16384 : BLOCK_ROW)) {
+                p.most_k = (int32_t)k; p.parts = (int32_t)parts; p.part = (int32_t)part;
+                p.rows = (int32_t)(n_rows < LONG_BLOCKS / parts ? n_rows : LONG_BLOCKS / parts);
+                p.bytes = align_up((size_t)n_rows * parts * k * 4, 256) * 2;
+                return p;
+            }
+        }
+    }
+    // about 2048 blocks, of 4096 to 32768 columns
+    int64_t part = 4096;
+    while (part < 32768 && n_rows * cdiv(n_cols, part) > 2048) part *= 2;
+    p.part = (int32_t)part; p.parts = (int32_t)cdiv(n_cols, part);
+    p.rows = (int32_t)(n_rows < 4096 ? n_rows : 4096);
+    if (p.rows > LONG_BLOCKS / p.parts) p.rows = (int32_t)(LONG_BLOCKS / p.parts);
+    if (p.rows < 1) p.rows = 1;
+    const size_t rows = (size_t)p.rows, parts = rows * p.parts, runs = parts * (part / 256);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at = align_up(at + bytes, 256); return here; };
+    p.off_most = take(parts * 4);
+    p.off_hist = take(rows * 6 * LONG_DIGITS * 8);
+    p.off_state = take(rows * 7 * sizeof(State));
+    p.off_sum = take(parts * 8);
+    p.off_ties = take(parts * 8);
+    p.off_run = take(runs * 8);
+    p.off_run_ties = take(runs * 8);
+    p.bytes = at;
+    return p;
+}
+
+template <bool BF16, int NT, int TILES, bool ONE, bool PARTS>
+int launch_rows(const Call &o, hipStream_t st)
+{
+    const int64_t blocks = NT == 64 ? cdiv(o.n_rows, 4) : o.n_rows;
+    k_rows<BF16, NT, TILES, ONE, PARTS><<<(unsigned)(blocks < 65536 ? blocks : 65536), NT == 64 ? 256 : NT, 0, st>>>(o);
+    KGE_LAUNCH_CHECK();
+    return KGE_OK;
+}
+
+template <bool BF16>
+int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
+{
+    if (o.n_cols <= 256) return launch_rows<BF16, 64, 1, true, false>(o, st);
+    if (o.n_cols <= 1024) return launch_rows<BF16, 64, 4, true, false>(o, st);
+    if (o.n_cols <= 4096) return launch_rows<BF16, 256, 4, true, false>(o, st);
+    if (o.n_cols <= 16384) return launch_rows<BF16, 1024, 4, true, false>(o, st);
+    if (p.parts == 0) return launch_rows<BF16, 1024, 4, false, false>(o, st);
+    if (p.most_k) {
+        uint32_t *part_key = (uint32_t *)ws;
+        int32_t *part_col = (int32_t *)(ws + p.bytes / 2);
+        for (int64_t row0 = 0; row0 < o.n_rows; row0 += p.rows) {
+            const int64_t rows = o.n_rows - row0 < p.rows ? o.n_rows - row0 : p.rows;
+            if (p.part == 4096) k_part_top<BF16, 256, 4><<<(unsigned)(rows * p.parts), 256, 0, st>>>(o, row0, p.parts, p.most_k, part_key, part_col);
+            else k_part_top<BF16, 1024, 4><<<(unsigned)(rows * p.parts), 1024, 0, st>>>(o, row0, p.parts, p.most_k, part_key, part_col);
+            KGE_LAUNCH_CHECK();
+        }
+        o.part_key = part_key; o.part_col = part_col; o.n_part = p.parts * p.most_k;
+        if (o.n_part <= 1024) return launch_rows<BF16, 64, 4, true, true>(o, st);
+        if (o.n_part <= 4096) return launch_rows<BF16, 256, 4, true, true>(o, st);
+        if (o.n_part <= 16384) return launch_rows<BF16, 1024, 4, true, true>(o, st);
+        return launch_rows<BF16, 1024, 4, false, true>(o, st);
+    }
+    Long a;
+    a.o = o; a.parts = p.parts; a.part = p.part;
+    a.most = (uint32_t *)(ws + p.off_most); a.hist = (u64 *)(ws + p.off_hist); a.state = (State *)(ws + p.off_state);
+    a.part_sum = (u64 *)(ws + p.off_sum); a.part_ties = (u64 *)(ws + p.off_ties);
+    a.run_sum = (u64 *)(ws + p.off_run); a.run_ties = (u64 *)(ws + p.off_run_ties);
+    const bool by_count = o.how.row_temperature || o.how.row_top_k || o.how.top_k > 0 || o.how.temperature == 0.f;
+    const bool by_weight = o.how.row_top_p || o.how.top_p < 1.f;
+    for (a.row0 = 0; a.row0 < o.n_rows; a.row0 += p.rows) {
+        const int64_t rows = o.n_rows - a.row0 < p.rows ? o.n_rows - a.row0 : p.rows;
+        const unsigned blocks = (unsigned)(rows * p.parts);
+        k_long_most<BF16><<<blocks, LONG_T, 0, st>>>(a);
+        KGE_LAUNCH_CHECK();
+        int before = -2, prev = -1;
+        for (int which = 0; which < 2; ++which) {
+            if (which == 0 ? !by_count : !by_weight) continue;
+            k_long_digit<BF16, 0><<<blocks, LONG_T, 0, st>>>(a, which, before, prev);
+            before = prev; prev = 3 * which;
+            k_long_digit<BF16, 1><<<blocks, LONG_T, 0, st>>>(a, which, before, prev);
+            before = prev; prev = 3 * which + 1;
+            k_long_digit<BF16, 2><<<blocks, LONG_T, 0, st>>>(a, which, before, prev);
+            before = prev; prev = 3 * which + 2;
+            KGE_LAUNCH_CHECK();
+        }
+        k_long_sums<BF16><<<blocks, LONG_T, 0, st>>>(a, before, prev);
+        KGE_LAUNCH_CHECK();
+        const int64_t draws = rows * o.n_draws;
+        for (int64_t d = 0; d < draws; d += LONG_BLOCKS * 4) {
+            k_long_draw<BF16><<<(unsigned)cdiv(draws - d < LONG_BLOCKS * 4 ? draws - d : LONG_BLOCKS * 4, 4), 256, 0, st>>>(a, d, draws);
+            KGE_LAUNCH_CHECK();
+        }
+    }
+    return KGE_OK;
+}
+
 int check_call(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
 {
     KGE_REQUIRE(how, KGE_EINVAL, "NULL argument");
     KGE_REQUIRE(n_rows >= 0 && n_cols >= 0, KGE_EINVAL, "negative size");
-    KGE_REQUIRE(n_rows <= 0x7fffffffll && n_cols <= 0x7fffffffll, KGE_ERANGE, "2^31 rows or columns or more");
+    KGE_REQUIRE(n_rows <= 0x7fffffffll && n_cols <= 0x7fff0000ll, KGE_ERANGE, "2^31 rows, or more than 2^31 - 2^16 columns");
     KGE_REQUIRE(how->row_temperature || (how->temperature >= 0.f && how->temperature <= 3.402823466e38f), KGE_EINVAL,
                 "temperature must be zero or more, and finite");
     KGE_REQUIRE(how->top_k >= 0, KGE_EINVAL, "top_k must be zero (off) or more");
@@ -291,7 +1019,7 @@ int check_call(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
 extern "C" size_t kge_sample_workspace_bytes(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
 {
     if (check_call(how, n_rows, n_cols) != KGE_OK) return 0;
-    return 256;
+    return plan_of(how, n_rows, n_cols).bytes;
 }
 
 extern "C" int kge_sample_scores(const kge_sampling *how, int64_t n_rows, int64_t n_cols, const void *scores, int32_t dtype, int64_t lds,
@@ -315,11 +1043,10 @@ extern "C" int kge_sample_scores(const kge_sampling *how, int64_t n_rows, int64_
     o.how = Sampling{how->temperature, how->top_p, how->min_p, how->top_k, how->row_temperature, how->row_top_p, how->row_min_p, how->row_top_k};
     o.scores = scores; o.u = u; o.choice = choice; o.prob = prob; o.n_rows = n_rows; o.lds = lds;
     o.n_cols = (int32_t)n_cols; o.n_draws = n_draws; o.bits = bits_of(n_cols); o.u64bit = u_bits == 64;
+    o.part_key = nullptr; o.part_col = nullptr; o.n_part = 0;
+    const Plan p = plan_of(how, n_rows, n_cols);
     KGE_PROF("sample_scores", st);
-    const unsigned blocks = (unsigned)(n_rows < 65536 ? n_rows : 65536);
-    (dtype == KGE_DT_BF16 ? k_sample_rows<true> : k_sample_rows<false>)<<<blocks, THREADS, 0, st>>>(o);
-    KGE_LAUNCH_CHECK();
-    return KGE_OK;
+    return dtype == KGE_DT_BF16 ? launch_call<true>(o, p, (char *)workspace, st) : launch_call<false>(o, p, (char *)workspace, st);
 }
 
 namespace {
