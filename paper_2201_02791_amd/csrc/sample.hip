@@ -42,7 +42,10 @@ struct Call {
     const uint32_t *part_key;      // [n_rows][n_part]: a row's first scores, in the order of their columns, and the columns
     const int32_t *part_col;
     int32_t n_part;
+    double per;                    // 256 / (T ln 2) of the call's temperature
 };
+
+__device__ __host__ __forceinline__ double per_of(float t) { return 369.329930467574627508 / (double)(t > 0.f ? t : 1.f); }
 
 // a row's settings
 struct Setting { float t, p, low; int32_t k; };
@@ -67,6 +70,11 @@ __device__ __forceinline__ uint32_t key_of(float l)
     const uint32_t k = b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u);
     return l > -INFINITY ? k : 0u;
 }
+__device__ __forceinline__ uint32_t key_in_order(float l)          // of a score that has a weight
+{
+    const uint32_t b = __float_as_uint(l + 0.f);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
 __device__ __forceinline__ float score_of(uint32_t key) { return __uint_as_float(key ^ ((int32_t)key < 0 ? 0x80000000u : 0xffffffffu)); }
 
 struct __attribute__((packed, aligned(4))) F4 { float x[4]; };
@@ -78,84 +86,116 @@ template <bool BF16>
 struct Scores {
     const void *row;
     int32_t n;
-    __device__ __forceinline__ void get4(int32_t c, uint32_t key[4]) const      // columns c .. c + 3
+    __device__ __forceinline__ float one(int32_t c) const { return BF16 ? __uint_as_float((uint32_t)((const uint16_t *)row)[c] << 16) : ((const float *)row)[c]; }
+    // columns c .. c + 3, all of them in the row
+    __device__ __forceinline__ void score4(int32_t c, float l[4]) const
     {
-        if (c + 4 <= n) {
-            if (BF16) {
-                const H4 q = *reinterpret_cast<const H4 *>((const uint16_t *)row + c);
+        if (BF16) {
+            const H4 q = *reinterpret_cast<const H4 *>((const uint16_t *)row + c);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) key[k] = key_of(__uint_as_float((uint32_t)q.x[k] << 16));
-            } else {
-                const F4 q = *reinterpret_cast<const F4 *>((const float *)row + c);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) key[k] = key_of(q.x[k]);
-            }
+            for (int k = 0; k < 4; ++k) l[k] = __uint_as_float((uint32_t)q.x[k] << 16);
         } else {
+            const F4 q = *reinterpret_cast<const F4 *>((const float *)row + c);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                key[k] = c + k >= n ? 0u : key_of(BF16 ? __uint_as_float((uint32_t)((const uint16_t *)row)[c + k] << 16) : ((const float *)row)[c + k]);
+            for (int k = 0; k < 4; ++k) l[k] = q.x[k];
         }
     }
+    __device__ __forceinline__ void whole4(int32_t c, uint32_t key[4]) const
+    {
+        float l[4];
+        score4(c, l);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) key[k] = key_of(l[k]);
+    }
+    __device__ __forceinline__ uint32_t key(int32_t c) const { return key_of(one(c)); }
     __device__ __forceinline__ int32_t column(int32_t c) const { return c; }
 };
 struct Parts {
-    const uint32_t *key_;
+    const uint32_t *keys;
     const int32_t *col;
     int32_t n;
-    __device__ __forceinline__ void get4(int32_t c, uint32_t key[4]) const
+    __device__ __forceinline__ void whole4(int32_t c, uint32_t key[4]) const
     {
-        if (c + 4 <= n) {
-            const U4 q = *reinterpret_cast<const U4 *>(key_ + c);
+        const U4 q = *reinterpret_cast<const U4 *>(keys + c);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) key[k] = q.x[k];
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) key[k] = c + k < n ? key_[c + k] : 0u;
-        }
+        for (int k = 0; k < 4; ++k) key[k] = q.x[k];
     }
+    __device__ __forceinline__ uint32_t key(int32_t c) const { return keys[c]; }
     __device__ __forceinline__ int32_t column(int32_t c) const { return col[c]; }
 };
+// keys of columns c .. c + 3, 0 past the end
+template <class Source>
+__device__ __forceinline__ void get4(const Source &src, int32_t c, uint32_t key[4])
+{
+    if (c + 4 <= src.n) src.whole4(c, key);
+    else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) key[k] = c + k < src.n ? src.key(c + k) : 0u;
+    }
+}
 
 // ---- weights
 
-// e^z, z = (l - m) / T <= 0, as 2^(x / 64): x = z 64 / ln 2 to its nearest whole number n by a table of 2^(j / 64), what is left,
-// |z'| <= ln 2 / 128, by five terms of the exponential series (the sixth is below 2^-51).  Double arithmetic throughout: a weight
-// is off by one unit at most, and that only within 2^-7 of a unit of a half of one (x carries an error of |x| 2^-53, 2^-42 at most).
-// Adding 2^52 rounds to a whole number.
+// e^z, z = (l - m) / T <= 0, as 2^(x / 256), x = z 256 / ln 2: its nearest whole number n is left in the low bits of x + 3 2^51, what is
+// left, r, goes through four terms of the exponential series of r ln 2 / 256 (the fifth is below 2^-54) and n mod 256 through a
+// table of 2^(b + j / 256).  Adding 2^52 to the number of units rounds it.  No branch: what is too small is held at `least` and rounds to
+// zero.  Double operations are as fast as float ones here.  A weight is off by one unit at most, and that only within 2^-7 of a unit
+// of a half of one (x carries an error of |x| 2^-53, 2^-39 at most).
+constexpr int POWERS = 256;
 struct Weigh {
-    double most, per, least;           // m, 64 / (T ln 2), and the x below which a weight rounds to zero
-    const double *pow;                 // LDS: 2^(j / 64)
+    double most, per, least;           // m, 256 / (T ln 2), and an x at which a weight rounds to zero
+    const double *pow;                 // LDS: 2^(b + j / 256)
     uint32_t most_key;
     int32_t bits;
-    __device__ __forceinline__ void init(uint32_t key, float t, int32_t b, const double *table)
+    bool endless;                      // m is infinite: what is equal to it has all the weight
+    __device__ __forceinline__ void init(uint32_t key, float t, const Call &o, const double *table)
     {
         most_key = key;
         most = (double)score_of(key);
-        per = 92.332482616893656877 / (double)t;
-        least = -64.0 * (b + 2);
-        bits = b;
+        per = o.how.row_temperature ? per_of(t) : o.per;
+        bits = o.bits;
+        least = -256.0 * (bits + 2);
         pow = table;
+        endless = score_of(key) == INFINITY;
     }
     __device__ __forceinline__ u64 unit() const { return 1ull << bits; }
+    // the weight of a score of a row whose largest is not infinite, in units, plus 2^52: rounded.  NaN and minus infinity: none
+    __device__ __forceinline__ double raised(float l) const
+    {
+        const double x = __builtin_fmax(((double)l - most) * per, least);
+        const double t = x + 0x1.8p52, r = x - (t - 0x1.8p52);
+        constexpr double c1 = 0.0027076061740622863, c2 = c1 * c1 / 2.0, c3 = c2 * c1 / 3.0, c4 = c3 * c1 / 4.0;
+        const int32_t i = (int32_t)__double_as_longlong(t);
+        const double e = fma(r, fma(r, fma(r, fma(r, c4, c3), c2), c1), 1.0) * pow[i & (POWERS - 1)];
+        const long long w = __double_as_longlong(e) + ((long long)((i & ~(POWERS - 1)) << 12) << 32);       // times 2^(i >> 8)
+        return __longlong_as_double(w) + 0x1p52;
+    }
+    __device__ __forceinline__ double units(uint32_t key) const
+    {
+        if (endless) return key == most_key ? (double)unit() : 0.0;
+        return raised(score_of(key)) - 0x1p52;
+    }
     __device__ __forceinline__ u64 operator()(uint32_t key) const
     {
-        if (key == 0u) return 0ull;
-        if (key == most_key) return unit();
-        const double x = ((double)score_of(key) - most) * per;
-        if (!(x > least)) return 0ull;
-        const double n = rint(x), r = (x - n) * 0.010830424696249145;
-        const double e = fma(r, fma(r, fma(r, fma(r, fma(r, 1.0 / 120.0, 1.0 / 24.0), 1.0 / 6.0), 0.5), 1.0), 1.0);
-        const int i = (int)n;
-        const double w = ldexp(pow[i & 63] * e, (i >> 6) + bits);
-        return (u64)__double_as_longlong(w + 0x1p52) & 0xfffffffffffffull;
+        if (endless) return key == most_key ? unit() : 0ull;
+        return (u64)__double_as_longlong(raised(score_of(key))) & 0xfffffffffffffull;
+    }
+    // no score of a lower key has a weight: all that round to one unit or more are above m - T ln 2 (b + 2)
+    __device__ __forceinline__ uint32_t lowest(float t) const
+    {
+        const float l = (float)(most - (double)t * (0.6931471805599453 * (bits + 2)));
+        return l > -3.402823466e38f ? key_of(l) : 0x00800000u;
     }
 };
 
-__device__ __forceinline__ void fill_pow(double *table)
+__device__ __forceinline__ void fill_pow(double *table, int32_t bits)
 {
-    if (threadIdx.x < 64) table[threadIdx.x] = exp2((double)threadIdx.x * (1.0 / 64.0));
+    if (threadIdx.x < POWERS) table[threadIdx.x] = exp2((double)threadIdx.x * (1.0 / POWERS) + bits);
     __syncthreads();
 }
+
+// a whole number of up to 52 bits, from and to double
+__device__ __forceinline__ u64 whole(double v) { return (u64)__double_as_longlong(v + 0x1p52) & 0xfffffffffffffull; }
 
 // ---- sums over a wavefront and over a team of NT threads (64: a wavefront, more: the block)
 
@@ -176,17 +216,40 @@ __device__ __forceinline__ u64 wave_scan(u64 v)
     v = dpp_add<0x142, 0xa>(v);
     return dpp_add<0x143, 0xc>(v);
 }
+// the same of whole numbers in double, below 2^53
+__device__ __forceinline__ double wave_scan(double v)
+{
+    const auto step = [](double x, int lo, int hi) { return x + __longlong_as_double((long long)((u64)(uint32_t)hi << 32 | (uint32_t)lo)); };
+#define SCAN_STEP(CTRL, ROWS) \
+    v = step(v, __builtin_amdgcn_update_dpp(0, (int)__double_as_longlong(v), CTRL, ROWS, 0xf, false), \
+             __builtin_amdgcn_update_dpp(0, (int)(__double_as_longlong(v) >> 32), CTRL, ROWS, 0xf, false));
+    SCAN_STEP(0x111, 0xf)
+    SCAN_STEP(0x112, 0xf)
+    SCAN_STEP(0x114, 0xf)
+    SCAN_STEP(0x118, 0xf)
+    SCAN_STEP(0x142, 0xa)
+    SCAN_STEP(0x143, 0xc)
+#undef SCAN_STEP
+    return v;
+}
 __device__ __forceinline__ u64 lane_of(u64 v, int lane)
 {
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
     return (u64)hi << 32 | lo;
 }
+__device__ __forceinline__ double lane_of(double v, int lane) { return __longlong_as_double((long long)lane_of((u64)__double_as_longlong(v), lane)); }
 __device__ __forceinline__ u64 wave_sum(u64 v) { return lane_of(wave_scan(v), 63); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) { return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false)); }
 __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, off, 64));
-    return v;
+    v = dpp_max<0x111, 0xf>(v);
+    v = dpp_max<0x112, 0xf>(v);
+    v = dpp_max<0x114, 0xf>(v);
+    v = dpp_max<0x118, 0xf>(v);
+    v = dpp_max<0x142, 0xa>(v);
+    v = dpp_max<0x143, 0xc>(v);
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
 template <int NT>
@@ -202,18 +265,20 @@ struct Team {
     }
     static __device__ __forceinline__ int tid() { return NT == 64 ? (int)(threadIdx.x & 63) : (int)threadIdx.x; }
     // inclusive sums over the threads, and their total; s: WAVES words of LDS
-    static __device__ __forceinline__ u64 scan(u64 v, u64 *s, u64 *total)
+    template <class N>
+    static __device__ __forceinline__ N scan(N v, void *words, N *total)
     {
+        N *s = (N *)words;
         v = wave_scan(v);
         if (NT == 64) { *total = lane_of(v, 63); return v; }
         const int wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 63) s[wave] = v;
         __syncthreads();
         const int at = threadIdx.x & 63;
-        const u64 sums = wave_scan(at < WAVES ? s[at] : 0ull);
+        const N sums = wave_scan(at < WAVES ? s[at] : N(0));
         __syncthreads();
         *total = lane_of(sums, WAVES - 1);
-        return v + (wave ? lane_of(sums, wave - 1) : 0ull);
+        return v + (wave ? lane_of(sums, wave - 1) : N(0));
     }
     static __device__ __forceinline__ uint32_t most(uint32_t v, u64 *s)
     {
@@ -236,19 +301,38 @@ struct Cut {
     u64 ties;
 };
 
-// The search for one: which = 0 by counts (top-k), 1 by weights (top-p)
+// The search for one: which = 0 by counts (top-k), 1 by weights (top-p).  Digits are those of a key's distance from `base`, which is not above
+// the key that is searched: few digits where the keys lie close together, and sums that spread over all values of a digit.
+constexpr uint32_t LEAST_KEY = 0x00800000u;   // of the lowest number
+template <int BITS>
 struct Search {
-    u64 goal, above;               // sum that the scores from the cut on reach; sum of the digits above what is found
-    uint32_t found;
-};
-
-template <int BITS, int LEVEL>
-struct Digit {                     // a key's digit at a level, most significant first; the last may be shorter
-    static constexpr int LEVELS = (32 + BITS - 1) / BITS;
-    static constexpr int SHIFT = LEVEL == LEVELS - 1 ? 0 : 32 - BITS * (LEVEL + 1), WIDTH = LEVEL == LEVELS - 1 ? 32 - BITS * LEVEL : BITS;
-    static constexpr uint32_t BEFORE = LEVEL == 0 ? 0u : ~0u << (32 - BITS * LEVEL);      // the digits above
-    static __device__ __forceinline__ uint32_t of(uint32_t key) { return (key >> SHIFT) & ((1u << WIDTH) - 1u); }
-    static __device__ __forceinline__ bool in(uint32_t key, uint32_t found) { return (key & BEFORE) == found; }
+    u64 goal, above;               // the sum that the scores from the cut on reach; the sum of the digits above what is found
+    uint32_t base, found;          // digits so far
+    int32_t shift, width;          // of the digit that is next
+    bool open;
+    __device__ __forceinline__ void begin(uint32_t low, uint32_t most)
+    {
+        goal = above = 0ull;
+        base = low; found = 0u;
+        const int bits = max(1, 32 - (int)__builtin_clz((most - low) | 1u));
+        shift = max(bits - BITS, 0);
+        width = bits - shift;
+        open = true;
+    }
+    __device__ __forceinline__ bool in(uint32_t key) const { return key >= base && (((key - base) >> shift) >> width) == found; }
+    __device__ __forceinline__ uint32_t digit(uint32_t key) const { return ((key - base) >> shift) & ((1u << width) - 1u); }
+    __device__ __forceinline__ void step(int digit, u64 more)
+    {
+        above += more;
+        found = found << width | (uint32_t)digit;
+        open = shift > 0;
+        width = min(BITS, shift);
+        shift -= width;
+    }
+    __device__ __forceinline__ uint32_t key() const { return base + found; }
+    // the least and the largest key that have the digits found
+    __device__ __forceinline__ uint32_t first() const { return base + ((found << width) << shift); }
+    __device__ __forceinline__ u64 last() const { return first() + ((1ull << (width + shift)) - 1ull); }
 };
 
 // The digit at which the sums, from the largest digit down, first reach `goal` (1 or more, their total at most); the sum of the digits above it
@@ -291,7 +375,7 @@ __device__ __forceinline__ int digit_at(const u64 (&v)[(1 << BITS) / NT], u64 up
 }
 
 // what the sums have to reach, from their total; 0: nothing is cut
-__device__ __forceinline__ u64 goal_of_count(u64 all, const Setting &set) { return all <= (u64)set.k ? 0ull : (u64)set.k; }
+__device__ __forceinline__ u64 goal_of_count(u64 all, const Setting &set) { return all < (u64)set.k ? 0ull : (u64)set.k; }
 __device__ __forceinline__ u64 goal_of_weight(u64 all, const Setting &set)
 {
     const double g = ceil((double)set.p * (double)all);
@@ -299,145 +383,161 @@ __device__ __forceinline__ u64 goal_of_weight(u64 all, const Setting &set)
     return goal > all ? all : goal;
 }
 
-__device__ __forceinline__ bool cuts(int which, const Setting &set, int32_t n) { return which == 0 ? set.k > 0 && set.k < n : set.p < 1.f; }
+// One score left is the largest, of equal ones the first: nothing to search
+__device__ __forceinline__ bool cuts(int which, const Setting &set, int32_t n) { return set.k != 1 && (which == 0 ? set.k > 0 && set.k < n : set.p < 1.f); }
+__device__ __forceinline__ Cut first_cut(const Setting &set, uint32_t most) { return set.k == 1 ? Cut{most, false, 1ull} : Cut{0u, true, 0ull}; }
 
-// a search ended at score `found`, whose sum is `own`, with `above` before it
-__device__ __forceinline__ Cut cut_at(int which, const Search &x, u64 own, const Cut &was, const Weigh &weigh)
+// a search has ended; `own`: the sum at its key
+template <class S>
+__device__ __forceinline__ Cut cut_at(int which, const S &x, u64 own, const Cut &was, const Weigh &weigh)
 {
     Cut c;
-    c.key = x.found;
+    c.key = x.key();
     if (which == 0) {
         c.ties = x.goal - x.above;
         c.every = c.ties == own;
     } else {
-        const u64 w = weigh(x.found);
+        const u64 w = weigh(c.key);
         c.ties = (x.goal - x.above + w - 1ull) / w;
-        c.every = c.ties * w == own && (x.found != was.key || was.every);
+        c.every = c.ties * w == own && (c.key != was.key || was.every);
     }
     return c;
 }
 
 // A row's keys, TILES tiles of 4 columns a thread at a time: thread t of NT has columns 4 (NT i + t) .. + 3 of tile i.  ONE: the row has no
-// more, and they stay in registers; else every pass reads them again, from the caches.
+// more, and they stay in registers, with the weights of those that top-k leaves where a thread has the registers (128 with 1024 threads to a
+// block); else every pass reads them again, from the caches, and weighs again.
 template <int NT, int TILES, bool ONE, class Source>
 struct Keys {
     static constexpr int V = 4 * TILES, BATCH = NT * V;
+    static constexpr bool HELD = ONE && NT < 1024;
     const Source &src;
     uint32_t key[V];
+    double w[HELD ? V : 1];
+    __device__ __forceinline__ void weigh_all(const Weigh &weigh, const Cut &cut)
+    {
+        if (!HELD) return;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            w[HELD ? i : 0] = 0.0;
+            if (key[i] >= cut.key) w[HELD ? i : 0] = weigh.units(key[i]);
+        }
+    }
+    __device__ __forceinline__ double weight(int i, const Weigh &weigh) const
+    {
+        if (HELD) return w[HELD ? i : 0];
+        uint32_t k = key[i];
+        asm volatile("" : "+v"(k));              // the compiler would hold the last pass's weights, in scratch memory
+        return weigh.units(k);
+    }
     __device__ __forceinline__ explicit Keys(const Source &s) : src(s) { if (ONE) load(0); }
     __device__ __forceinline__ void load(int32_t c0)
     {
+        // inside the row no branch parts the loads
+        if (c0 + BATCH <= src.n) {
 #pragma unroll
-        for (int i = 0; i < TILES; ++i) src.get4(c0 + 4 * (NT * i + Team<NT>::tid()), key + 4 * i);
+            for (int i = 0; i < TILES; ++i) src.whole4(c0 + 4 * (NT * i + Team<NT>::tid()), key + 4 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) get4(src, c0 + 4 * (NT * i + Team<NT>::tid()), key + 4 * i);
+        }
     }
-    // f(first column) for each batch, whose keys are then in `key`
+    // f(first column) for each batch from column c0 on, whose keys are then in `key`
     template <class F>
-    __device__ __forceinline__ void each(F f)
+    __device__ __forceinline__ void each(int32_t c0, F f)
     {
         if (ONE) { f(0); return; }
 #pragma unroll 1
-        for (int32_t c0 = 0; c0 < src.n; c0 += BATCH) {
+        for (; c0 < src.n; c0 += BATCH) {
             load(c0);
             f(c0);
         }
     }
 };
 
-template <int NT, int BITS, int LEVEL, class K>
-__device__ __forceinline__ void search_level(int which, K &keys, const Setting &set, const Weigh &weigh, Cut &cut, Search &x, u64 *hist, u64 *s, u64 *s_found)
+// limit: as soon as no more than so many scores are at or above the least that has the digits found, the search for top-k's cut ends; the cut is
+// then that score's key, and true is returned: what is left holds the first k, and may hold more
+template <int NT, int BITS, class K>
+__device__ __forceinline__ bool find_cut(int which, uint32_t limit, K &keys, const Setting &set, const Weigh &weigh, uint32_t low, uint32_t most, Cut &cut, u64 *hist, u64 *s,
+                                         u64 *s_found)
 {
-    typedef Digit<BITS, LEVEL> D;
+    if (!cuts(which, set, keys.src.n)) return false;
     const int tid = Team<NT>::tid();
-    if (LEVEL > 0 && x.goal == 0ull) return;
-    for (int i = tid; i < 1 << BITS; i += NT) hist[i] = 0ull;
-    Team<NT>::sync();
-    keys.each([&](int32_t) {
+    Search<BITS> x;
+    x.begin(low, most);
+#pragma unroll 1
+    for (bool first = true; x.open; first = false) {
+        for (int i = tid; i < 1 << BITS; i += NT) hist[i] = 0ull;
+        Team<NT>::sync();
+        keys.each(0, [&](int32_t) {
 #pragma unroll
-        for (int i = 0; i < K::V; ++i) {
-            const uint32_t key = keys.key[i];
-            if (key == 0u || !D::in(key, x.found) || (which == 1 && key <= cut.key)) continue;
-            const u64 w = which == 0 ? 1ull : weigh(key);
-            if (w) atomicAdd(&hist[D::of(key)], w);
+            for (int i = 0; i < K::V; ++i) {
+                const uint32_t key = keys.key[i];
+                if (!x.in(key) || (which == 1 && key <= cut.key)) continue;
+                const u64 w = which == 0 ? 1ull : whole(keys.weight(i, weigh));
+                if (w) atomicAdd(&hist[x.digit(key)], w);
+            }
+        });
+        if (which == 1 && tid == 0 && cut.key && x.in(cut.key)) atomicAdd(&hist[x.digit(cut.key)], cut.ties * weigh(cut.key));
+        Team<NT>::sync();
+        u64 v[(1 << BITS) / NT], upto, more, own;
+        const u64 all = digit_total<NT, BITS>(hist, v, &upto, s);
+        if (first) x.goal = which == 0 ? goal_of_count(all, set) : goal_of_weight(all, set);
+        if (x.goal == 0ull) return false;
+        const int digit = digit_at<NT, BITS>(v, upto, x.goal - x.above, s_found, &more, &own);
+        x.step(digit, more);
+        if (which == 0 && x.above + own <= (u64)limit) {
+            cut = Cut{x.first(), true, ~0ull};
+            return true;
         }
-    });
-    if (which == 1 && tid == 0 && cut.key && D::in(cut.key, x.found)) atomicAdd(&hist[D::of(cut.key)], cut.ties * weigh(cut.key));
-    Team<NT>::sync();
-    u64 v[(1 << BITS) / NT], upto, more, own;
-    const u64 all = digit_total<NT, BITS>(hist, v, &upto, s);
-    if (LEVEL == 0) x.goal = which == 0 ? goal_of_count(all, set) : goal_of_weight(all, set);
-    if (x.goal == 0ull) return;
-    const int digit = digit_at<NT, BITS>(v, upto, x.goal - x.above, s_found, &more, &own);
-    x.above += more;
-    x.found |= (uint32_t)digit << D::SHIFT;
-    if (LEVEL == D::LEVELS - 1) cut = cut_at(which, x, own, cut, weigh);
+        if (!x.open) cut = cut_at(which, x, own, cut, weigh);
+    }
+    return false;
 }
 
-template <int NT, int BITS, class K>
-__device__ __forceinline__ Cut find_cut(K &keys, const Setting &set, const Weigh &weigh, bool by_weight, u64 *hist, u64 *s, u64 *s_found)
+// a lower bound of the k-th largest key, from the threads' largest: NT scores at least are not below the least of those
+template <int NT>
+__device__ __forceinline__ uint32_t low_of(uint32_t mine, int32_t k, u64 *s)
 {
-    Cut cut{0u, true, 0ull};
-#pragma unroll 1
-    for (int which = 0; which < (by_weight ? 2 : 1); ++which) {
-        if (!cuts(which, set, keys.src.n)) continue;
-        Search x{0ull, 0ull, 0u};
-        search_level<NT, BITS, 0>(which, keys, set, weigh, cut, x, hist, s, s_found);
-        search_level<NT, BITS, 1>(which, keys, set, weigh, cut, x, hist, s, s_found);
-        search_level<NT, BITS, 2>(which, keys, set, weigh, cut, x, hist, s, s_found);
-        if constexpr (BITS == 8) search_level<NT, BITS, 3>(which, keys, set, weigh, cut, x, hist, s, s_found);
-    }
-    return cut;
+    if (k > NT) return LEAST_KEY;
+    return max(~Team<NT>::most(~mine, s), LEAST_KEY);
 }
 
 // ---- draws
 
+__device__ __forceinline__ double random_of(const Call &o, int64_t at) { return o.u64bit ? ((const double *)o.u)[at] : (double)((const float *)o.u)[at]; }
+
 __device__ __forceinline__ u64 goal_of_draw(const Call &o, int64_t at, u64 total)
 {
-    const double u = o.u64bit ? ((const double *)o.u)[at] : (double)((const float *)o.u)[at];
-    const double reach = u * (double)total;
+    const double reach = random_of(o, at) * (double)total;
     return reach >= (double)total ? total - 1ull : reach > 0.0 ? min((u64)reach, total - 1ull) : 0ull;
 }
+// totals that a double holds
+__device__ __forceinline__ double goal_of_draw(const Call &o, int64_t at, double total)
+{
+    return fmin(fmax(floor(random_of(o, at) * total), 0.0), total - 1.0);
+}
 
-__device__ __forceinline__ void answer(const Call &o, int64_t at, int32_t column, u64 w, u64 total)
+__device__ __forceinline__ void answer(const Call &o, int64_t at, int32_t column, double w, double inverse)
 {
     o.choice[at] = column;
-    if (o.prob) o.prob[at] = w ? (float)((double)w / (double)total) : 0.f;
+    if (o.prob) o.prob[at] = (float)(w * inverse);
+}
+// 1 / total, to 2^-50: the instruction's 2^-14 or better squared twice
+__device__ __forceinline__ double inverse_of(double total)
+{
+    double y = __builtin_amdgcn_rcp(total);
+    y = fma(fma(-total, y, 1.0), y, y);
+    return fma(fma(-total, y, 1.0), y, y);
 }
 
 // the least weight that min-p leaves
 __device__ __forceinline__ u64 least_weight(const Setting &set, const Weigh &weigh)
 {
-    const double low = set.low > 1.f ? 1.0 : set.low > 0.f ? (double)set.low : 0.0;
+    if (!(set.low > 0.f)) return 1ull;
+    const double low = set.low > 1.f ? 1.0 : (double)set.low;
     const u64 least = (u64)ceil(low * (double)weigh.unit());
     return least ? least : 1ull;
-}
-
-// the weight of a key that is above the cut, or one of the ties left; what min-p drops has none
-__device__ __forceinline__ u64 weight_left(uint32_t key, const Weigh &weigh, u64 least)
-{
-    const u64 w = weigh(key);
-    return w >= least ? w : 0ull;
-}
-
-// The weights that are left of 4 columns a lane, 256 columns of a wavefront in order; *equal: ties of the cut before them, counted on
-__device__ __forceinline__ void left4(const uint32_t key[4], const Cut &cut, const Weigh &weigh, u64 least, u64 *equal, u64 w[4])
-{
-    if (cut.every) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = key[k] >= cut.key ? weight_left(key[k], weigh, least) : 0ull;
-        return;
-    }
-    u64 mine = 0ull;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) mine += key[k] == cut.key ? 1ull : 0ull;
-    const u64 upto = wave_scan(mine);
-    u64 rank = *equal + upto - mine;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const bool tie = key[k] == cut.key;
-        w[k] = key[k] > cut.key || (tie && rank < cut.ties) ? weight_left(key[k], weigh, least) : 0ull;
-        rank += tie ? 1ull : 0ull;
-    }
-    *equal += lane_of(upto, 63);
 }
 
 __device__ __forceinline__ u64 ties_of(const uint32_t key[4], const Cut &cut)
@@ -448,8 +548,34 @@ __device__ __forceinline__ u64 ties_of(const uint32_t key[4], const Cut &cut)
     return n;
 }
 
+// The weights w that are left of 4 columns a lane, 256 columns of a wavefront in order: of keys above the cut and of the ties that are, and no fewer
+// units than `least`; *equal: ties of the cut before them, counted on
+__device__ __forceinline__ void left4(const uint32_t key[4], const Cut &cut, u64 least, u64 *equal, double w[4])
+{
+    if (least == 1ull && cut.key == 0u) return;
+    if (least > 1ull) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = w[k] >= (double)least ? w[k] : 0.0;
+    }
+    if (cut.every) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = key[k] >= cut.key ? w[k] : 0.0;
+        return;
+    }
+    const u64 mine = ties_of(key, cut), upto = wave_scan(mine);
+    u64 rank = *equal + upto - mine;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const bool tie = key[k] == cut.key;
+        w[k] = key[k] > cut.key || (tie && rank < cut.ties) ? w[k] : 0.0;
+        rank += tie ? 1ull : 0ull;
+    }
+    *equal += lane_of(upto, 63);
+}
+
 // The first of n sums, ascending, above the goal
-__device__ __forceinline__ int first_above(const u64 *sums, int n, u64 goal)
+template <class N>
+__device__ __forceinline__ int first_above(const N *sums, int n, N goal)
 {
     int lo = 0, hi = n - 1;
 #pragma unroll 1
@@ -461,9 +587,89 @@ __device__ __forceinline__ int first_above(const u64 *sums, int n, u64 goal)
     return lo;
 }
 
+// Of 256 columns, 4 a lane from column c on, the one at which the weights left pass the goal, if one does; `before`: the weights before them.
+// The weights left of them all
+template <class Source>
+__device__ __forceinline__ u64 pick4(const Call &o, int64_t at, const Source &src, int32_t c, const uint32_t key[4], const Cut &cut, const Weigh &weigh, u64 least,
+                                     u64 *equal, u64 goal, u64 before, u64 total)
+{
+    double w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = weigh.units(key[k]);
+    left4(key, cut, least, equal, w);
+    const double here = w[0] + w[1] + w[2] + w[3], upto = wave_scan(here);
+    u64 from = before + whole(upto - here);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const u64 x = whole(w[k]);
+        if (goal >= from && goal < from + x) answer(o, at, src.column(c + k), w[k], inverse_of((double)total));
+        from += x;
+    }
+    return whole(lane_of(upto, 63));
+}
+
 constexpr int RUN = 256;           // columns that a wavefront weighs at once
 constexpr int RUNS_MOST = 1024;    // of a row that a block takes
 constexpr int64_t ROW_MOST = RUN * RUNS_MOST;
+
+// A row of which up to FEW scores, top-k's among them, are at or above the cut: one wavefront has them, one a lane, and counts for each those before
+// it, by score and by column
+constexpr int FEW = 64;
+template <int NT, class K>
+__device__ __forceinline__ void draw_few(const Call &o, int64_t first, K &keys, const Setting &set, const Weigh &weigh, const Cut &cut, uint32_t *list, u64 *s_found)
+{
+    uint32_t *count = (uint32_t *)s_found;                       // list: keys, then columns, then sums
+    if (threadIdx.x == 0) *count = 0u;
+    __syncthreads();
+    keys.each(0, [&](int32_t c0) {
+#pragma unroll
+        for (int i = 0; i < K::V; ++i) {
+            if (keys.key[i] < cut.key) continue;
+            const uint32_t at = atomicAdd(count, 1u);
+            list[at] = keys.key[i];
+            list[FEW + at] = c0 + 4 * (NT * (i / 4) + threadIdx.x) + i % 4;
+        }
+    });
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        typedef Team<64> W;
+        u64 *sum = (u64 *)(list + 2 * FEW);
+        const int n = __builtin_amdgcn_readfirstlane((int)*count), lane = threadIdx.x;
+        const uint32_t key = lane < n ? list[lane] : 0u, at = lane < n ? list[FEW + lane] : ~0u;
+        const u64 order = (u64)key << 32 | (uint32_t)~at;
+        int by_score = 0, by_column = 0;
+        for (int j = 0; j < n; ++j) {
+            by_score += lane_of(order, j) > order;
+            by_column += (uint32_t)__builtin_amdgcn_readlane((int)at, j) < at;
+        }
+        if (lane >= n) by_score = by_column = lane;
+        u64 w = lane < n && by_score < set.k ? weigh(key) : 0ull;
+        if (set.p < 1.f) {
+            sum[by_score] = w;
+            W::sync();
+            const u64 mine = sum[lane], upto = wave_scan(mine);
+            W::sync();
+            sum[lane] = upto - mine;
+            W::sync();
+            if (sum[by_score] >= goal_of_weight(lane_of(upto, 63), set)) w = 0ull;
+            W::sync();
+        }
+        if (w < least_weight(set, weigh)) w = 0ull;
+        sum[by_column] = w;
+        W::sync();
+        const u64 mine = sum[lane], upto = wave_scan(mine), total = lane_of(upto, 63);
+        W::sync();
+        sum[lane] = upto - mine;
+        W::sync();
+        const u64 before = sum[by_column];
+        const double inverse = inverse_of((double)total);
+        for (int32_t i = 0; i < o.n_draws; ++i) {
+            const u64 goal = goal_of_draw(o, first + i, total);
+            if (goal >= before && goal < before + w) answer(o, first + i, keys.src.column((int32_t)at), (double)w, inverse);
+        }
+    }
+    __syncthreads();
+}
 
 // One row.  Up to 4096 columns the sums by column are in LDS, and a thread finds a draw by halving; beyond, the sums by runs of 256
 // columns are (sums[run]: of runs 0 .. run; ties[run], where not all ties are left: their number before the run), and a wavefront
@@ -477,53 +683,70 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
     const int tid = T::tid(), wave = NT == 64 ? 0 : (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const Setting set = setting_of(o.how, r);
     K keys(src);
-    uint32_t most = 0u;
-    keys.each([&](int32_t) {
+    uint32_t mine = 0u;
+    keys.each(0, [&](int32_t) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) most = max(most, keys.key[i]);
+        for (int i = 0; i < V; ++i) mine = max(mine, keys.key[i]);
     });
-    most = T::most(most, s);
+    const uint32_t most = T::most(mine, s);
     const int64_t first = r * o.n_draws;
     if (most == 0u) {                                            // a row without weights
-        for (int32_t i = tid; i < o.n_draws; i += NT) answer(o, first + i, -1, 0ull, 1ull);
+        for (int32_t i = tid; i < o.n_draws; i += NT) answer(o, first + i, -1, 0.0, 1.0);
         return;
     }
     Weigh weigh;
-    weigh.init(most, set.t, o.bits, pow);
-    const Cut cut = find_cut<NT, BITS>(keys, set, weigh, true, hist, s, s_found);
+    weigh.init(most, set.t, o, pow);
+    Cut cut = first_cut(set, most);
+    if (cuts(0, set, src.n)) {
+        const bool few = find_cut<NT, BITS>(0, NT > 64 && set.k <= FEW && o.n_draws <= FEW ? FEW : 0u, keys, set, weigh, low_of<NT>(mine, set.k, s), most, cut, hist,
+                                            s, s_found);
+        if constexpr (NT > 64) {
+            if (few) {
+                draw_few<NT>(o, first, keys, set, weigh, cut, (uint32_t *)sums, s_found);
+                return;
+            }
+        }
+    }
+    keys.weigh_all(weigh, cut);
+    find_cut<NT, BITS>(1, 0u, keys, set, weigh, max(cut.key, weigh.lowest(set.t)), most, cut, hist, s, s_found);
     const u64 least = least_weight(set, weigh);
-    u64 total = 0ull;
-    if constexpr (ONE && K::BATCH <= 4096) {
+    if constexpr (ONE && K::BATCH <= 4096) {                     // 4096 weights of 2^40 units: a double holds their sums
+        double *to = (double *)sums, total = 0.0;
         u64 equal = 0ull;                                        // ties in the tiles before and, in a block, in the wavefronts before
 #pragma unroll
         for (int i = 0; i < TILES; ++i) {
-            u64 w[4], before = equal;
+            u64 before = equal;
             if (NT > 64 && !cut.every) {                         // ties of the wavefronts before, in this tile
                 u64 here;
                 const u64 mine = ties_of(keys.key + 4 * i, cut), upto = T::scan(mine, s, &here);
                 before += lane_of(upto - mine, 0);
                 equal += here;
             }
-            left4(keys.key + 4 * i, cut, weigh, least, &before, w);
+            double w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = keys.weight(4 * i + k, weigh);
+            left4(keys.key + 4 * i, cut, least, &before, w);
             if (NT == 64) equal = before;
             w[1] += w[0]; w[2] += w[1]; w[3] += w[2];
-            u64 all;
-            const u64 base = total + T::scan(w[3], s, &all) - w[3];
+            double all;
+            const double base = total + (T::scan(w[3], s, &all) - w[3]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sums[4 * (NT * i + tid) + k] = base + w[k];
+            for (int k = 0; k < 4; ++k) to[4 * (NT * i + tid) + k] = base + w[k];
             total += all;
         }
         T::sync();
+        const double inverse = inverse_of(total);
         for (int32_t i = tid; i < o.n_draws; i += NT) {
-            const int at = first_above(sums, K::BATCH, goal_of_draw(o, first + i, total));
-            answer(o, first + i, src.column(at), sums[at] - (at ? sums[at - 1] : 0ull), total);
+            const int at = first_above(to, K::BATCH, goal_of_draw(o, first + i, total));
+            answer(o, first + i, src.column(at), to[at] - (at ? to[at - 1] : 0.0), inverse);
         }
         T::sync();
     } else {
         static_assert(RUNS_MOST <= NT, "a thread has a run");
+        u64 total;
         const int runs = (src.n + RUN - 1) / RUN;
         if (!cut.every) {
-            keys.each([&](int32_t c0) {
+            keys.each(0, [&](int32_t c0) {
 #pragma unroll
                 for (int i = 0; i < TILES; ++i) {
                     const u64 mine = wave_sum(ties_of(keys.key + 4 * i, cut));
@@ -538,13 +761,16 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
             if (tid < runs) ties[tid] = upto - mine;
             T::sync();
         }
-        keys.each([&](int32_t c0) {
+        keys.each(0, [&](int32_t c0) {
 #pragma unroll
             for (int i = 0; i < TILES; ++i) {
                 const int run = c0 / RUN + i * WAVES + wave;
-                u64 w[4], equal = cut.every || run >= runs ? 0ull : ties[run];
-                left4(keys.key + 4 * i, cut, weigh, least, &equal, w);
-                const u64 sum = wave_sum(w[0] + w[1] + w[2] + w[3]);
+                u64 equal = cut.every || run >= runs ? 0ull : ties[run];
+                double w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = keys.weight(4 * i + k, weigh);
+                left4(keys.key + 4 * i, cut, least, &equal, w);
+                const u64 sum = whole(lane_of(wave_scan(w[0] + w[1] + w[2] + w[3]), 63));
                 if (lane == 0 && run < runs) sums[run] = sum;
             }
         });
@@ -558,16 +784,9 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
             const int run = first_above(sums, runs, goal);
             const int32_t c = RUN * run + 4 * lane;
             uint32_t again[4];
-            src.get4(c, again);
-            u64 w[4], equal = cut.every ? 0ull : ties[run];
-            left4(again, cut, weigh, least, &equal, w);
-            const u64 here = w[0] + w[1] + w[2] + w[3];
-            u64 before = (run ? sums[run - 1] : 0ull) + wave_scan(here) - here;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (goal >= before && goal < before + w[k]) answer(o, first + i, src.column(c + k), w[k], total);
-                before += w[k];
-            }
+            get4(src, c, again);
+            u64 equal = cut.every ? 0ull : ties[run];
+            pick4(o, first + i, src, c, again, cut, weigh, least, &equal, goal, run ? sums[run - 1] : 0ull, total);
         }
         T::sync();
     }
@@ -577,12 +796,12 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
 template <bool BF16, int NT, int TILES, bool ONE, bool PARTS>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void k_rows(Call o)
 {
-    constexpr int BITS = NT == 64 ? 8 : 11, TEAMS = NT == 64 ? 4 : 1, COLUMNS = 4 * TILES * NT;
+    constexpr int BITS = NT == 64 ? 8 : NT == 256 ? 11 : 12, TEAMS = NT == 64 ? 4 : 1, COLUMNS = 4 * TILES * NT;
     constexpr bool BY_COLUMN = ONE && COLUMNS <= 4096;
     __shared__ u64 s_hist[TEAMS][1 << BITS], s_sums[TEAMS][BY_COLUMN ? COLUMNS : RUNS_MOST], s_ties[BY_COLUMN ? 1 : RUNS_MOST];
     __shared__ u64 s_part[TEAMS][16], s_found[TEAMS][4];
-    __shared__ double s_pow[64];
-    fill_pow(s_pow);
+    __shared__ double s_pow[POWERS];
+    fill_pow(s_pow, o.bits);
     const int team = NT == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     for (int64_t r = (int64_t)blockIdx.x * TEAMS + team; r < o.n_rows; r += (int64_t)gridDim.x * TEAMS) {
         if constexpr (PARTS) {
@@ -598,10 +817,11 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void k_rows(Call o)
 // ---- long rows, few scores left: the first k of a row are among the first k of its parts
 
 template <bool BF16, int NT, int TILES>
-__global__ __launch_bounds__(NT) void k_part_top(Call o, int64_t row0, int32_t parts, int32_t most_k, uint32_t *__restrict__ part_key, int32_t *__restrict__ part_col)
+__global__ __launch_bounds__(NT) void k_part_top(Call o, int64_t row0, int32_t parts, int32_t most_k, int32_t slots, uint32_t *__restrict__ part_key, int32_t *__restrict__ part_col)
 {
     typedef Team<NT> T;
-    __shared__ u64 s_hist[2048], s_part[16], s_found[4];
+    constexpr int BITS = NT == 1024 ? 12 : 11;
+    __shared__ u64 s_hist[1 << BITS], s_part[16], s_found[4];
     const int64_t r = row0 + blockIdx.x / (unsigned)parts;
     const int32_t part = (int32_t)(blockIdx.x % (unsigned)parts);
     constexpr int COLUMNS = 4 * TILES * NT;
@@ -611,10 +831,22 @@ __global__ __launch_bounds__(NT) void k_part_top(Call o, int64_t row0, int32_t p
     set.k = set.k > 0 ? min(set.k, most_k) : most_k;
     const int tid = T::tid();
     Keys<NT, TILES, true, Scores<BF16>> keys(src);
-    const Weigh none{};
-    const Cut cut = find_cut<NT, 11>(keys, set, none, false, s_hist, s_part, s_found);
-    uint32_t *out_key = part_key + (r * parts + part) * most_k;
-    int32_t *out_col = part_col + (r * parts + part) * most_k;
+    Cut cut{0u, true, 0ull};
+    if (set.k == 1) {
+        uint32_t most = 0u;
+#pragma unroll
+        for (int i = 0; i < 4 * TILES; ++i) most = max(most, keys.key[i]);
+        cut = first_cut(set, T::most(most, s_part));
+    } else {
+        const Weigh none{};
+        uint32_t mine = 0u;
+#pragma unroll
+        for (int i = 0; i < 4 * TILES; ++i) mine = max(mine, keys.key[i]);
+        const uint32_t most = T::most(mine, s_part);
+        if (most) find_cut<NT, BITS>(0, (uint32_t)slots, keys, set, none, low_of<NT>(mine, set.k, s_part), most, cut, s_hist, s_part, s_found);
+    }
+    uint32_t *out_key = part_key + (r * parts + part) * slots;
+    int32_t *out_col = part_col + (r * parts + part) * slots;
     u64 base = 0ull;                                             // scores written, and in the upper half ties met
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
@@ -642,13 +874,13 @@ __global__ __launch_bounds__(NT) void k_part_top(Call o, int64_t row0, int32_t p
         }
     }
     const int32_t written = (int32_t)((uint32_t)base + (uint32_t)min(base >> 32, cut.ties));
-    for (int32_t i = written + tid; i < most_k; i += NT) out_key[i] = 0u;
+    for (int32_t i = written + tid; i < slots; i += NT) out_key[i] = 0u;
 }
 
 // ---- long rows: a launch a digit
 
 struct State {                     // of a row, after a launch
-    Search x;
+    Search<11> x;
     Cut cut;
     uint32_t most;
 };
@@ -656,14 +888,15 @@ struct State {                     // of a row, after a launch
 struct Long {
     Call o;
     int64_t row0;                  // first row of this batch
-    int32_t parts, part;           // blocks to a row, and columns to a block (a multiple of 256)
+    int32_t parts, part;           // blocks to a row, and columns to a block (a multiple of LONG_RUN)
     uint32_t *most;                // [rows][parts]
     u64 *hist;                     // [rows][6][2048]
     State *state;                  // [rows][7]
     u64 *part_sum, *part_ties;     // [rows][parts]: weights above the cut, ties of it
-    u64 *run_sum, *run_ties;       // [rows][parts][part / 256]
+    u64 *run_sum, *run_ties;       // [rows][parts][part / LONG_RUN]
 };
 constexpr int LONG_T = 256, LONG_DIGITS = 2048;
+constexpr int LONG_RUN = 1024;      // columns whose weights are summed
 
 template <bool BF16>
 __global__ __launch_bounds__(LONG_T) void k_long_most(Long a)
@@ -673,19 +906,20 @@ __global__ __launch_bounds__(LONG_T) void k_long_most(Long a)
     const int32_t part = (int32_t)(blockIdx.x % (unsigned)a.parts), c0 = part * a.part;
     const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), min(a.o.n_cols, c0 + a.part)};
     uint32_t most = 0u;
-    for (int32_t c = c0 + 4 * (int)threadIdx.x; c < src.n; c += 4 * LONG_T) {
-        uint32_t key[4];
-        src.get4(c, key);
+    Keys<LONG_T, 4, false, Scores<BF16>> keys(src);
+    keys.each(c0, [&](int32_t) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) most = max(most, key[k]);
-    }
+        for (int k = 0; k < 16; ++k) most = max(most, keys.key[k]);
+    });
     most = Team<LONG_T>::most(most, s_part);
     if (threadIdx.x == 0) a.most[r * a.parts + part] = most;
     for (int32_t i = part * LONG_T + threadIdx.x; i < 6 * LONG_DIGITS; i += a.parts * LONG_T) a.hist[r * 6 * LONG_DIGITS + i] = 0ull;
 }
 
-// The row's state after stage `prev` (3 which + level), from the sums by digit that its launch left; prev < 0: before the first
-__device__ __forceinline__ State advance(const Long &a, int64_t r, int before, int prev, const Setting &set, Weigh *weigh, const double *pow, u64 *s, u64 *s_found)
+// The row's state after stage `prev` (3 which + level), from the sums by digit that its launch left; prev < 0: before the first.
+// `before`: the stage before that; `next`: which search the launch begins, or -1
+__device__ __forceinline__ State advance(const Long &a, int64_t r, int before, int prev, int next, const Setting &set, Weigh *weigh, const double *pow, u64 *s,
+                                         u64 *s_found)
 {
     typedef Team<LONG_T> T;
     State st;
@@ -693,59 +927,104 @@ __device__ __forceinline__ State advance(const Long &a, int64_t r, int before, i
         uint32_t most = 0u;
         for (int32_t i = threadIdx.x; i < a.parts; i += LONG_T) most = max(most, a.most[r * a.parts + i]);
         st.most = T::most(most, s);
-        st.x = Search{0ull, 0ull, 0u};
-        st.cut = Cut{0u, true, 0ull};
+        st.cut = first_cut(set, st.most);
+        st.x.open = false;
     } else st = a.state[r * 7 + 1 + before];
-    weigh->init(st.most, set.t, a.o.bits, pow);
-    if (prev < 0) return st;
-    const int which = prev / 3, level = prev % 3;
-    if (cuts(which, set, a.o.n_cols) && st.most && (level == 0 || st.x.goal)) {
+    weigh->init(st.most, set.t, a.o, pow);
+    if (prev >= 0 && st.x.open) {
+        const int which = prev / 3, level = prev % 3;
         u64 v[LONG_DIGITS / LONG_T], upto, more, own;
         const u64 all = digit_total<LONG_T, 11>(a.hist + (r * 6 + prev) * LONG_DIGITS, v, &upto, s);
         if (level == 0) st.x.goal = which == 0 ? goal_of_count(all, set) : goal_of_weight(all, set);
         if (st.x.goal) {
             const int digit = digit_at<LONG_T, 11>(v, upto, st.x.goal - st.x.above, s_found, &more, &own);
-            st.x.above += more;
-            st.x.found |= (uint32_t)digit << (level == 0 ? 21 : level == 1 ? 10 : 0);
-            if (level == 2) st.cut = cut_at(which, st.x, own, st.cut, *weigh);
-        }
+            st.x.step(digit, more);
+            if (!st.x.open) st.cut = cut_at(which, st.x, own, st.cut, *weigh);
+        } else st.x.open = false;
     }
-    if (level == 2) st.x = Search{0ull, 0ull, 0u};
+    if (next >= 0) {
+        if (st.most && cuts(next, set, a.o.n_cols)) st.x.begin(next == 0 ? LEAST_KEY : max(st.cut.key, weigh->lowest(set.t)), st.most);
+        else st.x.open = false;
+    }
     return st;
 }
 
-// sums by digit of stage `stage`; prev: the stage of the launch before, `before` the one before that
-template <bool BF16, int LEVEL>
-__global__ __launch_bounds__(LONG_T) void k_long_digit(Long a, int which, int before, int prev)
+// sums by digit of a search's level; prev: the stage of the launch before, `before` the one before that
+template <bool BF16>
+__global__ __launch_bounds__(LONG_T) void k_long_digit(Long a, int which, int level, int before, int prev)
 {
-    typedef Digit<11, LEVEL> D;
     __shared__ u64 s_hist[LONG_DIGITS], s_part[16], s_found[4];
-    __shared__ double s_pow[64];
-    fill_pow(s_pow);
+    __shared__ uint32_t s_queue[LONG_T / 64][9 * 64];
+    __shared__ double s_pow[POWERS];
+    fill_pow(s_pow, a.o.bits);
     const int64_t r = blockIdx.x / (unsigned)a.parts;
     const int32_t part = (int32_t)(blockIdx.x % (unsigned)a.parts), c0 = part * a.part;
     const Setting set = setting_of(a.o.how, a.row0 + r);
     Weigh weigh;
-    const State st = advance(a, r, before, prev, set, &weigh, s_pow, s_part, s_found);
+    const State st = advance(a, r, before, prev, level == 0 ? which : -1, set, &weigh, s_pow, s_part, s_found);
     if (part == 0 && threadIdx.x == 0) a.state[r * 7 + 1 + prev] = st;
-    if (!cuts(which, set, a.o.n_cols) || st.most == 0u || (LEVEL > 0 && st.x.goal == 0ull)) return;
+    if (!st.x.open) return;
     for (int i = threadIdx.x; i < LONG_DIGITS; i += LONG_T) s_hist[i] = 0ull;
     __syncthreads();
     const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), min(a.o.n_cols, c0 + a.part)};
-    for (int32_t c = c0 + 4 * (int)threadIdx.x; c < src.n; c += 4 * LONG_T) {
-        uint32_t key[4];
-        src.get4(c, key);
+    // what has the digits found before lies between two scores; of it top-p counts what is above top-k's cut
+    const uint32_t low = st.x.first(), high = (uint32_t)min(st.x.last(), (u64)st.most);
+    const float from = score_of(which == 1 && st.cut.key >= low ? st.cut.key + 1u : low), upto = score_of(high);
+    uint32_t *queue = s_queue[threadIdx.x >> 6];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int waiting = 0;
+    auto add = [&](float l, u64 w) { atomicAdd(&s_hist[st.x.digit(key_in_order(l))], w); };
+    auto weigh_some = [&](int first, int n) {
+        Team<64>::sync();
+        if (lane < n) {
+            const float l = __uint_as_float(queue[first + lane]);
+            add(l, weigh(key_of(l)));
+        }
+        Team<64>::sync();
+    };
+    for (int32_t c0w = c0 + LONG_RUN * wave; c0w < src.n; c0w += LONG_RUN * (LONG_T / 64)) {
+        const int32_t c = c0w + 4 * lane;
+        float l[16];
+        if (c0w + LONG_RUN <= src.n) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (key[k] == 0u || !D::in(key[k], st.x.found) || (which == 1 && key[k] <= st.cut.key)) continue;
-            const u64 w = which == 0 ? 1ull : weigh(key[k]);
-            if (w) atomicAdd(&s_hist[D::of(key[k])], w);
+            for (int j = 0; j < 4; ++j) src.score4(c + RUN * j, l + 4 * j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int32_t at = c + RUN * (j / 4) + j % 4;
+                l[j] = at < src.n ? src.one(at) : -INFINITY;
+            }
+        }
+        if (which == 0) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (l[k] >= from && l[k] <= upto) add(l[k], 1ull);
+        } else if (level == 0 && !weigh.endless) {               // all that have a weight, most scores
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (l[k] >= from) add(l[k], (u64)__double_as_longlong(weigh.raised(l[k])) & 0xfffffffffffffull);
+        } else {                                                 // few: they are gathered, so that whole wavefronts weigh
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const bool hit = l[k] >= from && l[k] <= upto;
+                const u64 all = __ballot(hit);
+                if (hit) queue[waiting + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0u))] = __float_as_uint(l[k]);
+                waiting += (int)__popcll(all);
+                if (k % 8 == 7) {
+#pragma unroll 1
+                    while (waiting >= 64) {
+                        waiting -= 64;
+                        weigh_some(waiting, 64);
+                    }
+                }
+            }
         }
     }
-    if (which == 1 && part == 0 && threadIdx.x == 0 && st.cut.key && D::in(st.cut.key, st.x.found))
-        atomicAdd(&s_hist[D::of(st.cut.key)], st.cut.ties * weigh(st.cut.key));
+    weigh_some(0, waiting);
+    if (which == 1 && part == 0 && threadIdx.x == 0 && st.cut.key && st.x.in(st.cut.key))
+        atomicAdd(&s_hist[st.x.digit(st.cut.key)], st.cut.ties * weigh(st.cut.key));
     __syncthreads();
-    u64 *hist = a.hist + (r * 6 + which * 3 + LEVEL) * LONG_DIGITS;
+    u64 *hist = a.hist + (r * 6 + which * 3 + level) * LONG_DIGITS;
     for (int i = threadIdx.x; i < LONG_DIGITS; i += LONG_T)
         if (s_hist[i]) atomicAdd(&hist[i], s_hist[i]);
 }
@@ -755,30 +1034,58 @@ template <bool BF16>
 __global__ __launch_bounds__(LONG_T) void k_long_sums(Long a, int before, int prev)
 {
     __shared__ u64 s_part[16], s_found[4];
-    __shared__ double s_pow[64];
-    fill_pow(s_pow);
+    __shared__ double s_pow[POWERS];
+    fill_pow(s_pow, a.o.bits);
     const int64_t r = blockIdx.x / (unsigned)a.parts;
     const int32_t part = (int32_t)(blockIdx.x % (unsigned)a.parts), c0 = part * a.part;
     const Setting set = setting_of(a.o.how, a.row0 + r);
     Weigh weigh;
-    const State st = advance(a, r, before, prev, set, &weigh, s_pow, s_part, s_found);
+    const State st = advance(a, r, before, prev, -1, set, &weigh, s_pow, s_part, s_found);
     if (part == 0 && threadIdx.x == 0) a.state[r * 7 + 6] = st;      // slot 6: the last stage's own, or of stages that none of this call's are
     const u64 least = least_weight(set, weigh);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), min(a.o.n_cols, c0 + a.part)};
-    const int32_t runs = a.part / 256;
+    const int32_t runs = a.part / LONG_RUN;
     u64 sum = 0ull, ties = 0ull;
-    for (int32_t i = wave; i < runs; i += LONG_T / 64) {
-        uint32_t key[4];
-        src.get4(c0 + 256 * i + 4 * lane, key);
-        u64 w = 0ull, t = 0ull;
+    // What counts as a range of scores: above the cut, and what is equal to it if all that is does.  1024 weights of 2^40 units are a whole
+    // number that a double holds
+    const float tie = score_of(st.cut.key), edge = st.cut.key == 0u ? -INFINITY : st.cut.every ? tie : score_of(st.cut.key + 1u);
+    const double fewest = (double)least;
+    const bool all = least <= 1ull;
+    for (int32_t i = wave; i < runs && c0 + LONG_RUN * i < src.n; i += LONG_T / 64) {
+        const int32_t c = c0 + LONG_RUN * i + 4 * lane;
+        float l[16];
+        if (c0 + LONG_RUN * (i + 1) <= src.n) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (st.most && key[k] && (key[k] > st.cut.key || (key[k] == st.cut.key && st.cut.every))) w += weight_left(key[k], weigh, least);
-            t += key[k] == st.cut.key && !st.cut.every ? 1ull : 0ull;
+            for (int j = 0; j < 4; ++j) src.score4(c + RUN * j, l + 4 * j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int32_t at = c + RUN * (j / 4) + j % 4;
+                l[j] = at < src.n ? src.one(at) : -INFINITY;
+            }
         }
-        w = wave_sum(w);
-        if (!st.cut.every) t = wave_sum(t);
+        u64 w = 0ull, t = 0ull;
+        double lanes = 0.0;
+        if (weigh.endless) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) lanes += l[k] == INFINITY && l[k] >= edge ? (double)weigh.unit() : 0.0;
+        } else if (all) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) lanes += weigh.raised(l[k] >= edge ? l[k] : -INFINITY) - 0x1p52;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const double v = weigh.raised(l[k] >= edge ? l[k] : -INFINITY) - 0x1p52;
+                lanes += v >= fewest ? v : 0.0;
+            }
+        }
+        w = st.most ? whole(lane_of(wave_scan(lanes), 63)) : 0ull;
+        if (!st.cut.every) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) t += l[k] == tie ? 1ull : 0ull;
+            t = wave_sum(t);
+        }
         if (lane == 0) {
             const int64_t at = (r * a.parts + part) * runs + i;
             a.run_sum[at] = w;
@@ -835,8 +1142,8 @@ __device__ __forceinline__ Found find_item(const u64 *sum, const u64 *tie, int32
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_long_draw(Long a, int64_t first, int64_t n)
 {
-    __shared__ double s_pow[64];
-    fill_pow(s_pow);
+    __shared__ double s_pow[POWERS];
+    fill_pow(s_pow, a.o.bits);
     const int lane = threadIdx.x & 63;
     const int64_t wave = first + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (wave >= n) return;
@@ -844,31 +1151,30 @@ __global__ __launch_bounds__(256) void k_long_draw(Long a, int64_t first, int64_
     const State st = a.state[r * 7 + 6];
     const Setting set = setting_of(a.o.how, a.row0 + r);
     Weigh weigh;
-    weigh.init(st.most, set.t, a.o.bits, s_pow);
+    weigh.init(st.most, set.t, a.o, s_pow);
     const u64 least = least_weight(set, weigh);
-    const u64 w_tie = st.most && !st.cut.every ? weight_left(st.cut.key, weigh, least) : 0ull;
+    u64 w_tie = st.most && !st.cut.every ? weigh(st.cut.key) : 0ull;
+    if (w_tie < least) w_tie = 0ull;
     const u64 *sum = a.part_sum + r * a.parts, *tie = a.part_ties + r * a.parts;
     const u64 total = find_item(sum, tie, a.parts, 0ull, 0ull, st.cut.ties, w_tie, false, 0ull).total;
     if (total == 0ull) {
-        if (lane == 0) answer(a.o, at, -1, 0ull, 1ull);
+        if (lane == 0) answer(a.o, at, -1, 0.0, 1.0);
         return;
     }
     const u64 goal = goal_of_draw(a.o, at, total);
     const Found p = find_item(sum, tie, a.parts, 0ull, 0ull, st.cut.ties, w_tie, true, goal);
-    const int32_t runs = a.part / 256;
+    const int32_t runs = a.part / LONG_RUN;
     const int64_t run0 = (r * a.parts + p.item) * runs;
-    const Found f = find_item(a.run_sum + run0, a.run_ties + run0, runs, p.before, p.ties, st.cut.ties, w_tie, true, goal);
-    const int32_t c = p.item * a.part + 256 * f.item + 4 * lane;
+    const int32_t last = (a.o.n_cols - p.item * a.part + LONG_RUN - 1) / LONG_RUN;      // the row may end in this part
+    const Found f = find_item(a.run_sum + run0, a.run_ties + run0, min(runs, last), p.before, p.ties, st.cut.ties, w_tie, true, goal);
     const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), a.o.n_cols};
-    uint32_t key[4];
-    src.get4(c, key);
-    u64 w[4], equal = f.ties;
-    left4(key, st.cut, weigh, least, &equal, w);
-    u64 before = f.before + wave_scan(w[0] + w[1] + w[2] + w[3]) - (w[0] + w[1] + w[2] + w[3]);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (goal >= before && goal < before + w[k]) answer(a.o, at, c + k, w[k], total);
-        before += w[k];
+    u64 equal = f.ties, upto = f.before;
+#pragma unroll 1
+    for (int i = 0; i < LONG_RUN / RUN && upto <= goal; ++i) {
+        const int32_t c = p.item * a.part + LONG_RUN * f.item + RUN * i + 4 * lane;
+        uint32_t key[4];
+        get4(src, c, key);
+        upto += pick4(a.o, at, src, c, key, st.cut, weigh, least, &equal, goal, upto, total);
     }
 }
 
@@ -888,7 +1194,7 @@ constexpr int64_t BLOCK_ROW = 65536, MANY_ROWS = 256;
 
 // How a call runs, by its sizes and what the host knows of its settings
 struct Plan {
-    int32_t most_k;                // 0: rows, or digits in launches; else k_part_top's
+    int32_t most_k, slots;         // 0: rows, or digits in launches; else k_part_top's
     int32_t parts, part, rows;     // parts of a row, columns of a part, rows a batch
     size_t off_most, off_hist, off_state, off_sum, off_ties, off_run, off_run_ties, bytes;
 };
@@ -901,13 +1207,15 @@ Plan plan_of(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
     const bool greedy = !how->row_temperature && how->temperature == 0.f;
     int64_t k = greedy ? 1 : how->top_k;
     if (k > 0) {
-        // parts of 4096 columns where their scores left are a row of 16384 at most, else of 16384
+        // parts of 4096 columns where their scores left are a row of 16384 at most, else of 16384.  A few more places than k spare most parts
+        // all digits but the first
+        const int64_t slots = k == 1 ? 1 : (k + k / 8 + 15) / 8 * 8;
         for (int64_t part = 4096; part <= 16384; part *= 4) {
             const int64_t parts = cdiv(n_cols, part);
-            if (k <= part && parts * k <= (part == 4096 ? 16384 : BLOCK_ROW)) {
-                p.most_k = (int32_t)k; p.parts = (int32_t)parts; p.part = (int32_t)part;
+            if (k <= part && parts * slots <= (part == 4096 ? 16384 : BLOCK_ROW)) {
+                p.most_k = (int32_t)k; p.slots = (int32_t)slots; p.parts = (int32_t)parts; p.part = (int32_t)part;
                 p.rows = (int32_t)(n_rows < LONG_BLOCKS / parts ? n_rows : LONG_BLOCKS / parts);
-                p.bytes = align_up((size_t)n_rows * parts * k * 4, 256) * 2;
+                p.bytes = align_up((size_t)n_rows * parts * slots * 4, 256) * 2;
                 return p;
             }
         }
@@ -919,7 +1227,7 @@ Plan plan_of(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
     p.rows = (int32_t)(n_rows < 4096 ? n_rows : 4096);
     if (p.rows > LONG_BLOCKS / p.parts) p.rows = (int32_t)(LONG_BLOCKS / p.parts);
     if (p.rows < 1) p.rows = 1;
-    const size_t rows = (size_t)p.rows, parts = rows * p.parts, runs = parts * (part / 256);
+    const size_t rows = (size_t)p.rows, parts = rows * p.parts, runs = parts * (part / LONG_RUN);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at = align_up(at + bytes, 256); return here; };
     p.off_most = take(parts * 4);
@@ -936,8 +1244,9 @@ Plan plan_of(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
 template <bool BF16, int NT, int TILES, bool ONE, bool PARTS>
 int launch_rows(const Call &o, hipStream_t st)
 {
-    const int64_t blocks = NT == 64 ? cdiv(o.n_rows, 4) : o.n_rows;
-    k_rows<BF16, NT, TILES, ONE, PARTS><<<(unsigned)(blocks < 65536 ? blocks : 65536), NT == 64 ? 256 : NT, 0, st>>>(o);
+    // a table of powers a block: its wavefronts take rows in turn
+    const int64_t blocks = NT == 64 ? cdiv(o.n_rows, 4) : o.n_rows, most = NT == 64 ? 2048 : 65536;
+    k_rows<BF16, NT, TILES, ONE, PARTS><<<(unsigned)(blocks < most ? blocks : most), NT == 64 ? 256 : NT, 0, st>>>(o);
     KGE_LAUNCH_CHECK();
     return KGE_OK;
 }
@@ -955,11 +1264,11 @@ int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
         int32_t *part_col = (int32_t *)(ws + p.bytes / 2);
         for (int64_t row0 = 0; row0 < o.n_rows; row0 += p.rows) {
             const int64_t rows = o.n_rows - row0 < p.rows ? o.n_rows - row0 : p.rows;
-            if (p.part == 4096) k_part_top<BF16, 256, 4><<<(unsigned)(rows * p.parts), 256, 0, st>>>(o, row0, p.parts, p.most_k, part_key, part_col);
-            else k_part_top<BF16, 1024, 4><<<(unsigned)(rows * p.parts), 1024, 0, st>>>(o, row0, p.parts, p.most_k, part_key, part_col);
+            if (p.part == 4096) k_part_top<BF16, 256, 4><<<(unsigned)(rows * p.parts), 256, 0, st>>>(o, row0, p.parts, p.most_k, p.slots, part_key, part_col);
+            else k_part_top<BF16, 1024, 4><<<(unsigned)(rows * p.parts), 1024, 0, st>>>(o, row0, p.parts, p.most_k, p.slots, part_key, part_col);
             KGE_LAUNCH_CHECK();
         }
-        o.part_key = part_key; o.part_col = part_col; o.n_part = p.parts * p.most_k;
+        o.part_key = part_key; o.part_col = part_col; o.n_part = p.parts * p.slots;
         if (o.n_part <= 1024) return launch_rows<BF16, 64, 4, true, true>(o, st);
         if (o.n_part <= 4096) return launch_rows<BF16, 256, 4, true, true>(o, st);
         if (o.n_part <= 16384) return launch_rows<BF16, 1024, 4, true, true>(o, st);
@@ -970,7 +1279,7 @@ int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
     a.most = (uint32_t *)(ws + p.off_most); a.hist = (u64 *)(ws + p.off_hist); a.state = (State *)(ws + p.off_state);
     a.part_sum = (u64 *)(ws + p.off_sum); a.part_ties = (u64 *)(ws + p.off_ties);
     a.run_sum = (u64 *)(ws + p.off_run); a.run_ties = (u64 *)(ws + p.off_run_ties);
-    const bool by_count = o.how.row_temperature || o.how.row_top_k || o.how.top_k > 0 || o.how.temperature == 0.f;
+    const bool by_count = o.how.row_top_k || o.how.top_k > 1;
     const bool by_weight = o.how.row_top_p || o.how.top_p < 1.f;
     for (a.row0 = 0; a.row0 < o.n_rows; a.row0 += p.rows) {
         const int64_t rows = o.n_rows - a.row0 < p.rows ? o.n_rows - a.row0 : p.rows;
@@ -980,12 +1289,11 @@ int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
         int before = -2, prev = -1;
         for (int which = 0; which < 2; ++which) {
             if (which == 0 ? !by_count : !by_weight) continue;
-            k_long_digit<BF16, 0><<<blocks, LONG_T, 0, st>>>(a, which, before, prev);
-            before = prev; prev = 3 * which;
-            k_long_digit<BF16, 1><<<blocks, LONG_T, 0, st>>>(a, which, before, prev);
-            before = prev; prev = 3 * which + 1;
-            k_long_digit<BF16, 2><<<blocks, LONG_T, 0, st>>>(a, which, before, prev);
-            before = prev; prev = 3 * which + 2;
+            for (int level = 0; level < 3; ++level) {
+                k_long_digit<BF16><<<blocks, LONG_T, 0, st>>>(a, which, level, before, prev);
+                before = prev;
+                prev = 3 * which + level;
+            }
             KGE_LAUNCH_CHECK();
         }
         k_long_sums<BF16><<<blocks, LONG_T, 0, st>>>(a, before, prev);
@@ -1043,7 +1351,7 @@ extern "C" int kge_sample_scores(const kge_sampling *how, int64_t n_rows, int64_
     o.how = Sampling{how->temperature, how->top_p, how->min_p, how->top_k, how->row_temperature, how->row_top_p, how->row_min_p, how->row_top_k};
     o.scores = scores; o.u = u; o.choice = choice; o.prob = prob; o.n_rows = n_rows; o.lds = lds;
     o.n_cols = (int32_t)n_cols; o.n_draws = n_draws; o.bits = bits_of(n_cols); o.u64bit = u_bits == 64;
-    o.part_key = nullptr; o.part_col = nullptr; o.n_part = 0;
+    o.part_key = nullptr; o.part_col = nullptr; o.n_part = 0; o.per = per_of(how->temperature);
     const Plan p = plan_of(how, n_rows, n_cols);
     KGE_PROF("sample_scores", st);
     return dtype == KGE_DT_BF16 ? launch_call<true>(o, p, (char *)workspace, st) : launch_call<false>(o, p, (char *)workspace, st);
