@@ -70,84 +70,105 @@ __device__ __forceinline__ uint32_t code_of(float x, float s)
     return c | (x < 0.f ? 8u : 0u);
 }
 
-// 4 lanes to a group, 8 elements each
+// Where a lane's 4 elements of a group are: group gi of the table as a whole, 8 lanes to a group
+struct Place {
+    int64_t row;
+    int32_t g, c;                  // the group in its row, and the first of the elements
+};
+__device__ __forceinline__ Place place_of(int64_t first, uint32_t local, int32_t groups)
+{
+    Place p;
+    const int64_t row0 = first / groups;                         // of the block: uniform
+    const uint32_t at = (uint32_t)(first - row0 * groups) + local, more = at / (uint32_t)groups;
+    p.row = row0 + more;
+    p.g = (int32_t)(at - more * (uint32_t)groups);
+    p.c = p.g * G + 4 * (int32_t)(threadIdx.x & 7);
+    return p;
+}
+
+constexpr int SETS = 4;            // of 32 groups, that a block of 256 takes at once
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) { return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true)); }
+
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_table4_encode(const void *__restrict__ X, int64_t ldx, int64_t n_rows, int32_t d, int32_t groups,
-                                                       uint32_t *__restrict__ codes, uint16_t *__restrict__ scales)
+                                                       uint16_t *__restrict__ codes, uint16_t *__restrict__ scales)
 {
-    const int64_t first = (int64_t)blockIdx.x * 64;              // this block's first group
-    const int64_t row0 = first / groups;
-    const uint32_t local = (uint32_t)(first - row0 * groups) + (threadIdx.x >> 2);
-    const int64_t row = row0 + local / (uint32_t)groups;
-    const int32_t g = (int32_t)(local % (uint32_t)groups), j = threadIdx.x & 3;
-    const int32_t c = g * G + 8 * j;
-    const int n = row < n_rows ? d - c : 0;
-    float x[8];
-    load4<BF16>(X, row * ldx + c, n, x);
-    load4<BF16>(X, row * ldx + c + 4, n - 4, x + 4);
-    uint32_t most = 0u;
+    const int64_t first = (int64_t)blockIdx.x * (32 * SETS);
+    float x[SETS][4];
+    Place p[SETS];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) most = max(most, __float_as_uint(x[k]) & 0x7fffffffu);
-    most = max(most, (uint32_t)__shfl_xor((int)most, 1, 64));
-    most = max(most, (uint32_t)__shfl_xor((int)most, 2, 64));
-    const uint32_t bits = group_scale(most);
-    const float s = __uint_as_float(bits);
-    uint32_t w = 0u;
-    if (s > 0.f) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w |= code_of(x[k], s) << (4 * k);
+    for (int i = 0; i < SETS; ++i) {
+        p[i] = place_of(first, 32 * i + (threadIdx.x >> 3), groups);
+        load4<BF16>(X, p[i].row * ldx + p[i].c, p[i].row < n_rows ? d - p[i].c : 0, x[i]);
     }
-    if (row < n_rows) {
-        const int64_t at = row * groups + g;
-        codes[at * 4 + j] = w;
-        if (j == 0) scales[at] = (uint16_t)(bits >> 16);
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) {
+        uint32_t most = 0u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) most = max(most, __float_as_uint(x[i][k]) & 0x7fffffffu);
+        most = dpp_max<0xb1>(most);                              // lanes 1 apart, 2 apart, and mirrored in 8
+        most = dpp_max<0x4e>(most);
+        most = dpp_max<0x141>(most);
+        const uint32_t bits = group_scale(most);
+        const float s = __uint_as_float(bits);
+        uint32_t w = 0u;
+        if (s > 0.f) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w |= code_of(x[i][k], s) << (4 * k);
+        }
+        if (p[i].row < n_rows) {
+            const int64_t at = p[i].row * groups + p[i].g;
+            codes[at * 8 + (threadIdx.x & 7)] = (uint16_t)w;
+            if ((threadIdx.x & 7) == 0) scales[at] = (uint16_t)(bits >> 16);
+        }
     }
 }
 
-// 4 lanes to a group, 8 elements each; ids null: rows in order
+// ids null: rows in order
 template <bool BF16>
-__global__ __launch_bounds__(256) void k_table4_decode(const uint32_t *__restrict__ codes, const uint16_t *__restrict__ scales, int64_t n_rows, int32_t d,
+__global__ __launch_bounds__(256) void k_table4_decode(const uint16_t *__restrict__ codes, const uint16_t *__restrict__ scales, int64_t n_rows, int32_t d,
                                                        int32_t groups, const int32_t *__restrict__ ids, int64_t n_out, void *__restrict__ out, int64_t ldo)
 {
-    const int64_t first = (int64_t)blockIdx.x * 64;
-    const int64_t row0 = first / groups;
-    const uint32_t local = (uint32_t)(first - row0 * groups) + (threadIdx.x >> 2);
-    const int64_t row = row0 + local / (uint32_t)groups;
-    const int32_t g = (int32_t)(local % (uint32_t)groups), j = threadIdx.x & 3;
-    const int32_t c = g * G + 8 * j;
-    if (row >= n_out || c >= d) return;
-    const int64_t src = ids ? ids[row] : row;
-    float s = __uint_as_float(0x7fc00000u);                      // a row that the table does not have
-    uint32_t w = 0u;
-    if (src >= 0 && src < n_rows) {
-        const int64_t at = src * groups + g;
-        w = codes[at * 4 + j];
-        s = bf16_float(scales[at]);
-    }
-    float y[8];
-    const floatx2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1);
-    const floatx2 p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3);
-    y[0] = p0.x * s; y[1] = p0.y * s; y[2] = p1.x * s; y[3] = p1.y * s;
-    y[4] = p2.x * s; y[5] = p2.y * s; y[6] = p3.x * s; y[7] = p3.y * s;
-    const int n = d - c;
+    const int64_t first = (int64_t)blockIdx.x * (32 * SETS);
+    Place p[SETS];
+    uint32_t w[SETS];
+    float s[SETS];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int i = 0; i < SETS; ++i) {
+        p[i] = place_of(first, 32 * i + (threadIdx.x >> 3), groups);
+        w[i] = 0u;
+        s[i] = __uint_as_float(0x7fc00000u);                     // a row that the table does not have
+        const int64_t src = p[i].row >= n_out ? -1 : ids ? ids[p[i].row] : p[i].row;
+        if (src >= 0 && src < n_rows) {
+            const int64_t at = src * groups + p[i].g;
+            w[i] = codes[at * 8 + (threadIdx.x & 7)];
+            s[i] = bf16_float(scales[at]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) {
+        const int n = p[i].row < n_out ? d - p[i].c : 0;
+        if (n <= 0) continue;
+        const floatx2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.f, 1);
+        const float y[4] = {a.x * s[i], a.y * s[i], b.x * s[i], b.y * s[i]};
         if (BF16) {
-            uint16_t *o = (uint16_t *)out + row * ldo + c + 4 * h;
+            uint16_t *o = (uint16_t *)out + p[i].row * ldo + p[i].c;
             H4 q;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) q.x[k] = __builtin_bit_cast(uint16_t, (__bf16)y[4 * h + k]);
-            if (n >= 4 * h + 4) *reinterpret_cast<H4 *>(o) = q;
+            for (int k = 0; k < 4; ++k) q.x[k] = __builtin_bit_cast(uint16_t, (__bf16)y[k]);
+            if (n >= 4) *reinterpret_cast<H4 *>(o) = q;
             else {
 #pragma unroll
-                for (int k = 0; k < 3; ++k) if (4 * h + k < n) o[k] = q.x[k];
+                for (int k = 0; k < 3; ++k) if (k < n) o[k] = q.x[k];
             }
         } else {
-            float *o = (float *)out + row * ldo + c + 4 * h;
-            if (n >= 4 * h + 4) *reinterpret_cast<F4 *>(o) = F4{{y[4 * h], y[4 * h + 1], y[4 * h + 2], y[4 * h + 3]}};
+            float *o = (float *)out + p[i].row * ldo + p[i].c;
+            if (n >= 4) *reinterpret_cast<F4 *>(o) = F4{{y[0], y[1], y[2], y[3]}};
             else {
 #pragma unroll
-                for (int k = 0; k < 3; ++k) if (4 * h + k < n) o[k] = y[4 * h + k];
+                for (int k = 0; k < 3; ++k) if (k < n) o[k] = y[k];
             }
         }
     }
@@ -175,26 +196,48 @@ struct Questions {
     int64_t ldx, ldm, n_x, n_m, n;
 };
 
+// elements k .. k + 7 of question q, zeros past its end
 template <bool BF16>
-__device__ __forceinline__ float question(const Questions &Q, int64_t q, int32_t k, int32_t d)
+__device__ __forceinline__ void question8(const Questions &Q, int64_t q, int32_t k, int32_t d, float x[8])
 {
-    if (q >= Q.n || k >= d) return 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = 0.f;
+    if (q >= Q.n || k >= d) return;
     const int64_t i = Q.fixed ? Q.fixed[q] : q, r = Q.rel ? Q.rel[q] : q;
-    if (i < 0 || i >= Q.n_x || (Q.M && (r < 0 || r >= Q.n_m))) return __uint_as_float(0x7fc00000u);
-    const float x = BF16 ? bf16_float(((const uint16_t *)Q.X)[i * Q.ldx + k]) : ((const float *)Q.X)[i * Q.ldx + k];
-    return Q.M ? x * Q.M[r * Q.ldm + k] : x;
+    const bool bad = i < 0 || i >= Q.n_x || (Q.M && (r < 0 || r >= Q.n_m));
+    if (!bad) {
+        load4<BF16>(Q.X, i * Q.ldx + k, d - k, x);
+        load4<BF16>(Q.X, i * Q.ldx + k + 4, d - k - 4, x + 4);
+        if (Q.M) {
+            float m[8];
+            load4<false>(Q.M, r * Q.ldm + k, d - k, m);
+            load4<false>(Q.M, r * Q.ldm + k + 4, d - k - 4, m + 4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= m[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(0x7fc00000u);
+    }
 }
 
 // part p of x: what bf16 cuts off x, of the rest what it cuts off, and what is left; their sum is x
-__device__ __forceinline__ uint16_t part_of(float x, int p)
+__device__ __forceinline__ uint32_t part_of(float x, int p)
 {
     const uint32_t hi = __float_as_uint(x) & 0xffff0000u;
-    if (split_not_finite(x)) return p == 0 ? (x != x ? 0x7fc0 : hi >> 16) : 0;
+    if (split_not_finite(x)) return p == 0 ? (x != x ? 0x7fc0u : hi >> 16) : 0u;
     if (p == 0) return hi >> 16;
     const float r = x - __uint_as_float(hi);
     const uint32_t mid = __float_as_uint(r) & 0xffff0000u;
     if (p == 1) return mid >> 16;
     return __float_as_uint(r - __uint_as_float(mid)) >> 16;
+}
+__device__ __forceinline__ uint4 parts_of(const float x[8], int p)
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = part_of(x[2 * i], p) | part_of(x[2 * i + 1], p) << 16;
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // four registers by four groups of 16 lanes, transposed
@@ -221,7 +264,27 @@ __device__ __forceinline__ split_bf16x8 codes_bf16(uint32_t w)
     return split_bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, e.x, e.y};
 }
 
-// PARTS: of a question; TILES: of 16 questions, 0: up to four questions, their parts as rows of one tile.
+// What a wavefront has of four groups of 16 rows: their codes, a group a lane, and its row's four scales
+struct Four { uint4 w; H4 s; };
+
+__device__ __forceinline__ Four four_groups(const uint4 *__restrict__ codes, const uint16_t *__restrict__ scales, int64_t row, int32_t groups, int32_t g0, int j)
+{
+    Four f;
+    const int64_t at = row * groups + g0;
+    if (g0 + 4 <= groups) {
+        f.w = codes[at + j];
+        f.s = *reinterpret_cast<const H4 *>(scales + at);
+    } else {
+        f.w = make_uint4(0u, 0u, 0u, 0u);
+        if (g0 + j < groups) f.w = codes[at + j];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) f.s.x[h] = g0 + h < groups ? scales[at + h] : 0;
+    }
+    return f;
+}
+
+// PARTS: of a question; TILES: of 16 questions, 0: up to four questions, their parts as rows of one tile; a wavefront takes 32 rows at a time,
+// and has the next four groups on their way while it multiplies.
 // LDS: [group][tile][part] 1 KB each, what a lane hands the matrix instruction
 template <bool BF16, int PARTS, int TILES>
 __global__ __launch_bounds__(256) void k_table4_scores(const uint4 *__restrict__ codes, const uint16_t *__restrict__ scales, int64_t n_rows, int32_t d,
@@ -231,65 +294,103 @@ __global__ __launch_bounds__(256) void k_table4_scores(const uint4 *__restrict__
     extern __shared__ uint4 s_q[];
     const int lane = threadIdx.x & 63, i16 = lane & 15, j = lane >> 4;
     const int64_t q0 = (int64_t)blockIdx.y * (TILES ? 16 * TILES : 4);
-    uint16_t *sq = (uint16_t *)s_q;
-    for (int e = threadIdx.x; e < groups * PER * 512; e += 256) {                // element e: lane and place in its 8 numbers
-        const int at = e & 7, l = (e >> 3) & 63, op = e >> 9;
-        const int g = op / PER, t = op % PER / P, p = op % P, row = l & 15, k = g * G + 8 * (l >> 4) + at;
-        if (TILES) sq[e] = part_of(question<BF16>(Q, q0 + 16 * t + row, k, d), p);
-        else sq[e] = row >> 2 < PARTS ? part_of(question<BF16>(Q, q0 + (row & 3), k, d), row >> 2) : 0;
+    for (int e = threadIdx.x; e < groups * T * 64; e += 256) {                   // a lane's part of a group's operands
+        const int l = e & 63, op = e >> 6, row = l & 15, k = op / T * G + 8 * (l >> 4);
+        float x[8];
+        if (TILES) {
+            question8<BF16>(Q, q0 + 16 * (op % T) + row, k, d, x);
+#pragma unroll
+            for (int p = 0; p < P; ++p) s_q[(op * P + p) * 64 + l] = parts_of(x, p);
+        } else if (row < 4) {
+            question8<BF16>(Q, q0 + row, k, d, x);
+#pragma unroll
+            for (int p = 0; p < 4; ++p) s_q[op * 64 + l + 4 * p] = p < PARTS ? parts_of(x, p) : make_uint4(0u, 0u, 0u, 0u);
+        }
     }
     __syncthreads();
-    const int64_t tiles = (n_rows + 15) >> 4, step = (int64_t)gridDim.x * 4;
-    for (int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); tile < tiles; tile += step) {
-        const int64_t row = tile * 16 + i16, src = row < n_rows ? row : n_rows - 1;
-        floatx4 acc[T];
+    const int64_t tiles = (n_rows + 31) >> 5, step = (int64_t)gridDim.x * 4;
+    int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (tile >= tiles) return;
+    floatx4 acc[2][T];
 #pragma unroll
-        for (int t = 0; t < T; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-        for (int g0 = 0; g0 < groups; g0 += 4) {
-            uint4 w = make_uint4(0u, 0u, 0u, 0u);
-            if (g0 + j < groups) w = codes[src * groups + g0 + j];
-            float s[4];
+    for (int a = 0; a < 2; ++a)
 #pragma unroll
-            for (int h = 0; h < 4; ++h) s[h] = bf16_float(scales[src * groups + min(g0 + h, groups - 1)]);
-            uint32_t r[4] = {w.x, w.y, w.z, w.w};
-            transpose4(r);
+        for (int t = 0; t < T; ++t) acc[a][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    Four now[2];
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                if (g0 + h >= groups) break;
-                const split_bf16x8 c = codes_bf16(r[h]);
+    for (int a = 0; a < 2; ++a) now[a] = four_groups(codes, scales, min(tile * 32 + 16 * a + i16, n_rows - 1), groups, 0, j);
+    int32_t g0 = 0;
+    for (;;) {
+        const bool last = g0 + 4 >= groups;
+        const int64_t next_tile = last ? tile + step : tile;
+        const int32_t next_g0 = last ? 0 : g0 + 4;
+        Four next[2];
+        if (next_tile < tiles) {
 #pragma unroll
-                for (int t = 0; t < T; ++t) {
-                    floatx4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int p = P - 1; p >= 0; --p)
-                        v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(split_bf16x8, s_q[((g0 + h) * PER + t * P + p) * 64 + lane]), c, v, 0, 0, 0);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[t][k] = fmaf(s[h], v[k], acc[t][k]);
-                }
-            }
+            for (int a = 0; a < 2; ++a) next[a] = four_groups(codes, scales, min(next_tile * 32 + 16 * a + i16, n_rows - 1), groups, next_g0, j);
         }
-        // a lane holds its row's sums with rows 4 j .. 4 j + 3 of each tile of questions
-        if (TILES) {
+        uint32_t r[2][4];
 #pragma unroll
-            for (int t = 0; t < T; ++t)
+        for (int a = 0; a < 2; ++a) {
+            r[a][0] = now[a].w.x; r[a][1] = now[a].w.y; r[a][2] = now[a].w.z; r[a][3] = now[a].w.w;
+            transpose4(r[a]);
+        }
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            if (g0 + h >= groups) break;
+            const split_bf16x8 c0 = codes_bf16(r[0][h]), c1 = codes_bf16(r[1][h]);
+            const float s0 = bf16_float(now[0].s.x[h]), s1 = bf16_float(now[1].s.x[h]);
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+                floatx4 v0 = {0.f, 0.f, 0.f, 0.f}, v1 = v0;
+#pragma unroll
+                for (int p = P - 1; p >= 0; --p) {
+                    const split_bf16x8 q = __builtin_bit_cast(split_bf16x8, s_q[((g0 + h) * PER + t * P + p) * 64 + lane]);
+                    v0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, c0, v0, 0, 0, 0);
+                    v1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, c1, v1, 0, 0, 0);
+                }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int64_t q = q0 + 16 * t + 4 * j + k;
-                    if (q < Q.n && row < n_rows) out[q * ldo + row] = acc[t][k];
+                    acc[0][t][k] = fmaf(s0, v0[k], acc[0][t][k]);
+                    acc[1][t][k] = fmaf(s1, v1[k], acc[1][t][k]);
                 }
-        } else {
-            float v[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                v[k] = acc[0][k];
-                if (PARTS == 3) {
-                    const float mid = __shfl(v[k], i16 + 16, 64), low = __shfl(v[k], i16 + 32, 64);
-                    v[k] = __shfl(v[k], i16, 64) + (mid + low);
-                } else v[k] = __shfl(v[k], i16, 64);
             }
-            const float mine = j == 0 ? v[0] : j == 1 ? v[1] : j == 2 ? v[2] : v[3];
-            if (q0 + j < Q.n && row < n_rows) out[(q0 + j) * ldo + row] = mine;
         }
+        if (last) {
+            // a lane holds its row's sums with rows 4 j .. 4 j + 3 of each tile of questions
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                const int64_t row = tile * 32 + 16 * a + i16;
+                if (TILES) {
+#pragma unroll
+                    for (int t = 0; t < T; ++t)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int64_t q = q0 + 16 * t + 4 * j + k;
+                            if (q < Q.n && row < n_rows) out[q * ldo + row] = acc[a][t][k];
+                        }
+                } else {
+                    float v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        v[k] = acc[a][0][k];
+                        if (PARTS == 3) {
+                            const float mid = __shfl(v[k], i16 + 16, 64), low = __shfl(v[k], i16 + 32, 64);
+                            v[k] = __shfl(v[k], i16, 64) + (mid + low);
+                        } else v[k] = __shfl(v[k], i16, 64);
+                    }
+                    const float mine = j == 0 ? v[0] : j == 1 ? v[1] : j == 2 ? v[2] : v[3];
+                    if (q0 + j < Q.n && row < n_rows) out[(q0 + j) * ldo + row] = mine;
+                }
+#pragma unroll
+                for (int t = 0; t < T; ++t) acc[a][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+            }
+            if (next_tile >= tiles) break;
+        }
+        tile = next_tile;
+        g0 = next_g0;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) now[a] = next[a];
     }
 }
 
@@ -299,9 +400,9 @@ template <bool BF16, int PARTS, int TILES>
 int launch_scores(const kge_table4 *t, int32_t groups, const Questions &Q, float *scores, int64_t lds, hipStream_t st)
 {
     const int bytes = groups * (TILES ? TILES * PARTS : 1) * 1024;
-    const int64_t batches = cdiv(Q.n, TILES ? 16 * TILES : 4), tiles = cdiv(t->n_rows, 16);
+    const int64_t batches = cdiv(Q.n, TILES ? 16 * TILES : 4), tiles = cdiv(t->n_rows, 32);
     int64_t blocks = cdiv(tiles, 4);
-    if (blocks > 2048) blocks = 2048;
+    if (blocks > 1024) blocks = 1024;
     auto kernel = k_table4_scores<BF16, PARTS, TILES>;
     if (bytes > 64 << 10) KGE_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
     for (int64_t b = 0; b < batches; b += 65535) {
@@ -325,7 +426,8 @@ int scores_of(const kge_table4 *t, int32_t groups, const Questions &Q, float *sc
     const int tile = groups * PARTS * 1024;
     if (Q.n <= 4 || tile > LDS_MOST) return launch_scores<BF16, PARTS, 0>(t, groups, Q, scores, lds, st);
     if (Q.n <= 16 || 2 * tile > LDS_MOST) return launch_scores<BF16, PARTS, 1>(t, groups, Q, scores, lds, st);
-    if (Q.n <= 32 || 4 * tile > LDS_MOST) return launch_scores<BF16, PARTS, 2>(t, groups, Q, scores, lds, st);
+    if (Q.n <= 32 || 3 * tile > LDS_MOST) return launch_scores<BF16, PARTS, 2>(t, groups, Q, scores, lds, st);
+    if (Q.n <= 48 || 4 * tile > LDS_MOST) return launch_scores<BF16, PARTS, 3>(t, groups, Q, scores, lds, st);
     return launch_scores<BF16, PARTS, 4>(t, groups, Q, scores, lds, st);
 }
 
@@ -358,11 +460,11 @@ extern "C" int kge_table4_encode(const kge_table4 *table, int32_t dtype, const v
     if (rc != KGE_OK || table->n_rows == 0) return rc;
     hipStream_t st = (hipStream_t)stream;
     const int32_t groups = (int32_t)cdiv(table->d, G);
-    const int64_t blocks = cdiv(table->n_rows * groups, 64);
-    KGE_REQUIRE(blocks <= 0x7fffffffll / 256, KGE_ERANGE, "2^29 groups or more");
+    const int64_t blocks = cdiv(table->n_rows * groups, 32 * SETS);
+    KGE_REQUIRE(blocks <= 0x7fffffffll / 256, KGE_ERANGE, "2^30 groups or more");
     KGE_PROF("table4_encode", st);
     (dtype == KGE_DT_BF16 ? k_table4_encode<true> : k_table4_encode<false>)<<<(unsigned)blocks, 256, 0, st>>>(X, ldx, table->n_rows, table->d, groups,
-                                                                                                            (uint32_t *)table->codes, table->scales);
+                                                                                                            (uint16_t *)table->codes, table->scales);
     KGE_LAUNCH_CHECK();
     return KGE_OK;
 }
@@ -376,10 +478,10 @@ extern "C" int kge_table4_decode(const kge_table4 *table, const int32_t *rows, i
     if (rc != KGE_OK || n == 0) return rc;
     hipStream_t st = (hipStream_t)stream;
     const int32_t groups = (int32_t)cdiv(table->d, G);
-    KGE_REQUIRE(n <= 0x7fffffffll && cdiv(n * groups, 64) <= 0x7fffffffll / 256, KGE_ERANGE, "2^29 groups or more");
+    KGE_REQUIRE(n <= 0x7fffffffll && cdiv(n * groups, 32 * SETS) <= 0x7fffffffll / 256, KGE_ERANGE, "2^30 groups or more");
     KGE_PROF("table4_decode", st);
-    (dtype == KGE_DT_BF16 ? k_table4_decode<true> : k_table4_decode<false>)<<<(unsigned)cdiv(n * groups, 64), 256, 0, st>>>(
-        (const uint32_t *)table->codes, table->scales, table->n_rows, table->d, groups, rows, n, out, ldo);
+    (dtype == KGE_DT_BF16 ? k_table4_decode<true> : k_table4_decode<false>)<<<(unsigned)cdiv(n * groups, 32 * SETS), 256, 0, st>>>(
+        (const uint16_t *)table->codes, table->scales, table->n_rows, table->d, groups, rows, n, out, ldo);
     KGE_LAUNCH_CHECK();
     return KGE_OK;
 }
