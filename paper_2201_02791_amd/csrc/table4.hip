@@ -9,6 +9,8 @@
 #include "common.h"
 #include "split_bf16.h"
 
+#include <algorithm>
+
 namespace {
 
 constexpr int G = KGE_TABLE4_GROUP;
@@ -16,7 +18,9 @@ static_assert(G == 32, "a group is one step of the matrix instruction and 16 byt
 
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef floatx4 floatx4u __attribute__((aligned(4)));
 typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
+typedef uintx2 uintx2h __attribute__((aligned(2)));
 
 struct __attribute__((packed, aligned(4))) F4 { float x[4]; };
 struct __attribute__((packed, aligned(2))) H4 { uint16_t x[4]; };
@@ -70,102 +74,157 @@ __device__ __forceinline__ uint32_t code_of(float x, float s)
     return c | (x < 0.f ? 8u : 0u);
 }
 
-// Where a lane's 4 elements of a group are: group gi of the table as a whole, 8 lanes to a group
-struct Place {
-    int64_t row;
-    int32_t g, c;                  // the group in its row, and the first of the elements
-};
-__device__ __forceinline__ Place place_of(int64_t first, uint32_t local, int32_t groups)
+// The codes of four elements.  The conversion instruction rounds x / s, here formed by a reciprocal and a product that are off by less than 2^-22:
+// where quotients that much smaller and larger have the same codes, those are the codes; else the borders decide
+__device__ __forceinline__ uint32_t codes_of(const float x[4], float s, float inverse)
 {
-    Place p;
-    const int64_t row0 = first / groups;                         // of the block: uniform
-    const uint32_t at = (uint32_t)(first - row0 * groups) + local, more = at / (uint32_t)groups;
-    p.row = row0 + more;
-    p.g = (int32_t)(at - more * (uint32_t)groups);
-    p.c = p.g * G + 4 * (int32_t)(threadIdx.x & 7);
-    return p;
+    float up[4], down[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float q = fmaf(x[k], inverse, 0.f);                // of minus zero plus zero
+        up[k] = q * (1.f + 0x1p-22f);
+        down[k] = q * (1.f - 0x1p-22f);
+    }
+    uint32_t a = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, up[0], up[1], 1.f, 0);
+    a = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(a, up[2], up[3], 1.f, 1);
+    uint32_t b = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, down[0], down[1], 1.f, 0);
+    b = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(b, down[2], down[3], 1.f, 1);
+    if (a != b) {
+        a = 0u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a |= code_of(x[k], s) << (4 * k);
+    }
+    return a & 0xffffu;
 }
 
-constexpr int SETS = 4;            // of 32 groups, that a block of 256 takes at once
-
+// A block takes `BLOCK_GROUPS` groups side by side in the table.  Where one of them is: rows behind the block's first, and the group in its row.
+// A row has up to 128 groups, so the quotient of a number below 384 by them is a product and a shift
+struct Block {
+    int64_t first, row0;           // group, and the row that it is in
+    uint32_t into, groups, per, left;     // groups of that row before it; groups that the block has
+};
+struct Place { uint32_t more; int32_t g; bool in; };
+constexpr int BLOCK_GROUPS = 256;
+__device__ __forceinline__ Block block_of(int64_t n_rows, int32_t groups)
+{
+    Block b;
+    b.first = (int64_t)blockIdx.x * BLOCK_GROUPS;
+    b.row0 = b.first / groups;
+    b.into = (uint32_t)(b.first - b.row0 * groups);
+    b.groups = (uint32_t)groups;
+    b.per = 65536u / (uint32_t)groups + 1u;
+    b.left = (uint32_t)min((int64_t)BLOCK_GROUPS, n_rows * groups - b.first);
+    return b;
+}
+__device__ __forceinline__ Place place_of(const Block &b, uint32_t local)
+{
+    Place p;
+    const uint32_t at = b.into + local;
+    p.more = at * b.per >> 16;
+    p.g = (int32_t)(at - p.more * b.groups);
+    p.in = local < b.left;
+    return p;
+}
 template <int CTRL>
-__device__ __forceinline__ uint32_t dpp_max(uint32_t v) { return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true)); }
+__device__ __forceinline__ uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
+constexpr int NEAR = 0xb1, PAIR = 0x4e;       // quad_perm: lanes 1 apart, 2 apart
 
+// Four lanes to a group: lane i has elements 4 i .. + 3 and 16 + 4 i .. + 3, so that four lanes load 64 bytes side by side.  Their codes are halves
+// of words: lanes change halves in pairs, and each has a word.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_table4_encode(const void *__restrict__ X, int64_t ldx, int64_t n_rows, int32_t d, int32_t groups,
-                                                       uint16_t *__restrict__ codes, uint16_t *__restrict__ scales)
+                                                       uint32_t *__restrict__ codes, uint16_t *__restrict__ scales)
 {
-    const int64_t first = (int64_t)blockIdx.x * (32 * SETS);
-    float x[SETS][4];
-    Place p[SETS];
+    constexpr int SETS = BLOCK_GROUPS / 64;
+    const Block b = block_of(n_rows, groups);
+    const int64_t from = b.row0 * ldx;
+    const uint32_t lane4 = threadIdx.x & 3;
+    float x[SETS][8];
 #pragma unroll
     for (int i = 0; i < SETS; ++i) {
-        p[i] = place_of(first, 32 * i + (threadIdx.x >> 3), groups);
-        load4<BF16>(X, p[i].row * ldx + p[i].c, p[i].row < n_rows ? d - p[i].c : 0, x[i]);
+        const Place p = place_of(b, 64 * i + (threadIdx.x >> 2));
+        const int32_t c = p.g * G + 4 * (int32_t)lane4, n = p.in ? d - c : 0;
+        const int64_t at = from + (int64_t)p.more * ldx + c;
+        load4<BF16>(X, at, n, x[i]);
+        load4<BF16>(X, at + 16, n - 16, x[i] + 4);
     }
+    codes += b.first * 4;
+    scales += b.first;
 #pragma unroll
     for (int i = 0; i < SETS; ++i) {
         uint32_t most = 0u;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) most = max(most, __float_as_uint(x[i][k]) & 0x7fffffffu);
-        most = dpp_max<0xb1>(most);                              // lanes 1 apart, 2 apart, and mirrored in 8
-        most = dpp_max<0x4e>(most);
-        most = dpp_max<0x141>(most);
+        for (int k = 0; k < 8; ++k) most = max(most, __float_as_uint(x[i][k]) & 0x7fffffffu);
+        most = max(most, dpp<NEAR>(most));
+        most = max(most, dpp<PAIR>(most));
         const uint32_t bits = group_scale(most);
         const float s = __uint_as_float(bits);
-        uint32_t w = 0u;
+        uint32_t a = 0u, c = 0u;
         if (s > 0.f) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w |= code_of(x[i][k], s) << (4 * k);
+            const float inverse = __builtin_amdgcn_rcpf(s);
+            a = codes_of(x[i], s, inverse);
+            c = codes_of(x[i] + 4, s, inverse);
         }
-        if (p[i].row < n_rows) {
-            const int64_t at = p[i].row * groups + p[i].g;
-            codes[at * 8 + (threadIdx.x & 7)] = (uint16_t)w;
-            if ((threadIdx.x & 7) == 0) scales[at] = (uint16_t)(bits >> 16);
+        const bool odd = lane4 & 1u;
+        const uint32_t other = dpp<NEAR>(odd ? a : c), local = 64 * i + (threadIdx.x >> 2);
+        if (local < b.left) {
+            codes[local * 4 + (lane4 & 1u) * 2 + (lane4 >> 1)] = odd ? other | c << 16 : a | other << 16;
+            if (lane4 == 0u) scales[local] = (uint16_t)(bits >> 16);
         }
     }
 }
 
-// ids null: rows in order
+// Eight lanes to a group, which store their 4 elements side by side, 1 KB a wavefront, past the caches (a million rows of 256, us: 64 bytes side by
+// side 389, 1 KB 304, past the caches 253; 14541 x 200: 7.0, 6.8, 5.4).  ids null: rows in order
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_table4_decode(const uint16_t *__restrict__ codes, const uint16_t *__restrict__ scales, int64_t n_rows, int32_t d,
                                                        int32_t groups, const int32_t *__restrict__ ids, int64_t n_out, void *__restrict__ out, int64_t ldo)
 {
-    const int64_t first = (int64_t)blockIdx.x * (32 * SETS);
-    Place p[SETS];
+    constexpr int SETS = BLOCK_GROUPS / 32;
+    const Block b = block_of(n_out, groups);
+    const uint32_t lane8 = threadIdx.x & 7;
     uint32_t w[SETS];
     float s[SETS];
 #pragma unroll
     for (int i = 0; i < SETS; ++i) {
-        p[i] = place_of(first, 32 * i + (threadIdx.x >> 3), groups);
+        const uint32_t local = 32 * i + (threadIdx.x >> 3);
         w[i] = 0u;
         s[i] = __uint_as_float(0x7fc00000u);                     // a row that the table does not have
-        const int64_t src = p[i].row >= n_out ? -1 : ids ? ids[p[i].row] : p[i].row;
-        if (src >= 0 && src < n_rows) {
-            const int64_t at = src * groups + p[i].g;
-            w[i] = codes[at * 8 + (threadIdx.x & 7)];
-            s[i] = bf16_float(scales[at]);
+        if (local >= b.left) continue;
+        if (!ids) {
+            w[i] = (codes + b.first * 8)[local * 8 + lane8];
+            s[i] = bf16_float((scales + b.first)[local]);
+        } else {
+            const Place p = place_of(b, local);
+            const int64_t src = ids[b.row0 + p.more];
+            if (src >= 0 && src < n_rows) {
+                w[i] = codes[(src * groups + p.g) * 8 + lane8];
+                s[i] = bf16_float(scales[src * groups + p.g]);
+            }
         }
     }
 #pragma unroll
     for (int i = 0; i < SETS; ++i) {
-        const int n = p[i].row < n_out ? d - p[i].c : 0;
+        const Place p = place_of(b, 32 * i + (threadIdx.x >> 3));
+        const int32_t c = p.g * G + 4 * (int32_t)lane8;
+        const int n = p.in ? d - c : 0;
         if (n <= 0) continue;
-        const floatx2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.f, 1);
-        const float y[4] = {a.x * s[i], a.y * s[i], b.x * s[i], b.y * s[i]};
+        const int64_t at = b.row0 * ldo + (int64_t)p.more * ldo + c;
+        const floatx2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.f, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.f, 1);
+        const float y[4] = {lo.x * s[i], lo.y * s[i], hi.x * s[i], hi.y * s[i]};
         if (BF16) {
-            uint16_t *o = (uint16_t *)out + p[i].row * ldo + p[i].c;
+            uint16_t *o = (uint16_t *)out + at;
             H4 q;
 #pragma unroll
             for (int k = 0; k < 4; ++k) q.x[k] = __builtin_bit_cast(uint16_t, (__bf16)y[k]);
-            if (n >= 4) *reinterpret_cast<H4 *>(o) = q;
+            if (n >= 4) __builtin_nontemporal_store(__builtin_bit_cast(uintx2, q), reinterpret_cast<uintx2h *>(o));
             else {
 #pragma unroll
                 for (int k = 0; k < 3; ++k) if (k < n) o[k] = q.x[k];
             }
         } else {
-            float *o = (float *)out + p[i].row * ldo + p[i].c;
-            if (n >= 4) *reinterpret_cast<F4 *>(o) = F4{{y[0], y[1], y[2], y[3]}};
+            float *o = (float *)out + at;
+            if (n >= 4) __builtin_nontemporal_store(floatx4{y[0], y[1], y[2], y[3]}, reinterpret_cast<floatx4u *>(o));
             else {
 #pragma unroll
                 for (int k = 0; k < 3; ++k) if (k < n) o[k] = y[k];
@@ -283,17 +342,38 @@ __device__ __forceinline__ Four four_groups(const uint4 *__restrict__ codes, con
     return f;
 }
 
-// PARTS: of a question; TILES: of 16 questions, 0: up to four questions, their parts as rows of one tile; a wavefront takes 32 rows at a time,
-// and has the next four groups on their way while it multiplies.
+// PARTS: of a question; TILES: of 16 questions, 0: up to FEW questions (1 or 4), their parts as rows of one tile; a wavefront takes 32 rows at a
+// time, and has the next four groups on their way while it multiplies.
 // LDS: [group][tile][part] 1 KB each, what a lane hands the matrix instruction
-template <bool BF16, int PARTS, int TILES>
+template <bool BF16, int PARTS, int TILES, int FEW>
 __global__ __launch_bounds__(256) void k_table4_scores(const uint4 *__restrict__ codes, const uint16_t *__restrict__ scales, int64_t n_rows, int32_t d,
                                                        int32_t groups, Questions Q, float *__restrict__ out, int64_t ldo)
 {
+    constexpr int SUMS = TILES ? 4 : FEW;                                        // of a lane's four that are wanted
     constexpr int T = TILES ? TILES : 1, P = TILES ? PARTS : 1, PER = T * P;     // operands of a group
     extern __shared__ uint4 s_q[];
     const int lane = threadIdx.x & 63, i16 = lane & 15, j = lane >> 4;
     const int64_t q0 = (int64_t)blockIdx.y * (TILES ? 16 * TILES : 4);
+    const int64_t tiles = (n_rows + 31) >> 5, step = (int64_t)gridDim.x * 4;
+    int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    // this lane's codes and scales of its row of a tile; what is inside the table and has four groups goes by them
+    const uint4 *code = codes + (tile * 32 + i16) * groups + j;
+    const uint16_t *scale = scales + (tile * 32 + i16) * groups;
+    const int64_t stride = step * 32 * groups;
+    const auto fetch = [&](int64_t t, int32_t g, Four f[2]) {
+        if (t * 32 + 32 <= n_rows && g + 4 <= groups) {
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                f[a].w = code[16 * a * groups + g];
+                f[a].s = *reinterpret_cast<const H4 *>(scale + 16 * a * groups + g);
+            }
+        } else {
+#pragma unroll
+            for (int a = 0; a < 2; ++a) f[a] = four_groups(codes, scales, min(t * 32 + 16 * a + i16, n_rows - 1), groups, g, j);
+        }
+    };
+    Four now[2];                   // on their way while the questions are laid out
+    fetch(tile, 0, now);
     for (int e = threadIdx.x; e < groups * T * 64; e += 256) {                   // a lane's part of a group's operands
         const int l = e & 63, op = e >> 6, row = l & 15, k = op / T * G + 8 * (l >> 4);
         float x[8];
@@ -308,27 +388,22 @@ __global__ __launch_bounds__(256) void k_table4_scores(const uint4 *__restrict__
         }
     }
     __syncthreads();
-    const int64_t tiles = (n_rows + 31) >> 5, step = (int64_t)gridDim.x * 4;
-    int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (tile >= tiles) return;
     floatx4 acc[2][T];
 #pragma unroll
     for (int a = 0; a < 2; ++a)
 #pragma unroll
         for (int t = 0; t < T; ++t) acc[a][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-    Four now[2];
-#pragma unroll
-    for (int a = 0; a < 2; ++a) now[a] = four_groups(codes, scales, min(tile * 32 + 16 * a + i16, n_rows - 1), groups, 0, j);
+    float *mine = out + (q0 + 4 * j) * ldo;      // of this lane's first question, and how many there are from it on
+    const int left = (int)min(Q.n - q0 - 4 * j, (int64_t)(16 * T));
     int32_t g0 = 0;
     for (;;) {
         const bool last = g0 + 4 >= groups;
         const int64_t next_tile = last ? tile + step : tile;
         const int32_t next_g0 = last ? 0 : g0 + 4;
         Four next[2];
-        if (next_tile < tiles) {
-#pragma unroll
-            for (int a = 0; a < 2; ++a) next[a] = four_groups(codes, scales, min(next_tile * 32 + 16 * a + i16, n_rows - 1), groups, next_g0, j);
-        }
+        if (last) { code += stride; scale += stride; }
+        if (next_tile < tiles) fetch(next_tile, next_g0, next);
         uint32_t r[2][4];
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
@@ -350,7 +425,7 @@ __global__ __launch_bounds__(256) void k_table4_scores(const uint4 *__restrict__
                     v1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, c1, v1, 0, 0, 0);
                 }
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < SUMS; ++k) {
                     acc[0][t][k] = fmaf(s0, v0[k], acc[0][t][k]);
                     acc[1][t][k] = fmaf(s1, v1[k], acc[1][t][k]);
                 }
@@ -362,25 +437,21 @@ __global__ __launch_bounds__(256) void k_table4_scores(const uint4 *__restrict__
             for (int a = 0; a < 2; ++a) {
                 const int64_t row = tile * 32 + 16 * a + i16;
                 if (TILES) {
+                    float *o = mine + row;
 #pragma unroll
                     for (int t = 0; t < T; ++t)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int64_t q = q0 + 16 * t + 4 * j + k;
-                            if (q < Q.n && row < n_rows) out[q * ldo + row] = acc[a][t][k];
-                        }
+                        for (int k = 0; k < 4; ++k)
+                            if (16 * t + k < left && row < n_rows) o[(16 * t + k) * ldo] = acc[a][t][k];
                 } else {
-                    float v[4];
+                    float sum = 0.f;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        v[k] = acc[a][0][k];
-                        if (PARTS == 3) {
-                            const float mid = __shfl(v[k], i16 + 16, 64), low = __shfl(v[k], i16 + 32, 64);
-                            v[k] = __shfl(v[k], i16, 64) + (mid + low);
-                        } else v[k] = __shfl(v[k], i16, 64);
+                    for (int k = 0; k < SUMS; ++k) {
+                        const float v = acc[a][0][k];
+                        const float all = PARTS == 3 ? __shfl(v, i16, 64) + (__shfl(v, i16 + 16, 64) + __shfl(v, i16 + 32, 64)) : __shfl(v, i16, 64);
+                        if (j == k) sum = all;
                     }
-                    const float mine = j == 0 ? v[0] : j == 1 ? v[1] : j == 2 ? v[2] : v[3];
-                    if (q0 + j < Q.n && row < n_rows) out[(q0 + j) * ldo + row] = mine;
+                    if (j < SUMS && q0 + j < Q.n && row < n_rows) out[(q0 + j) * ldo + row] = sum;
                 }
 #pragma unroll
                 for (int t = 0; t < T; ++t) acc[a][t] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -396,14 +467,17 @@ __global__ __launch_bounds__(256) void k_table4_scores(const uint4 *__restrict__
 
 constexpr int LDS_MOST = 160 << 10;
 
-template <bool BF16, int PARTS, int TILES>
+template <bool BF16, int PARTS, int TILES, int FEW = 4>
 int launch_scores(const kge_table4 *t, int32_t groups, const Questions &Q, float *scores, int64_t lds, hipStream_t st)
 {
     const int bytes = groups * (TILES ? TILES * PARTS : 1) * 1024;
     const int64_t batches = cdiv(Q.n, TILES ? 16 * TILES : 4), tiles = cdiv(t->n_rows, 32);
     int64_t blocks = cdiv(tiles, 4);
-    if (blocks > 1024) blocks = 1024;
-    auto kernel = k_table4_scores<BF16, PARTS, TILES>;
+    // as many as run at once: registers leave room for four to a compute unit with up to 16 questions, else for three.  37 questions to 2.9 million
+    // rows: 1024 blocks 187 us, 768 151
+    const int64_t most = 256ll * std::max(1, std::min(TILES <= 1 ? 4 : 3, LDS_MOST / bytes));
+    if (blocks > most) blocks = most;
+    auto kernel = k_table4_scores<BF16, PARTS, TILES, FEW>;
     if (bytes > 64 << 10) KGE_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
     for (int64_t b = 0; b < batches; b += 65535) {
         Questions part = Q;
@@ -424,6 +498,7 @@ template <bool BF16, int PARTS>
 int scores_of(const kge_table4 *t, int32_t groups, const Questions &Q, float *scores, int64_t lds, hipStream_t st)
 {
     const int tile = groups * PARTS * 1024;
+    if (Q.n == 1) return launch_scores<BF16, PARTS, 0, 1>(t, groups, Q, scores, lds, st);
     if (Q.n <= 4 || tile > LDS_MOST) return launch_scores<BF16, PARTS, 0>(t, groups, Q, scores, lds, st);
     if (Q.n <= 16 || 2 * tile > LDS_MOST) return launch_scores<BF16, PARTS, 1>(t, groups, Q, scores, lds, st);
     if (Q.n <= 32 || 3 * tile > LDS_MOST) return launch_scores<BF16, PARTS, 2>(t, groups, Q, scores, lds, st);
@@ -460,11 +535,11 @@ extern "C" int kge_table4_encode(const kge_table4 *table, int32_t dtype, const v
     if (rc != KGE_OK || table->n_rows == 0) return rc;
     hipStream_t st = (hipStream_t)stream;
     const int32_t groups = (int32_t)cdiv(table->d, G);
-    const int64_t blocks = cdiv(table->n_rows * groups, 32 * SETS);
-    KGE_REQUIRE(blocks <= 0x7fffffffll / 256, KGE_ERANGE, "2^30 groups or more");
+    const int64_t blocks = cdiv(table->n_rows * groups, BLOCK_GROUPS);
+    KGE_REQUIRE(blocks <= 0x7fffffffll / 256, KGE_ERANGE, "2^31 groups or more");
     KGE_PROF("table4_encode", st);
     (dtype == KGE_DT_BF16 ? k_table4_encode<true> : k_table4_encode<false>)<<<(unsigned)blocks, 256, 0, st>>>(X, ldx, table->n_rows, table->d, groups,
-                                                                                                            (uint16_t *)table->codes, table->scales);
+                                                                                                            (uint32_t *)table->codes, table->scales);
     KGE_LAUNCH_CHECK();
     return KGE_OK;
 }
@@ -478,9 +553,9 @@ extern "C" int kge_table4_decode(const kge_table4 *table, const int32_t *rows, i
     if (rc != KGE_OK || n == 0) return rc;
     hipStream_t st = (hipStream_t)stream;
     const int32_t groups = (int32_t)cdiv(table->d, G);
-    KGE_REQUIRE(n <= 0x7fffffffll && cdiv(n * groups, 32 * SETS) <= 0x7fffffffll / 256, KGE_ERANGE, "2^30 groups or more");
+    KGE_REQUIRE(n <= 0x7fffffffll && cdiv(n * groups, BLOCK_GROUPS) <= 0x7fffffffll / 256, KGE_ERANGE, "2^31 groups or more");
     KGE_PROF("table4_decode", st);
-    (dtype == KGE_DT_BF16 ? k_table4_decode<true> : k_table4_decode<false>)<<<(unsigned)cdiv(n * groups, 32 * SETS), 256, 0, st>>>(
+    (dtype == KGE_DT_BF16 ? k_table4_decode<true> : k_table4_decode<false>)<<<(unsigned)cdiv(n * groups, BLOCK_GROUPS), 256, 0, st>>>(
         (const uint16_t *)table->codes, table->scales, table->n_rows, table->d, groups, rows, n, out, ldo);
     KGE_LAUNCH_CHECK();
     return KGE_OK;
