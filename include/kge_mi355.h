@@ -583,9 +583,10 @@ int kge_table4_scores(const kge_table4 *table, int32_t dtype, const void *X, int
  *   u: DEVICE [n_rows][n_draws], float (u_bits 32) or double (64), in [0, 1); what is outside counts as the nearest inside, NaN as 0
  *   choice: DEVICE int32 [n_rows][n_draws], the column; -1 for every draw of a row without weights (no columns, or only minus infinity and NaN)
  *   prob: NULL, or DEVICE float [n_rows][n_draws]: the column's share of the weights left; 0 beside -1
- *   n_rows below 2^31, n_cols at most 2^31 - 2^16.  workspace: DEVICE, 256-byte aligned, at least kge_sample_workspace_bytes(how, n_rows, n_cols) bytes (0: invalid
- *   arguments); calls on different streams need different ones.
+ *   n_rows below 2^31, n_cols at most 2^31 - 2^16.  workspace: DEVICE, 256-byte aligned, at least kge_sample_workspace_bytes(how, n_rows, n_cols)
+ *   bytes (0: invalid arguments), calls on different streams need different ones; with up to KGE_SAMPLE_ROW columns none is looked at.
  */
+#define KGE_SAMPLE_ROW 65536
 typedef struct kge_sampling {
     float temperature;
     int32_t top_k;

@@ -806,6 +806,7 @@ def clip_grads(grads, max_norm: float, norm=None, factor=None, workspace=None, s
 # ---- answers: tables of 4 bits, their scores, draws from scores ------------------------------------
 
 TABLE4_GROUP = 32
+SAMPLE_ROW = 65536                # KGE_SAMPLE_ROW: rows of up to so many columns need no workspace
 
 
 class Table4:
@@ -833,7 +834,8 @@ def table4_encode(X, table: Table4 = None, stream=None) -> Table4:
     if table is None:
         groups = -(-d // TABLE4_GROUP)
         table = Table4(_new(X, (n, 16 * groups), torch.uint8, stream), _new(X, (n, groups), torch.bfloat16, stream), d)
-    _need((table.n_rows, table.d) == (n, d), "the table is of another shape than X")
+    elif table.n_rows != n or table.d != d:
+        raise KgeError(-1, "the table is of another shape than X")
     _call(load().kge_table4_encode, stream, X, (table.codes, table.scales), C.byref(table.struct), dt, x, ldx)
     return table
 
@@ -874,24 +876,25 @@ def table4_scores(table: Table4, X, fixed=None, M=None, rel=None, out=None, stre
     return out
 
 
-def _setting(v, name: str, scalar, kind, n_rows: int):
-    """(the call's value, address of the rows' values, tensor or None)"""
-    if not hasattr(v, "data_ptr"):
-        return v, 0, None
-    _need(v.dtype == kind and v.is_contiguous() and v.numel() == n_rows, "%s: a number, or contiguous %s for each row" % (name, kind))
-    return scalar, v.data_ptr(), v
-
-
-def _sampling(torch, temperature, top_k, top_p, min_p, most_k, n_rows):
-    t, pt, ht = _setting(temperature, "temperature", 1.0, torch.float32, n_rows)
-    k, pk, hk = _setting(top_k, "top_k", int(most_k), torch.int32, n_rows)
-    p, pp, hp = _setting(top_p, "top_p", 1.0, torch.float32, n_rows)
-    m, pm, hm = _setting(min_p, "min_p", 0.0, torch.float32, n_rows)
-    return _Sampling(t, k, p, m, pt, pk, pp, pm), (ht, hk, hp, hm)
+def _sampling(temperature, top_k, top_p, min_p, most_k, n_rows):
+    """(the settings, the tensors among them): a setting is a number, or a tensor with one for each row."""
+    if not any(hasattr(v, "data_ptr") for v in (temperature, top_k, top_p, min_p)):
+        return _Sampling(temperature, top_k, top_p, min_p, None, None, None, None), ()
+    torch = sys.modules["torch"]
+    call, rows, kept = [1.0, int(most_k), 1.0, 0.0], [None] * 4, []
+    for i, (v, name) in enumerate(((temperature, "temperature"), (top_k, "top_k"), (top_p, "top_p"), (min_p, "min_p"))):
+        if not hasattr(v, "data_ptr"):
+            call[i] = v
+            continue
+        kind = torch.int32 if i == 1 else torch.float32
+        _need(v.dtype == kind and v.is_contiguous() and v.numel() == n_rows, "%s: a number, or contiguous %s for each row" % (name, kind))
+        rows[i] = v.data_ptr()
+        kept.append(v)
+    return _Sampling(*call, *rows), tuple(kept)
 
 
 def sample_workspace_bytes(n_rows: int, n_cols: int, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, most_k: int = 0) -> int:
-    how, _ = _sampling(sys.modules["torch"], temperature, top_k, top_p, min_p, most_k, n_rows)
+    how, _ = _sampling(temperature, top_k, top_p, min_p, most_k, n_rows)
     n = load().kge_sample_workspace_bytes(C.byref(how), n_rows, n_cols)
     if n == 0:
         raise KgeError(-1, load().kge_last_error().decode())
@@ -911,19 +914,23 @@ def sample_scores(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mos
     _need(u.dim() == 2 and u.shape[0] == n and u.is_contiguous() and u.dtype in (torch.float32, torch.float64),
           "u: contiguous float32 or float64 is wanted, a row for each row of scores")
     draws = u.shape[1]
-    how, kept = _sampling(torch, temperature, top_k, top_p, min_p, most_k, n)
+    how, kept = _sampling(temperature, top_k, top_p, min_p, most_k, n)
     choice = _new(scores, (n, draws), torch.int32, stream) if choice is None else choice
     if prob is None and want_prob:
         prob = _new(scores, (n, draws), torch.float32, stream)
     _need(choice.dtype == torch.int32 and choice.is_contiguous() and choice.numel() == n * draws, "choice: contiguous int32 is wanted, one for each draw")
     pp = _vector(prob, "prob", n * draws)
-    need = load().kge_sample_workspace_bytes(C.byref(how), n, cols)
-    if need == 0:
-        raise KgeError(-1, load().kge_last_error().decode())
-    workspace = _workspace(workspace, need, scores, stream)
+    at = size = 0
+    if cols <= SAMPLE_ROW:
+        workspace = None
+    else:
+        size = load().kge_sample_workspace_bytes(C.byref(how), n, cols)
+        if size == 0:
+            raise KgeError(-1, load().kge_last_error().decode())
+        workspace = _workspace(workspace, size, scores, stream)
+        at, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _call(load().kge_sample_scores, stream, scores, (u, choice, prob, workspace) + kept, C.byref(how), n, cols, s, dt, lds, u.data_ptr(),
-          64 if u.dtype == torch.float64 else 32, draws, choice.data_ptr(), pp, workspace.data_ptr(),
-          workspace.numel() * workspace.element_size())
+          64 if u.dtype == torch.float64 else 32, draws, choice.data_ptr(), pp, at, size)
     return choice, prob
 
 

@@ -353,7 +353,7 @@ __device__ __forceinline__ u64 digit_total(const u64 *hist, u64 (&v)[(1 << BITS)
     return total;
 }
 template <int NT, int BITS>
-__device__ __forceinline__ int digit_at(const u64 (&v)[(1 << BITS) / NT], u64 upto, u64 goal, u64 *s_found, u64 *above, u64 *own)
+__device__ __forceinline__ int digit_at(const u64 (&v)[(1 << BITS) / NT], u64 upto, u64 goal, u64 *s_found, u64 *above, u64 *own, const uint32_t *counts = nullptr)
 {
     constexpr int PER = (1 << BITS) / NT;
     const int hi = (1 << BITS) - 1 - PER * Team<NT>::tid();
@@ -363,7 +363,10 @@ __device__ __forceinline__ int digit_at(const u64 (&v)[(1 << BITS) / NT], u64 up
     if (before < goal && goal <= upto) {
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            if (before < goal && goal <= before + v[k]) { s_found[0] = hi - k; s_found[1] = before; s_found[2] = v[k]; }
+            if (before < goal && goal <= before + v[k]) {
+                s_found[0] = hi - k; s_found[1] = before; s_found[2] = v[k];
+                if (counts) s_found[3] = counts[k];
+            }
             before += v[k];
         }
     }
@@ -410,7 +413,7 @@ __device__ __forceinline__ Cut cut_at(int which, const S &x, u64 own, const Cut 
 template <int NT, int TILES, bool ONE, class Source>
 struct Keys {
     static constexpr int V = 4 * TILES, BATCH = NT * V;
-    static constexpr bool HELD = ONE && NT < 1024;
+    static constexpr bool WHOLE = ONE, HELD = ONE && NT < 1024;
     const Source &src;
     uint32_t key[V];
     double w[HELD ? V : 1];
@@ -455,6 +458,37 @@ struct Keys {
     }
 };
 
+// The cut of top-k for a wavefront's row, bit by bit from the first at which the largest key and a lower bound differ: a comparison and a count of
+// lanes for each key is all a bit takes.  Ends where exactly k keys are not below what is tried.
+template <class K>
+__device__ __forceinline__ void find_kth(K &keys, int32_t k, uint32_t low, uint32_t most, Cut &cut)
+{
+    const auto from = [&](uint32_t at) {         // keys not below it
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < K::V; ++i) n += (int)__popcll(__ballot(keys.key[i] >= at));
+        return n;
+    };
+    if (from(low) < k) return;                   // fewer scores than k
+    int bits = 32 - (int)__builtin_clz((most ^ low) | 1u), n = 0;
+    uint32_t at = bits < 32 ? most >> bits << bits : 0u;
+    for (; bits > 0; --bits) {
+        const uint32_t next = at | 1u << (bits - 1);
+        const int here = from(next);
+        if (here < k) continue;
+        at = next;
+        n = here;
+        if (n == k) break;
+    }
+    // the least of those keys
+    uint32_t least = 0xffffffffu;
+#pragma unroll
+    for (int i = 0; i < K::V; ++i) least = min(least, keys.key[i] >= at ? keys.key[i] : 0xffffffffu);
+    least = ~wave_max(~least);
+    const int above = from(least + 1u), all = from(least);
+    cut = Cut{least, all == k, (u64)(k - above)};
+}
+
 // limit: as soon as no more than so many scores are at or above the least that has the digits found, the search for top-k's cut ends; the cut is
 // then that score's key, and true is returned: what is left holds the first k, and may hold more
 template <int NT, int BITS, class K>
@@ -462,6 +496,8 @@ __device__ __forceinline__ bool find_cut(int which, uint32_t limit, K &keys, con
                                          u64 *s_found)
 {
     if (!cuts(which, set, keys.src.n)) return false;
+    // a wavefront's row has up to 1024 scores: their number fits beside their weights, and where a digit has one score the search ends
+    constexpr int PACK = NT == 64 && K::WHOLE ? 11 : 0;
     const int tid = Team<NT>::tid();
     Search<BITS> x;
     x.begin(low, most);
@@ -475,17 +511,33 @@ __device__ __forceinline__ bool find_cut(int which, uint32_t limit, K &keys, con
                 const uint32_t key = keys.key[i];
                 if (!x.in(key) || (which == 1 && key <= cut.key)) continue;
                 const u64 w = which == 0 ? 1ull : whole(keys.weight(i, weigh));
-                if (w) atomicAdd(&hist[x.digit(key)], w);
+                if (w) atomicAdd(&hist[x.digit(key)], PACK ? w << PACK | 1ull : w);
             }
         });
-        if (which == 1 && tid == 0 && cut.key && x.in(cut.key)) atomicAdd(&hist[x.digit(cut.key)], cut.ties * weigh(cut.key));
+        if (which == 1 && tid == 0 && cut.key && x.in(cut.key)) {
+            const u64 w = cut.ties * weigh(cut.key);
+            atomicAdd(&hist[x.digit(cut.key)], PACK ? w << PACK | cut.ties : w);
+        }
         Team<NT>::sync();
         u64 v[(1 << BITS) / NT], upto, more, own;
-        const u64 all = digit_total<NT, BITS>(hist, v, &upto, s);
+        uint32_t counts[(1 << BITS) / NT];
+        const u64 all = digit_total<NT, BITS>(hist, v, &upto, s) >> PACK;
+        upto >>= PACK;
+#pragma unroll
+        for (int k = 0; k < (1 << BITS) / NT; ++k) {
+            counts[k] = (uint32_t)v[k] & ((1u << PACK) - 1u);
+            v[k] >>= PACK;
+        }
         if (first) x.goal = which == 0 ? goal_of_count(all, set) : goal_of_weight(all, set);
         if (x.goal == 0ull) return false;
-        const int digit = digit_at<NT, BITS>(v, upto, x.goal - x.above, s_found, &more, &own);
+        const int digit = digit_at<NT, BITS>(v, upto, x.goal - x.above, s_found, &more, &own, PACK ? counts : nullptr);
+        const bool lone = PACK && s_found[3] == 1ull;
+        Team<NT>::sync();
         x.step(digit, more);
+        if (lone && (x.first() > cut.key || cut.every)) {
+            cut = Cut{x.first(), true, 1ull};
+            return true;
+        }
         if (which == 0 && x.above + own <= (u64)limit) {
             cut = Cut{x.first(), true, ~0ull};
             return true;
@@ -609,8 +661,7 @@ __device__ __forceinline__ u64 pick4(const Call &o, int64_t at, const Source &sr
 }
 
 constexpr int RUN = 256;           // columns that a wavefront weighs at once
-constexpr int RUNS_MOST = 1024;    // of a row that a block takes
-constexpr int64_t ROW_MOST = RUN * RUNS_MOST;
+constexpr int64_t ROW_MOST = RUN * 1024;      // columns of a row that a block takes: a thread has a run
 
 // A row of which up to FEW scores, top-k's among them, are at or above the cut: one wavefront has them, one a lane, and counts for each those before
 // it, by score and by column
@@ -694,11 +745,23 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
         for (int32_t i = tid; i < o.n_draws; i += NT) answer(o, first + i, -1, 0.0, 1.0);
         return;
     }
+    if (set.k == 1) {                                            // the first column of the largest score
+        uint32_t at = ~0u;
+        keys.each(0, [&](int32_t c0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (keys.key[i] == most) at = min(at, (uint32_t)(c0 + 4 * (NT * (i / 4) + tid) + i % 4));
+        });
+        at = ~T::most(~at, s);
+        for (int32_t i = tid; i < o.n_draws; i += NT) answer(o, first + i, src.column((int32_t)at), 1.0, 1.0);
+        return;
+    }
     Weigh weigh;
     weigh.init(most, set.t, o, pow);
-    Cut cut = first_cut(set, most);
+    Cut cut{0u, true, 0ull};
     if (cuts(0, set, src.n)) {
-        const bool few = find_cut<NT, BITS>(0, NT > 64 && set.k <= FEW && o.n_draws <= FEW ? FEW : 0u, keys, set, weigh, low_of<NT>(mine, set.k, s), most, cut, hist,
+        if constexpr (NT == 64 && ONE) find_kth(keys, set.k, low_of<NT>(mine, set.k, s), most, cut);
+        const bool few = !(NT == 64 && ONE) && find_cut<NT, BITS>(0, NT > 64 && set.k <= FEW && o.n_draws <= FEW ? FEW : 0u, keys, set, weigh, low_of<NT>(mine, set.k, s), most, cut, hist,
                                             s, s_found);
         if constexpr (NT > 64) {
             if (few) {
@@ -742,7 +805,6 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
         }
         T::sync();
     } else {
-        static_assert(RUNS_MOST <= NT, "a thread has a run");
         u64 total;
         const int runs = (src.n + RUN - 1) / RUN;
         if (!cut.every) {
@@ -792,13 +854,14 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
     }
 }
 
-// NT 64: four rows a block, a wavefront each
+// NT 64: four rows a block, a wavefront each.  Wavefronts at once to a SIMD: what LDS leaves room for
+constexpr int waves_of(int nt, int tiles, bool one) { return nt == 64 && one ? (tiles == 1 ? 5 : 3) : 4; }
 template <bool BF16, int NT, int TILES, bool ONE, bool PARTS>
-__global__ __launch_bounds__(NT == 64 ? 256 : NT) void k_rows(Call o)
+__global__ __launch_bounds__(NT == 64 ? 256 : NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT, TILES, ONE)))) void k_rows(Call o)
 {
     constexpr int BITS = NT == 64 ? 8 : NT == 256 ? 11 : 12, TEAMS = NT == 64 ? 4 : 1, COLUMNS = 4 * TILES * NT;
     constexpr bool BY_COLUMN = ONE && COLUMNS <= 4096;
-    __shared__ u64 s_hist[TEAMS][1 << BITS], s_sums[TEAMS][BY_COLUMN ? COLUMNS : RUNS_MOST], s_ties[BY_COLUMN ? 1 : RUNS_MOST];
+    __shared__ u64 s_hist[TEAMS][1 << BITS], s_sums[TEAMS][BY_COLUMN ? COLUMNS : NT], s_ties[TEAMS][BY_COLUMN ? 1 : NT];
     __shared__ u64 s_part[TEAMS][16], s_found[TEAMS][4];
     __shared__ double s_pow[POWERS];
     fill_pow(s_pow, o.bits);
@@ -806,10 +869,10 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void k_rows(Call o)
     for (int64_t r = (int64_t)blockIdx.x * TEAMS + team; r < o.n_rows; r += (int64_t)gridDim.x * TEAMS) {
         if constexpr (PARTS) {
             const Parts src{o.part_key + r * o.n_part, o.part_col + r * o.n_part, o.n_part};
-            draw_row<NT, TILES, ONE, BITS>(o, r, src, s_hist[team], s_sums[team], s_ties, s_part[team], s_found[team], s_pow);
+            draw_row<NT, TILES, ONE, BITS>(o, r, src, s_hist[team], s_sums[team], s_ties[team], s_part[team], s_found[team], s_pow);
         } else {
             const Scores<BF16> src{(const char *)o.scores + r * o.lds * (BF16 ? 2 : 4), o.n_cols};
-            draw_row<NT, TILES, ONE, BITS>(o, r, src, s_hist[team], s_sums[team], s_ties, s_part[team], s_found[team], s_pow);
+            draw_row<NT, TILES, ONE, BITS>(o, r, src, s_hist[team], s_sums[team], s_ties[team], s_part[team], s_found[team], s_pow);
         }
     }
 }
@@ -1190,7 +1253,7 @@ int bits_of(int64_t n_cols)
 constexpr int64_t LONG_BLOCKS = 1 << 22;      // of one launch
 
 // Rows that a block takes whole, however few there are, and rows enough for a block each
-constexpr int64_t BLOCK_ROW = 65536, MANY_ROWS = 256;
+constexpr int64_t BLOCK_ROW = KGE_SAMPLE_ROW, MANY_ROWS = 256;
 
 // How a call runs, by its sizes and what the host knows of its settings
 struct Plan {
@@ -1256,7 +1319,13 @@ int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
 {
     if (o.n_cols <= 256) return launch_rows<BF16, 64, 1, true, false>(o, st);
     if (o.n_cols <= 1024) return launch_rows<BF16, 64, 4, true, false>(o, st);
-    if (o.n_cols <= 4096) return launch_rows<BF16, 256, 4, true, false>(o, st);
+    // Rows of little more: a wavefront a row, which reads them again, or a block.  No settings, us, wavefront / block: 16384 x 1100 96 / 157, 8192 x 2000
+    // 52 / 83, 4096 x 4000 45 / 48, 2048 x 4000 29 / 26, 1024 x 1100 15 / 13
+    if (o.n_cols <= 2048 && o.n_rows >= 4096) return launch_rows<BF16, 64, 4, false, false>(o, st);
+    if (o.n_cols <= 4096) return launch_rows<BF16, 256, 4, false, false>(o, st);
+    // Rows enough for several blocks to a compute unit: small ones, whose waits overlap.  No settings, us, 256 threads / 1024: 2048 x 14541 66 / 96, 600 x
+    // 60000 89 / 101, 300 x 14541 24 with 1024
+    if (o.n_cols <= RUN * 256 && o.n_rows >= 512) return launch_rows<BF16, 256, 4, false, false>(o, st);
     if (o.n_cols <= 16384) return launch_rows<BF16, 1024, 4, true, false>(o, st);
     if (p.parts == 0) return launch_rows<BF16, 1024, 4, false, false>(o, st);
     if (p.most_k) {
@@ -1270,7 +1339,7 @@ int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
         }
         o.part_key = part_key; o.part_col = part_col; o.n_part = p.parts * p.slots;
         if (o.n_part <= 1024) return launch_rows<BF16, 64, 4, true, true>(o, st);
-        if (o.n_part <= 4096) return launch_rows<BF16, 256, 4, true, true>(o, st);
+        if (o.n_part <= 4096) return launch_rows<BF16, 256, 4, false, true>(o, st);
         if (o.n_part <= 16384) return launch_rows<BF16, 1024, 4, true, true>(o, st);
         return launch_rows<BF16, 1024, 4, false, true>(o, st);
     }
@@ -1344,15 +1413,17 @@ extern "C" int kge_sample_scores(const kge_sampling *how, int64_t n_rows, int64_
     KGE_REQUIRE((scores || n_cols == 0) && u && choice, KGE_EINVAL, "NULL array");
     KGE_REQUIRE((uintptr_t)scores % (dtype == KGE_DT_F32 ? 4 : 2) == 0 && (uintptr_t)u % (u_bits / 8) == 0 && (uintptr_t)choice % 4 == 0 &&
                     (uintptr_t)prob % 4 == 0, KGE_EINVAL, "an array is not aligned to its elements");
-    KGE_REQUIRE(workspace && (uintptr_t)workspace % 256 == 0, KGE_EINVAL, "the workspace is NULL or not aligned to 256 bytes");
-    KGE_REQUIRE(ws_bytes >= kge_sample_workspace_bytes(how, n_rows, n_cols), KGE_ENOMEM, "the workspace is too small");
+    const Plan p = plan_of(how, n_rows, n_cols);
+    if (n_cols > KGE_SAMPLE_ROW) {
+        KGE_REQUIRE(workspace && (uintptr_t)workspace % 256 == 0, KGE_EINVAL, "the workspace is NULL or not aligned to 256 bytes");
+        KGE_REQUIRE(ws_bytes >= p.bytes, KGE_ENOMEM, "the workspace is too small");
+    }
     hipStream_t st = (hipStream_t)stream;
     Call o;
     o.how = Sampling{how->temperature, how->top_p, how->min_p, how->top_k, how->row_temperature, how->row_top_p, how->row_min_p, how->row_top_k};
     o.scores = scores; o.u = u; o.choice = choice; o.prob = prob; o.n_rows = n_rows; o.lds = lds;
     o.n_cols = (int32_t)n_cols; o.n_draws = n_draws; o.bits = bits_of(n_cols); o.u64bit = u_bits == 64;
     o.part_key = nullptr; o.part_col = nullptr; o.n_part = 0; o.per = per_of(how->temperature);
-    const Plan p = plan_of(how, n_rows, n_cols);
     KGE_PROF("sample_scores", st);
     return dtype == KGE_DT_BF16 ? launch_call<true>(o, p, (char *)workspace, st) : launch_call<false>(o, p, (char *)workspace, st);
 }

@@ -110,7 +110,8 @@ def test_table4_scores(kb, change, status, word):
     (dict(p=0.0), EINVAL, "top_p"), (dict(p=1.5), EINVAL, "top_p"), (dict(p=math.nan), EINVAL, "top_p"), (dict(m=-0.1), EINVAL, "min_p"), (dict(m=1.1), EINVAL, "min_p"),
     (dict(dtype=2), EINVAL, "type"), (dict(ub=16), EINVAL, "bits"), (dict(draws=-1), EINVAL, "draws"), (dict(lds=9), EINVAL, "stride"), (dict(s=None), EINVAL, "NULL"),
     (dict(u=None), EINVAL, "NULL"), (dict(choice=None), EINVAL, "NULL"), (dict(s=4098), EINVAL, "aligned"), (dict(u=4100, ub=64), EINVAL, "aligned"),
-    (dict(ws=None), EINVAL, "workspace"), (dict(ws=64), EINVAL, "workspace"), (dict(size=0), ENOMEM, "workspace"), (dict(row_k=4098), EINVAL, "settings")])
+    (dict(ws=None, cols=65537, lds=65537), EINVAL, "workspace"), (dict(ws=64, cols=65537, lds=65537), EINVAL, "workspace"),
+    (dict(size=0, cols=65537, lds=65537), ENOMEM, "workspace"), (dict(row_k=4098), EINVAL, "settings")])
 def test_sample_scores(kb, change, status, word):
     a = dict(rows=3, cols=10, t=1.0, k=5, p=0.9, m=0.1, dtype=0, ub=32, draws=2, lds=10, s=4096, u=4096, choice=4096, ws=4096, size=1 << 30, row_k=None)
     a.update(change)
@@ -118,7 +119,7 @@ def test_sample_scores(kb, change, status, word):
     rc = kb.load().kge_sample_scores(C.byref(how), a["rows"], a["cols"], a["s"], a["dtype"], a["lds"], a["u"], a["ub"], a["draws"], a["choice"], None, a["ws"],
                                      a["size"], None)
     assert rc == status and said(kb, word)
-    if set(change) & {"rows", "cols", "t", "k", "p", "m", "row_k"}:
+    if set(change) & {"rows", "t", "k", "p", "m", "row_k"} or a["cols"] < 0 or a["cols"] >= 1 << 31:
         assert kb.load().kge_sample_workspace_bytes(C.byref(how), a["rows"], a["cols"]) == 0
 
 
