@@ -107,6 +107,21 @@ struct Scores {
 #pragma unroll
         for (int k = 0; k < 4; ++k) key[k] = key_of(l[k]);
     }
+    // 1024 columns of a wavefront from column c0 on: 4 j .. + 3 of each 256 for lane j, minus infinity past the end
+    __device__ __forceinline__ void run16(int32_t c0, int lane, float l[16]) const
+    {
+        const int32_t c = c0 + 4 * lane;
+        if (c0 + 1024 <= n) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) score4(c + 256 * j, l + 4 * j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int32_t at = c + 256 * (j / 4) + j % 4;
+                l[j] = at < n ? one(at) : -INFINITY;
+            }
+        }
+    }
     __device__ __forceinline__ uint32_t key(int32_t c) const { return key_of(one(c)); }
     __device__ __forceinline__ int32_t column(int32_t c) const { return c; }
 };
@@ -940,7 +955,9 @@ __global__ __launch_bounds__(NT) void k_part_top(Call o, int64_t row0, int32_t p
     for (int32_t i = written + tid; i < slots; i += NT) out_key[i] = 0u;
 }
 
-// ---- long rows: a launch a digit
+// ---- long rows: a launch a digit.  Once top-p's first digit is found, what has a larger one is left for certain: the next launch sums its weights, by
+// runs of columns, beside the sums by the second digit, and lists the scores with the first; the third digit and the sums of what is
+// left of the list read the list alone.  A part with more of them than its list has room for is read again.
 
 struct State {                     // of a row, after a launch
     Search<11> x;
@@ -957,7 +974,10 @@ struct Long {
     State *state;                  // [rows][7]
     u64 *part_sum, *part_ties;     // [rows][parts]: weights above the cut, ties of it
     u64 *run_sum, *run_ties;       // [rows][parts][part / LONG_RUN]
+    uint2 *list;                   // [rows][parts][part / LIST_PART]: scores with top-p's first digit, and their columns
+    uint32_t *listed;              // [rows][parts]: their number, which may be more than there is room for
 };
+constexpr int LIST_PART = 4;
 constexpr int LONG_T = 256, LONG_DIGITS = 2048;
 constexpr int LONG_RUN = 1024;      // columns whose weights are summed
 
@@ -1012,12 +1032,11 @@ __device__ __forceinline__ State advance(const Long &a, int64_t r, int before, i
     return st;
 }
 
-// sums by digit of a search's level; prev: the stage of the launch before, `before` the one before that
+// sums by digit of a search's level - of top-p's the first; prev: the stage of the launch before, `before` the one before that
 template <bool BF16>
 __global__ __launch_bounds__(LONG_T) void k_long_digit(Long a, int which, int level, int before, int prev)
 {
     __shared__ u64 s_hist[LONG_DIGITS], s_part[16], s_found[4];
-    __shared__ uint32_t s_queue[LONG_T / 64][9 * 64];
     __shared__ double s_pow[POWERS];
     fill_pow(s_pow, a.o.bits);
     const int64_t r = blockIdx.x / (unsigned)a.parts;
@@ -1033,57 +1052,25 @@ __global__ __launch_bounds__(LONG_T) void k_long_digit(Long a, int which, int le
     // what has the digits found before lies between two scores; of it top-p counts what is above top-k's cut
     const uint32_t low = st.x.first(), high = (uint32_t)min(st.x.last(), (u64)st.most);
     const float from = score_of(which == 1 && st.cut.key >= low ? st.cut.key + 1u : low), upto = score_of(high);
-    uint32_t *queue = s_queue[threadIdx.x >> 6];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int waiting = 0;
     auto add = [&](float l, u64 w) { atomicAdd(&s_hist[st.x.digit(key_in_order(l))], w); };
-    auto weigh_some = [&](int first, int n) {
-        Team<64>::sync();
-        if (lane < n) {
-            const float l = __uint_as_float(queue[first + lane]);
-            add(l, weigh(key_of(l)));
-        }
-        Team<64>::sync();
-    };
     for (int32_t c0w = c0 + LONG_RUN * wave; c0w < src.n; c0w += LONG_RUN * (LONG_T / 64)) {
-        const int32_t c = c0w + 4 * lane;
         float l[16];
-        if (c0w + LONG_RUN <= src.n) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) src.score4(c + RUN * j, l + 4 * j);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const int32_t at = c + RUN * (j / 4) + j % 4;
-                l[j] = at < src.n ? src.one(at) : -INFINITY;
-            }
-        }
+        src.run16(c0w, lane, l);
         if (which == 0) {
 #pragma unroll
             for (int k = 0; k < 16; ++k)
                 if (l[k] >= from && l[k] <= upto) add(l[k], 1ull);
-        } else if (level == 0 && !weigh.endless) {               // all that have a weight, most scores
+        } else if (!weigh.endless) {
 #pragma unroll
             for (int k = 0; k < 16; ++k)
                 if (l[k] >= from) add(l[k], (u64)__double_as_longlong(weigh.raised(l[k])) & 0xfffffffffffffull);
-        } else {                                                 // few: they are gathered, so that whole wavefronts weigh
+        } else {
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const bool hit = l[k] >= from && l[k] <= upto;
-                const u64 all = __ballot(hit);
-                if (hit) queue[waiting + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0u))] = __float_as_uint(l[k]);
-                waiting += (int)__popcll(all);
-                if (k % 8 == 7) {
-#pragma unroll 1
-                    while (waiting >= 64) {
-                        waiting -= 64;
-                        weigh_some(waiting, 64);
-                    }
-                }
-            }
+            for (int k = 0; k < 16; ++k)
+                if (l[k] >= from && l[k] == INFINITY) add(l[k], weigh.unit());
         }
     }
-    weigh_some(0, waiting);
     if (which == 1 && part == 0 && threadIdx.x == 0 && st.cut.key && st.x.in(st.cut.key))
         atomicAdd(&s_hist[st.x.digit(st.cut.key)], st.cut.ties * weigh(st.cut.key));
     __syncthreads();
@@ -1092,42 +1079,66 @@ __global__ __launch_bounds__(LONG_T) void k_long_digit(Long a, int which, int le
         if (s_hist[i]) atomicAdd(&hist[i], s_hist[i]);
 }
 
-// the weights above the cut and the ties of it, by runs of 256 columns and by part
-template <bool BF16>
-__global__ __launch_bounds__(LONG_T) void k_long_sums(Long a, int before, int prev)
+// scores that a search's digits found leave open, from top-k's cut on
+struct Range { float from, upto; };
+__device__ __forceinline__ Range range_of(const State &st)
 {
-    __shared__ u64 s_part[16], s_found[4];
+    return Range{score_of(max(st.x.first(), st.cut.key)), score_of((uint32_t)min(st.x.last(), (u64)st.most))};
+}
+
+// The weights above the cut and the ties of it, by runs of columns and by part.  Where top-p's search is open (its first digit is found), what is
+// above that digit counts; what has it is listed, and its weights go to the sums by the second digit
+template <bool BF16>
+__global__ __launch_bounds__(LONG_T) void k_long_sums(Long a, int before, int prev, int slot)
+{
+    __shared__ u64 s_hist[LONG_DIGITS], s_part[16], s_found[4];
+    __shared__ uint2 s_queue[LONG_T / 64][5 * 64];
     __shared__ double s_pow[POWERS];
+    __shared__ uint32_t s_listed;
+    if (threadIdx.x == 0) s_listed = 0u;
     fill_pow(s_pow, a.o.bits);
-    const int64_t r = blockIdx.x / (unsigned)a.parts;
+    const int64_t r = blockIdx.x / (unsigned)a.parts, here = blockIdx.x;
     const int32_t part = (int32_t)(blockIdx.x % (unsigned)a.parts), c0 = part * a.part;
     const Setting set = setting_of(a.o.how, a.row0 + r);
     Weigh weigh;
     const State st = advance(a, r, before, prev, -1, set, &weigh, s_pow, s_part, s_found);
-    if (part == 0 && threadIdx.x == 0) a.state[r * 7 + 6] = st;      // slot 6: the last stage's own, or of stages that none of this call's are
+    if (part == 0 && threadIdx.x == 0) a.state[r * 7 + slot] = st;
+    const bool open = st.x.open;
+    if (open) {
+        for (int i = threadIdx.x; i < LONG_DIGITS; i += LONG_T) s_hist[i] = 0ull;
+        __syncthreads();
+    }
     const u64 least = least_weight(set, weigh);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), min(a.o.n_cols, c0 + a.part)};
     const int32_t runs = a.part / LONG_RUN;
-    u64 sum = 0ull, ties = 0ull;
     // What counts as a range of scores: above the cut, and what is equal to it if all that is does.  1024 weights of 2^40 units are a whole
     // number that a double holds
-    const float tie = score_of(st.cut.key), edge = st.cut.key == 0u ? -INFINITY : st.cut.every ? tie : score_of(st.cut.key + 1u);
+    const Range maybe = range_of(st);
+    const float tie = score_of(st.cut.key);
+    const float edge = open ? (st.x.last() >= st.most ? NAN : score_of((uint32_t)st.x.last() + 1u))
+                            : st.cut.key == 0u ? -INFINITY : st.cut.every ? tie : score_of(st.cut.key + 1u);
     const double fewest = (double)least;
-    const bool all = least <= 1ull;
-    for (int32_t i = wave; i < runs && c0 + LONG_RUN * i < src.n; i += LONG_T / 64) {
-        const int32_t c = c0 + LONG_RUN * i + 4 * lane;
-        float l[16];
-        if (c0 + LONG_RUN * (i + 1) <= src.n) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) src.score4(c + RUN * j, l + 4 * j);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const int32_t at = c + RUN * (j / 4) + j % 4;
-                l[j] = at < src.n ? src.one(at) : -INFINITY;
-            }
+    const bool all = least <= 1ull, count_ties = !open && !st.cut.every;
+    uint2 *list = a.list + here * (a.part / LIST_PART), *queue = s_queue[wave];
+    int waiting = 0;
+    const auto weigh_some = [&](int first, int n) {
+        Team<64>::sync();
+        uint32_t at = 0u;
+        if (lane == 0) at = atomicAdd(&s_listed, (uint32_t)n);
+        at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at) + lane;
+        if (lane < n) {
+            const uint2 e = queue[first + lane];
+            const uint32_t key = key_in_order(__uint_as_float(e.x));
+            if (at < (uint32_t)(a.part / LIST_PART)) list[at] = e;
+            if (key > st.cut.key) atomicAdd(&s_hist[st.x.digit(key)], weigh(key));
         }
+        Team<64>::sync();
+    };
+    u64 sum = 0ull, ties = 0ull;
+    for (int32_t i = wave; i < runs && c0 + LONG_RUN * i < src.n; i += LONG_T / 64) {
+        float l[16];
+        src.run16(c0 + LONG_RUN * i, lane, l);
         u64 w = 0ull, t = 0ull;
         double lanes = 0.0;
         if (weigh.endless) {
@@ -1144,27 +1155,143 @@ __global__ __launch_bounds__(LONG_T) void k_long_sums(Long a, int before, int pr
             }
         }
         w = st.most ? whole(lane_of(wave_scan(lanes), 63)) : 0ull;
-        if (!st.cut.every) {
+        if (count_ties) {
 #pragma unroll
             for (int k = 0; k < 16; ++k) t += l[k] == tie ? 1ull : 0ull;
             t = wave_sum(t);
         }
         if (lane == 0) {
-            const int64_t at = (r * a.parts + part) * runs + i;
-            a.run_sum[at] = w;
-            a.run_ties[at] = t;
+            a.run_sum[here * runs + i] = w;
+            a.run_ties[here * runs + i] = t;
         }
         sum += w;
         ties += t;
+        if (open) {                                              // gathered, so that whole wavefronts weigh
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const bool hit = l[k] >= maybe.from && l[k] <= maybe.upto;
+                const u64 hits = __ballot(hit);
+                if (hit) {
+                    const int at = waiting + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, 0u));
+                    queue[at] = make_uint2(__float_as_uint(l[k]), (uint32_t)(c0 + LONG_RUN * i + RUN * (k / 4) + 4 * lane + k % 4));
+                }
+                waiting += (int)__popcll(hits);
+                if (k % 4 == 3) {
+#pragma unroll 1
+                    while (waiting >= 64) {
+                        waiting -= 64;
+                        weigh_some(waiting, 64);
+                    }
+                }
+            }
+        }
     }
+    if (open) weigh_some(0, waiting);
     // every lane of a wavefront has its sums
     if (lane == 0) { s_part[wave] = sum; s_part[8 + wave] = ties; }
+    if (open && part == 0 && threadIdx.x == 0 && st.cut.key && st.x.in(st.cut.key)) atomicAdd(&s_hist[st.x.digit(st.cut.key)], st.cut.ties * weigh(st.cut.key));
     __syncthreads();
     if (threadIdx.x == 0) {
         sum = ties = 0ull;
         for (int i = 0; i < LONG_T / 64; ++i) { sum += s_part[i]; ties += s_part[8 + i]; }
-        a.part_sum[r * a.parts + part] = sum;
-        a.part_ties[r * a.parts + part] = ties;
+        a.part_sum[here] = sum;
+        a.part_ties[here] = ties;
+        a.listed[here] = s_listed;
+    }
+    if (!open) return;
+    u64 *hist = a.hist + (r * 6 + 4) * LONG_DIGITS;
+    for (int i = threadIdx.x; i < LONG_DIGITS; i += LONG_T)
+        if (s_hist[i]) atomicAdd(&hist[i], s_hist[i]);
+}
+
+// f(score, column) for what a part's list holds, or should: scores in `range`
+template <bool BF16, class F>
+__device__ __forceinline__ void each_listed(const Long &a, int64_t here, const Scores<BF16> &src, int32_t c0, const Range &range, F f)
+{
+    const uint32_t n = a.listed[here];
+    if (n <= (uint32_t)(a.part / LIST_PART)) {
+        const uint2 *list = a.list + here * (a.part / LIST_PART);
+        for (uint32_t i = threadIdx.x; i < n; i += LONG_T) f(__uint_as_float(list[i].x), (int32_t)list[i].y);
+    } else {
+#pragma unroll 1
+        for (int32_t c = c0 + (int)threadIdx.x; c < src.n; c += LONG_T) {
+            const float l = src.one(c);
+            if (l >= range.from && l <= range.upto) f(l, c);
+        }
+    }
+}
+
+// sums by top-p's third digit
+template <bool BF16>
+__global__ __launch_bounds__(LONG_T) void k_long_third(Long a)
+{
+    __shared__ u64 s_hist[LONG_DIGITS], s_part[16], s_found[4];
+    __shared__ double s_pow[POWERS];
+    fill_pow(s_pow, a.o.bits);
+    const int64_t r = blockIdx.x / (unsigned)a.parts, here = blockIdx.x;
+    const int32_t part = (int32_t)(blockIdx.x % (unsigned)a.parts), c0 = part * a.part;
+    const Setting set = setting_of(a.o.how, a.row0 + r);
+    Weigh weigh;
+    const State st = advance(a, r, 3, 4, -1, set, &weigh, s_pow, s_part, s_found);
+    if (part == 0 && threadIdx.x == 0) a.state[r * 7 + 5] = st;
+    if (!st.x.open) return;
+    for (int i = threadIdx.x; i < LONG_DIGITS; i += LONG_T) s_hist[i] = 0ull;
+    __syncthreads();
+    const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), min(a.o.n_cols, c0 + a.part)};
+    each_listed(a, here, src, c0, range_of(a.state[r * 7 + 4]), [&](float l, int32_t) {
+        const uint32_t key = key_in_order(l);
+        if (key > st.cut.key && st.x.in(key)) atomicAdd(&s_hist[st.x.digit(key)], weigh(key));
+    });
+    if (part == 0 && threadIdx.x == 0 && st.cut.key && st.x.in(st.cut.key)) atomicAdd(&s_hist[st.x.digit(st.cut.key)], st.cut.ties * weigh(st.cut.key));
+    __syncthreads();
+    u64 *hist = a.hist + (r * 6 + 5) * LONG_DIGITS;
+    for (int i = threadIdx.x; i < LONG_DIGITS; i += LONG_T)
+        if (s_hist[i]) atomicAdd(&hist[i], s_hist[i]);
+}
+
+// what is left of the lists, added to the sums by runs and parts
+template <bool BF16>
+__global__ __launch_bounds__(LONG_T) void k_long_rest(Long a)
+{
+    constexpr int RUNS_MOST = 32;
+    __shared__ u64 s_part[16], s_found[4], s_sum[RUNS_MOST], s_ties[RUNS_MOST];
+    __shared__ double s_pow[POWERS];
+    if (threadIdx.x < RUNS_MOST) s_sum[threadIdx.x] = s_ties[threadIdx.x] = 0ull;
+    fill_pow(s_pow, a.o.bits);
+    const int64_t r = blockIdx.x / (unsigned)a.parts, here = blockIdx.x;
+    const int32_t part = (int32_t)(blockIdx.x % (unsigned)a.parts), c0 = part * a.part;
+    const Setting set = setting_of(a.o.how, a.row0 + r);
+    Weigh weigh;
+    const State st = advance(a, r, 4, 5, -1, set, &weigh, s_pow, s_part, s_found), was = a.state[r * 7 + 4];
+    if (part == 0 && threadIdx.x == 0) a.state[r * 7 + 6] = st;
+    if (!was.x.open) return;                                     // nothing was listed: the sums are whole
+    const u64 least = least_weight(set, weigh);
+    const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), min(a.o.n_cols, c0 + a.part)};
+    each_listed(a, here, src, c0, range_of(was), [&](float l, int32_t c) {
+        const uint32_t key = key_in_order(l);
+        if (key < st.cut.key) return;
+        const int run = (c - c0) / LONG_RUN;
+        if (key == st.cut.key && !st.cut.every) atomicAdd(&s_ties[run], 1ull);
+        else {
+            const u64 w = weigh(key);
+            if (w >= least) atomicAdd(&s_sum[run], w);
+        }
+    });
+    __syncthreads();
+    const int32_t runs = a.part / LONG_RUN;
+    if (threadIdx.x < 64) {
+        const int i = threadIdx.x;
+        u64 w = 0ull, t = 0ull;
+        if (i < runs && c0 + LONG_RUN * i < src.n) {
+            w = a.run_sum[here * runs + i] += s_sum[i];
+            t = a.run_ties[here * runs + i] = s_ties[i];
+        }
+        w = wave_sum(w);
+        t = wave_sum(t);
+        if (i == 0) {
+            a.part_sum[here] = w;
+            a.part_ties[here] = t;
+        }
     }
 }
 
@@ -1259,7 +1386,7 @@ constexpr int64_t BLOCK_ROW = KGE_SAMPLE_ROW, MANY_ROWS = 256;
 struct Plan {
     int32_t most_k, slots;         // 0: rows, or digits in launches; else k_part_top's
     int32_t parts, part, rows;     // parts of a row, columns of a part, rows a batch
-    size_t off_most, off_hist, off_state, off_sum, off_ties, off_run, off_run_ties, bytes;
+    size_t off_most, off_hist, off_state, off_sum, off_ties, off_run, off_run_ties, off_list, off_listed, bytes;
 };
 
 Plan plan_of(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
@@ -1300,6 +1427,8 @@ Plan plan_of(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
     p.off_ties = take(parts * 8);
     p.off_run = take(runs * 8);
     p.off_run_ties = take(runs * 8);
+    p.off_list = take(parts * (part / LIST_PART) * 8);
+    p.off_listed = take(parts * 4);
     p.bytes = at;
     return p;
 }
@@ -1348,6 +1477,7 @@ int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
     a.most = (uint32_t *)(ws + p.off_most); a.hist = (u64 *)(ws + p.off_hist); a.state = (State *)(ws + p.off_state);
     a.part_sum = (u64 *)(ws + p.off_sum); a.part_ties = (u64 *)(ws + p.off_ties);
     a.run_sum = (u64 *)(ws + p.off_run); a.run_ties = (u64 *)(ws + p.off_run_ties);
+    a.list = (uint2 *)(ws + p.off_list); a.listed = (uint32_t *)(ws + p.off_listed);
     const bool by_count = o.how.row_top_k || o.how.top_k > 1;
     const bool by_weight = o.how.row_top_p || o.how.top_p < 1.f;
     for (a.row0 = 0; a.row0 < o.n_rows; a.row0 += p.rows) {
@@ -1358,15 +1488,20 @@ int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
         int before = -2, prev = -1;
         for (int which = 0; which < 2; ++which) {
             if (which == 0 ? !by_count : !by_weight) continue;
-            for (int level = 0; level < 3; ++level) {
+            for (int level = 0; level < (which == 0 ? 3 : 1); ++level) {
                 k_long_digit<BF16><<<blocks, LONG_T, 0, st>>>(a, which, level, before, prev);
                 before = prev;
                 prev = 3 * which + level;
             }
             KGE_LAUNCH_CHECK();
         }
-        k_long_sums<BF16><<<blocks, LONG_T, 0, st>>>(a, before, prev);
+        k_long_sums<BF16><<<blocks, LONG_T, 0, st>>>(a, before, prev, by_weight ? 4 : 6);
         KGE_LAUNCH_CHECK();
+        if (by_weight) {
+            k_long_third<BF16><<<blocks, LONG_T, 0, st>>>(a);
+            k_long_rest<BF16><<<blocks, LONG_T, 0, st>>>(a);
+            KGE_LAUNCH_CHECK();
+        }
         const int64_t draws = rows * o.n_draws;
         for (int64_t d = 0; d < draws; d += LONG_BLOCKS * 4) {
             k_long_draw<BF16><<<(unsigned)cdiv(draws - d < LONG_BLOCKS * 4 ? draws - d : LONG_BLOCKS * 4, 4), 256, 0, st>>>(a, d, draws);
