@@ -77,6 +77,9 @@ __device__ __forceinline__ uint32_t key_in_order(float l)          // of a score
 }
 __device__ __forceinline__ float score_of(uint32_t key) { return __uint_as_float(key ^ ((int32_t)key < 0 ? 0x80000000u : 0xffffffffu)); }
 
+// the largest score of keys up to this one: 0x7fffffff would be minus zero, which no key is, and which equals zero
+__device__ __forceinline__ float score_upto(uint32_t key) { return score_of(key == 0x7fffffffu ? 0x7ffffffeu : key); }
+
 struct __attribute__((packed, aligned(4))) F4 { float x[4]; };
 struct __attribute__((packed, aligned(2))) H4 { uint16_t x[4]; };
 struct __attribute__((packed, aligned(4))) U4 { uint32_t x[4]; };
@@ -1051,7 +1054,7 @@ __global__ __launch_bounds__(LONG_T) void k_long_digit(Long a, int which, int le
     const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), min(a.o.n_cols, c0 + a.part)};
     // what has the digits found before lies between two scores; of it top-p counts what is above top-k's cut
     const uint32_t low = st.x.first(), high = (uint32_t)min(st.x.last(), (u64)st.most);
-    const float from = score_of(which == 1 && st.cut.key >= low ? st.cut.key + 1u : low), upto = score_of(high);
+    const float from = score_of(which == 1 && st.cut.key >= low ? st.cut.key + 1u : low), upto = score_upto(high);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     auto add = [&](float l, u64 w) { atomicAdd(&s_hist[st.x.digit(key_in_order(l))], w); };
     for (int32_t c0w = c0 + LONG_RUN * wave; c0w < src.n; c0w += LONG_RUN * (LONG_T / 64)) {
@@ -1083,7 +1086,7 @@ __global__ __launch_bounds__(LONG_T) void k_long_digit(Long a, int which, int le
 struct Range { float from, upto; };
 __device__ __forceinline__ Range range_of(const State &st)
 {
-    return Range{score_of(max(st.x.first(), st.cut.key)), score_of((uint32_t)min(st.x.last(), (u64)st.most))};
+    return Range{score_of(max(st.x.first(), st.cut.key)), score_upto((uint32_t)min(st.x.last(), (u64)st.most))};
 }
 
 // The weights above the cut and the ties of it, by runs of columns and by part.  Where top-p's search is open (its first digit is found), what is

@@ -117,6 +117,8 @@ class TrainStep:
     def set_candidates(self, n_cand: int):
         """Candidates per positive of run_hard, from which set_batch's n_neg negatives are drawn."""
         torch, n_pos = self.torch, self.pos.numel()
+        if n_cand < 1:
+            raise ValueError("one candidate at least is wanted")
         new = lambda *shape, dtype: torch.empty(shape, dtype=dtype, device=self.dev)  # noqa: E731
         self.cand_ent, self.cand_side = new(n_pos, n_cand, dtype=torch.int32), new(n_pos, n_cand, dtype=torch.uint8)
         self.cand_scores = new(n_pos, 1 + n_cand, dtype=torch.float32)
@@ -189,8 +191,13 @@ class TrainStep:
         draws negatives) n_neg are drawn by their scores' softmax at `temperature`, of the top_k, top_p and min_p that are
         left, from the random numbers u ([n_pos][n_neg] in [0, 1)).  A candidate that is the positive itself is not drawn,
         unless a positive has no other."""
+        cand = getattr(self, "cand_ent", None)
+        if cand is None or cand.shape[0] != self.pos.numel() or self.choice.shape[1] != self.n_neg or self.n_neg == 0:
+            raise ValueError("set_candidates comes after set_batch, and before a step that draws negatives from them")
+        if tuple(u.shape) != tuple(self.choice.shape):
+            raise ValueError("u: a number for each negative is wanted, %d x %d" % tuple(self.choice.shape))
         self.set_dropout_state(seed, step)
-        n_cand = self.cand_ent.shape[1]
+        n_cand = cand.shape[1]
         kb.sample_negatives(self.part, self.pos, n_cand, mode, seed, step, self.cand_ent, self.cand_side, stream)
         if self.cg is not None:              # holds the negatives too: they are among the candidates
             kb.compute_graph(self.part, self.cg, self.pos, self.cand_ent, stream)

@@ -137,6 +137,15 @@ def test_pick_negatives(kb):
     assert call(None, None, 0, None, 0, 2, None, None, None) == 0 and call(None, None, 0, None, 3, 0, None, None, None) == 0
 
 
+def test_hide_positives(kb):
+    call = kb.load().kge_hide_positives
+    assert call(None, 4096, 3, 4096, 4096, 4, 4096, 4, None) == EINVAL and said(kb, "partition")
+    assert call(4096, 4096, -1, 4096, 4096, 4, 4096, 4, None) == EINVAL and call(4096, 4096, 3, 4096, 4096, 4, 4096, 3, None) == EINVAL
+    assert call(4096, 4096, 1 << 31, 4096, 4096, 4, 4096, 4, None) == ERANGE
+    assert call(4096, 4096, 3, 4096, None, 4, 4096, 4, None) == EINVAL and said(kb, "NULL array")
+    assert call(4096, None, 0, None, None, 4, None, 4, None) == 0
+
+
 def test_nothing_to_do_is_no_error(kb):
     lib = kb.load()
     t = kb._Table4(0, 40, None, None)

@@ -86,6 +86,27 @@ def test_a_step_on_drawn_negatives(kb, orc, cone, n_cand, how):  # noqa: F811
         assert drawn.mean() > np.where(own, 0.0, got).sum() / (~own).sum()
 
 
+def test_candidates_of_another_batch_are_refused(kb):  # noqa: F811
+    import torch
+    spec, part, pos, step = make(kb)
+    ts = step()
+    u = torch.rand(len(pos), 3, device="cuda")
+    with pytest.raises(ValueError):
+        ts.run_hard(spec.neg_mode, SEED, 0, u)
+    with pytest.raises(ValueError):
+        ts.set_candidates(0)
+    ts.set_candidates(20)
+    with pytest.raises(ValueError):
+        ts.run_hard(spec.neg_mode, SEED, 0, u[:, :2])
+    for other, n_neg in ((pos[:300], 3), (np.concatenate([pos, pos]), 3), (pos, 2), (pos, 0)):
+        ts.set_batch(other, n_neg)
+        with pytest.raises(ValueError):
+            ts.run_hard(spec.neg_mode, SEED, 0, torch.rand(len(other), max(n_neg, 1), device="cuda"))
+    ts.set_batch(pos[:300], 2)
+    ts.set_candidates(5)
+    ts.run_hard(spec.neg_mode, SEED, 0, u[:300, :2].contiguous())
+
+
 def test_positives_that_have_no_other_candidate(kb):  # noqa: F811
     """Every candidate hidden: the row is empty, and the candidates themselves are taken, as a uniform step would"""
     import torch

@@ -264,3 +264,55 @@ def test_pick_negatives(kb):  # noqa: F811
     kb.pick_negatives(gpu(ent), gpu(side), gpu(choice), ne, ns)
     c = np.where((choice < 0) | (choice >= 9), np.arange(20)[None, :] % 9, choice)
     assert np.array_equal(ne.cpu().numpy(), np.take_along_axis(ent, c, 1)) and np.array_equal(ns.cpu().numpy(), np.take_along_axis(side, c, 1))
+
+
+def test_long_rows_of_zeros_and_negative_scores(kb):  # noqa: F811
+    """Zero is where the digits of a score's bits have a border: scores of exactly zero, of either sign, beside those just below and above"""
+    cols = 200000
+    rng = np.random.default_rng(5)
+    below = -np.abs(rng.normal(0, 2, cols)).astype(np.float32)
+    below[:50000] *= np.float32(1e-40)                           # subnormal, and next to zero
+    rows = []
+    for zeros in (0.0, -0.0):
+        s = below.copy()
+        s[rng.permutation(cols)[:60000]] = zeros
+        rows.append(s)
+    rows.append(np.where(rng.random(cols) < 0.3, 0.0, below).astype(np.float32))
+    rows.append(np.where(rng.random(cols) < 0.1, -rows[2], rows[2]).astype(np.float32))
+    rows.append(np.where(rng.random(cols) < 0.5, np.float32(-1e-45), np.float32(0)).astype(np.float32))
+    s, u = np.array(rows), rng.random((5, 9))
+    above = [int((r >= 0).sum()) for r in s]
+    for k in (59990, 60000, 60010, above[2] + 1, above[3] - 1, above[4], above[4] + 5):
+        for how in (dict(top_k=k), dict(top_k=k, top_p=0.9999), dict(top_k=k, temperature=3e38, top_p=0.5)):
+            say(k, how)
+            check(kb, s, u, **how)
+    for p in (0.2, 0.299, 0.3, 0.31, 0.5, 0.9):
+        for t in (3e38, 1.0, 1e-3):
+            say(p, t)
+            check(kb, s, u, top_p=p, temperature=t)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_rows_of_millions(kb, kind):  # noqa: F811
+    """More columns than 2^22, where a weight's unit is 2^-39, in every way that long rows go; lists that have no room"""
+    s, u = scores_of(1, 4200001, 77, kind=kind)
+    s[0, 1000000:1040000] = 3.0
+    for how in (dict(), dict(top_k=10), dict(top_k=100000), dict(top_p=0.95), dict(top_p=0.5, min_p=0.01), dict(top_k=3000000, top_p=0.8), dict(temperature=0.0)):
+        say(kind, how)
+        check(kb, s, u, kind, **how)
+
+
+def test_more_long_rows_than_a_batch(kb):  # noqa: F811
+    import torch
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    rows, cols = 4100, 262200
+    s = torch.randn(rows, cols, device="cuda", dtype=torch.bfloat16)
+    u = torch.rand(rows, 2, dtype=torch.float64, device="cuda")
+    some = [0, 1, 4095, 4096, 4099]
+    for how in (dict(top_p=0.9), dict(top_k=30000, top_p=0.9), dict(top_k=20), dict()):
+        say(rows, cols, how)
+        choice, prob = kb.sample_scores(s, u, want_prob=True, **how)
+        want, share = ref.sample(s[some].double().cpu().numpy(), u[some].cpu().numpy(), **how)
+        assert np.array_equal(choice[some].cpu().numpy(), want) and (np.abs(prob[some].double().cpu().numpy() - share) <= U * share).all()
+        assert bool((choice >= 0).all()) and bool((choice < cols).all()) and bool((prob > 0).all())
