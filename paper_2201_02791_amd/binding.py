@@ -769,6 +769,7 @@ class GradTensors:
         places.sort()
         for at, after in zip(places, places[1:]):
             _need(after[0] >= at[1], "gradients %d and %d overlap" % (at[2], after[2]))
+        self.workspace_bytes = grad_norm_workspace_bytes(len(self.tensors))
 
 
 def grad_norm_workspace_bytes(n_tensors: int) -> int:
@@ -786,7 +787,7 @@ def _grad_norm(function, grads, max_norm, norm, factor, workspace, stream):
     norm = _new(first, (), torch.float32, stream) if norm is None else norm
     factor = _new(first, (), torch.float32, stream) if factor is None else factor
     pn, pf = _vector(norm, "norm", 1), _vector(factor, "factor", 1)
-    workspace = _workspace(workspace, grad_norm_workspace_bytes(n), first, stream)
+    workspace = _workspace(workspace, plan.workspace_bytes, first, stream)
     _call(function, stream, first, (norm, factor, workspace), plan.array, n, max_norm, pn, pf, workspace.data_ptr(),
           workspace.numel() * workspace.element_size())
     return norm, factor
@@ -821,8 +822,12 @@ class Table4:
         _need(scales.dtype == torch.bfloat16 and scales.is_contiguous() and tuple(scales.shape) == (codes.shape[0], groups),
               "scales: contiguous bfloat16 is wanted, one for each group")
         _need(scales.device == codes.device, "all tensors of a call must be on one device")
-        self.codes, self.scales, self.n_rows, self.d = codes, scales, codes.shape[0], int(d)
-        self.struct = _Table4(self.n_rows, self.d, codes.data_ptr(), scales.data_ptr())
+        self._set(codes, scales, codes.shape[0], int(d))
+
+    def _set(self, codes, scales, n_rows: int, d: int):
+        self.codes, self.scales, self.n_rows, self.d = codes, scales, n_rows, d
+        self.struct = _Table4(n_rows, d, codes.data_ptr(), scales.data_ptr())
+        return self
 
 
 def table4_encode(X, table: Table4 = None, stream=None) -> Table4:
@@ -832,8 +837,8 @@ def table4_encode(X, table: Table4 = None, stream=None) -> Table4:
     x, ldx = _rows(X, "X")
     n, d = X.shape
     if table is None:
-        groups = -(-d // TABLE4_GROUP)
-        table = Table4(_new(X, (n, 16 * groups), torch.uint8, stream), _new(X, (n, groups), torch.bfloat16, stream), d)
+        groups = -(-d // TABLE4_GROUP)                           # what the library refuses, it refuses below
+        table = object.__new__(Table4)._set(_new(X, (n, 16 * groups), torch.uint8, stream), _new(X, (n, groups), torch.bfloat16, stream), n, d)
     elif table.n_rows != n or table.d != d:
         raise KgeError(-1, "the table is of another shape than X")
     _call(load().kge_table4_encode, stream, X, (table.codes, table.scales), C.byref(table.struct), dt, x, ldx)
