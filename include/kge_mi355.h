@@ -468,9 +468,9 @@ typedef struct kge_grad_tensor {
     int32_t dtype;
 } kge_grad_tensor;
 size_t kge_grad_norm_workspace_bytes(int32_t n_tensors);
-int kge_grad_norm(const kge_grad_tensor *tensors, int32_t n_tensors, float max_norm, float *norm, float *factor, void *workspace,
+int kge_grad_norm(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, float *factor, void *workspace,
                   size_t ws_bytes, void *stream);
-int kge_clip_grads(const kge_grad_tensor *tensors, int32_t n_tensors, float max_norm, float *norm, float *factor, void *workspace,
+int kge_clip_grads(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, float *factor, void *workspace,
                    size_t ws_bytes, void *stream);
 
 /*
@@ -586,7 +586,7 @@ int kge_table4_scores(const kge_table4 *table, int32_t dtype, const void *X, int
  *   n_rows below 2^31, n_cols at most 2^31 - 2^16.  workspace: DEVICE, 256-byte aligned, at least kge_sample_workspace_bytes(how, n_rows, n_cols)
  *   bytes (0: invalid arguments), calls on different streams need different ones; with up to KGE_SAMPLE_ROW columns none is looked at.
  */
-#define KGE_SAMPLE_ROW 65536
+#define KGE_SAMPLE_ROW 32768
 typedef struct kge_sampling {
     float temperature;
     int32_t top_k;

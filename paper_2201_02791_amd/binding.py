@@ -156,7 +156,7 @@ def load():
             getattr(lib, name).restype = size
         i32 = C.c_int32
         lib.kge_grad_norm_workspace_bytes.argtypes = [i32]
-        lib.kge_grad_norm.argtypes = lib.kge_clip_grads.argtypes = [p, i32, C.c_float, p, p, p, size, p]
+        lib.kge_grad_norm.argtypes = lib.kge_clip_grads.argtypes = [p, i32, C.c_double, p, p, p, size, p]
         lib.kge_table4_encode.argtypes = [p, i32, p, i64, p]
         lib.kge_table4_decode.argtypes = [p, p, i64, i32, p, i64, p]
         lib.kge_table4_scores.argtypes = [p, i32, p, i64, i64, p, p, i64, i64, p, i64, p, i64, p]
@@ -807,7 +807,7 @@ def clip_grads(grads, max_norm: float, norm=None, factor=None, workspace=None, s
 # ---- answers: tables of 4 bits, their scores, draws from scores ------------------------------------
 
 TABLE4_GROUP = 32
-SAMPLE_ROW = 65536                # KGE_SAMPLE_ROW: rows of up to so many columns need no workspace
+SAMPLE_ROW = 32768                # KGE_SAMPLE_ROW: rows of up to so many columns need no workspace
 
 
 class Table4:

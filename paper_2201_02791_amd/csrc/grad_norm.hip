@@ -235,11 +235,11 @@ void make_list(const kge_grad_tensor *tensors, int32_t n_tensors, int32_t from, 
     }
 }
 
-int check_list(const kge_grad_tensor *tensors, int32_t n_tensors, float max_norm)
+int check_list(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm)
 {
     KGE_REQUIRE(n_tensors >= 0, KGE_EINVAL, "negative number of tensors");
     KGE_REQUIRE(tensors || n_tensors == 0, KGE_EINVAL, "NULL argument");
-    KGE_REQUIRE(max_norm >= 0.f, KGE_EINVAL, "max_norm must be zero or more");
+    KGE_REQUIRE(max_norm >= 0.0, KGE_EINVAL, "max_norm must be zero or more");
     for (int32_t i = 0; i < n_tensors; ++i) {
         const kge_grad_tensor &x = tensors[i];
         KGE_REQUIRE(x.n_rows >= 0 && x.d >= 0, KGE_EINVAL, "tensor %d: negative size", i);
@@ -252,7 +252,7 @@ int check_list(const kge_grad_tensor *tensors, int32_t n_tensors, float max_norm
     return KGE_OK;
 }
 
-int run(const kge_grad_tensor *tensors, int32_t n_tensors, float max_norm, bool scale, float *norm, float *factor, void *workspace,
+int run(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, bool scale, float *norm, float *factor, void *workspace,
         size_t ws_bytes, hipStream_t st)
 {
     int rc = check_list(tensors, n_tensors, max_norm);
@@ -300,13 +300,13 @@ extern "C" size_t kge_grad_norm_workspace_bytes(int32_t n_tensors)
     return (size_t)lists_of(n_tensors) * BLOCKS_MAX * sizeof(double);
 }
 
-extern "C" int kge_grad_norm(const kge_grad_tensor *tensors, int32_t n_tensors, float max_norm, float *norm, float *factor, void *workspace,
+extern "C" int kge_grad_norm(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, float *factor, void *workspace,
                              size_t ws_bytes, void *stream)
 {
     return run(tensors, n_tensors, max_norm, false, norm, factor, workspace, ws_bytes, (hipStream_t)stream);
 }
 
-extern "C" int kge_clip_grads(const kge_grad_tensor *tensors, int32_t n_tensors, float max_norm, float *norm, float *factor, void *workspace,
+extern "C" int kge_clip_grads(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, float *factor, void *workspace,
                               size_t ws_bytes, void *stream)
 {
     return run(tensors, n_tensors, max_norm, true, norm, factor, workspace, ws_bytes, (hipStream_t)stream);

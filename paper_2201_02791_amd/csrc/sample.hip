@@ -12,7 +12,7 @@
 // Nothing is sorted.  What top-k and top-p leave is all scores above one and, of those equal to it, the first few ("the cut").
 // That score is found digit by digit of its bits, from counts or sums of weights by digit in LDS:
 //   up to 1024 columns      a wavefront a row, digits of 8 bits, the row's keys in registers
-//   up to 65536             a block a row, digits of 11 bits; up to 16384 columns in registers, beyond read again by each pass
+//   up to 32768 at least    a block a row, digits of 11 or 12 bits; read again by each pass, or up to 16384 columns in registers
 //   more, a small top_k     blocks take their part of a row and leave its first k scores (k_part_top); those, in the order
 //                           of columns, are a short row for a block
 //   more                    a launch for each digit; blocks add their parts' sums by digit to the row's in memory (k_long_digit)
@@ -1382,8 +1382,10 @@ int bits_of(int64_t n_cols)
 
 constexpr int64_t LONG_BLOCKS = 1 << 22;      // of one launch
 
-// Rows that a block takes whole, however few there are, and rows enough for a block each
-constexpr int64_t BLOCK_ROW = KGE_SAMPLE_ROW, MANY_ROWS = 256;
+// Up to KGE_SAMPLE_ROW columns a block takes a row whole, up to twice as many where there are rows for half the compute units, up to ROW_MOST where for
+// all; else rows are split.  No settings / top_k 50 / top_p 0.9, us, whole against split: 1 x 17000 18 / 17 / 40 against 18 / 19 / 33; 1 x 30000 18 / 18 / 48
+// against 19 / 20 / 34; 1 x 65000 30 / 26 / 86 against 18 / 19 / 33; 128 x 65000 33 / 29 / 91 against 28 / 34 / 69; 200 x 30000 19 / 18 / 49 against 25 / 31 / 67
+constexpr int64_t BLOCK_ROW = 65536;
 
 // How a call runs, by its sizes and what the host knows of its settings
 struct Plan {
@@ -1396,7 +1398,7 @@ Plan plan_of(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
 {
     Plan p{};
     p.bytes = 256;
-    if (n_cols <= BLOCK_ROW || (n_cols <= ROW_MOST && n_rows >= MANY_ROWS) || n_rows == 0) return p;
+    if (n_cols <= KGE_SAMPLE_ROW || (n_cols <= BLOCK_ROW && n_rows >= 128) || (n_cols <= ROW_MOST && n_rows >= 256) || n_rows == 0) return p;
     const bool greedy = !how->row_temperature && how->temperature == 0.f;
     int64_t k = greedy ? 1 : how->top_k;
     if (k > 0) {
