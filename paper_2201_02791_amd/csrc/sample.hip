@@ -16,6 +16,9 @@
 //   more, a small top_k     blocks take their part of a row and leave its first k scores (k_part_top); those, in the order
 //                           of columns, are a short row for a block
 //   more                    a launch for each digit; blocks add their parts' sums by digit to the row's in memory (k_long_digit)
+//
+// Bound by vector instructions where rows are many (65536 rows of 256, 64 draws each: 54 us, 345 instructions a row, 2.5 TB/s; 16 rows of 2.9 million
+// at top_p 0.9: 185 us in six launches), by waits where they are few (one row of a million at top_k 50: 9 + 18 us).
 #include "common.h"
 
 #include <math.h>
@@ -426,12 +429,12 @@ __device__ __forceinline__ Cut cut_at(int which, const S &x, u64 own, const Cut 
 }
 
 // A row's keys, TILES tiles of 4 columns a thread at a time: thread t of NT has columns 4 (NT i + t) .. + 3 of tile i.  ONE: the row has no
-// more, and they stay in registers, with the weights of those that top-k leaves where a thread has the registers (128 with 1024 threads to a
-// block); else every pass reads them again, from the caches, and weighs again.
+// more, and they stay in registers, with the weights of those that top-k leaves where a wavefront has the row (a thread of a block of 1024 has 128
+// registers, too few for them); else every pass reads them again, from the caches, and weighs again.
 template <int NT, int TILES, bool ONE, class Source>
 struct Keys {
     static constexpr int V = 4 * TILES, BATCH = NT * V;
-    static constexpr bool WHOLE = ONE, HELD = ONE && NT < 1024;
+    static constexpr bool HELD = ONE && NT == 64;
     const Source &src;
     uint32_t key[V];
     double w[HELD ? V : 1];
@@ -515,7 +518,7 @@ __device__ __forceinline__ bool find_cut(int which, uint32_t limit, K &keys, con
 {
     if (!cuts(which, set, keys.src.n)) return false;
     // a wavefront's row has up to 1024 scores: their number fits beside their weights, and where a digit has one score the search ends
-    constexpr int PACK = NT == 64 && K::WHOLE ? 11 : 0;
+    constexpr int PACK = K::HELD ? 11 : 0;
     const int tid = Team<NT>::tid();
     Search<BITS> x;
     x.begin(low, most);
@@ -740,7 +743,7 @@ __device__ __forceinline__ void draw_few(const Call &o, int64_t first, K &keys, 
     __syncthreads();
 }
 
-// One row.  Up to 4096 columns the sums by column are in LDS, and a thread finds a draw by halving; beyond, the sums by runs of 256
+// One row.  Up to 1024 columns the sums by column are in LDS, and a lane finds a draw by halving; beyond, the sums by runs of 256
 // columns are (sums[run]: of runs 0 .. run; ties[run], where not all ties are left: their number before the run), and a wavefront
 // weighs the run of a draw again.
 template <int NT, int TILES, bool ONE, int BITS, class Source>
@@ -778,36 +781,31 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
     weigh.init(most, set.t, o, pow);
     Cut cut{0u, true, 0ull};
     if (cuts(0, set, src.n)) {
-        if constexpr (NT == 64 && ONE) find_kth(keys, set.k, low_of<NT>(mine, set.k, s), most, cut);
-        const bool few = !(NT == 64 && ONE) && find_cut<NT, BITS>(0, NT > 64 && set.k <= FEW && o.n_draws <= FEW ? FEW : 0u, keys, set, weigh, low_of<NT>(mine, set.k, s), most, cut, hist,
-                                            s, s_found);
-        if constexpr (NT > 64) {
-            if (few) {
-                draw_few<NT>(o, first, keys, set, weigh, cut, (uint32_t *)sums, s_found);
-                return;
+        const uint32_t low = low_of<NT>(mine, set.k, s);
+        if constexpr (K::HELD) find_kth(keys, set.k, low, most, cut);
+        else {
+            const uint32_t limit = NT > 64 && set.k <= FEW && o.n_draws <= FEW ? FEW : 0u;
+            const bool few = find_cut<NT, BITS>(0, limit, keys, set, weigh, low, most, cut, hist, s, s_found);
+            if constexpr (NT > 64) {
+                if (few) {
+                    draw_few<NT>(o, first, keys, set, weigh, cut, (uint32_t *)sums, s_found);
+                    return;
+                }
             }
         }
     }
     keys.weigh_all(weigh, cut);
     find_cut<NT, BITS>(1, 0u, keys, set, weigh, max(cut.key, weigh.lowest(set.t)), most, cut, hist, s, s_found);
     const u64 least = least_weight(set, weigh);
-    if constexpr (ONE && K::BATCH <= 4096) {                     // 4096 weights of 2^40 units: a double holds their sums
+    if constexpr (K::HELD) {                                     // 1024 weights of 2^40 units: a double holds their sums
         double *to = (double *)sums, total = 0.0;
-        u64 equal = 0ull;                                        // ties in the tiles before and, in a block, in the wavefronts before
+        u64 equal = 0ull;                                        // ties in the tiles before
 #pragma unroll
         for (int i = 0; i < TILES; ++i) {
-            u64 before = equal;
-            if (NT > 64 && !cut.every) {                         // ties of the wavefronts before, in this tile
-                u64 here;
-                const u64 mine = ties_of(keys.key + 4 * i, cut), upto = T::scan(mine, s, &here);
-                before += lane_of(upto - mine, 0);
-                equal += here;
-            }
             double w[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) w[k] = keys.weight(4 * i + k, weigh);
-            left4(keys.key + 4 * i, cut, least, &before, w);
-            if (NT == 64) equal = before;
+            left4(keys.key + 4 * i, cut, least, &equal, w);
             w[1] += w[0]; w[2] += w[1]; w[3] += w[2];
             double all;
             const double base = total + (T::scan(w[3], s, &all) - w[3]);
@@ -878,7 +876,7 @@ template <bool BF16, int NT, int TILES, bool ONE, bool PARTS>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT, TILES, ONE)))) void k_rows(Call o)
 {
     constexpr int BITS = NT == 64 ? 8 : NT == 256 ? 11 : 12, TEAMS = NT == 64 ? 4 : 1, COLUMNS = 4 * TILES * NT;
-    constexpr bool BY_COLUMN = ONE && COLUMNS <= 4096;
+    constexpr bool BY_COLUMN = ONE && NT == 64;
     __shared__ u64 s_hist[TEAMS][1 << BITS], s_sums[TEAMS][BY_COLUMN ? COLUMNS : NT], s_ties[TEAMS][BY_COLUMN ? 1 : NT];
     __shared__ u64 s_part[TEAMS][16], s_found[TEAMS][4];
     __shared__ double s_pow[POWERS];
@@ -1472,10 +1470,10 @@ int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
             KGE_LAUNCH_CHECK();
         }
         o.part_key = part_key; o.part_col = part_col; o.n_part = p.parts * p.slots;
-        if (o.n_part <= 1024) return launch_rows<BF16, 64, 4, true, true>(o, st);
-        if (o.n_part <= 4096) return launch_rows<BF16, 256, 4, false, true>(o, st);
-        if (o.n_part <= 16384) return launch_rows<BF16, 1024, 4, true, true>(o, st);
-        return launch_rows<BF16, 1024, 4, false, true>(o, st);
+        if (o.n_part <= 1024) return launch_rows<false, 64, 4, true, true>(o, st);
+        if (o.n_part <= 4096) return launch_rows<false, 256, 4, false, true>(o, st);
+        if (o.n_part <= 16384) return launch_rows<false, 1024, 4, true, true>(o, st);
+        return launch_rows<false, 1024, 4, false, true>(o, st);
     }
     Long a;
     a.o = o; a.parts = p.parts; a.part = p.part;

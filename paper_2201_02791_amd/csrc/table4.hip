@@ -6,6 +6,8 @@
 //
 // Encoding compares magnitudes with the borders between two numbers, s times 1/4, 3/4, 5/4, 7/4, 5/2, 7/2 and 5: products
 // of at most 11 bits, exact in fp32, so that every element goes to the nearest number (of two as near, to the even code).
+//
+// Both ways are bound by memory: a million rows of 256 floats 219 us encoded, 5.3 TB/s, and 252 us back, 4.6 TB/s.
 #include "common.h"
 #include "split_bf16.h"
 
@@ -246,7 +248,12 @@ __global__ __launch_bounds__(256) void k_table4_decode(const uint16_t *__restric
 // lanes are then transposed by lane swaps, so that each matrix instruction meets one group: the table stays in plain order.
 //
 // Up to four questions: their parts are rows 4 part + question of one instruction, and the parts' sums are added at the end.
-// More: 16 questions a tile, the parts' products chained, smallest first.
+// More: 16 questions a tile, the parts' products chained, smallest first.  A lane's results are one table row's in either case, with the one
+// scale: with the operands changed over it would have four rows of one question to store at once, but need four scales, and 16 lanes would
+// store to 16 questions' rows (16 questions to a million rows of 256 98 us instead of 51).
+//
+// Measured, a million rows of 256: one question 31 us, 4.8 TB/s, 369 vector instructions for 32 rows (with addresses formed anew for each load
+// 564, and 40 us); 16 questions 47 us; 37 bf16 questions to 2.9 million rows of 128 149 us, 4.3 TB/s, two thirds of it results.
 
 struct Questions {
     const void *X;
