@@ -453,7 +453,8 @@ int kge_adamw_step_scaled(const kge_adamw *opt, const kge_adamw_tensor *tensors,
  * Each tensor is n_rows rows of d elements, dense, of dtype KGE_DT_F32 or KGE_DT_BF16, fewer than 2^36 (KGE_ERANGE).  row_mask: NULL, or DEVICE
  * uint8 [n_rows]: rows where it is 0 are neither read nor scaled (what they hold is no gradient, e.g. rows that kge_adamw_step leaves out by
  * KGE_ROWS_MASK).  Squares and sums are in 64 bits: nothing overflows, and the result repeats bit for bit.  norm, factor: DEVICE float [1];
- * either may be NULL, with kge_grad_norm one of them at most.  A gradient that is not finite: norm is infinite or NaN, factor NaN.
+ * either may be NULL, with kge_grad_norm one of them at most.  A gradient that is not finite: norm is infinite or NaN, factor NaN
+ * (a norm beyond the largest float reads as infinity, with its factor).
  *   kge_grad_norm   norm and factor alone, for a step that takes the factor along (kge_adamw_step_scaled)
  *   kge_clip_grads  the gradients are scaled as well, in place (rounded once, after fp32's product, where they are bf16); with a factor of 1
  *                   they are not written, with a NaN they all become NaN.  No two tensors may overlap.
@@ -545,14 +546,15 @@ int kge_eval_rank_all_static(const kge_eval_filter *filter, const float *H, int6
  * the high half; a half is a number of the format e2m1 (sign, then 0, 1/2, 1, 3/2, 2, 3, 4, 6).  scales: DEVICE bf16 [n_rows][groups].  An element
  * is its number times its group's scale.
  * kge_table4_encode: X [n_rows][d] of dtype, rows ldx elements apart (ldx >= d).  A group's scale is the smallest bf16 number, 2^-126 or
- *   more, six of which reach its largest magnitude (0 for a group of zeros); each element goes to the nearest number, of two as near to the even
- *   code.  A group with an infinity or a NaN reads as NaN.
+ *   more, six of which reach its largest magnitude (0 for a group of zeros), but six of which are a float; each element goes to the nearest
+ *   number, of two as near to the even code.  A group with an infinity or a NaN reads as NaN.
  * kge_table4_decode: out [n][d] of dtype, rows ldo apart: rows rows[0..n) (DEVICE int32) of the table, or with rows NULL its first n.  A
  *   row number that the table does not have gives a row of NaN.  bf16 results are rounded once.
  * kge_table4_scores: scores[q][i] = sum_k x_q[k] row_i[k], float, rows lds apart (lds >= n_rows), for questions q in [0, n_questions):
  *   x_q = X[fixed[q]] * M[rel[q]], the product in fp32 (Eq. 4's question: one entity's embedding and the relation's diagonal), or X[fixed[q]]
  *   with M NULL.  fixed NULL: X[q]; rel NULL: M[q].  X [n_x][d] of dtype, M [n_m][d] float; fixed, rel DEVICE int32.  An id outside [0, n_x)
- *   or [0, n_m) is never an address: that question's scores are NaN.  Products are exact, sums fp32; the scale multiplies a group's sum, so
+ *   or [0, n_m) is never an address: that question's scores are NaN.  Products are exact (of what x_q has
+ *   from 2^-133 on), sums fp32; the scale multiplies a group's sum, so
  *   infinities in x_q give infinities or NaN.
  */
 #define KGE_TABLE4_GROUP 32

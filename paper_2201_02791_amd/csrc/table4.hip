@@ -2,7 +2,8 @@
 //
 // A row is cut into groups of 32 elements; a group has a scale s, a bf16 number, and its elements are numbers c of the format
 // e2m1 (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives) times s.  s is the smallest bf16 number, 2^-126 or more, with
-// 6 s >= the group's largest magnitude, so nothing saturates; 4.5 bits an element in all.
+// 6 s >= the group's largest magnitude, so nothing saturates, and 1.328125 2^125 at most, so that 6 s is a float (elements past bf16's
+// largest number become that); 4.5 bits an element in all.
 //
 // Encoding compares magnitudes with the borders between two numbers, s times 1/4, 3/4, 5/4, 7/4, 5/2, 7/2 and 5: products
 // of at most 11 bits, exact in fp32, so that every element goes to the nearest number (of two as near, to the even code).
@@ -56,7 +57,8 @@ __device__ __forceinline__ void load4(const void *X, int64_t at, int n, float x[
     }
 }
 
-// the bits of the smallest bf16 number, 2^-126 or more, six of which reach `most`; NaN where a member is not finite
+// the bits of the smallest bf16 number, 2^-126 or more, six of which reach `most`, or of the largest six of which are a float; NaN where a member is not
+// finite
 __device__ __forceinline__ uint32_t group_scale(uint32_t most)
 {
     if (most == 0u) return 0u;
@@ -66,7 +68,7 @@ __device__ __forceinline__ uint32_t group_scale(uint32_t most)
 #pragma unroll
     for (int k = 0; k < 2; ++k)      // the product is rounded and then cut: at most two steps short
         if (6.f * s < a) s = __uint_as_float(__float_as_uint(s) + 0x10000u);
-    return __float_as_uint(s);
+    return min(__float_as_uint(s), 0x7e2a0000u);
 }
 
 __device__ __forceinline__ uint32_t code_of(float x, float s)
@@ -287,7 +289,7 @@ __device__ __forceinline__ void question8(const Questions &Q, int64_t q, int32_t
     }
 }
 
-// part p of x: what bf16 cuts off x, of the rest what it cuts off, and what is left; their sum is x
+// part p of x: what bf16 cuts off x, of the rest what it cuts off, and what is left; their sum is x, but for bits below 2^-133, bf16's last
 __device__ __forceinline__ uint32_t part_of(float x, int p)
 {
     const uint32_t hi = __float_as_uint(x) & 0xffff0000u;

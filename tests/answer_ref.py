@@ -21,7 +21,8 @@ def bf16(x):
 # ---- tables
 
 def smallest_scale(most):
-    """The smallest number of 8 significant bits, 2^-126 or more, six of which reach `most`: by trying them all in an octave"""
+    """The smallest number of 8 significant bits, 2^-126 or more, six of which reach `most`: by trying them all in an octave; but six of which
+    are a float"""
     if most == 0.0:
         return 0.0
     if not math.isfinite(most):
@@ -31,7 +32,7 @@ def smallest_scale(most):
         for m in range(128, 256):
             s = math.ldexp(m, e - 7)
             if 6.0 * s >= most:
-                return s
+                return s if 6.0 * s <= float(np.finfo(np.float32).max) else 170 * 2.0 ** 118
         e += 1
 
 

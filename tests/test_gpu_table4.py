@@ -74,6 +74,22 @@ def test_scales_at_the_ends_of_the_range(kb):  # noqa: F811
     assert np.array_equal(t.scales.double().cpu().numpy(), scales) and np.array_equal(t.codes.cpu().numpy(), ref.pack(codes))
 
 
+def test_numbers_up_to_the_largest_stay_finite(kb):  # noqa: F811
+    """Past bf16's largest number, 255 2^120, six of the next scale would be infinite"""
+    import torch
+    most, edge = np.finfo(np.float32).max, np.float32(255 * 2.0 ** 120)
+    x = np.zeros((6, 40), np.float32)
+    x[:, 3] = [most, -most, edge, np.nextafter(edge, most), np.nextafter(edge, np.float32(0)), most / 2]
+    x[:, 35] = x[::-1, 3] / 5
+    codes, scales = ref.encode(x)
+    t = kb.table4_encode(gpu(x))
+    assert np.array_equal(t.scales.double().cpu().numpy(), scales) and np.array_equal(t.codes.cpu().numpy(), ref.pack(codes))
+    want = ref.decode(codes, scales, 40)
+    got = kb.table4_decode(t).double().cpu().numpy()
+    assert np.isfinite(got).all() and np.array_equal(got, want) and abs(got[0, 3]) == float(edge)
+    assert np.array_equal(kb.table4_decode(t, dtype=torch.bfloat16).double().cpu().numpy(), ref.bf16(want))
+
+
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
 def test_groups_that_are_not_finite(kb, bad):  # noqa: F811
     x = rows_of(4, 70, 1)
