@@ -1378,7 +1378,8 @@ int bits_of(int64_t n_cols)
     return 62 - log < 40 ? 62 - log : 40;
 }
 
-constexpr int64_t LONG_BLOCKS = 1 << 22;      // of one launch
+constexpr int64_t LONG_BLOCKS = (1 << 22) - 1;           // of one launch: fewer than 2^32 threads
+static_assert(LONG_BLOCKS * 1024 < 1ll << 32, "k_part_top has 1024 threads to a block");
 
 // Up to KGE_SAMPLE_ROW columns a block takes a row whole, up to twice as many where there are rows for half the compute units, up to ROW_MOST where for
 // all; else rows are split.  No settings / top_k 50 / top_p 0.9, us, whole against split: 1 x 17000 18 / 17 / 40 against 18 / 19 / 33; 1 x 30000 18 / 18 / 48

@@ -208,7 +208,7 @@ class TrainStep:
         kb.hide_positives(self.part, self.pos, self.cand_ent, self.cand_side, scores, stream)
         need = kb.sample_workspace_bytes(*scores.shape, temperature, top_k, top_p, min_p)
         if self.cand_workspace is None or self.cand_workspace.numel() < need:          # the first step of these settings
-            self.cand_workspace = self.torch.empty(need, dtype=self.torch.uint8, device=self.dev)
+            self.cand_workspace = kb._workspace(None, need, scores, stream)
         kb.sample_scores(scores, u, temperature, top_k, top_p, min_p, choice=self.choice, workspace=self.cand_workspace, stream=stream)
         kb.pick_negatives(self.cand_ent, self.cand_side, self.choice, self.neg_ent, self.neg_side, stream)
         self.score_loss(stream)
@@ -247,11 +247,10 @@ class TrainStep:
 
     def _clip(self, call, max_norm: float, stream):
         if not hasattr(self, "grad_plan"):
-            torch, mask = self.torch, self.cg.input_rows_ptr() if self.cg is not None else None
+            mask = self.cg.input_rows_ptr() if self.cg is not None else None
             self.grad_plan = kb.GradTensors([dict(grad=g, row_mask=mask if rows else None) for _, _, g, rows in self._opt_pairs()])
-            n = len(self.grad_plan.tensors)
-            self.grad_norm, self.grad_factor = (torch.empty((), dtype=torch.float32, device=self.M.device) for _ in range(2))
-            self.grad_workspace = torch.empty(kb.grad_norm_workspace_bytes(n), dtype=torch.uint8, device=self.M.device)
+            self.grad_norm, self.grad_factor = (kb._new(self.M, (), self.torch.float32, stream) for _ in range(2))
+            self.grad_workspace = kb._workspace(None, self.grad_plan.workspace_bytes, self.M, stream)
         call(self.grad_plan, max_norm, self.grad_norm, self.grad_factor, self.grad_workspace, stream)
 
     @staticmethod

@@ -171,6 +171,24 @@ def test_updates_with_a_largest_norm(kb, name, cone):  # noqa: F811
         assert math.isinf(float(a.grad_norm)) and all(torch.equal(x, p) for x, (_, p, _, _) in zip(was, a._opt_pairs()))
 
 
+def test_what_a_step_allocates_is_its_streams(kb):  # noqa: F811
+    """Memory of another stream's would be given to that one's tensors while this one may still use it"""
+    import torch
+    spec, part, pos, step = make(kb)
+    ts = step()
+    ts.init_optimizer(kb.OPT_ADAMW)
+    ts.set_candidates(20)
+    u, side = torch.rand(len(pos), 3, device="cuda"), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    ts.run_hard(spec.neg_mode, SEED, 0, u, stream=side)
+    ts.optimizer_step(kb.OPT_ADAMW, max_norm=1.0, stream=side)
+    torch.cuda.synchronize()
+    segments = torch.cuda.memory_snapshot()
+    for t in (ts.cand_workspace, ts.grad_workspace, ts.grad_norm, ts.grad_factor):
+        at, = [s for s in segments if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]]
+        assert at["stream"] == side.cuda_stream
+
+
 def test_a_block_and_bf16_take_a_largest_norm_too(kb):  # noqa: F811
     import torch
     from test_gpu_feature_block import small
