@@ -90,6 +90,7 @@ struct __attribute__((packed, aligned(4))) U4 { uint32_t x[4]; };
 // Where a row's keys come from: scores, or the first scores of its parts
 template <bool BF16>
 struct Scores {
+    static constexpr bool PLAIN = true;
     const void *row;
     int32_t n;
     __device__ __forceinline__ float one(int32_t c) const { return BF16 ? __uint_as_float((uint32_t)((const uint16_t *)row)[c] << 16) : ((const float *)row)[c]; }
@@ -132,6 +133,7 @@ struct Scores {
     __device__ __forceinline__ int32_t column(int32_t c) const { return c; }
 };
 struct Parts {
+    static constexpr bool PLAIN = false;         // there is a top-k
     const uint32_t *keys;
     const int32_t *col;
     int32_t n;
@@ -743,6 +745,129 @@ __device__ __forceinline__ void draw_few(const Call &o, int64_t first, K &keys, 
     __syncthreads();
 }
 
+// The sums by column of a row that a wavefront holds (w: its weights left, 4 columns a lane a tile), 1024 weights of 2^40 units at most, which a
+// double holds; a lane finds a draw by halving.
+template <int TILES, class W, class Source>
+__device__ __forceinline__ void draw_by_column(const Call &o, int64_t first, const Source &src, double *to, W weights)
+{
+    typedef Team<64> T;
+    const int lane = T::tid();
+    double total = 0.0;
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+        double w[4];
+        weights(i, w);
+        w[1] += w[0]; w[2] += w[1]; w[3] += w[2];
+        const double upto = wave_scan(w[3]), base = total + (upto - w[3]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) to[4 * (64 * i + lane) + k] = base + w[k];
+        total += lane_of(upto, 63);
+    }
+    T::sync();
+    const double inverse = inverse_of(total);
+    for (int32_t i = lane; i < o.n_draws; i += 64) {
+        const int at = first_above(to, 256 * TILES, goal_of_draw(o, first + i, total));
+        answer(o, first + i, src.column(at), to[at] - (at ? to[at - 1] : 0.0), inverse);
+    }
+    T::sync();
+}
+
+// The sums of the runs of 256 columns are there (sums; ties: of the cut, by runs, their number before each); a wavefront weighs the run of a draw
+// again
+template <int NT, class Source>
+__device__ __forceinline__ void draw_by_run(const Call &o, int64_t first, const Source &src, const Cut &cut, const Weigh &weigh, u64 least, u64 *sums, const u64 *ties, u64 *s)
+{
+    typedef Team<NT> T;
+    const int tid = T::tid(), wave = NT == 64 ? 0 : (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int runs = (src.n + RUN - 1) / RUN;
+    u64 total;
+    T::sync();
+    const u64 mine = tid < runs ? sums[tid] : 0ull;
+    const u64 upto = T::scan(mine, s, &total);
+    if (tid < runs) sums[tid] = upto;
+    T::sync();
+    for (int32_t i = wave; i < o.n_draws; i += NT / 64) {
+        const u64 goal = goal_of_draw(o, first + i, total);
+        const int run = first_above(sums, runs, goal);
+        const int32_t c = RUN * run + 4 * lane;
+        uint32_t again[4];
+        get4(src, c, again);
+        u64 equal = cut.every ? 0ull : ties[run];
+        pick4(o, first + i, src, c, again, cut, weigh, least, &equal, goal, run ? sums[run - 1] : 0ull, total);
+    }
+    T::sync();
+}
+
+// A row of which neither top-k nor top-p takes anything: its scores are no more than numbers, their order does not matter.  False: its largest score
+// is infinite, and nothing is done
+template <int NT, int TILES, bool ONE, bool BF16>
+__device__ __forceinline__ bool draw_plain(const Call &o, int64_t first, const Setting &set, const Scores<BF16> &src, u64 *sums, u64 *s, const double *pow)
+{
+    typedef Team<NT> T;
+    constexpr int V = 4 * TILES, BATCH = NT * V, WAVES = NT / 64;
+    const int wave = NT == 64 ? 0 : (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    float l[V];
+    const auto load = [&](int32_t c0) {
+        if (c0 + BATCH <= src.n) {
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) src.score4(c0 + 4 * (NT * i + T::tid()), l + 4 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) {
+                const int32_t c = c0 + 4 * (NT * i + T::tid());
+                if (c + 4 <= src.n) src.score4(c, l + 4 * i);
+                else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) l[4 * i + k] = c + k < src.n ? src.one(c + k) : -INFINITY;
+                }
+            }
+        }
+    };
+    float mine = -INFINITY;
+#pragma unroll 1
+    for (int32_t c0 = 0; c0 < src.n; c0 += BATCH) {
+        load(c0);
+#pragma unroll
+        for (int k = 0; k < V; ++k) mine = __builtin_fmaxf(mine, l[k]);          // of NaN and a number the number
+    }
+    const uint32_t most = T::most(key_of(mine), s);
+    if (most == 0u) {
+        for (int32_t i = T::tid(); i < o.n_draws; i += NT) answer(o, first + i, -1, 0.0, 1.0);
+        return true;
+    }
+    Weigh weigh;
+    weigh.init(most, set.t, o, pow);
+    if (weigh.endless) return false;
+    const u64 least = least_weight(set, weigh);
+    const double fewest = (double)least;
+    const auto weigh4 = [&](int i, double w[4]) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = weigh.raised(l[4 * i + k]) - 0x1p52;
+        if (least > 1ull) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = w[k] >= fewest ? w[k] : 0.0;
+        }
+    };
+    if constexpr (ONE && NT == 64) draw_by_column<TILES>(o, first, src, (double *)sums, weigh4);
+    else {
+        const int runs = (src.n + RUN - 1) / RUN;
+#pragma unroll 1
+        for (int32_t c0 = 0; c0 < src.n; c0 += BATCH) {
+            if (!ONE) load(c0);
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) {
+                double w[4];
+                weigh4(i, w);
+                const u64 sum = whole(lane_of(wave_scan(w[0] + w[1] + w[2] + w[3]), 63));
+                const int run = c0 / RUN + i * WAVES + wave;
+                if (lane == 0 && run < runs) sums[run] = sum;
+            }
+        }
+        draw_by_run<NT>(o, first, src, Cut{0u, true, 0ull}, weigh, least, sums, nullptr, s);
+    }
+    return true;
+}
+
 // One row.  Up to 1024 columns the sums by column are in LDS, and a lane finds a draw by halving; beyond, the sums by runs of 256
 // columns are (sums[run]: of runs 0 .. run; ties[run], where not all ties are left: their number before the run), and a wavefront
 // weighs the run of a draw again.
@@ -754,6 +879,9 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
     constexpr int V = K::V, WAVES = NT / 64;
     const int tid = T::tid(), wave = NT == 64 ? 0 : (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const Setting set = setting_of(o.how, r);
+    if constexpr (Source::PLAIN) {
+        if (set.k != 1 && !cuts(0, set, src.n) && !cuts(1, set, src.n) && draw_plain<NT, TILES, ONE>(o, r * o.n_draws, set, src, sums, s, pow)) return;
+    }
     K keys(src);
     uint32_t mine = 0u;
     keys.each(0, [&](int32_t) {
@@ -797,31 +925,14 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
     keys.weigh_all(weigh, cut);
     find_cut<NT, BITS>(1, 0u, keys, set, weigh, max(cut.key, weigh.lowest(set.t)), most, cut, hist, s, s_found);
     const u64 least = least_weight(set, weigh);
-    if constexpr (K::HELD) {                                     // 1024 weights of 2^40 units: a double holds their sums
-        double *to = (double *)sums, total = 0.0;
+    if constexpr (K::HELD) {
         u64 equal = 0ull;                                        // ties in the tiles before
-#pragma unroll
-        for (int i = 0; i < TILES; ++i) {
-            double w[4];
+        draw_by_column<TILES>(o, first, src, (double *)sums, [&](int i, double w[4]) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) w[k] = keys.weight(4 * i + k, weigh);
             left4(keys.key + 4 * i, cut, least, &equal, w);
-            w[1] += w[0]; w[2] += w[1]; w[3] += w[2];
-            double all;
-            const double base = total + (T::scan(w[3], s, &all) - w[3]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) to[4 * (NT * i + tid) + k] = base + w[k];
-            total += all;
-        }
-        T::sync();
-        const double inverse = inverse_of(total);
-        for (int32_t i = tid; i < o.n_draws; i += NT) {
-            const int at = first_above(to, K::BATCH, goal_of_draw(o, first + i, total));
-            answer(o, first + i, src.column(at), to[at] - (at ? to[at - 1] : 0.0), inverse);
-        }
-        T::sync();
+        });
     } else {
-        u64 total;
         const int runs = (src.n + RUN - 1) / RUN;
         if (!cut.every) {
             keys.each(0, [&](int32_t c0) {
@@ -852,21 +963,7 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
                 if (lane == 0 && run < runs) sums[run] = sum;
             }
         });
-        T::sync();
-        const u64 mine = tid < runs ? sums[tid] : 0ull;
-        const u64 upto = T::scan(mine, s, &total);
-        if (tid < runs) sums[tid] = upto;
-        T::sync();
-        for (int32_t i = wave; i < o.n_draws; i += WAVES) {
-            const u64 goal = goal_of_draw(o, first + i, total);
-            const int run = first_above(sums, runs, goal);
-            const int32_t c = RUN * run + 4 * lane;
-            uint32_t again[4];
-            get4(src, c, again);
-            u64 equal = cut.every ? 0ull : ties[run];
-            pick4(o, first + i, src, c, again, cut, weigh, least, &equal, goal, run ? sums[run - 1] : 0ull, total);
-        }
-        T::sync();
+        draw_by_run<NT>(o, first, src, cut, weigh, least, sums, ties, s);
     }
 }
 
