@@ -17,8 +17,8 @@
 //                           of columns, are a short row for a block
 //   more                    a launch for each digit; blocks add their parts' sums by digit to the row's in memory (k_long_digit)
 //
-// Bound by vector instructions where rows are many (65536 rows of 256, 64 draws each: 54 us, 345 instructions a row, 2.5 TB/s; 16 rows of 2.9 million
-// at top_p 0.9: 185 us in six launches), by waits where they are few (one row of a million at top_k 50: 9 + 18 us).
+// Bound by vector instructions where rows are many (65536 rows of 256, 64 draws each: 44 us, 3.1 TB/s; 16 rows of 2.9 million
+// at top_p 0.9: 168 us in six launches), by waits where they are few (one row of a million at top_k 50: 9 + 18 us).
 #include "common.h"
 
 #include <math.h>
@@ -1056,6 +1056,8 @@ __global__ __launch_bounds__(NT) void k_part_top(Call o, int64_t row0, int32_t p
 // ---- long rows: a launch a digit.  Once top-p's first digit is found, what has a larger one is left for certain: the next launch sums its weights, by
 // runs of columns, beside the sums by the second digit, and lists the scores with the first; the third digit and the sums of what is
 // left of the list read the list alone.  A part with more of them than its list has room for is read again.
+// Where draws are few nothing is summed by runs: a part's weights above the first digit are sums of its own sums by digit, and a draw weighs
+// the part that it is in.
 
 struct State {                     // of a row, after a launch
     Search<11> x;
@@ -1071,7 +1073,8 @@ struct Long {
     u64 *hist;                     // [rows][6][2048]
     State *state;                  // [rows][7]
     u64 *part_sum, *part_ties;     // [rows][parts]: weights above the cut, ties of it
-    u64 *run_sum, *run_ties;       // [rows][parts][part / LONG_RUN]
+    u64 *run_sum, *run_ties;       // [rows][parts][part / LONG_RUN]; null: a draw weighs its part again
+    u64 *part_hist;                // beside that [rows][parts][2048]: the parts' sums by top-p's first digit
     uint2 *list;                   // [rows][parts][part / LIST_PART]: scores with top-p's first digit, and their columns
     uint32_t *listed;              // [rows][parts]: their number, which may be more than there is room for
 };
@@ -1175,6 +1178,8 @@ __global__ __launch_bounds__(LONG_T) void k_long_digit(Long a, int which, int le
     u64 *hist = a.hist + (r * 6 + which * 3 + level) * LONG_DIGITS;
     for (int i = threadIdx.x; i < LONG_DIGITS; i += LONG_T)
         if (s_hist[i]) atomicAdd(&hist[i], s_hist[i]);
+    if (which == 1 && a.part_hist)
+        for (int i = threadIdx.x; i < LONG_DIGITS; i += LONG_T) a.part_hist[(int64_t)blockIdx.x * LONG_DIGITS + i] = s_hist[i];
 }
 
 // scores that a search's digits found leave open, from top-k's cut on
@@ -1184,13 +1189,43 @@ __device__ __forceinline__ Range range_of(const State &st)
     return Range{score_of(max(st.x.first(), st.cut.key)), score_upto((uint32_t)min(st.x.last(), (u64)st.most))};
 }
 
+// Of 16 columns a lane, the weights of scores from `edge` on (above the cut, and what is equal to it if all that is is left), no fewer units than
+// `least`; 1024 weights of 2^40 units are a whole number that a double holds
+__device__ __forceinline__ u64 run_weight(const float l[16], float edge, u64 least, const Weigh &weigh)
+{
+    double lanes = 0.0;
+    if (weigh.endless) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) lanes += l[k] == INFINITY && l[k] >= edge ? (double)weigh.unit() : 0.0;
+    } else if (least <= 1ull) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) lanes += weigh.raised(l[k] >= edge ? l[k] : -INFINITY) - 0x1p52;
+    } else {
+        const double fewest = (double)least;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const double v = weigh.raised(l[k] >= edge ? l[k] : -INFINITY) - 0x1p52;
+            lanes += v >= fewest ? v : 0.0;
+        }
+    }
+    return whole(lane_of(wave_scan(lanes), 63));
+}
+__device__ __forceinline__ u64 run_ties(const float l[16], float tie)
+{
+    u64 t = 0ull;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) t += l[k] == tie ? 1ull : 0ull;
+    return wave_sum(t);
+}
+__device__ __forceinline__ float edge_of(const Cut &cut) { return cut.key == 0u ? -INFINITY : score_of(cut.every ? cut.key : cut.key + 1u); }
+
 // The weights above the cut and the ties of it, by runs of columns and by part.  Where top-p's search is open (its first digit is found), what is
 // above that digit counts; what has it is listed, and its weights go to the sums by the second digit
+// Six blocks to a compute unit, so that the 1424 of 16 rows of 2.9 million run at once (51 us, of five 57)
 template <bool BF16>
-__global__ __launch_bounds__(LONG_T) void k_long_sums(Long a, int before, int prev, int slot)
+__global__ __launch_bounds__(LONG_T) __attribute__((amdgpu_waves_per_eu(6))) void k_long_sums(Long a, int before, int prev, int slot)
 {
     __shared__ u64 s_hist[LONG_DIGITS], s_part[16], s_found[4];
-    __shared__ uint2 s_queue[LONG_T / 64][5 * 64];
     __shared__ double s_pow[POWERS];
     __shared__ uint32_t s_listed;
     if (threadIdx.x == 0) s_listed = 0u;
@@ -1210,81 +1245,43 @@ __global__ __launch_bounds__(LONG_T) void k_long_sums(Long a, int before, int pr
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), min(a.o.n_cols, c0 + a.part)};
     const int32_t runs = a.part / LONG_RUN;
-    // What counts as a range of scores: above the cut, and what is equal to it if all that is does.  1024 weights of 2^40 units are a whole
-    // number that a double holds
     const Range maybe = range_of(st);
-    const float tie = score_of(st.cut.key);
-    const float edge = open ? (st.x.last() >= st.most ? NAN : score_of((uint32_t)st.x.last() + 1u))
-                            : st.cut.key == 0u ? -INFINITY : st.cut.every ? tie : score_of(st.cut.key + 1u);
-    const double fewest = (double)least;
-    const bool all = least <= 1ull, count_ties = !open && !st.cut.every;
-    uint2 *list = a.list + here * (a.part / LIST_PART), *queue = s_queue[wave];
-    int waiting = 0;
-    const auto weigh_some = [&](int first, int n) {
-        Team<64>::sync();
-        uint32_t at = 0u;
-        if (lane == 0) at = atomicAdd(&s_listed, (uint32_t)n);
-        at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at) + lane;
-        if (lane < n) {
-            const uint2 e = queue[first + lane];
-            const uint32_t key = key_in_order(__uint_as_float(e.x));
-            if (at < (uint32_t)(a.part / LIST_PART)) list[at] = e;
-            if (key > st.cut.key) atomicAdd(&s_hist[st.x.digit(key)], weigh(key));
-        }
-        Team<64>::sync();
-    };
+    const bool above = st.x.last() < st.most, count_ties = !open && !st.cut.every;
+    const float edge = !open ? edge_of(st.cut) : above ? score_of((uint32_t)st.x.last() + 1u) : NAN;
+    // The sums by the first digit hold what min-p takes: they serve where it takes nothing above that digit, by more than a weight's rounding
+    const bool by_digit = open && a.part_hist && (least <= 1ull || !above || weigh((uint32_t)st.x.last() + 1u) >= least + 2ull);
+    uint2 *list = a.list + here * (a.part / LIST_PART);
     u64 sum = 0ull, ties = 0ull;
     for (int32_t i = wave; i < runs && c0 + LONG_RUN * i < src.n; i += LONG_T / 64) {
         float l[16];
         src.run16(c0 + LONG_RUN * i, lane, l);
-        u64 w = 0ull, t = 0ull;
-        double lanes = 0.0;
-        if (weigh.endless) {
-#pragma unroll
-            for (int k = 0; k < 16; ++k) lanes += l[k] == INFINITY && l[k] >= edge ? (double)weigh.unit() : 0.0;
-        } else if (all) {
-#pragma unroll
-            for (int k = 0; k < 16; ++k) lanes += weigh.raised(l[k] >= edge ? l[k] : -INFINITY) - 0x1p52;
-        } else {
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const double v = weigh.raised(l[k] >= edge ? l[k] : -INFINITY) - 0x1p52;
-                lanes += v >= fewest ? v : 0.0;
-            }
-        }
-        w = st.most ? whole(lane_of(wave_scan(lanes), 63)) : 0ull;
-        if (count_ties) {
-#pragma unroll
-            for (int k = 0; k < 16; ++k) t += l[k] == tie ? 1ull : 0ull;
-            t = wave_sum(t);
-        }
-        if (lane == 0) {
+        const u64 w = st.most && !by_digit ? run_weight(l, edge, least, weigh) : 0ull, t = count_ties ? run_ties(l, score_of(st.cut.key)) : 0ull;
+        if (lane == 0 && a.run_sum) {
             a.run_sum[here * runs + i] = w;
             a.run_ties[here * runs + i] = t;
         }
         sum += w;
         ties += t;
-        if (open) {                                              // gathered, so that whole wavefronts weigh
+        if (open) {
+            uint32_t hits = 0u;
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const bool hit = l[k] >= maybe.from && l[k] <= maybe.upto;
-                const u64 hits = __ballot(hit);
-                if (hit) {
-                    const int at = waiting + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, 0u));
-                    queue[at] = make_uint2(__float_as_uint(l[k]), (uint32_t)(c0 + LONG_RUN * i + RUN * (k / 4) + 4 * lane + k % 4));
-                }
-                waiting += (int)__popcll(hits);
-                if (k % 4 == 3) {
+            for (int k = 0; k < 16; ++k) hits |= l[k] >= maybe.from && l[k] <= maybe.upto ? 1u << k : 0u;
 #pragma unroll 1
-                    while (waiting >= 64) {
-                        waiting -= 64;
-                        weigh_some(waiting, 64);
-                    }
-                }
+            while (hits) {                                       // few: read again, so that no register is named by a number
+                const int k = __builtin_ctz(hits);
+                hits &= hits - 1u;
+                const int32_t c = c0 + LONG_RUN * i + RUN * (k / 4) + 4 * lane + k % 4;
+                const float x = src.one(c);
+                const uint32_t key = key_in_order(x), at = atomicAdd(&s_listed, 1u);
+                if (at < (uint32_t)(a.part / LIST_PART)) list[at] = make_uint2(__float_as_uint(x), (uint32_t)c);
+                if (key > st.cut.key) atomicAdd(&s_hist[st.x.digit(key)], weigh(key));
             }
         }
     }
-    if (open) weigh_some(0, waiting);
+    if (by_digit) {
+        for (int i = (int)st.x.found + 1 + (int)threadIdx.x; i < LONG_DIGITS; i += LONG_T) sum += a.part_hist[here * LONG_DIGITS + i];
+        sum = wave_sum(sum);
+    }
     // every lane of a wavefront has its sums
     if (lane == 0) { s_part[wave] = sum; s_part[8 + wave] = ties; }
     if (open && part == 0 && threadIdx.x == 0 && st.cut.key && st.x.in(st.cut.key)) atomicAdd(&s_hist[st.x.digit(st.cut.key)], st.cut.ties * weigh(st.cut.key));
@@ -1381,13 +1378,17 @@ __global__ __launch_bounds__(LONG_T) void k_long_rest(Long a)
         const int i = threadIdx.x;
         u64 w = 0ull, t = 0ull;
         if (i < runs && c0 + LONG_RUN * i < src.n) {
-            w = a.run_sum[here * runs + i] += s_sum[i];
-            t = a.run_ties[here * runs + i] = s_ties[i];
+            w = s_sum[i];
+            t = s_ties[i];
+            if (a.run_sum) {
+                a.run_sum[here * runs + i] += w;
+                a.run_ties[here * runs + i] = t;
+            }
         }
         w = wave_sum(w);
         t = wave_sum(t);
         if (i == 0) {
-            a.part_sum[here] = w;
+            a.part_sum[here] += w;
             a.part_ties[here] = t;
         }
     }
@@ -1426,16 +1427,18 @@ __device__ __forceinline__ Found find_item(const u64 *sum, const u64 *tie, int32
     return f;
 }
 
-// a wavefront a draw
-template <bool BF16>
-__global__ __launch_bounds__(256) void k_long_draw(Long a, int64_t first, int64_t n)
+// A draw by WAVES wavefronts: one, which finds the run in its part, or those of a block, which weigh the part again
+template <bool BF16, int WAVES>
+__global__ __launch_bounds__(WAVES > 1 ? 64 * WAVES : 256) void k_long_draw(Long a, int64_t first, int64_t n)
 {
+    constexpr int RUNS_MOST = 32;
+    __shared__ u64 s_sum[WAVES > 1 ? RUNS_MOST : 1], s_ties[WAVES > 1 ? RUNS_MOST : 1];
     __shared__ double s_pow[POWERS];
     fill_pow(s_pow, a.o.bits);
-    const int lane = threadIdx.x & 63;
-    const int64_t wave = first + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (wave >= n) return;
-    const int64_t r = wave / a.o.n_draws, at = a.row0 * a.o.n_draws + wave;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t draw = first + (WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave);
+    if (draw >= n) return;
+    const int64_t r = draw / a.o.n_draws, at = a.row0 * a.o.n_draws + draw;
     const State st = a.state[r * 7 + 6];
     const Setting set = setting_of(a.o.how, a.row0 + r);
     Weigh weigh;
@@ -1446,20 +1449,35 @@ __global__ __launch_bounds__(256) void k_long_draw(Long a, int64_t first, int64_
     const u64 *sum = a.part_sum + r * a.parts, *tie = a.part_ties + r * a.parts;
     const u64 total = find_item(sum, tie, a.parts, 0ull, 0ull, st.cut.ties, w_tie, false, 0ull).total;
     if (total == 0ull) {
-        if (lane == 0) answer(a.o, at, -1, 0.0, 1.0);
+        if (lane == 0 && (WAVES == 1 || wave == 0)) answer(a.o, at, -1, 0.0, 1.0);
         return;
     }
     const u64 goal = goal_of_draw(a.o, at, total);
     const Found p = find_item(sum, tie, a.parts, 0ull, 0ull, st.cut.ties, w_tie, true, goal);
-    const int32_t runs = a.part / LONG_RUN;
-    const int64_t run0 = (r * a.parts + p.item) * runs;
-    const int32_t last = (a.o.n_cols - p.item * a.part + LONG_RUN - 1) / LONG_RUN;      // the row may end in this part
-    const Found f = find_item(a.run_sum + run0, a.run_ties + run0, min(runs, last), p.before, p.ties, st.cut.ties, w_tie, true, goal);
     const Scores<BF16> src{(const char *)a.o.scores + (a.row0 + r) * a.o.lds * (BF16 ? 2 : 4), a.o.n_cols};
+    const int32_t c0 = p.item * a.part, last = (src.n - c0 + LONG_RUN - 1) / LONG_RUN, runs = min(a.part / LONG_RUN, last);       // the row may end in this part
+    const u64 *run_sum = a.run_sum, *run_tie = a.run_ties;
+    if (WAVES == 1) {
+        run_sum += (r * a.parts + p.item) * (a.part / LONG_RUN);
+        run_tie += (r * a.parts + p.item) * (a.part / LONG_RUN);
+    } else {
+        const float edge = edge_of(st.cut);
+        for (int32_t i = wave; i < runs; i += WAVES) {
+            float l[16];
+            src.run16(c0 + LONG_RUN * i, lane, l);
+            const u64 w = run_weight(l, edge, least, weigh), t = st.cut.every ? 0ull : run_ties(l, score_of(st.cut.key));
+            if (lane == 0) { s_sum[i] = w; s_ties[i] = t; }
+        }
+        __syncthreads();
+        if (wave > 0) return;
+        run_sum = s_sum;
+        run_tie = s_ties;
+    }
+    const Found f = find_item(run_sum, run_tie, runs, p.before, p.ties, st.cut.ties, w_tie, true, goal);
     u64 equal = f.ties, upto = f.before;
 #pragma unroll 1
     for (int i = 0; i < LONG_RUN / RUN && upto <= goal; ++i) {
-        const int32_t c = p.item * a.part + LONG_RUN * f.item + RUN * i + 4 * lane;
+        const int32_t c = c0 + LONG_RUN * f.item + RUN * i + 4 * lane;
         uint32_t key[4];
         get4(src, c, key);
         upto += pick4(a.o, at, src, c, key, st.cut, weigh, least, &equal, goal, upto, total);
@@ -1487,8 +1505,12 @@ constexpr int64_t BLOCK_ROW = 65536;
 struct Plan {
     int32_t most_k, slots;         // 0: rows, or digits in launches; else k_part_top's
     int32_t parts, part, rows;     // parts of a row, columns of a part, rows a batch
-    size_t off_most, off_hist, off_state, off_sum, off_ties, off_run, off_run_ties, off_list, off_listed, bytes;
+    size_t off_most, off_hist, off_state, off_sum, off_ties, off_run, off_run_ties, off_part_hist, off_list, off_listed, bytes;
 };
+
+// Whether parts may keep their sums by digit: parts that are several times as many scores
+template <class How>
+bool parts_digits(const How &how, int64_t part) { return part >= 16384 && (how.row_top_p || how.top_p < 1.f); }
 
 Plan plan_of(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
 {
@@ -1528,6 +1550,7 @@ Plan plan_of(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
     p.off_ties = take(parts * 8);
     p.off_run = take(runs * 8);
     p.off_run_ties = take(runs * 8);
+    p.off_part_hist = take(parts_digits(*how, p.part) ? parts * LONG_DIGITS * 8 : 0);
     p.off_list = take(parts * (part / LIST_PART) * 8);
     p.off_listed = take(parts * 4);
     p.bytes = at;
@@ -1581,6 +1604,11 @@ int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
     a.list = (uint2 *)(ws + p.off_list); a.listed = (uint32_t *)(ws + p.off_listed);
     const bool by_count = o.how.row_top_k || o.how.top_k > 1;
     const bool by_weight = o.how.row_top_p || o.how.top_p < 1.f;
+    // Draws that weigh a quarter of the row again at most.  top_p 0.9, 4 draws, us, weighing again / sums by runs: 16 x 2.9 million 168 / 185, 40 x a million
+    // 145 / 155; parts of 4096, 1 x 2.9 million 66 / 62
+    const bool again = parts_digits(o.how, p.part) && o.n_draws <= o.n_cols / p.part / 4;
+    if (again) a.run_sum = a.run_ties = nullptr;
+    a.part_hist = again ? (u64 *)(ws + p.off_part_hist) : nullptr;
     for (a.row0 = 0; a.row0 < o.n_rows; a.row0 += p.rows) {
         const int64_t rows = o.n_rows - a.row0 < p.rows ? o.n_rows - a.row0 : p.rows;
         const unsigned blocks = (unsigned)(rows * p.parts);
@@ -1604,8 +1632,10 @@ int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
             KGE_LAUNCH_CHECK();
         }
         const int64_t draws = rows * o.n_draws;
-        for (int64_t d = 0; d < draws; d += LONG_BLOCKS * 4) {
-            k_long_draw<BF16><<<(unsigned)cdiv(draws - d < LONG_BLOCKS * 4 ? draws - d : LONG_BLOCKS * 4, 4), 256, 0, st>>>(a, d, draws);
+        for (int64_t d = 0; d < draws; d += LONG_BLOCKS) {
+            const int64_t here = draws - d < LONG_BLOCKS ? draws - d : LONG_BLOCKS;
+            if (again) k_long_draw<BF16, 16><<<(unsigned)here, 1024, 0, st>>>(a, d, draws);
+            else k_long_draw<BF16, 1><<<(unsigned)cdiv(here, 4), 256, 0, st>>>(a, d, d + here);
             KGE_LAUNCH_CHECK();
         }
     }

@@ -302,6 +302,24 @@ def test_rows_of_millions(kb, kind):  # noqa: F811
         check(kb, s, u, kind, **how)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_few_draws_of_long_rows(kb, kind):  # noqa: F811
+    """Enough rows for parts of 16384, and so few draws that each weighs its part again; rows of every kind in one call: a plain top-p, no top-p,
+    one score, min-p above top-p's first digit and below it, ties of both cuts, infinities, nothing"""
+    rows, cols = 9, 2_900_000
+    s, u = scores_of(rows, cols, 77, 2.0, out=0.01, kind=kind)
+    s[4] = np.round(s[4] * 2) / 2
+    s[5] = np.round(s[5] * 2) / 2
+    s[6, [17, 40_000, 2_899_999]] = np.inf
+    s[7] = np.nan
+    s[8, 1_000_000:] = -np.inf
+    say(kind)
+    check(kb, s, u, kind, temperature=np.array([0.9, 1, 0, 1.5, 0.8, 1, 1, 1, 3], np.float32), top_k=np.array([0, 0, 0, 0, 0, 200_000, 0, 5, 700_000], np.int32),
+          top_p=np.array([0.9, 1, 0.5, 0.95, 0.7, 0.8, 0.6, 0.5, 0.3], np.float32), min_p=np.array([0, 0, 0, 0.4, 0.001, 0, 0.5, 0, 1e-4], np.float32))
+    check(kb, s, u, kind, temperature=1.1, top_p=0.97, min_p=0.01)
+    check(kb, s[:, :2_000_001], u, kind, temperature=2.0, top_p=0.4)
+
+
 def test_more_long_rows_than_a_batch(kb):  # noqa: F811
     import torch
     if torch.cuda.mem_get_info()[0] < 24 << 30:
