@@ -746,7 +746,9 @@ __device__ __forceinline__ void draw_few(const Call &o, int64_t first, K &keys, 
 }
 
 // The sums by column of a row that a wavefront holds (w: its weights left, 4 columns a lane a tile), 1024 weights of 2^40 units at most, which a
-// double holds; a lane finds a draw by halving.
+// double holds; a lane finds a draw by halving.  A place is left free after every 32 sums: lanes that halve read places a power of two apart, which would
+// be in a few of the banks (65536 rows of 256, 64 draws: 46 us without, and with a search that takes any length, 39)
+constexpr int padded(int i) { return i + i / 32; }
 template <int TILES, class W, class Source>
 __device__ __forceinline__ void draw_by_column(const Call &o, int64_t first, const Source &src, double *to, W weights)
 {
@@ -760,14 +762,19 @@ __device__ __forceinline__ void draw_by_column(const Call &o, int64_t first, con
         w[1] += w[0]; w[2] += w[1]; w[3] += w[2];
         const double upto = wave_scan(w[3]), base = total + (upto - w[3]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) to[4 * (64 * i + lane) + k] = base + w[k];
+        for (int k = 0; k < 4; ++k) to[padded(256 * i) + 4 * lane + (lane >> 3) + k] = base + w[k];
         total += lane_of(upto, 63);
     }
     T::sync();
     const double inverse = inverse_of(total);
     for (int32_t i = lane; i < o.n_draws; i += 64) {
-        const int at = first_above(to, 256 * TILES, goal_of_draw(o, first + i, total));
-        answer(o, first + i, src.column(at), to[at] - (at ? to[at - 1] : 0.0), inverse);
+        const double goal = goal_of_draw(o, first + i, total);
+        int place = 0;                                           // of the first sum above the goal
+#pragma unroll
+        for (int step = 128 * TILES; step > 0; step /= 2)
+            if (to[place + padded(step - 1)] <= goal) place += padded(step);
+        const int at = place - place / 33;
+        answer(o, first + i, src.column(at), to[place] - (place ? to[place - 1 - (at % 32 == 0)] : 0.0), inverse);
     }
     T::sync();
 }
@@ -974,7 +981,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) __attribute__((amdgpu_waves_pe
 {
     constexpr int BITS = NT == 64 ? 8 : NT == 256 ? 11 : 12, TEAMS = NT == 64 ? 4 : 1, COLUMNS = 4 * TILES * NT;
     constexpr bool BY_COLUMN = ONE && NT == 64;
-    __shared__ u64 s_hist[TEAMS][1 << BITS], s_sums[TEAMS][BY_COLUMN ? COLUMNS : NT], s_ties[TEAMS][BY_COLUMN ? 1 : NT];
+    __shared__ u64 s_hist[TEAMS][1 << BITS], s_sums[TEAMS][BY_COLUMN ? padded(COLUMNS) : NT], s_ties[TEAMS][BY_COLUMN ? 1 : NT];
     __shared__ u64 s_part[TEAMS][16], s_found[TEAMS][4];
     __shared__ double s_pow[POWERS];
     fill_pow(s_pow, o.bits);
