@@ -805,10 +805,9 @@ __device__ __forceinline__ void draw_by_run(const Call &o, int64_t first, const 
     T::sync();
 }
 
-// A row of which neither top-k nor top-p takes anything: its scores are no more than numbers, their order does not matter.  False: its largest score
-// is infinite, and nothing is done
+// A row of which neither top-k nor top-p takes anything: its scores are no more than numbers, their order does not matter
 template <int NT, int TILES, bool ONE, bool BF16>
-__device__ __forceinline__ bool draw_plain(const Call &o, int64_t first, const Setting &set, const Scores<BF16> &src, u64 *sums, u64 *s, const double *pow)
+__device__ __forceinline__ void draw_plain(const Call &o, int64_t first, const Setting &set, const Scores<BF16> &src, u64 *sums, u64 *s, const double *pow)
 {
     typedef Team<NT> T;
     constexpr int V = 4 * TILES, BATCH = NT * V, WAVES = NT / 64;
@@ -840,16 +839,19 @@ __device__ __forceinline__ bool draw_plain(const Call &o, int64_t first, const S
     const uint32_t most = T::most(key_of(mine), s);
     if (most == 0u) {
         for (int32_t i = T::tid(); i < o.n_draws; i += NT) answer(o, first + i, -1, 0.0, 1.0);
-        return true;
+        return;
     }
     Weigh weigh;
     weigh.init(most, set.t, o, pow);
-    if (weigh.endless) return false;
     const u64 least = least_weight(set, weigh);
     const double fewest = (double)least;
     const auto weigh4 = [&](int i, double w[4]) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) w[k] = weigh.raised(l[4 * i + k]) - 0x1p52;
+        if (weigh.endless) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = l[4 * i + k] == INFINITY ? (double)weigh.unit() : 0.0;
+        }
         if (least > 1ull) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) w[k] = w[k] >= fewest ? w[k] : 0.0;
@@ -872,7 +874,6 @@ __device__ __forceinline__ bool draw_plain(const Call &o, int64_t first, const S
         }
         draw_by_run<NT>(o, first, src, Cut{0u, true, 0ull}, weigh, least, sums, nullptr, s);
     }
-    return true;
 }
 
 // One row.  Up to 1024 columns the sums by column are in LDS, and a lane finds a draw by halving; beyond, the sums by runs of 256
@@ -887,7 +888,10 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
     const int tid = T::tid(), wave = NT == 64 ? 0 : (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const Setting set = setting_of(o.how, r);
     if constexpr (Source::PLAIN) {
-        if (set.k != 1 && !cuts(0, set, src.n) && !cuts(1, set, src.n) && draw_plain<NT, TILES, ONE>(o, r * o.n_draws, set, src, sums, s, pow)) return;
+        if (set.k != 1 && !cuts(0, set, src.n) && !cuts(1, set, src.n)) {
+            draw_plain<NT, TILES, ONE>(o, r * o.n_draws, set, src, sums, s, pow);
+            return;
+        }
     }
     K keys(src);
     uint32_t mine = 0u;
@@ -974,25 +978,33 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
     }
 }
 
-// NT 64: four rows a block, a wavefront each.  Wavefronts at once to a SIMD: what LDS leaves room for
-constexpr int waves_of(int nt, int tiles, bool one) { return nt == 64 && one ? (tiles == 1 ? 5 : 3) : 4; }
-template <bool BF16, int NT, int TILES, bool ONE, bool PARTS>
-__global__ __launch_bounds__(NT == 64 ? 256 : NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT, TILES, ONE)))) void k_rows(Call o)
+// What a kernel's rows are: scores, scores of which nothing is cut (the host knows: no row is looked at for it, and registers and LDS are less),
+// the first scores of parts
+enum { CUT, PLAIN, PARTS };
+// NT 64: four rows a block, a wavefront each.  Wavefronts at once to a SIMD: what LDS and registers leave room for
+constexpr int waves_of(int nt, int tiles, bool one, int kind)
+{
+    if (kind == PLAIN) return nt == 64 && one ? (tiles == 1 ? 8 : 4) : nt == 1024 ? 4 : 6;
+    return nt == 64 && one ? (tiles == 1 ? 5 : 3) : 4;
+}
+template <bool BF16, int NT, int TILES, bool ONE, int KIND>
+__global__ __launch_bounds__(NT == 64 ? 256 : NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT, TILES, ONE, KIND)))) void k_rows(Call o)
 {
     constexpr int BITS = NT == 64 ? 8 : NT == 256 ? 11 : 12, TEAMS = NT == 64 ? 4 : 1, COLUMNS = 4 * TILES * NT;
     constexpr bool BY_COLUMN = ONE && NT == 64;
-    __shared__ u64 s_hist[TEAMS][1 << BITS], s_sums[TEAMS][BY_COLUMN ? padded(COLUMNS) : NT], s_ties[TEAMS][BY_COLUMN ? 1 : NT];
+    __shared__ u64 s_hist[TEAMS][KIND == PLAIN ? 1 : 1 << BITS], s_sums[TEAMS][BY_COLUMN ? padded(COLUMNS) : NT], s_ties[TEAMS][BY_COLUMN || KIND == PLAIN ? 1 : NT];
     __shared__ u64 s_part[TEAMS][16], s_found[TEAMS][4];
     __shared__ double s_pow[POWERS];
     fill_pow(s_pow, o.bits);
     const int team = NT == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     for (int64_t r = (int64_t)blockIdx.x * TEAMS + team; r < o.n_rows; r += (int64_t)gridDim.x * TEAMS) {
-        if constexpr (PARTS) {
+        if constexpr (KIND == PARTS) {
             const Parts src{o.part_key + r * o.n_part, o.part_col + r * o.n_part, o.n_part};
             draw_row<NT, TILES, ONE, BITS>(o, r, src, s_hist[team], s_sums[team], s_ties[team], s_part[team], s_found[team], s_pow);
         } else {
             const Scores<BF16> src{(const char *)o.scores + r * o.lds * (BF16 ? 2 : 4), o.n_cols};
-            draw_row<NT, TILES, ONE, BITS>(o, r, src, s_hist[team], s_sums[team], s_ties[team], s_part[team], s_found[team], s_pow);
+            if constexpr (KIND == PLAIN) draw_plain<NT, TILES, ONE>(o, r * o.n_draws, setting_of(o.how, r), src, s_sums[team], s_part[team], s_pow);
+            else draw_row<NT, TILES, ONE, BITS>(o, r, src, s_hist[team], s_sums[team], s_ties[team], s_part[team], s_found[team], s_pow);
         }
     }
 }
@@ -1564,30 +1576,40 @@ Plan plan_of(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
     return p;
 }
 
-template <bool BF16, int NT, int TILES, bool ONE, bool PARTS>
+template <bool BF16, int NT, int TILES, bool ONE, int KIND>
 int launch_rows(const Call &o, hipStream_t st)
 {
     // a table of powers a block: its wavefronts take rows in turn
     const int64_t blocks = NT == 64 ? cdiv(o.n_rows, 4) : o.n_rows, most = NT == 64 ? 2048 : 65536;
-    k_rows<BF16, NT, TILES, ONE, PARTS><<<(unsigned)(blocks < most ? blocks : most), NT == 64 ? 256 : NT, 0, st>>>(o);
+    k_rows<BF16, NT, TILES, ONE, KIND><<<(unsigned)(blocks < most ? blocks : most), NT == 64 ? 256 : NT, 0, st>>>(o);
     KGE_LAUNCH_CHECK();
     return KGE_OK;
+}
+
+// rows that are taken whole
+template <bool BF16, int KIND>
+int launch_whole(const Call &o, hipStream_t st)
+{
+    if (o.n_cols <= 256) return launch_rows<BF16, 64, 1, true, KIND>(o, st);
+    if (o.n_cols <= 1024) return launch_rows<BF16, 64, 4, true, KIND>(o, st);
+    // Rows of little more: a wavefront a row, which reads them again, or a block.  No settings, us, wavefront / block: 16384 x 1100 96 / 157, 8192 x 2000
+    // 52 / 83, 4096 x 4000 45 / 48, 2048 x 4000 29 / 26, 1024 x 1100 15 / 13
+    if (o.n_cols <= 2048 && o.n_rows >= 4096) return launch_rows<BF16, 64, 4, false, KIND>(o, st);
+    if (o.n_cols <= 4096) return launch_rows<BF16, 256, 4, false, KIND>(o, st);
+    // Rows enough for several blocks to a compute unit: small ones, whose waits overlap.  No settings, us, 256 threads / 1024: 2048 x 14541 66 / 96, 600 x
+    // 60000 89 / 101, 300 x 14541 24 with 1024
+    if (o.n_cols <= RUN * 256 && o.n_rows >= 512) return launch_rows<BF16, 256, 4, false, KIND>(o, st);
+    if (o.n_cols <= 16384) return launch_rows<BF16, 1024, 4, true, KIND>(o, st);
+    return launch_rows<BF16, 1024, 4, false, KIND>(o, st);
 }
 
 template <bool BF16>
 int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
 {
-    if (o.n_cols <= 256) return launch_rows<BF16, 64, 1, true, false>(o, st);
-    if (o.n_cols <= 1024) return launch_rows<BF16, 64, 4, true, false>(o, st);
-    // Rows of little more: a wavefront a row, which reads them again, or a block.  No settings, us, wavefront / block: 16384 x 1100 96 / 157, 8192 x 2000
-    // 52 / 83, 4096 x 4000 45 / 48, 2048 x 4000 29 / 26, 1024 x 1100 15 / 13
-    if (o.n_cols <= 2048 && o.n_rows >= 4096) return launch_rows<BF16, 64, 4, false, false>(o, st);
-    if (o.n_cols <= 4096) return launch_rows<BF16, 256, 4, false, false>(o, st);
-    // Rows enough for several blocks to a compute unit: small ones, whose waits overlap.  No settings, us, 256 threads / 1024: 2048 x 14541 66 / 96, 600 x
-    // 60000 89 / 101, 300 x 14541 24 with 1024
-    if (o.n_cols <= RUN * 256 && o.n_rows >= 512) return launch_rows<BF16, 256, 4, false, false>(o, st);
-    if (o.n_cols <= 16384) return launch_rows<BF16, 1024, 4, true, false>(o, st);
-    if (p.parts == 0) return launch_rows<BF16, 1024, 4, false, false>(o, st);
+    if (p.parts == 0) {
+        const bool cut = o.how.row_temperature || !(o.how.temperature > 0.f) || o.how.row_top_k || o.how.top_k > 0 || o.how.row_top_p || o.how.top_p < 1.f;
+        return cut ? launch_whole<BF16, CUT>(o, st) : launch_whole<BF16, PLAIN>(o, st);
+    }
     if (p.most_k) {
         uint32_t *part_key = (uint32_t *)ws;
         int32_t *part_col = (int32_t *)(ws + p.bytes / 2);
@@ -1598,10 +1620,10 @@ int launch_call(Call o, const Plan &p, char *ws, hipStream_t st)
             KGE_LAUNCH_CHECK();
         }
         o.part_key = part_key; o.part_col = part_col; o.n_part = p.parts * p.slots;
-        if (o.n_part <= 1024) return launch_rows<false, 64, 4, true, true>(o, st);
-        if (o.n_part <= 4096) return launch_rows<false, 256, 4, false, true>(o, st);
-        if (o.n_part <= 16384) return launch_rows<false, 1024, 4, true, true>(o, st);
-        return launch_rows<false, 1024, 4, false, true>(o, st);
+        if (o.n_part <= 1024) return launch_rows<false, 64, 4, true, PARTS>(o, st);
+        if (o.n_part <= 4096) return launch_rows<false, 256, 4, false, PARTS>(o, st);
+        if (o.n_part <= 16384) return launch_rows<false, 1024, 4, true, PARTS>(o, st);
+        return launch_rows<false, 1024, 4, false, PARTS>(o, st);
     }
     Long a;
     a.o = o; a.parts = p.parts; a.part = p.part;
