@@ -17,7 +17,7 @@
 //                           of columns, are a short row for a block
 //   more                    a launch for each digit; blocks add their parts' sums by digit to the row's in memory (k_long_digit)
 //
-// Bound by vector instructions where rows are many (65536 rows of 256, 64 draws each: 44 us, 3.1 TB/s; 16 rows of 2.9 million
+// Bound by vector instructions where rows are many (65536 rows of 256, 64 draws each: 35 us, 3.9 TB/s; 16 rows of 2.9 million
 // at top_p 0.9: 168 us in six launches), by waits where they are few (one row of a million at top_k 50: 9 + 18 us).
 #include "common.h"
 
@@ -747,7 +747,7 @@ __device__ __forceinline__ void draw_few(const Call &o, int64_t first, K &keys, 
 
 // The sums by column of a row that a wavefront holds (w: its weights left, 4 columns a lane a tile), 1024 weights of 2^40 units at most, which a
 // double holds; a lane finds a draw by halving.  A place is left free after every 32 sums: lanes that halve read places a power of two apart, which would
-// be in a few of the banks (65536 rows of 256, 64 draws: 46 us without, and with a search that takes any length, 39)
+// be in a few of the banks (65536 rows of 256, 64 draws: 46 us without, and with a search that takes any length, 40)
 constexpr int padded(int i) { return i + i / 32; }
 template <int TILES, class W, class Source>
 __device__ __forceinline__ void draw_by_column(const Call &o, int64_t first, const Source &src, double *to, W weights)
@@ -978,8 +978,8 @@ __device__ __forceinline__ void draw_row(const Call &o, int64_t r, const Source 
     }
 }
 
-// What a kernel's rows are: scores, scores of which nothing is cut (the host knows: no row is looked at for it, and registers and LDS are less),
-// the first scores of parts
+// What a kernel's rows are: scores, scores of which the host knows that nothing is cut (half the registers and no sums by digit: 65536 rows of 256, 64
+// draws, 40 us as a branch of the first kernel, 35 here), the first scores of parts
 enum { CUT, PLAIN, PARTS };
 // NT 64: four rows a block, a wavefront each.  Wavefronts at once to a SIMD: what LDS and registers leave room for
 constexpr int waves_of(int nt, int tiles, bool one, int kind)
@@ -1593,7 +1593,7 @@ int launch_whole(const Call &o, hipStream_t st)
     if (o.n_cols <= 256) return launch_rows<BF16, 64, 1, true, KIND>(o, st);
     if (o.n_cols <= 1024) return launch_rows<BF16, 64, 4, true, KIND>(o, st);
     // Rows of little more: a wavefront a row, which reads them again, or a block.  No settings, us, wavefront / block: 16384 x 1100 96 / 157, 8192 x 2000
-    // 52 / 83, 4096 x 4000 45 / 48, 2048 x 4000 29 / 26, 1024 x 1100 15 / 13
+    // 52 / 83, 4096 x 4000 45 / 48, 2048 x 4000 29 / 26, 1024 x 1100 15 / 13 (top-p's kernels; those that cut nothing are faster alike)
     if (o.n_cols <= 2048 && o.n_rows >= 4096) return launch_rows<BF16, 64, 4, false, KIND>(o, st);
     if (o.n_cols <= 4096) return launch_rows<BF16, 256, 4, false, KIND>(o, st);
     // Rows enough for several blocks to a compute unit: small ones, whose waits overlap.  No settings, us, 256 threads / 1024: 2048 x 14541 66 / 96, 600 x
