@@ -834,7 +834,7 @@ __device__ __forceinline__ void draw_plain(const Call &o, int64_t first, const S
     for (int32_t c0 = 0; c0 < src.n; c0 += BATCH) {
         load(c0);
 #pragma unroll
-        for (int k = 0; k < V; ++k) mine = __builtin_fmaxf(mine, l[k]);          // of NaN and a number the number
+        for (int k = 0; k < V; ++k) mine = l[k] > mine ? l[k] : mine;          // the instruction for the larger one makes NaN of a signalling NaN
     }
     const uint32_t most = T::most(key_of(mine), s);
     if (most == 0u) {
@@ -1592,12 +1592,12 @@ int launch_whole(const Call &o, hipStream_t st)
 {
     if (o.n_cols <= 256) return launch_rows<BF16, 64, 1, true, KIND>(o, st);
     if (o.n_cols <= 1024) return launch_rows<BF16, 64, 4, true, KIND>(o, st);
-    // Rows of little more: a wavefront a row, which reads them again, or a block.  No settings, us, wavefront / block: 16384 x 1100 96 / 157, 8192 x 2000
-    // 52 / 83, 4096 x 4000 45 / 48, 2048 x 4000 29 / 26, 1024 x 1100 15 / 13 (top-p's kernels; those that cut nothing are faster alike)
+    // Rows of little more: a wavefront a row, which reads them again, or a block.  No settings, us, wavefront / block: 16384 x 1100 68 / 110, 8192 x 2000
+    // 38 / 56, 4096 x 2000 21 / 30; top_p 0.9: 196 / 343, 128 / 185, 67 / 96
     if (o.n_cols <= 2048 && o.n_rows >= 4096) return launch_rows<BF16, 64, 4, false, KIND>(o, st);
     if (o.n_cols <= 4096) return launch_rows<BF16, 256, 4, false, KIND>(o, st);
-    // Rows enough for several blocks to a compute unit: small ones, whose waits overlap.  No settings, us, 256 threads / 1024: 2048 x 14541 66 / 96, 600 x
-    // 60000 89 / 101, 300 x 14541 24 with 1024
+    // Rows enough for several blocks to a compute unit: small ones, whose waits overlap.  No settings, us, 256 threads / 1024: 2048 x 14541 51 / 73, 600 x
+    // 60000 70 / 77, 600 x 14541 21 / 27; top_p 0.9: 178 / 226, 276 / 270, 79 / 87
     if (o.n_cols <= RUN * 256 && o.n_rows >= 512) return launch_rows<BF16, 256, 4, false, KIND>(o, st);
     if (o.n_cols <= 16384) return launch_rows<BF16, 1024, 4, true, KIND>(o, st);
     return launch_rows<BF16, 1024, 4, false, KIND>(o, st);

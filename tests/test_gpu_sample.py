@@ -302,6 +302,27 @@ def test_rows_of_millions(kb, kind):  # noqa: F811
         check(kb, s, u, kind, **how)
 
 
+@pytest.mark.parametrize("cols", [3, 100, 700, 1500, 9000, 40000, 70000])
+def test_signalling_nan(kb, cols):  # noqa: F811
+    """A NaN of any bits is no score, wherever it stands: beside the largest, first and last"""
+    import torch
+    s, u = scores_of(5, cols, cols, 1.0)
+    bits = s.view(np.uint32)
+    for r, at in enumerate((0, cols - 1, cols // 2, 1)):
+        bits[r, at] = (0x7f800001, 0xff800001, 0x7fa00000, 0xffbfffff)[r]
+        s[r, (at + 1) % cols] = 6.0
+    s[4] = -np.inf
+    bits[4, 0] = 0x7f800001
+    half = torch.from_numpy((bits >> 16 | (np.isnan(s) * 1)).astype(np.uint16).view(np.int16)).cuda().view(torch.bfloat16)
+    for how in (dict(), dict(temperature=0.0), dict(top_k=2), dict(top_p=0.9), dict(min_p=0.3)):
+        say(cols, how)
+        t = torch.from_numpy(s.view(np.int32).copy()).cuda().view(torch.float32)
+        clean = np.where(np.isnan(s), -np.inf, s)
+        check(kb, clean, u, scores=t, **how)
+        clean = np.where(np.isnan(s), -np.inf, (bits & np.uint32(0xffff0000)).view(np.float32))
+        check(kb, clean, u, "bf16", scores=half, **how)
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 def test_few_draws_of_long_rows(kb, kind):  # noqa: F811
     """Enough rows for parts of 16384, and so few draws that each weighs its part again; rows of every kind in one call: a plain top-p, no top-p,
