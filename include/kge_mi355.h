@@ -252,7 +252,9 @@ int kge_rgcn_forward(const kge_partition *p, const kge_cgraph *cg, const kge_lay
  *   dH0    : device float [N][layers[0].d_in] or NULL (NULL when the layer-1 input is a fixed
  *            feature matrix and needs no gradient)
  *   cg     : the same object (or NULL) the forward call got; dH_out must then be zero outside
- *            the batch's vertices, as kge_distmult_score_loss writes it
+ *            the batch's vertices, as kge_distmult_score_loss writes it.  Between the two calls
+ *            kge_compute_graph may have filled it for a smaller batch, whose vertices are all among
+ *            those of the first: its sub-graph lies inside the one that was propagated
  */
 int kge_rgcn_backward(const kge_partition *p, const kge_cgraph *cg, const kge_layer *layers,
                       int32_t n_layers, int32_t msg_dtype, const float *H0, void *workspace,

@@ -199,7 +199,7 @@ class TrainStep:
         self.set_dropout_state(seed, step)
         n_cand = cand.shape[1]
         kb.sample_negatives(self.part, self.pos, n_cand, mode, seed, step, self.cand_ent, self.cand_side, stream)
-        if self.cg is not None:              # holds the negatives too: they are among the candidates
+        if self.cg is not None:
             kb.compute_graph(self.part, self.cg, self.pos, self.cand_ent, stream)
         self.forward(stream)
         kb.distmult_score_loss(self.part, self.H_out, self.M, self.pos, self.cand_ent, self.cand_side, n_cand, self.cand_scores,
@@ -211,6 +211,9 @@ class TrainStep:
             self.cand_workspace = kb._workspace(None, need, scores, stream)
         kb.sample_scores(scores, u, temperature, top_k, top_p, min_p, choice=self.choice, workspace=self.cand_workspace, stream=stream)
         kb.pick_negatives(self.cand_ent, self.cand_side, self.choice, self.neg_ent, self.neg_side, stream)
+        # from here on the step is that on the drawn negatives: its sub-graph lies in the one that was propagated, and its flags name
+        # the rows that have gradients, which are those an update takes
+        self.compute_graph(stream)
         self.score_loss(stream)
         self.backward(stream)
 
