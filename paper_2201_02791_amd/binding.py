@@ -881,12 +881,19 @@ def table4_scores(table: Table4, X, fixed=None, M=None, rel=None, out=None, stre
     return out
 
 
+def _count(k):
+    """A top_k for the library's 32 bits: no row has more than 2^31 - 1 columns, and what is below zero stays so, to be refused."""
+    return -1 if k < 0 else k if k <= 0x7fffffff else 0x7fffffff
+
+
 def _sampling(temperature, top_k, top_p, min_p, most_k, n_rows):
     """(the settings, the tensors among them): a setting is a number, or a tensor with one for each row."""
+    if not hasattr(top_k, "data_ptr"):
+        top_k = _count(top_k)
     if not any(hasattr(v, "data_ptr") for v in (temperature, top_k, top_p, min_p)):
         return _Sampling(temperature, top_k, top_p, min_p, None, None, None, None), ()
     torch = sys.modules["torch"]
-    call, rows, kept = [1.0, int(most_k), 1.0, 0.0], [None] * 4, []
+    call, rows, kept = [1.0, _count(int(most_k)), 1.0, 0.0], [None] * 4, []
     for i, (v, name) in enumerate(((temperature, "temperature"), (top_k, "top_k"), (top_p, "top_p"), (min_p, "min_p"))):
         if not hasattr(v, "data_ptr"):
             call[i] = v

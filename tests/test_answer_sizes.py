@@ -1,0 +1,44 @@
+"""Settings and sizes of the answering operators that a 32-bit argument does not hold are never cut to what it does.  None of it needs a GPU."""
+import os
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def kb():
+    from paper_2201_02791_amd import build, binding
+    if not os.path.exists(binding.LIB_PATH):
+        build.build(verbose=False)
+    binding.load()
+    return binding
+
+
+MOST = 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("k", [MOST, 2 ** 31, 2 ** 32, 2 ** 32 + 5, 10 ** 12, 2 ** 63, 2 ** 70])
+def test_a_top_k_that_is_more_than_any_row_has(kb, k):
+    """As many as there are, however large the number: the largest that the library takes, which no row reaches"""
+    import torch
+    assert kb._sampling(1.0, k, 1.0, 0.0, 0, 3)[0].top_k == MOST
+    rows = torch.ones(3, dtype=torch.int32)
+    assert kb._sampling(1.0, rows, 1.0, 0.0, k, 3)[0].top_k == MOST
+    assert kb._sampling(torch.ones(3), k, 1.0, 0.0, 0, 3)[0].top_k == MOST
+    assert kb.sample_workspace_bytes(3, 100000, top_k=k) == kb.sample_workspace_bytes(3, 100000, top_k=MOST)
+
+
+@pytest.mark.parametrize("k", [-1, -2 ** 31, -2 ** 31 - 1, -2 ** 32, -2 ** 32 + 5, -2 ** 70])
+def test_a_top_k_below_zero_is_refused(kb, k):
+    import torch
+    for how in (dict(top_k=k), dict(top_k=torch.ones(3, dtype=torch.int32), most_k=k), dict(top_k=k, temperature=torch.ones(3))):
+        with pytest.raises(kb.KgeError, match="top_k"):
+            kb.sample_workspace_bytes(3, 100000, **how)
+        with pytest.raises(kb.KgeError, match="top_k|device"):
+            kb.sample_scores(torch.zeros(3, 9), torch.zeros(3, 4), **how)
+
+
+def test_settings_in_range_are_kept(kb):
+    for k in (0, 1, 50, MOST - 1):
+        assert kb._sampling(0.5, k, 0.9, 0.1, 0, 3)[0].top_k == k
+    with pytest.raises(TypeError):
+        kb._sampling(0.5, 2.5, 0.9, 0.1, 0, 3)
