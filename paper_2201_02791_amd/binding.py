@@ -837,7 +837,8 @@ def table4_encode(X, table: Table4 = None, stream=None) -> Table4:
     x, ldx = _rows(X, "X")
     n, d = X.shape
     if table is None:
-        groups = -(-d // TABLE4_GROUP)                           # what the library refuses, it refuses below
+        _need(d <= 4096, "rows have 1 to 4096 elements")         # of more, the library would see the low 32 bits; none, it refuses
+        groups = -(-d // TABLE4_GROUP)
         table = object.__new__(Table4)._set(_new(X, (n, 16 * groups), torch.uint8, stream), _new(X, (n, groups), torch.bfloat16, stream), n, d)
     elif table.n_rows != n or table.d != d:
         raise KgeError(-1, "the table is of another shape than X")
@@ -926,6 +927,7 @@ def sample_scores(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mos
     _need(u.dim() == 2 and u.shape[0] == n and u.is_contiguous() and u.dtype in (torch.float32, torch.float64),
           "u: contiguous float32 or float64 is wanted, a row for each row of scores")
     draws = u.shape[1]
+    _need(draws < 1 << 31, "u: 2^31 draws or more of a row")
     how, kept = _sampling(temperature, top_k, top_p, min_p, most_k, n)
     choice = _new(scores, (n, draws), torch.int32, stream) if choice is None else choice
     if prob is None and want_prob:
@@ -952,6 +954,7 @@ def hide_positives(part: Partition, pos_core_idx, cand_ent, cand_side, scores, s
     for t, name, kind in ((cand_ent, "cand_ent", torch.int32), (cand_side, "cand_side", torch.uint8)):
         _need(t.dim() == 2 and t.dtype == kind and t.is_contiguous(), "%s: a contiguous matrix of %s is wanted" % (name, kind))
     n, cand = cand_ent.shape
+    _need(cand < 1 << 31, "cand_ent: 2^31 candidates or more of a positive")
     _need(cand_side.shape == cand_ent.shape, "cand_side: of cand_ent's shape")
     pos, _ = _ids(pos_core_idx, "pos_core_idx", n)
     s, lds = _rows(scores, "scores", cand, n, torch.float32)
@@ -967,6 +970,8 @@ def pick_negatives(cand_ent, cand_side, choice, neg_ent, neg_side, stream=None):
                           (neg_ent, "neg_ent", torch.int32), (neg_side, "neg_side", torch.uint8)):
         _need(t.dim() == 2 and t.dtype == kind and t.is_contiguous(), "%s: a contiguous matrix of %s is wanted" % (name, kind))
     _need(cand_side.shape == cand_ent.shape, "cand_side: of cand_ent's shape")
+    _need(cand_ent.shape[1] < 1 << 31, "cand_ent: 2^31 candidates or more of a positive")
+    _need(choice.shape[1] < 1 << 31, "choice: 2^31 negatives or more of a positive")
     _need(choice.shape[0] == cand_ent.shape[0] and neg_ent.shape == choice.shape and neg_side.shape == choice.shape,
           "choice, neg_ent and neg_side: of one shape, a row for each positive")
     _call(load().kge_pick_negatives, stream, cand_ent, (cand_side, choice, neg_ent, neg_side), cand_ent.data_ptr(), cand_side.data_ptr(),

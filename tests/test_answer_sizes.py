@@ -42,3 +42,24 @@ def test_settings_in_range_are_kept(kb):
         assert kb._sampling(0.5, k, 0.9, 0.1, 0, 3)[0].top_k == k
     with pytest.raises(TypeError):
         kb._sampling(0.5, 2.5, 0.9, 0.1, 0, 3)
+
+
+@pytest.mark.parametrize("wide", [2 ** 31, 2 ** 32, 2 ** 32 + 40])
+def test_sizes_past_32_bits_are_refused(kb, wide):
+    """Tensors without memory: what is checked is the argument, before any launch"""
+    import torch
+    at = lambda *s, dtype=torch.float32: torch.empty(*s, dtype=dtype, device="meta")  # noqa: E731
+    i32, u8 = torch.int32, torch.uint8
+    with pytest.raises(kb.KgeError, match="4096"):
+        kb.table4_encode(at(1, wide))
+    with pytest.raises(kb.KgeError, match="draws"):
+        kb.sample_scores(at(1, 9), at(1, wide))
+    with pytest.raises(kb.KgeError, match="candidates"):
+        kb.pick_negatives(at(1, wide, dtype=i32), at(1, wide, dtype=u8), at(1, 4, dtype=i32), at(1, 4, dtype=i32), at(1, 4, dtype=u8))
+    with pytest.raises(kb.KgeError, match="negatives"):
+        kb.pick_negatives(at(1, 9, dtype=i32), at(1, 9, dtype=u8), at(1, wide, dtype=i32), at(1, wide, dtype=i32), at(1, wide, dtype=u8))
+
+    class Part:
+        handle = None
+    with pytest.raises(kb.KgeError, match="candidates"):
+        kb.hide_positives(Part(), at(1, dtype=i32), at(1, wide, dtype=i32), at(1, wide, dtype=u8), at(1, wide))
