@@ -446,7 +446,8 @@ typedef struct kge_adamw {
 } kge_adamw;
 int kge_adamw_step(const kge_adamw *opt, const kge_adamw_tensor *tensors, int32_t n_tensors, void *stream);
 /* The same step with every gradient multiplied by *factor first (DEVICE float, read when the launch runs; e.g. what kge_grad_norm
- * left there).  KGE_ROWS_NONZERO goes by the gradients as they are.  A factor that is NaN: nothing is written. */
+ * left there).  KGE_ROWS_NONZERO goes by the gradients as they are.  A factor that is NaN: nothing is written, and t_dev, which the caller
+ * advances, should not have grown (kge_grad_norm_step sees to that). */
 int kge_adamw_step_scaled(const kge_adamw *opt, const kge_adamw_tensor *tensors, int32_t n_tensors, const float *factor, void *stream);
 
 /*
@@ -458,6 +459,8 @@ int kge_adamw_step_scaled(const kge_adamw *opt, const kge_adamw_tensor *tensors,
  * either may be NULL, with kge_grad_norm one of them at most.  A gradient that is not finite: norm is infinite or NaN, factor NaN
  * (a norm beyond the largest float reads as infinity, with its factor).
  *   kge_grad_norm   norm and factor alone, for a step that takes the factor along (kge_adamw_step_scaled)
+ *   kge_grad_norm_step  the same, and *t_dev (DEVICE int64, the number of the last step) grows by one where the factor is a number: as t_dev of
+ *                   that step it numbers those that are made, and a step that is left out has none
  *   kge_clip_grads  the gradients are scaled as well, in place (rounded once, after fp32's product, where they are bf16); with a factor of 1
  *                   they are not written, with a NaN they all become NaN.  No two tensors may overlap.
  *   max_norm: zero or more; infinity scales nothing.  workspace: DEVICE, 256-byte aligned, at least kge_grad_norm_workspace_bytes(n_tensors)
@@ -473,6 +476,8 @@ typedef struct kge_grad_tensor {
 size_t kge_grad_norm_workspace_bytes(int32_t n_tensors);
 int kge_grad_norm(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, float *factor, void *workspace,
                   size_t ws_bytes, void *stream);
+int kge_grad_norm_step(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, float *factor, int64_t *t_dev,
+                       void *workspace, size_t ws_bytes, void *stream);
 int kge_clip_grads(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, float *factor, void *workspace,
                    size_t ws_bytes, void *stream);
 

@@ -28,7 +28,7 @@ EXPORTED = ["kge_build_partition", "kge_partition_info", "kge_partition_export",
             "kge_partition_bad_ids", "kge_test_set_rel_slab", "kge_test_pair_query", "kge_dense_forward",
             "kge_dense_workspace_bytes", "kge_dense_backward", "kge_layer_norm_forward", "kge_layer_norm_workspace_bytes",
             "kge_layer_norm_backward", "kge_adamw_step", "kge_adamw_step_scaled", "kge_grad_norm_workspace_bytes", "kge_grad_norm",
-            "kge_clip_grads", "kge_table4_encode", "kge_table4_decode", "kge_table4_scores", "kge_sample_workspace_bytes",
+            "kge_grad_norm_step", "kge_clip_grads", "kge_table4_encode", "kge_table4_decode", "kge_table4_scores", "kge_sample_workspace_bytes",
             "kge_sample_scores", "kge_hide_positives", "kge_pick_negatives"]
 
 ACT_IDENTITY, ACT_RELU, ACT_SILU = 0, 1, 2       # ACT_SILU: dense layers only
@@ -157,6 +157,7 @@ def load():
         i32 = C.c_int32
         lib.kge_grad_norm_workspace_bytes.argtypes = [i32]
         lib.kge_grad_norm.argtypes = lib.kge_clip_grads.argtypes = [p, i32, C.c_double, p, p, p, size, p]
+        lib.kge_grad_norm_step.argtypes = [p, i32, C.c_double, p, p, p, p, size, p]
         lib.kge_table4_encode.argtypes = [p, i32, p, i64, p]
         lib.kge_table4_decode.argtypes = [p, p, i64, i32, p, i64, p]
         lib.kge_table4_scores.argtypes = [p, i32, p, i64, i64, p, p, i64, i64, p, i64, p, i64, p]
@@ -740,6 +741,11 @@ def adamw_step(tensors, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, t=1, t_dev=No
         _call(load().kge_adamw_step_scaled, stream, first, (t_dev, factor), C.byref(o), plan.array, n, pf)
 
 
+def check_adamw(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8):
+    """Refuses what adamw_step would of these settings, and does nothing else."""
+    _check(load().kge_adamw_step(C.byref(_AdamW(lr, beta1, beta2, eps, 1, None)), None, 0, None))
+
+
 # ---- the norm of all gradients, and clipping -----------------------------------------------------
 
 class GradTensors:
@@ -779,7 +785,7 @@ def grad_norm_workspace_bytes(n_tensors: int) -> int:
     return int(n)
 
 
-def _grad_norm(function, grads, max_norm, norm, factor, workspace, stream):
+def _grad_norm(function, grads, max_norm, norm, factor, workspace, stream, t_dev=None):
     torch = sys.modules["torch"]
     plan = grads if isinstance(grads, GradTensors) else GradTensors(grads)
     _need(plan.tensors, "no gradients: there is no device to put a norm on")
@@ -788,15 +794,21 @@ def _grad_norm(function, grads, max_norm, norm, factor, workspace, stream):
     factor = _new(first, (), torch.float32, stream) if factor is None else factor
     pn, pf = _vector(norm, "norm", 1), _vector(factor, "factor", 1)
     workspace = _workspace(workspace, plan.workspace_bytes, first, stream)
-    _call(function, stream, first, (norm, factor, workspace), plan.array, n, max_norm, pn, pf, workspace.data_ptr(),
+    counter = () if t_dev is None else (t_dev.data_ptr(),)
+    _call(function, stream, first, (norm, factor, workspace, t_dev), plan.array, n, max_norm, pn, pf, *counter, workspace.data_ptr(),
           workspace.numel() * workspace.element_size())
     return norm, factor
 
 
-def grad_norm(grads, max_norm: float = float("inf"), norm=None, factor=None, workspace=None, stream=None):
+def grad_norm(grads, max_norm: float = float("inf"), norm=None, factor=None, workspace=None, stream=None, t_dev=None):
     """(norm, factor), device floats: the norm of all gradients (a GradTensors or a list for one) and min(1, max_norm / norm), which
-    adamw_step takes along; the gradients stay as they are."""
-    return _grad_norm(load().kge_grad_norm, grads, max_norm, norm, factor, workspace, stream)
+    adamw_step takes along; the gradients stay as they are.  t_dev: the number of the last step, a device int64, which grows by one unless
+    the factor is NaN: as adamw_step's t_dev it does not count steps that are left out."""
+    torch = sys.modules["torch"]
+    if t_dev is None:
+        return _grad_norm(load().kge_grad_norm, grads, max_norm, norm, factor, workspace, stream)
+    _need(t_dev.dtype == torch.int64 and t_dev.numel() == 1, "t_dev: one int64 is wanted")
+    return _grad_norm(load().kge_grad_norm_step, grads, max_norm, norm, factor, workspace, stream, t_dev)
 
 
 def clip_grads(grads, max_norm: float, norm=None, factor=None, workspace=None, stream=None):

@@ -182,14 +182,15 @@ __global__ __launch_bounds__(256) void k_square_sums(List o, double *__restrict_
     if (threadIdx.x == 0) sums[blockIdx.x] = v;
 }
 
-// what follows from the sum of all squares.  One that is not finite: a factor that is NaN
-__device__ __forceinline__ float finish(double v, double max_norm, float *norm, float *factor)
+// what follows from the sum of all squares.  One that is not finite: a factor that is NaN, and no step that counts
+__device__ __forceinline__ float finish(double v, double max_norm, float *norm, float *factor, int64_t *t_dev)
 {
     const double root = sqrt(v);
     const float f = !(v < INFINITY) ? NAN : v > 0.0 && max_norm < root ? (float)(max_norm / root) : 1.f;
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         if (norm) *norm = (float)root;
         if (factor) *factor = f;
+        if (t_dev && f == f) ++*t_dev;
     }
     return f;
 }
@@ -202,14 +203,14 @@ __device__ __forceinline__ double all_sums(const double *__restrict__ sums, int 
     return block_sum(v);
 }
 
-__global__ __launch_bounds__(256) void k_norm(const double *__restrict__ sums, int n_sums, double max_norm, float *norm, float *factor)
+__global__ __launch_bounds__(256) void k_norm(const double *__restrict__ sums, int n_sums, double max_norm, float *norm, float *factor, int64_t *t_dev)
 {
-    finish(all_sums(sums, n_sums), max_norm, norm, factor);
+    finish(all_sums(sums, n_sums), max_norm, norm, factor, t_dev);
 }
 
 __global__ __launch_bounds__(256) void k_norm_scale(List o, const double *__restrict__ sums, int n_sums, double max_norm, float *norm, float *factor)
 {
-    const float f = finish(all_sums(sums, n_sums), max_norm, norm, factor);
+    const float f = finish(all_sums(sums, n_sums), max_norm, norm, factor, nullptr);
     if (f == 1.f) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     scale_by(o, (int64_t)blockIdx.x * 4 + wave, (int64_t)gridDim.x * 4, threadIdx.x & 63, f);
@@ -254,8 +255,9 @@ int check_list(const kge_grad_tensor *tensors, int32_t n_tensors, double max_nor
     return KGE_OK;
 }
 
-int run(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, bool scale, float *norm, float *factor, void *workspace,
-        size_t ws_bytes, hipStream_t st)
+// t_dev: with the norm alone
+int run(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, bool scale, float *norm, float *factor, int64_t *t_dev,
+        void *workspace, size_t ws_bytes, hipStream_t st)
 {
     int rc = check_list(tensors, n_tensors, max_norm);
     if (rc != KGE_OK) return rc;
@@ -285,7 +287,7 @@ int run(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, bool
         told = true;
     }
     if (!told) {
-        k_norm<<<1, 256, 0, st>>>(sums, n_sums, max_norm, norm, factor);
+        k_norm<<<1, 256, 0, st>>>(sums, n_sums, max_norm, norm, factor, t_dev);
         KGE_LAUNCH_CHECK();
     }
     return KGE_OK;
@@ -305,11 +307,18 @@ extern "C" size_t kge_grad_norm_workspace_bytes(int32_t n_tensors)
 extern "C" int kge_grad_norm(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, float *factor, void *workspace,
                              size_t ws_bytes, void *stream)
 {
-    return run(tensors, n_tensors, max_norm, false, norm, factor, workspace, ws_bytes, (hipStream_t)stream);
+    return run(tensors, n_tensors, max_norm, false, norm, factor, nullptr, workspace, ws_bytes, (hipStream_t)stream);
+}
+
+extern "C" int kge_grad_norm_step(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, float *factor,
+                                  int64_t *t_dev, void *workspace, size_t ws_bytes, void *stream)
+{
+    KGE_REQUIRE(t_dev && (uintptr_t)t_dev % 8 == 0, KGE_EINVAL, "t_dev: the address of an int64 is wanted");
+    return run(tensors, n_tensors, max_norm, false, norm, factor, t_dev, workspace, ws_bytes, (hipStream_t)stream);
 }
 
 extern "C" int kge_clip_grads(const kge_grad_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, float *factor, void *workspace,
                               size_t ws_bytes, void *stream)
 {
-    return run(tensors, n_tensors, max_norm, true, norm, factor, workspace, ws_bytes, (hipStream_t)stream);
+    return run(tensors, n_tensors, max_norm, true, norm, factor, nullptr, workspace, ws_bytes, (hipStream_t)stream);
 }

@@ -223,38 +223,90 @@ class TrainStep:
         """The state is that of init_optimizer, or of the first call's kind; plain gradient descent needs none.  A call that is
         refused is no step: the next one has its number.  max_norm: the gradients of all parameters together are scaled to this
         norm where theirs is larger; self.grad_norm (device) is theirs before.  OPT_ADAMW takes the factor along and leaves the
-        gradients as they are; where they are not finite, it leaves the parameters and its state as they are."""
+        gradients as they are; where they are not finite, it leaves the parameters and its state as they are, and the next step
+        has this one's number."""
         self._check_kind(kind)
         if kind != kb.OPT_ADAMW and self.block is not None and self.block.W_rows is not self.block.W:
             raise ValueError("a feature block in bf16 takes OPT_ADAMW, which writes the bf16 copy of its weight")
-        if not hasattr(self, "opt_t"):
+        if not hasattr(self, "_opt_t"):
             self.init_optimizer(kind)
         if kind not in (kb.OPT_SGD, self.opt_kind):
             raise ValueError("the optimizer's state is of another kind: init_optimizer makes this one's")
-        t = self.opt_t + 1
-        if max_norm is not None:
-            self._clip(kb.grad_norm if kind == kb.OPT_ADAMW else kb.clip_grads, max_norm, stream)
         if kind == kb.OPT_ADAMW:
-            more = {} if max_norm is None else dict(factor=self.grad_factor)
-            kb.adamw_step(self.opt_plan, lr, beta1, beta2, eps, t, stream=stream, **more)
-            self.opt_t = t
+            self._adamw_step(lr, beta1, beta2, eps, stream, max_norm)
             return
+        if max_norm is not None:
+            self._clip(kb.clip_grads, max_norm, stream)
         # the entity table: only the rows the step read (flags of the sub-graph's input rows; without a
         # sub-graph the kernel skips rows whose gradient is all zero)
         mask = self.cg.input_rows_ptr() if self.cg is not None else None
+        t = 1 if self._opt_t is None else self._opt_t + 1        # None: the state is AdamW's, and descent has no use for a number
         for name, p, g, rows in self._opt_pairs():
             m, v = self.opt_state.get(name, (None, None)) if kind == kb.OPT_ADAM else (None, None)
             kb.optimizer_step(kind, p, g, m, v, lr, beta1, beta2, eps, t, rows=rows,
                               row_mask=mask if rows else None, stream=stream)
-        self.opt_t = t
+        self._count(stream)
 
-    def _clip(self, call, max_norm: float, stream):
+    def _adamw_step(self, lr, beta1, beta2, eps, stream, max_norm):
+        if max_norm is None and self._opt_t is not None:
+            kb.adamw_step(self.opt_plan, lr, beta1, beta2, eps, self._opt_t + 1, stream=stream)
+            self._count(stream)
+            return
+        kb.check_adamw(lr, beta1, beta2, eps)                    # before the number grows
+        if max_norm is None:
+            self._count(stream)
+            kb.adamw_step(self.opt_plan, lr, beta1, beta2, eps, t_dev=self.opt_t_dev, stream=stream)
+            return
+        # whether the gradients are finite only the device knows: from here on the number is there.  A call that is captured while it is not makes
+        # nothing yet: its replays have the number that it has now, as those of a call without max_norm do
+        number, captured = self.opt_t_dev, False
+        if self._opt_t is not None:
+            with self._on(stream):
+                captured = self.torch.cuda.is_current_stream_capturing()
+                if captured:
+                    number = self.torch.empty_like(number)
+                number.fill_(self._opt_t)
+            if not captured:
+                self._opt_t = None
+        self._clip(kb.grad_norm, max_norm, stream, t_dev=number)
+        kb.adamw_step(self.opt_plan, lr, beta1, beta2, eps, t_dev=number, stream=stream, factor=self.grad_factor)
+        if captured:
+            self._opt_t += 1
+
+    @property
+    def opt_t(self) -> int:
+        """Steps so far.  Once AdamW has made a step with a largest norm, their number is on the device, which reading it waits for; a step
+        captured from then on counts at each replay."""
+        if self._opt_t is not None:
+            return self._opt_t
+        self.torch.cuda.synchronize(self.dev)
+        return int(self.opt_t_dev)
+
+    @opt_t.setter
+    def opt_t(self, steps: int):
+        self._opt_t = int(steps)
+
+    def _count(self, stream):
+        if self._opt_t is not None:
+            self._opt_t += 1
+            return
+        with self._on(stream):
+            self.opt_t_dev.add_(1)
+
+    def _on(self, stream):
+        """torch's own calls on the stream of a library call"""
+        torch = self.torch
+        if stream is not None and not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(stream, self.M.device) if stream else torch.cuda.default_stream(self.M.device)
+        return torch.cuda.stream(stream)
+
+    def _clip(self, call, max_norm: float, stream, **more):
         if not hasattr(self, "grad_plan"):
             mask = self.cg.input_rows_ptr() if self.cg is not None else None
             self.grad_plan = kb.GradTensors([dict(grad=g, row_mask=mask if rows else None) for _, _, g, rows in self._opt_pairs()])
             self.grad_norm, self.grad_factor = (kb._new(self.M, (), self.torch.float32, stream) for _ in range(2))
             self.grad_workspace = kb._workspace(None, self.grad_plan.workspace_bytes, self.M, stream)
-        call(self.grad_plan, max_norm, self.grad_norm, self.grad_factor, self.grad_workspace, stream)
+        call(self.grad_plan, max_norm, self.grad_norm, self.grad_factor, self.grad_workspace, stream, **more)
 
     @staticmethod
     def _check_kind(kind):
@@ -298,3 +350,4 @@ class TrainStep:
                     t["copy"] = self.block.W_rows
                 tensors.append(t)
             self.opt_plan = kb.AdamWTensors(tensors)
+            self.opt_t_dev = self.torch.empty((), dtype=self.torch.int64, device=self.dev)      # filled when the number moves there

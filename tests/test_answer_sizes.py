@@ -63,3 +63,17 @@ def test_sizes_past_32_bits_are_refused(kb, wide):
         handle = None
     with pytest.raises(kb.KgeError, match="candidates"):
         kb.hide_positives(Part(), at(1, dtype=i32), at(1, wide, dtype=i32), at(1, wide, dtype=u8), at(1, wide))
+
+
+def test_a_step_number_is_an_aligned_address(kb):
+    t = (kb._GradTensor * 1)()
+    for at in (None, 4100):
+        assert kb.load().kge_grad_norm_step(t, 1, 1.0, 4096, 4096, at, 4096, 1 << 20, None) == -1 and b"t_dev" in kb.load().kge_last_error()
+    assert kb.load().kge_grad_norm_step(t, 1, -1.0, 4096, 4096, 4096, 4096, 1 << 20, None) == -1 and b"max_norm" in kb.load().kge_last_error()
+
+
+def test_settings_of_adamw_are_checked_alone(kb):
+    kb.check_adamw(0.1, 0.0, 0.5, 1e-8)
+    for how in (dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=float("nan"))):
+        with pytest.raises(kb.KgeError, match="beta"):
+            kb.check_adamw(**how)

@@ -41,6 +41,161 @@ def copy_gradients(a, b):
         h.copy_(g)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("cone", [True, False])
+def test_a_step_that_is_left_out_has_no_number(kb, cone, bits):  # noqa: F811
+    """Gradients that are not finite leave parameters, moments and the number of the step as they are: what follows is what would have
+    followed without that step, the first one's bias corrections among it"""
+    say(cone, bits)
+    spec, part, pos, step = make(kb, cone)
+    a, b = step(), step()
+    for ts in (a, b):
+        ts.init_optimizer(kb.OPT_ADAMW, bits)
+    for number, (before, after) in enumerate([(1, 0), (0, 2), (3, 0)]):
+        a.run(spec.neg_mode, SEED, number)
+        kept = a.dM[0, 0].item()
+        for _ in range(before):
+            a.dM[0, 0] = math.inf if number else math.nan
+            a.optimizer_step(kb.OPT_ADAMW, lr=0.05, max_norm=1.0)
+        a.dM[0, 0] = kept
+        b.run(spec.neg_mode, SEED, number)                      # for its sub-graph's rows
+        copy_gradients(a, b)
+        for ts in (a, b):
+            ts.optimizer_step(kb.OPT_ADAMW, lr=0.05, max_norm=1.0)
+        for _ in range(after):
+            a.dM[0, 0] = -math.inf
+            a.optimizer_step(kb.OPT_ADAMW, lr=0.05, max_norm=1.0)
+        same(a, b)
+        assert a.opt_t == b.opt_t == number + 1
+
+
+def test_steps_with_and_without_a_largest_norm_are_numbered_together(kb):  # noqa: F811
+    """A norm that nothing reaches scales nothing: steps with it, left-out ones among them, and steps without it are the steps without it"""
+    import torch
+    spec, part, pos, step = make(kb)
+    a, b = step(), step()
+    for ts in (a, b):
+        ts.init_optimizer(kb.OPT_ADAMW)
+        ts.run(spec.neg_mode, SEED, 0)
+    copy_gradients(a, b)
+    kept = a.dM[0, 0].item()
+    steps = 0
+    for how in ("plain", "norm", "bad", "plain", "bad", "norm", "sgd", "plain", "bad", "sgd", "norm"):
+        say(how)
+        if how == "bad":
+            a.dM[0, 0] = math.nan
+            a.optimizer_step(kb.OPT_ADAMW, lr=0.05, max_norm=1e30)
+            a.dM[0, 0] = kept
+            continue
+        steps += 1
+        kind = kb.OPT_SGD if how == "sgd" else kb.OPT_ADAMW
+        a.optimizer_step(kind, lr=0.05, **(dict(max_norm=1e30) if how == "norm" else {}))
+        b.optimizer_step(kind, lr=0.05)
+        for (k, p, _, _), (_, q, _, _) in zip(a._opt_pairs(), b._opt_pairs()):
+            # of a step, lr at most while the gradients stay: the two corrections come from the host's pow there and from products here, off by a
+            # rounding each, and so may be what follows (two products, a root and a reciprocal of two roundings each, the product with lr): 16
+            # are allowed.  The update's own rounding may fall to the other side: two halves of a step of a number that was up to 0.6 larger
+            assert bool(((p - q).abs() <= steps * U * (16 * 0.05 + 2 * (q.abs() + 0.6))).all()), k
+    assert a.opt_t == b.opt_t == steps
+    a.opt_t = b.opt_t = 40                                       # as a program that goes on from saved moments sets it
+    for ts in (a, b):
+        ts.optimizer_step(kb.OPT_ADAMW, lr=0.05, max_norm=1e30)
+    assert a.opt_t == b.opt_t == 41
+    torch.cuda.synchronize()
+
+
+def test_the_norm_counts_steps_that_are_made(kb):  # noqa: F811
+    import torch
+    g = [torch.randn(300, 7, device="cuda"), torch.randn(5000, device="cuda")]
+    number = torch.full((1,), 2 ** 40, dtype=torch.int64, device="cuda")
+    want = [float(x) for x in kb.grad_norm(g, 0.5)]
+    for bad in (None, math.inf, None, math.nan, -math.inf, None):
+        if bad is not None:
+            g[0][2, 3], kept = bad, g[0][2, 3].item()
+        norm, factor = kb.grad_norm(g, 0.5, t_dev=number)
+        if bad is not None:
+            assert math.isnan(float(factor))
+            g[0][2, 3] = kept
+        else:
+            assert [float(norm), float(factor)] == want
+    assert int(number) == 2 ** 40 + 3
+    ones = [torch.ones(1, device="cuda") for _ in range(100)]    # more tensors than a launch has
+    kb.grad_norm(ones, 0.5, t_dev=number)
+    assert int(number) == 2 ** 40 + 4
+    for other in (torch.zeros(1, device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda"), torch.zeros(1, dtype=torch.int64)):
+        with pytest.raises(kb.KgeError):
+            kb.grad_norm(ones, 0.5, t_dev=other)
+
+
+def test_replays_of_a_captured_step_are_steps(kb):  # noqa: F811
+    """A step captured after an eager one counts on the device: each replay has a number of its own, but for those that are left out"""
+    import torch
+    spec, part, pos, step = make(kb)
+    a, b = step(), step()
+    for ts in (a, b):
+        ts.init_optimizer(kb.OPT_ADAMW)
+        ts.run(spec.neg_mode, SEED, 0)
+    copy_gradients(a, b)
+    for ts in (a, b):
+        ts.optimizer_step(kb.OPT_ADAMW, lr=0.05, max_norm=0.01)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.optimizer_step(kb.OPT_ADAMW, lr=0.05, max_norm=0.01)
+    kept = a.dM[0, 0].item()
+    for number in (2, 3, 4):
+        graph.replay()
+        a.dM[0, 0] = math.inf
+        graph.replay()                                           # left out
+        a.dM[0, 0] = kept
+        b.optimizer_step(kb.OPT_ADAMW, lr=0.05, max_norm=0.01)
+        same(a, b)
+        assert a.opt_t == b.opt_t == number
+    for ts in (a, b):
+        ts.optimizer_step(kb.OPT_ADAMW, lr=0.05)
+    same(a, b)
+
+
+def test_replays_of_a_step_captured_before_any_have_its_number(kb):  # noqa: F811
+    import torch
+    spec, part, pos, step = make(kb)
+    a, b = step(), step()
+    for ts in (a, b):
+        ts.init_optimizer(kb.OPT_ADAMW)
+        ts.run(spec.neg_mode, SEED, 0)
+        ts.opt_t = 5
+    copy_gradients(a, b)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.optimizer_step(kb.OPT_ADAMW, lr=0.05, max_norm=0.01)
+    assert a.opt_t == 6
+    kept = a.dM[0, 0].item()
+    for _ in range(3):
+        a.dM[0, 0] = math.nan
+        graph.replay()                                           # left out
+        a.dM[0, 0] = kept
+        graph.replay()
+        torch.cuda.synchronize()
+        b.opt_t = 5
+        b.optimizer_step(kb.OPT_ADAMW, lr=0.05, max_norm=0.01)
+        same(a, b)
+        assert b.opt_t == 6 and a.opt_t == 6
+    for how in (dict(max_norm=0.01), dict(), dict(max_norm=0.01)):
+        for ts in (a, b):
+            ts.optimizer_step(kb.OPT_ADAMW, lr=0.05, **how)
+        if how:
+            graph.replay()                                       # its number is its own
+            b.opt_t, kept_t = 5, b.opt_t
+            b.optimizer_step(kb.OPT_ADAMW, lr=0.05, max_norm=0.01)
+            assert b.opt_t == 6
+            b.opt_t = kept_t
+        assert a.opt_t == b.opt_t
+    for (k, p, _, _), (_, q, _, _) in zip(a._opt_pairs(), b._opt_pairs()):
+        # the step without max_norm takes its corrections from the device for one, from the host for the other: a rounding of each
+        assert bool(((p - q).abs() <= 7 * U * (16 * 0.05 + 2 * (q.abs() + 0.6))).all()), k
+
+
 def warm(ts, bits):
     """Moments of many steps before: every row has some"""
     import torch
