@@ -446,6 +446,12 @@ def optimizer_step(kind: int, param, grad, m=None, v=None, lr=0.01, beta1=0.9, b
                                          C.c_int64(param.numel()), _stream(stream)))
 
 
+def check_optimizer(kind: int, param, lr=0.01, beta1=0.9, beta2=0.999, eps=1e-8):
+    """Refuses what optimizer_step would of these settings, and does nothing else."""
+    o, p = _Opt(kind, lr, beta1, beta2, eps, 1), _ptr(param)
+    _check(load().kge_optimizer_step(C.byref(o), p, p, p, p, C.c_int64(0), None))
+
+
 # ---- vertex-feature block (dense layer, layer norm) and AdamW over a list of tensors ------------
 
 # These calls are short enough for the host's time to count: a caller's tensors mean that torch is loaded, and looking it up is

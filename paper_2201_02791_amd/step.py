@@ -236,6 +236,7 @@ class TrainStep:
             self._adamw_step(lr, beta1, beta2, eps, stream, max_norm)
             return
         if max_norm is not None:
+            kb.check_optimizer(kind, self.M, lr, beta1, beta2, eps)      # before the gradients are scaled
             self._clip(kb.clip_grads, max_norm, stream)
         # the entity table: only the rows the step read (flags of the sub-graph's input rows; without a
         # sub-graph the kernel skips rows whose gradient is all zero)

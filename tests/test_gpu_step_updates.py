@@ -127,6 +127,23 @@ def test_the_norm_counts_steps_that_are_made(kb):  # noqa: F811
             kb.grad_norm(ones, 0.5, t_dev=other)
 
 
+def test_a_refused_step_has_no_number_and_leaves_the_gradients(kb):  # noqa: F811
+    import torch
+    spec, part, pos, step = make(kb)
+    for kind in (kb.OPT_ADAM, kb.OPT_ADAMW):
+        ts = step()
+        ts.init_optimizer(kind)
+        ts.run(spec.neg_mode, SEED, 0)
+        was = [(p.clone(), g.clone()) for _, p, g, _ in ts._opt_pairs()]
+        for how in (dict(beta1=1.0), dict(beta2=-0.5), dict(max_norm=-1.0), dict(max_norm=math.nan)):
+            with pytest.raises(kb.KgeError):
+                ts.optimizer_step(kind, **dict(dict(max_norm=1e-3), **how))
+            assert ts.opt_t == 0
+            assert all(torch.equal(x, p) and torch.equal(y, g) for (x, y), (_, p, g, _) in zip(was, ts._opt_pairs()))
+        ts.optimizer_step(kind, max_norm=1e-3)
+        assert ts.opt_t == 1
+
+
 def test_replays_of_a_captured_step_are_steps(kb):  # noqa: F811
     """A step captured after an eager one counts on the device: each replay has a number of its own, but for those that are left out"""
     import torch
