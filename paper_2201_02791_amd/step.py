@@ -124,7 +124,7 @@ class TrainStep:
         self.cand_scores = new(n_pos, 1 + n_cand, dtype=torch.float32)
         self.choice = new(n_pos, self.n_neg, dtype=torch.int32)
         self.cand_index = (kb.ScoreIndex(self.part, max(n_pos, 1), n_cand, self.H_out.shape[1]) if self.want_index else None)
-        self.cand_workspace = None
+        self.cand_workspace, self.cand_workspaces = None, []
 
     def stage_batches(self, batches):
         """Copy several mini-batches (equal-length index arrays) to the device ahead of a loop; returns the
@@ -209,6 +209,7 @@ class TrainStep:
         need = kb.sample_workspace_bytes(*scores.shape, temperature, top_k, top_p, min_p)
         if self.cand_workspace is None or self.cand_workspace.numel() < need:          # the first step of these settings
             self.cand_workspace = kb._workspace(None, need, scores, stream)
+            self.cand_workspaces.append(self.cand_workspace)     # a graph may have been captured with the last one: it is kept
         kb.sample_scores(scores, u, temperature, top_k, top_p, min_p, choice=self.choice, workspace=self.cand_workspace, stream=stream)
         kb.pick_negatives(self.cand_ent, self.cand_side, self.choice, self.neg_ent, self.neg_side, stream)
         # from here on the step is that on the drawn negatives: its sub-graph lies in the one that was propagated, and its flags name

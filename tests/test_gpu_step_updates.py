@@ -267,6 +267,34 @@ def test_rows_that_only_candidates_reach_are_left(kb, name, bits, cone, most):  
             assert torch.equal(states(a)["H0", k].view(torch.uint8)[left], was["H0", k].view(torch.uint8)[left])
 
 
+def test_a_captured_step_keeps_its_workspace(kb):  # noqa: F811
+    """Draws of other settings want a larger workspace: the one that a graph was captured with is not given away"""
+    import torch
+    spec, part, pos, step = make(kb, n_pos=8, n_neg=3)
+    ts = step()
+    ts.set_candidates(40000)
+    u = torch.rand(len(pos), 3, device="cuda")
+    ts.run_hard(spec.neg_mode, SEED, 0, u, top_k=10)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ts.run_hard(spec.neg_mode, SEED, 0, u, top_k=10)
+    small = ts.cand_workspace.numel()
+    ts.run_hard(spec.neg_mode, SEED, 0, u, top_p=0.9)
+    assert ts.cand_workspace.numel() > small
+    others = [torch.full((small,), 7, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    torch.cuda.synchronize()
+    for i in range(3):
+        u.copy_(torch.rand(len(pos), 3, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = ts.choice.clone(), ts.neg_ent.clone()
+        assert all(bool((t == 7).all()) for t in others)
+        ts.run_hard(spec.neg_mode, SEED, 0, u, top_k=10)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], ts.choice) and torch.equal(got[1], ts.neg_ent)
+
+
 @pytest.mark.parametrize("dropout", [0.0, 0.3])
 @pytest.mark.parametrize("msg", [0, 1])
 @pytest.mark.parametrize("order", ["ORDER_PROJECT_FIRST", "ORDER_RELATION_WEIGHTS"])
