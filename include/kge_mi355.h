@@ -594,6 +594,8 @@ int kge_table4_scores(const kge_table4 *table, int32_t dtype, const void *X, int
  *   prob: NULL, or DEVICE float [n_rows][n_draws]: the column's share of the weights left; 0 beside -1
  *   n_rows below 2^31, n_cols at most 2^31 - 2^16.  workspace: DEVICE, 256-byte aligned, at least kge_sample_workspace_bytes(how, n_rows, n_cols)
  *   bytes (0: invalid arguments), calls on different streams need different ones; with up to KGE_SAMPLE_ROW columns none is looked at.
+ *   Where rows are split (few of them, or of more than 2^18 columns) it has, for up to 4096 rows at once, about 100 KB a row, and with top_p 2 to
+ *   3 bytes a column besides; with a small top_k instead 8 bytes for each of the first scores of parts of 4096 columns or more.
  */
 #define KGE_SAMPLE_ROW 32768
 typedef struct kge_sampling {

@@ -1570,7 +1570,7 @@ Plan plan_of(const kge_sampling *how, int64_t n_rows, int64_t n_cols)
     p.off_run = take(runs * 8);
     p.off_run_ties = take(runs * 8);
     p.off_part_hist = take(parts_digits(*how, p.part) ? parts * LONG_DIGITS * 8 : 0);
-    p.off_list = take(parts * (part / LIST_PART) * 8);
+    p.off_list = take(how->row_top_p || how->top_p < 1.f ? parts * (part / LIST_PART) * 8 : 0);     // of top-p's search alone
     p.off_listed = take(parts * 4);
     p.bytes = at;
     return p;

@@ -77,3 +77,15 @@ def test_settings_of_adamw_are_checked_alone(kb):
     for how in (dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=float("nan"))):
         with pytest.raises(kb.KgeError, match="beta"):
             kb.check_adamw(**how)
+
+
+@pytest.mark.parametrize("rows,cols", [(16, 2900000), (1, 1000000), (4096, 300000), (9000, 300000)])
+def test_workspaces_of_long_rows(kb, rows, cols):
+    """Lists of scores are claimed where top-p's search writes them, and there alone: sums of 16 bytes for 1024 columns and those by digit are
+    what the others need"""
+    at_once = min(rows, 4096)
+    without = at_once * (6 * 2048 * 8 + 1024 + 16 * cols // 1024 + 40 * (cols // 4096 + 1)) + 4096
+    for how in (dict(), dict(min_p=0.1), dict(top_k=cols // 2), dict(top_k=cols // 2, temperature=0.5, min_p=0.01)):
+        assert kb.sample_workspace_bytes(rows, cols, **how) <= without, how
+    for how in (dict(top_p=0.9), dict(top_p=0.9, top_k=cols // 2)):
+        assert 2 * at_once * cols <= kb.sample_workspace_bytes(rows, cols, **how) <= without + 3 * at_once * (cols + 65536), how
