@@ -8,9 +8,9 @@
 //
 // Two launches: blocks that each leave one sum in the workspace, then blocks that all add those sums up in the same order and
 // scale what is theirs; for the norm alone one block adds them up.  No atomics, nothing to clear beforehand.
-// Bandwidth bound: 285 million floats, of which nine in ten count, 158 us (6.5 TB/s, a part of it from the last-level cache; 195 us after their
-// scaling) and scaled 334 us, 6.2 TB/s.  Scaling goes from the last gradient to the first, the cache's order, and stores past it (359 us without).
-// (One block for a small model, in one launch, waits longer for its loads than the second launch takes: 51,000 elements 16.6 us against
+// Bandwidth bound: 265 million floats, of which 239 million count (958 MB), 158 us (6.1 TB/s, a part of it from the last-level cache; 195 us after
+// their scaling) and scaled 334 us, 5.7 TB/s.  Scaling goes from the last gradient to the first, the cache's order, and stores past it (359 us without).
+// (One block for a small model, in one launch, waits longer for its loads than the second launch takes: 43,000 elements 16.6 us against
 // 5.3 + 6.0.)
 #include "common.h"
 

@@ -1516,8 +1516,14 @@ constexpr int64_t LONG_BLOCKS = (1 << 22) - 1;           // of one launch: fewer
 static_assert(LONG_BLOCKS * 1024 < 1ll << 32, "k_part_top has 1024 threads to a block");
 
 // Up to KGE_SAMPLE_ROW columns a block takes a row whole, up to twice as many where there are rows for half the compute units, up to ROW_MOST where for
-// all; else rows are split.  No settings / top_k 50 / top_p 0.9, us, whole against split: 1 x 17000 18 / 17 / 40 against 18 / 19 / 33; 1 x 30000 18 / 18 / 48
-// against 19 / 20 / 34; 1 x 65000 30 / 26 / 86 against 18 / 19 / 33; 128 x 65000 33 / 29 / 91 against 28 / 34 / 69; 200 x 30000 19 / 18 / 49 against 25 / 31 / 67
+// all; else rows are split.  Nothing cut / top_k 50 / top_p 0.9, us, whole against split:
+//   1 x 17000      18 / 17 / 40 against 18 / 19 / 33         256 x 65000     31 / 40 / 103 against 43 / 50 / 97
+//   1 x 65000      30 / 26 / 86 against 18 / 19 / 33         256 x 262144    103 / 123 / 414 against 111 / 135 / 240
+//   64 x 130000    38 / 51 / 170 against 29 / 36 / 69        600 x 65000     76 / 102 / 296 against 79 / 92 / 170
+//   100 x 65000    23 / 31 / 93 against 26 / 32 / 63         600 x 262144    281 / 388 / 1087 against 279 / 295 / 556
+//   128 x 40000    19 / 22 / 65 against 23 / 29 / 58         2048 x 40000    116 / 169 / 435 against 235 / 171 / 474
+//   128 x 65000    24 / 33 / 95 against 28 / 35 / 70         2048 x 262144   753 / 1042 / 2951 against 888 / 960 / 1810
+// The rule goes by sizes alone and suits draws of which nothing is cut and small top_k; with a top_p most of these rows would rather be split.
 constexpr int64_t BLOCK_ROW = 65536;
 
 // How a call runs, by its sizes and what the host knows of its settings
