@@ -281,7 +281,7 @@ class TrainStep:
         captured from then on counts at each replay."""
         if self._opt_t is not None:
             return self._opt_t
-        self.torch.cuda.synchronize(self.dev)
+        self.torch.cuda.synchronize(self.M.device)
         return int(self.opt_t_dev)
 
     @opt_t.setter
@@ -352,4 +352,4 @@ class TrainStep:
                     t["copy"] = self.block.W_rows
                 tensors.append(t)
             self.opt_plan = kb.AdamWTensors(tensors)
-            self.opt_t_dev = self.torch.empty((), dtype=self.torch.int64, device=self.dev)      # filled when the number moves there
+            self.opt_t_dev = self.torch.empty((), dtype=self.torch.int64, device=self.M.device)      # filled when the number moves there

@@ -319,3 +319,25 @@ def test_gradients_by_the_drawn_negatives_sub_graph_only_candidates_left_out(kb,
         # the same terms in another order; messages in bf16 may be rounded to the other side, by 2^-8 of one of them
         assert rel_err(x.cpu().numpy(), y.cpu().numpy()) <= (2.0 ** -7 if msg else 1e-5), k
         assert k == "M" or float(y.abs().max()) > 0
+
+
+@pytest.mark.parametrize("number", [True, False])
+def test_steps_on_another_stream_count_there(kb, number):  # noqa: F811
+    """The number of a step is written and read in the order of the stream that the step runs on, also while that one lags behind"""
+    import torch
+    spec, part, pos, step = make(kb)
+    a, b = step(), step()
+    for ts in (a, b):
+        ts.init_optimizer(kb.OPT_ADAMW)
+        ts.run(spec.neg_mode, SEED, 0)
+    copy_gradients(a, b)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    stream = side.cuda_stream if number else side
+    for how in (dict(), dict(max_norm=0.01), dict(), dict(max_norm=0.01), dict(kind=kb.OPT_SGD), dict(max_norm=0.01)):
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(2_000_000)
+        a.optimizer_step(**dict(dict(kind=kb.OPT_ADAMW, lr=0.05, stream=stream), **how))
+        b.optimizer_step(**dict(dict(kind=kb.OPT_ADAMW, lr=0.05), **how))
+    assert a.opt_t == b.opt_t == 6
+    same(a, b)
