@@ -580,6 +580,7 @@ int kge_table4_scores(const kge_table4 *table, int32_t dtype, const void *X, int
 /*
  * Draws from rows of scores, from random numbers that the caller gives.  For each row of n_cols scores (dtype, rows lds apart):
  *   weight of a score l, m the row's largest:  e^((l - m) / temperature), rounded to a multiple of 2^-b, b = min(40, 62 - ceil(log2 n_cols));
+ *     (by one multiple to the other side at most, within 2^-7 of one of the middle between two);
  *     minus infinity and NaN have none, and where the largest is plus infinity, only plus infinity has one
  *   order: descending scores, equal ones by column.  top_k leaves the first top_k, top_p of those the shortest beginning whose weights reach
  *     top_p times theirs (one at least), min_p of those what has min_p times the largest weight or more
