@@ -446,9 +446,9 @@ def optimizer_step(kind: int, param, grad, m=None, v=None, lr=0.01, beta1=0.9, b
                                          C.c_int64(param.numel()), _stream(stream)))
 
 
-def check_optimizer(kind: int, param, lr=0.01, beta1=0.9, beta2=0.999, eps=1e-8):
+def check_optimizer(kind: int, param, lr=0.01, beta1=0.9, beta2=0.999, eps=1e-8, t=1):
     """Refuses what optimizer_step would of these settings, and does nothing else."""
-    o, p = _Opt(kind, lr, beta1, beta2, eps, 1), _ptr(param)
+    o, p = _Opt(kind, lr, beta1, beta2, eps, t), _ptr(param)
     _check(load().kge_optimizer_step(C.byref(o), p, p, p, p, C.c_int64(0), None))
 
 
@@ -747,9 +747,9 @@ def adamw_step(tensors, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, t=1, t_dev=No
         _call(load().kge_adamw_step_scaled, stream, first, (t_dev, factor), C.byref(o), plan.array, n, pf)
 
 
-def check_adamw(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8):
+def check_adamw(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, t=1):
     """Refuses what adamw_step would of these settings, and does nothing else."""
-    _check(load().kge_adamw_step(C.byref(_AdamW(lr, beta1, beta2, eps, 1, None)), None, 0, None))
+    _check(load().kge_adamw_step(C.byref(_AdamW(lr, beta1, beta2, eps, int(t), None)), None, 0, None))
 
 
 # ---- the norm of all gradients, and clipping -----------------------------------------------------

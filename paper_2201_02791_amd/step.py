@@ -236,13 +236,13 @@ class TrainStep:
         if kind == kb.OPT_ADAMW:
             self._adamw_step(lr, beta1, beta2, eps, stream, max_norm)
             return
+        t = 1 if self._opt_t is None else self._opt_t + 1        # None: the state is AdamW's, and descent has no use for a number
         if max_norm is not None:
-            kb.check_optimizer(kind, self.M, lr, beta1, beta2, eps)      # before the gradients are scaled
+            kb.check_optimizer(kind, self.M, lr, beta1, beta2, eps, t)   # before the gradients are scaled
             self._clip(kb.clip_grads, max_norm, stream)
         # the entity table: only the rows the step read (flags of the sub-graph's input rows; without a
         # sub-graph the kernel skips rows whose gradient is all zero)
         mask = self.cg.input_rows_ptr() if self.cg is not None else None
-        t = 1 if self._opt_t is None else self._opt_t + 1        # None: the state is AdamW's, and descent has no use for a number
         for name, p, g, rows in self._opt_pairs():
             m, v = self.opt_state.get(name, (None, None)) if kind == kb.OPT_ADAM else (None, None)
             kb.optimizer_step(kind, p, g, m, v, lr, beta1, beta2, eps, t, rows=rows,
@@ -254,7 +254,7 @@ class TrainStep:
             kb.adamw_step(self.opt_plan, lr, beta1, beta2, eps, self._opt_t + 1, stream=stream)
             self._count(stream)
             return
-        kb.check_adamw(lr, beta1, beta2, eps)                    # before the number grows
+        kb.check_adamw(lr, beta1, beta2, eps, 1 if self._opt_t is None else self._opt_t + 1)       # before the number grows
         if max_norm is None:
             self._count(stream)
             kb.adamw_step(self.opt_plan, lr, beta1, beta2, eps, t_dev=self.opt_t_dev, stream=stream)

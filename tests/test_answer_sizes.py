@@ -89,3 +89,6 @@ def test_workspaces_of_long_rows(kb, rows, cols):
         assert kb.sample_workspace_bytes(rows, cols, **how) <= without, how
     for how in (dict(top_p=0.9), dict(top_p=0.9, top_k=cols // 2)):
         assert 2 * at_once * cols <= kb.sample_workspace_bytes(rows, cols, **how) <= without + 3 * at_once * (cols + 65536), how
+    kb.check_adamw(t=2 ** 40)
+    with pytest.raises(kb.KgeError, match="starts at 1"):
+        kb.check_adamw(t=0)

@@ -341,3 +341,19 @@ def test_steps_on_another_stream_count_there(kb, number):  # noqa: F811
         b.optimizer_step(**dict(dict(kind=kb.OPT_ADAMW, lr=0.05), **how))
     assert a.opt_t == b.opt_t == 6
     same(a, b)
+
+
+def test_numbers_below_one_are_refused(kb):  # noqa: F811
+    import torch
+    spec, part, pos, step = make(kb)
+    for kind in (kb.OPT_ADAM, kb.OPT_ADAMW):
+        ts = step()
+        ts.init_optimizer(kind)
+        ts.run(spec.neg_mode, SEED, 0)
+        was = [(p.clone(), g.clone()) for _, p, g, _ in ts._opt_pairs()]
+        for how in (dict(max_norm=1e-3), dict()):
+            ts.opt_t = -1
+            with pytest.raises(kb.KgeError, match="starts at 1"):
+                ts.optimizer_step(kind, **how)
+            assert ts.opt_t == -1
+            assert all(torch.equal(x, p) and torch.equal(y, g) for (x, y), (_, p, g, _) in zip(was, ts._opt_pairs()))
